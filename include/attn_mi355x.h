@@ -75,12 +75,15 @@ enum {
   ATTN_OK = 0,
   ATTN_E_NULL = -1,        /* a required pointer is NULL */
   ATTN_E_SHAPE = -2,       /* B, H or n < 1, or the problem is too large to index */
-  ATTN_E_UNSUPPORTED = -3, /* d not in {32, 64, 128}, or unknown dtype */
-  ATTN_E_ALIGN = -4,       /* a tensor is not 16-byte aligned (L/workspace: 4-byte) */
+  ATTN_E_UNSUPPORTED = -3, /* d not in {32, 64, 128}, unknown dtype, rotated columns or
+                              page size (below) out of range */
+  ATTN_E_ALIGN = -4,       /* a tensor (or its strides) is not 16-byte aligned (L/workspace:
+                              4-byte) */
   ATTN_E_WORKSPACE = -5,   /* workspace_bytes < attn_workspace_bytes(B, H, n, d), or
                               p_bytes < attn_mat_bytes(B, H, n, dtype) */
   ATTN_E_HIP = -6,         /* the HIP runtime rejected a kernel launch */
-  ATTN_E_ARG = -7,         /* scale not finite, or causal not 0/1 */
+  ATTN_E_ARG = -7,         /* scale or amplitude not finite, causal or interleaved not 0/1,
+                              or an output whose rows overlap */
   ATTN_E_SCRATCH = -8      /* attn_fwd_bwd_noalloc: B*H*n > attn_noalloc_max_rows() */
 };
 
@@ -261,6 +264,104 @@ int attn_decode(const void* q, const void* k_new, const void* v_new, void* k_cac
                 const int* cache_lens, void* O, float* L, void* workspace, size_t workspace_bytes,
                 int B, int Hq, int Hkv, int n, int n_cap, int d, float scale, int dtype,
                 void* stream);
+
+/* ---- Rotary positions ----------------------------------------------------
+ * Not an operation of the paper: what a model does to Q and K between their
+ * projection and the attention above, and to dQ and dK on the way back.
+ * The first r columns of a head are taken in pairs, (x_i, x_{i + r/2}) or, with
+ * interleaved = 1, (x_{2i}, x_{2i+1}), i < r/2; pair i of the token at position p
+ * becomes
+ *   u' = a (u cos t - w sin t),  w' = a (w cos t + u sin t),  t = p freqs[i],
+ * and columns from r on are copied. attn_rope_bwd is the gradient: the same
+ * with sin t negated (from dq, dk of the rotated tensors to those of the
+ * originals). r is a multiple of 16, 16 <= r <= d. freqs is a device array of r/2
+ * float64 (radians per position) and a the amplitude: every scaling for long
+ * contexts is a choice of these two. Angles are reduced in 64 bits, so far
+ * positions are as exact as near ones.
+ *
+ * Layout: q, q_out [B, Hq, n, d], k, k_out [B, Hk, n, d] (k and k_out NULL: q
+ * alone). `strides` (a host array) holds the elements between sequences, heads and
+ * tokens, three each for q, k, q_out, k_out, or is NULL for dense tensors: views
+ * of a fused projection [B, n, Hq + 2 Hk, d] and of its gradient need no
+ * copy. Strides are not negative, rows start at multiples of 16 bytes, and the rows
+ * of an output must not overlap (ATTN_E_ARG). A tensor may be rotated in place
+ * (same pointer and strides); otherwise outputs must not overlap inputs.
+ *
+ * Positions: token i of sequence b is at positions[b * pos_stride + i] (device
+ * int32; pos_stride 0: shared by all sequences), or at start + i where positions
+ * is NULL. Positions may be negative. */
+int attn_rope(const void* q, const void* k, void* q_out, void* k_out, const long long* strides,
+              const double* freqs, const int* positions, long long pos_stride, int start,
+              int B, int Hq, int Hk, int n, int d, int r, float amplitude, int interleaved, int dtype,
+              void* stream);
+
+int attn_rope_bwd(const void* dq, const void* dk, void* dq_in, void* dk_in, const long long* strides,
+                  const double* freqs, const int* positions, long long pos_stride, int start,
+                  int B, int Hq, int Hk, int n, int d, int r, float amplitude, int interleaved, int dtype,
+                  void* stream);
+
+/* ---- Paged cache ----------------------------------------------------------
+ * Not an operation of the paper: the KV cache of a batch whose sequences come,
+ * grow and go, as pages of one pool. Pools k_pages, v_pages are [num_pages, Hkv,
+ * page_size, d]; a page holds page_size consecutive tokens of one sequence
+ * (page_size a power of two, 16 to 2^20), and block_table (device int32 [B,
+ * table_width]) names sequence b's pages in order: token p is row p % page_size of
+ * page block_table[b, p / page_size]. lens (device int32 [B]) holds the tokens
+ * cached before the call; no call changes it. Entries behind a sequence's pages are
+ * never used. A page number outside [0, num_pages) that a call does meet is
+ * skipped: tokens there are not written, read back as zeros and take no part
+ * in attention. Pages may be shared between sequences for reading; a row that
+ * one call writes twice holds either value.
+ *
+ * Pages are bfloat16 (dtype; ATTN_E_UNSUPPORTED otherwise), or, with k_scales and
+ * v_scales given, 4 bits: pools of bytes [num_pages, Hkv, page_size, d/2] (column
+ * 2i in the low half of byte i) and scales [num_pages, Hkv, page_size, d/32], the
+ * microscaling format with E2M1 elements and one E8M0 scale per 32 columns.
+ * A code is a sign and one of 0, .5, 1, 1.5, 2, 3, 4, 6, scale byte x stands for
+ * 2^(x-127), 255 for "not a number". Written blocks take the smallest power
+ * 2^e >= 2^-125 with every magnitude below 7 2^e, each value the nearest code (ties to
+ * the even one) that stands for a finite bfloat16; rotated keys are rounded once, from 64 bits. A block with a
+ * value that is not finite is stored as not-a-number. All four pools are 16-byte
+ * aligned. */
+
+/* Appends T tokens per sequence: token t < new_lens[b] (device int32 [B]; NULL:
+ * T) of k_new, v_new [B, Hkv, T, d] becomes token lens[b] + t. Keys are rotated on
+ * the way where freqs is given (as attn_rope; position positions[b, t], device
+ * int32 [B, T], or lens[b] + t where NULL), values are not. `strides`: host array,
+ * (sequence, head, token) for k_new, then v_new, or NULL (dense). Tokens that the
+ * table has no room for are not written. */
+int attn_paged_append(const void* k_new, const void* v_new, const long long* strides, void* k_pages,
+                      void* v_pages, void* k_scales, void* v_scales, const int* block_table,
+                      const int* lens, const int* new_lens, const double* freqs, const int* positions,
+                      int B, int Hkv, int T, int num_pages, int page_size, int table_width, int d, int r,
+                      float amplitude, int interleaved, int dtype, void* stream);
+
+/* Reads rows back: K, V [B, Hkv, n, d] (bfloat16, dense) get tokens starts[b] +
+ * [0, n) (device int32 [B]; NULL: 0) of every sequence, zeros where a token does not
+ * exist (from lens[b] on, before 0, in no page). */
+int attn_paged_gather(const void* k_pages, const void* v_pages, const void* k_scales,
+                      const void* v_scales, const int* block_table, const int* lens, const int* starts,
+                      void* K, void* V, int B, int Hkv, int n, int num_pages, int page_size,
+                      int table_width, int d, int dtype, void* stream);
+
+/* attn_decode over pages: appends k_new, v_new [B, Hkv, d] (both NULL: no append) as
+ * token len_b, and attends q [B, Hq, d] to the first T_b = len_b + 1 tokens (len_b
+ * without an append), with len_b = lens[b] clamped to [0, n]; grouped heads, O, L,
+ * empty sequences and the workspace as in attn_decode. With freqs, q and k_new are
+ * rotated on the way, to position positions[b] (device int32 [B]) or T_b - 1; the
+ * rotated query keeps 16 bits. `strides`: host array, the elements between
+ * sequences of q, k_new and v_new, or NULL (dense; a row [H, d] is always dense).
+ * n + 1 tokens (n without an append) have to fit table_width pages. With more
+ * than 32 query heads per cache head the append is a launch of its own before
+ * the attention. Positions only turn: which keys are seen goes by the lengths. */
+size_t attn_paged_decode_workspace_bytes(int B, int Hq, int Hkv, int n, int d, int append, int bits);
+
+int attn_paged_decode(const void* q, const void* k_new, const void* v_new, const long long* strides,
+                      void* k_pages, void* v_pages, void* k_scales, void* v_scales,
+                      const int* block_table, const int* lens, const double* freqs, const int* positions,
+                      void* O, float* L, void* workspace, size_t workspace_bytes,
+                      int B, int Hq, int Hkv, int n, int num_pages, int page_size, int table_width, int d,
+                      int r, float amplitude, int interleaved, float scale, int dtype, void* stream);
 
 /* Not an operation of the paper: error reporting of this interface.
  * Static, NUL-terminated description of a status code (never NULL). */

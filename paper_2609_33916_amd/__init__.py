@@ -12,6 +12,14 @@ memory and the current stream.
 
 Tensors are contiguous [B, H, n, d] on one GPU, all bfloat16 or all float32;
 L is float32 [B, H, n] (natural-log log-sum-exp of the scaled, masked scores).
+Rotary positions and a paged key/value cache, in bfloat16 or 4 bits, stand beside them:
+
+    q, k = attn_rope(q, k, freqs)                           # strided views too
+    dq, dk = attn_rope_bwd(dq, dk, freqs)
+    attn_paged_append(k, v, k_pages, v_pages, block_table, lens, freqs=freqs)
+    O, L = attn_paged_decode(q, k_pages, v_pages, block_table, lens, k_new, v_new, freqs=freqs)
+    K, V = attn_paged_gather(k_pages, v_pages, block_table, lens, n)
+
 There is no fallback: if the library is missing or the device is not a GPU,
 the call raises.
 """
@@ -30,6 +38,8 @@ __all__ = ["attn_fwd", "attn_fwd_bwd", "attn_fwd_bwd_timed", "attn_fwd_bwd_noall
            "attn_bwd", "attn_workspace_bytes", "attn_strerror",
            "attn_mat_bytes", "attn_mat_lda", "attn_mat_fwd", "attn_mat_bwd", "attn_mat_fwd_bwd",
            "attn_fwd_bwd_atomic", "attn_workspace_bytes_atomic", "attn_decode", "attn_decode_workspace_bytes",
+           "attn_rope", "attn_rope_bwd", "attn_rope_freqs", "attn_paged_append", "attn_paged_gather",
+           "attn_paged_decode", "attn_paged_decode_workspace_bytes",
            "AttnError", "lib", "LIB_PATH", "ATTN_BF16", "ATTN_F32"]
 
 # ATTN_MI355X_LIB may name another build of the same library (A/B comparison
@@ -91,6 +101,22 @@ def lib() -> ctypes.CDLL:
     L.attn_mat_fwd_bwd.argtypes = [vp, vp, vp, vp, vp, vp, vp, sz, vp, vp, vp, vp, sz,
                                    i, i, i, i, f, i, i, vp]
     L.attn_mat_fwd_bwd.restype = i
+    ll = ctypes.c_longlong
+    rope = [vp, vp, vp, vp, ctypes.POINTER(ll), vp, vp, ll, i, i, i, i, i, i, i, f, i, i, vp]
+    L.attn_rope.argtypes = rope
+    L.attn_rope.restype = i
+    L.attn_rope_bwd.argtypes = rope
+    L.attn_rope_bwd.restype = i
+    L.attn_paged_append.argtypes = [vp, vp, ctypes.POINTER(ll), vp, vp, vp, vp, vp, vp, vp, vp, vp,
+                                    i, i, i, i, i, i, i, i, f, i, i, vp]
+    L.attn_paged_append.restype = i
+    L.attn_paged_gather.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, i, i, i, i, i, i, i, i, vp]
+    L.attn_paged_gather.restype = i
+    L.attn_paged_decode_workspace_bytes.argtypes = [i, i, i, i, i, i, i]
+    L.attn_paged_decode_workspace_bytes.restype = sz
+    L.attn_paged_decode.argtypes = [vp, vp, vp, ctypes.POINTER(ll), vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz,
+                                    i, i, i, i, i, i, i, i, i, f, i, f, i, vp]
+    L.attn_paged_decode.restype = i
     L.attn_strerror.argtypes = [i]
     L.attn_strerror.restype = ctypes.c_char_p
     _lib = L
@@ -122,6 +148,9 @@ def _bind_native(L: ctypes.CDLL) -> None:
             for f in ("attn_workspace_bytes", "attn_decode_workspace_bytes", "attn_fwd", "attn_fwd_bwd", "attn_bwd",
                       "attn_decode")]
     _binding.bind(*addr, torch._C._cuda_getCurrentRawStream)
+    _binding.bind_paged(*(ctypes.cast(getattr(L, f), ctypes.c_void_p).value
+                          for f in ("attn_rope", "attn_rope_bwd", "attn_paged_append", "attn_paged_gather",
+                                    "attn_paged_decode_workspace_bytes", "attn_paged_decode")))
     _native, _native_lib = _binding, L
 
 
@@ -526,4 +555,256 @@ def attn_decode(q, k_cache, v_cache, k_new=None, v_new=None, cache_lens=None, n:
                            B, Hq, Hkv, n, n_cap, d, _scale(scale, d), _dtype_code(q), _stream(q.device))
     if rc != 0:
         raise AttnError(rc, "attn_decode")
+    return O, L
+
+
+# ------------------------------------------------------------ rotary positions --
+def _need(ok: bool, message: str) -> None:
+    if not ok:
+        raise ValueError(message)
+
+
+def _rows(name: str, t, shape, ref: torch.Tensor, dtype: Optional[torch.dtype] = None) -> None:
+    """A GPU tensor of `shape` on ref's device whose last axis is dense; the other
+    strides are the library's business."""
+    _need(isinstance(t, torch.Tensor) and t.is_cuda and t.device == ref.device,
+          f"{name} must be a GPU tensor on the other tensors' device")
+    _need(t.dtype == (ref.dtype if dtype is None else dtype), f"{name} must be {ref.dtype if dtype is None else dtype}")
+    _need(tuple(t.shape) == tuple(shape), f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    _need(t.stride(-1) == 1, f"{name}'s last axis must be contiguous")
+
+
+def _ints(name: str, t, shapes, ref: torch.Tensor) -> Optional[int]:
+    """The address of an optional int32 GPU tensor of one of `shapes`."""
+    if t is None:
+        return None
+    _need(isinstance(t, torch.Tensor) and t.is_cuda and t.device == ref.device and t.dtype == torch.int32
+          and tuple(t.shape) in shapes and t.is_contiguous(),
+          f"{name} must be a contiguous int32 GPU tensor of shape {' or '.join(map(str, shapes))}")
+    return t.data_ptr()
+
+
+def _rotation(freqs, d: int, ref: torch.Tensor):
+    """(address, rotated columns) of an optional table of frequencies."""
+    if freqs is None:
+        return None, 0
+    _need(isinstance(freqs, torch.Tensor) and freqs.is_cuda and freqs.device == ref.device
+          and freqs.dtype == torch.float64 and freqs.dim() == 1 and freqs.is_contiguous(),
+          "freqs must be a contiguous float64 GPU tensor of one axis")
+    _need(2 * freqs.numel() <= d, f"freqs holds {freqs.numel()} frequencies, {d} columns have {d // 2} pairs")
+    return freqs.data_ptr(), 2 * freqs.numel()
+
+
+def _call(name: str, dev: torch.device, *args) -> None:
+    """A library call with the tensors' device current, on its current stream."""
+    with torch.cuda.device(dev):
+        rc = getattr(lib(), name)(*args, _stream(dev))
+    if rc != 0:
+        raise AttnError(rc, name)
+
+
+def attn_rope_freqs(r: int, base: float = 10000.0, scaling: Optional[str] = None, factor: float = 1.0,
+                    original_length: Optional[int] = None, low: float = 1.0, high: float = 32.0,
+                    amplitude: Optional[float] = None, device="cuda") -> Tuple[torch.Tensor, float]:
+    """Frequencies (float64 [r/2] on `device`) and amplitude for r rotated columns:
+    base^(-2i/r), scaled for contexts `factor` times longer than trained on:
+
+    None      as they are
+    "linear"  all divided by `factor` (positions interpolated)
+    "base"    a base larger by factor^(r/(r-2)): the slowest pair is stretched by
+              `factor`, the fastest not at all
+    "ramp"    by the turns a pair makes in `original_length` positions: divided
+              by `factor` up to `low` turns, as they are from `high`, a linear ramp
+              between (YaRN, arXiv:2309.00071); the amplitude defaults to
+              0.1 ln(factor) + 1, elsewhere to 1."""
+    _need(isinstance(r, int) and r >= 16 and r % 16 == 0, "r must be a positive multiple of 16")
+    _need(base > 0 and factor > 0 and math.isfinite(base) and math.isfinite(factor), "base and factor must be positive")
+    if scaling == "base":
+        base *= factor ** (r / (r - 2))
+    f = [base ** (-2.0 * i / r) for i in range(r // 2)]
+    if scaling == "linear":
+        f = [x / factor for x in f]
+    elif scaling == "ramp":
+        _need(original_length is not None and original_length > 0, "scaling='ramp' needs original_length")
+        _need(0 <= low < high, "0 <= low < high")
+        for i, x in enumerate(f):
+            keep = min(max((original_length * x / (2 * math.pi) - low) / (high - low), 0.0), 1.0)
+            f[i] = x * (keep + (1 - keep) / factor)
+        if amplitude is None:
+            amplitude = 0.1 * math.log(factor) + 1
+    else:
+        _need(scaling in (None, "base"), f"unknown scaling {scaling!r} (None, 'linear', 'base' or 'ramp')")
+    return torch.tensor(f, dtype=torch.float64, device=device), 1.0 if amplitude is None else float(amplitude)
+
+
+def attn_rope(q, k, freqs, amplitude: float = 1.0, interleaved: bool = False, positions=None, start: int = 0, out=None):
+    """Rotates q [B, Hq, n, d] and k [B, Hk, n, d] (or None) to their positions:
+    positions ([n] or [B, n], int32 on the GPU) or start + token. Views (of a fused
+    projection, say) are taken as they are; returns (q, k), dense, or ``out``, which may be views
+    too, or (q, k) themselves. The first 2 len(freqs) columns turn, in pairs (i,
+    i + len(freqs)) or, ``interleaved``, (2i, 2i + 1)."""
+    return _rope("attn_rope", q, k, freqs, amplitude, interleaved, positions, start, out)
+
+
+def attn_rope_bwd(dq, dk, freqs, amplitude: float = 1.0, interleaved: bool = False, positions=None, start: int = 0,
+                  out=None):
+    """The gradients of attn_rope's inputs from those of its results; arguments as there."""
+    return _rope("attn_rope_bwd", dq, dk, freqs, amplitude, interleaved, positions, start, out)
+
+
+def _rope(name, q, k, freqs, amplitude, interleaved, positions, start, out):
+    if lib() is _native_lib:
+        r = _native.rope(q, k, freqs, amplitude, interleaved, positions, start, out, name == "attn_rope_bwd")
+        if r is not NotImplemented:
+            return _status(r, name)
+    _need(isinstance(q, torch.Tensor) and q.dim() == 4, "q must be [B, H, n, d]")
+    B, Hq, n, d = q.shape
+    _rows("q", q, q.shape, q)
+    if k is not None:
+        _need(isinstance(k, torch.Tensor) and k.dim() == 4, "k must be [B, H, n, d]")
+        _rows("k", k, (B, k.shape[1], n, d), q)
+    _need(freqs is not None, "freqs is required")
+    f_ptr, r = _rotation(freqs, d, q)
+    pos = _ints("positions", positions, ((n,), (B, n)), q)
+    _need(-2**31 <= start < 2**31, "start must fit 32 bits")
+    if out is None:
+        out = tuple(None if t is None else torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k))
+    else:
+        _need(len(out) == 2 and (out[1] is None) == (k is None), "out must hold (q, k)")
+        _rows("out[0]", out[0], q.shape, q)
+        if k is not None:
+            _rows("out[1]", out[1], k.shape, q)
+    code = _dtype_code(q)
+    all4 = (q, k, out[0], out[1])
+    strides = (ctypes.c_longlong * 12)(*(s for t in all4 for s in ((0, 0, 0) if t is None else t.stride()[:3])))
+    ptr = [None if t is None else t.data_ptr() for t in all4]
+    _call(name, q.device, *ptr, strides, f_ptr, pos, n if positions is not None and positions.dim() == 2 else 0,
+          0 if positions is not None else int(start), B, Hq, 0 if k is None else k.shape[1], n, d, r, float(amplitude),
+          int(bool(interleaved)), code)
+    return tuple(out)
+
+
+# ---------------------------------------------------------------- paged cache --
+def _pool(k_pages, v_pages, k_scales, v_scales, block_table, lens):
+    """Checks a pool and its tables: (addresses, B, Hkv, num_pages, page_size, width, d)."""
+    _need(isinstance(k_pages, torch.Tensor) and k_pages.dim() == 4 and k_pages.is_cuda,
+          "k_pages must be a GPU tensor [num_pages, Hkv, page_size, d] (d / 2 bytes for 4 bits)")
+    _need((k_scales is None) == (v_scales is None), "4-bit pages need k_scales and v_scales")
+    P, Hkv, ps, w = k_pages.shape
+    four = k_scales is not None
+    d = 2 * w if four else w
+    for name, t, shape, dtype in (("k_pages", k_pages, (P, Hkv, ps, w), torch.uint8 if four else torch.bfloat16),
+                                  ("v_pages", v_pages, (P, Hkv, ps, w), torch.uint8 if four else torch.bfloat16),
+                                  ("k_scales", k_scales, (P, Hkv, ps, d // 32), torch.uint8),
+                                  ("v_scales", v_scales, (P, Hkv, ps, d // 32), torch.uint8)):
+        if t is not None:
+            _check_out(name, t, shape, dtype, k_pages)
+    _need(isinstance(block_table, torch.Tensor) and block_table.dim() == 2, "block_table must be int32 [B, width]")
+    B, width = block_table.shape
+    table = _ints("block_table", block_table, ((B, width),), k_pages)
+    _need(lens is not None, "lens is required")
+    l_ptr = _ints("lens", lens, ((B,),), k_pages)
+    return ((k_pages.data_ptr(), v_pages.data_ptr(), k_scales.data_ptr() if four else None,
+             v_scales.data_ptr() if four else None, table, l_ptr), B, Hkv, P, ps, width, d)
+
+
+def attn_paged_append(k_new, v_new, k_pages, v_pages, block_table, lens, new_lens=None, k_scales=None, v_scales=None,
+                      freqs=None, amplitude: float = 1.0, interleaved: bool = False, positions=None) -> None:
+    """Writes T tokens per sequence, k_new and v_new [B, Hkv, T, d] (views are
+    taken as they are), behind the lens[b] cached ones: the first new_lens[b] (all
+    where None). Pools, updated in place, are [num_pages, Hkv, page_size, d] bfloat16, or bytes
+    [..., d/2] with scales [..., d/32] (4 bits). Keys are rotated on the way where freqs
+    is given, to positions ([B, T], int32) or their places in the sequence. lens is
+    not changed."""
+    if lib() is _native_lib:
+        r = _native.paged_append(k_new, v_new, k_pages, v_pages, block_table, lens, new_lens, k_scales, v_scales, freqs,
+                                 amplitude, interleaved, positions)
+        if r is not NotImplemented:
+            return _status(r, "attn_paged_append")
+    ptr, B, Hkv, P, ps, width, d = _pool(k_pages, v_pages, k_scales, v_scales, block_table, lens)
+    _need(isinstance(k_new, torch.Tensor) and k_new.dim() == 4, "k_new must be [B, Hkv, T, d]")
+    T = k_new.shape[2]
+    for name, t in (("k_new", k_new), ("v_new", v_new)):
+        _rows(name, t, (B, Hkv, T, d), k_pages, torch.bfloat16)
+    f_ptr, r = _rotation(freqs, d, k_pages)
+    strides = (ctypes.c_longlong * 6)(*k_new.stride()[:3], *v_new.stride()[:3])
+    _call("attn_paged_append", k_pages.device, k_new.data_ptr(), v_new.data_ptr(), strides, *ptr,
+          _ints("new_lens", new_lens, ((B,),), k_pages), f_ptr, _ints("positions", positions, ((B, T),), k_pages), B, Hkv, T,
+          P, ps, width, d, r, float(amplitude), int(bool(interleaved)), ATTN_BF16)
+
+
+def attn_paged_gather(k_pages, v_pages, block_table, lens, n: int, starts=None, k_scales=None, v_scales=None, out=None):
+    """Tokens starts[b] + [0, n) (starts None: from 0) of every sequence as dense
+    bfloat16 (K, V) [B, Hkv, n, d], zeros where a sequence has no such token."""
+    if lib() is _native_lib:
+        r = _native.paged_gather(k_pages, v_pages, block_table, lens, n, starts, k_scales, v_scales, out)
+        if r is not NotImplemented:
+            return _status(r, "attn_paged_gather")
+    ptr, B, Hkv, P, ps, width, d = _pool(k_pages, v_pages, k_scales, v_scales, block_table, lens)
+    n = int(n)
+    _need(0 < n < 2**31, "n must be positive")
+    s_ptr = _ints("starts", starts, ((B,),), k_pages)
+    shape = (B, Hkv, n, d)
+    if out is None:
+        out = tuple(torch.empty(shape, dtype=torch.bfloat16, device=k_pages.device) for _ in range(2))
+    else:
+        _need(len(out) == 2, "out must hold (K, V)")
+        for name, t in zip(("out[0]", "out[1]"), out):
+            _check_out(name, t, shape, torch.bfloat16, k_pages)
+    _call("attn_paged_gather", k_pages.device, *ptr, s_ptr, out[0].data_ptr(),
+          out[1].data_ptr(), B, Hkv, n, P, ps, width, d, ATTN_BF16)
+    return tuple(out)
+
+
+def attn_paged_decode_workspace_bytes(B: int, Hq: int, Hkv: int, n: int, d: int, append: bool = True, bits: int = 16) -> int:
+    return int(lib().attn_paged_decode_workspace_bytes(B, Hq, Hkv, n, d, int(bool(append)), bits))
+
+
+def attn_paged_decode(q, k_pages, v_pages, block_table, lens, k_new=None, v_new=None, n: Optional[int] = None,
+                      scale: Optional[float] = None, k_scales=None, v_scales=None, freqs=None, amplitude: float = 1.0,
+                      interleaved: bool = False, positions=None, out=None, workspace=None):
+    """attn_decode over pages: appends k_new/v_new ([B, Hkv, d]) as token lens[b]
+    and attends q ([B, Hq, d]) to the first lens[b] + 1 tokens (lens[b] without an
+    append). n bounds the lengths (default: what the table has room for); the work
+    is split by it. Pools as in attn_paged_append. With freqs, q and k_new are
+    rotated on the way, to positions ([B], int32) or the last token's place. q,
+    k_new and v_new may be rows of a fused projection. Returns (O, L)."""
+    if lib() is _native_lib:
+        r = _native.paged_decode(q, k_pages, v_pages, block_table, lens, k_new, v_new, n, scale, k_scales, v_scales, freqs,
+                                 amplitude, interleaved, positions, out, workspace)
+        if r is not NotImplemented:
+            return _status(r, "attn_paged_decode")
+    ptr, B, Hkv, P, ps, width, d = _pool(k_pages, v_pages, k_scales, v_scales, block_table, lens)
+    _need(isinstance(q, torch.Tensor) and q.dim() == 3, "q must be [B, Hq, d]")
+    Hq = q.shape[1]
+    append = k_new is not None
+    _need(append == (v_new is not None), "k_new and v_new belong together")
+    rows = (("q", q, Hq),) + ((("k_new", k_new, Hkv), ("v_new", v_new, Hkv)) if append else ())
+    for name, t, H in rows:
+        _rows(name, t, (B, H, d), k_pages, torch.bfloat16)
+        _need(H == 1 or t.stride(1) == d, f"{name}: a sequence's heads must be contiguous")
+    if n is None:
+        n = min(width * ps - append, 2**31 - 2048)
+    n = int(n)
+    _need(-2**31 <= n < 2**31, "n must fit 32 bits")
+    f_ptr, r = _rotation(freqs, d, k_pages)
+    p_ptr = _ints("positions", positions, ((B,),), k_pages)
+    if out is None:
+        O = torch.empty((B, Hq, d), dtype=torch.bfloat16, device=q.device)
+        L = torch.empty((B, Hq), dtype=torch.float32, device=q.device)
+    else:
+        _need(len(out) == 2, "out must hold (O, L)")
+        O, L = out
+        _check_out("O", O, (B, Hq, d), torch.bfloat16, q)
+        if L is not None:
+            _check_out("L", L, (B, Hq), torch.float32, q)
+    wsb = attn_paged_decode_workspace_bytes(B, Hq, Hkv, n, d, append, 16 if k_scales is None else 4)
+    if workspace is None and wsb > 0:
+        workspace = torch.empty(wsb, dtype=torch.uint8, device=q.device)
+    ws_ptr, ws_len = (None, 0) if workspace is None else _check_workspace(workspace, wsb, q)
+    strides = (ctypes.c_longlong * 3)(q.stride(0), *((k_new.stride(0), v_new.stride(0)) if append else (0, 0)))
+    _call("attn_paged_decode", q.device, q.data_ptr(), k_new.data_ptr() if append else None,
+          v_new.data_ptr() if append else None, strides, *ptr, f_ptr, p_ptr, O.data_ptr(),
+          L.data_ptr() if L is not None else None, ws_ptr, ws_len, B, Hq, Hkv, n, P, ps, width, d, r, float(amplitude),
+          int(bool(interleaved)), _scale(scale, d), ATTN_BF16)
     return O, L

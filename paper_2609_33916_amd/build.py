@@ -30,6 +30,7 @@ SOURCES = {
     "dkdv.hip": [],
     "split.hip": [],
     "f32x3.hip": [],
+    "paged.hip": [],
     "bwd.hip": ["-mllvm", "-amdgpu-sched-strategy=iterative-ilp"],
 }
 

@@ -294,6 +294,15 @@ long long mat_lda(int n) { return ((long long)n + 127) / 128 * 128; }
 
 }  // namespace
 
+namespace attn {
+void launch_paged_combine(const float* part, void* o, float* lse, int rows, int nsplit, int d, hipStream_t st) {
+  const dim3 grid((unsigned)rows), block(256);
+  if (d == 32) hipLaunchKernelGGL((decode_combine_kernel<bf16, 32, true>), grid, block, 0, st, part, o, lse, rows, nsplit);
+  else if (d == 64) hipLaunchKernelGGL((decode_combine_kernel<bf16, 64, true>), grid, block, 0, st, part, o, lse, rows, nsplit);
+  else hipLaunchKernelGGL((decode_combine_kernel<bf16, 128, true>), grid, block, 0, st, part, o, lse, rows, nsplit);
+}
+}  // namespace attn
+
 extern "C" {
 
 size_t attn_workspace_bytes(int B, int H, int n, int d) {
@@ -715,11 +724,11 @@ const char* attn_strerror(int code) {
     case ATTN_OK: return "success";
     case ATTN_E_NULL: return "a required pointer is NULL";
     case ATTN_E_SHAPE: return "B, H or n < 1, or the problem is too large to index";
-    case ATTN_E_UNSUPPORTED: return "unsupported head dimension (d must be 32, 64 or 128) or dtype";
-    case ATTN_E_ALIGN: return "a tensor is not 16-byte aligned (L and workspace: 4-byte)";
+    case ATTN_E_UNSUPPORTED: return "unsupported head dimension (d must be 32, 64 or 128), dtype, rotated columns or page size";
+    case ATTN_E_ALIGN: return "a tensor or its strides are not 16-byte aligned (L and workspace: 4-byte)";
     case ATTN_E_WORKSPACE: return "workspace smaller than attn_workspace_bytes(), or P smaller than attn_mat_bytes()";
     case ATTN_E_HIP: return "the HIP runtime rejected a kernel launch";
-    case ATTN_E_ARG: return "scale is not finite, or causal is not 0 or 1";
+    case ATTN_E_ARG: return "scale or amplitude not finite, a flag not 0 or 1, or an output whose rows overlap";
     case ATTN_E_SCRATCH:
       return "B * H * n exceeds attn_noalloc_max_rows(), the rows the fixed scratch of attn_fwd_bwd_noalloc holds";
     default: return "unknown attn status code";

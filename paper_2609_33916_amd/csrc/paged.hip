@@ -1,0 +1,361 @@
+// C ABI of the rotary positions and the paged key/value cache (declared in
+// include/attn_mi355x.h): argument validation, plans and launches. As in attn.hip,
+// everything is validated on the host before any HIP call.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <climits>
+#include <cmath>
+#include <cstdint>
+#include <type_traits>
+#include <utility>
+
+#include "attn_mi355x.h"
+#include "launch.hpp"
+#include "paged.hpp"
+
+namespace {
+
+using attn::bf16;
+using attn::Strides;
+
+bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+
+bool good_d(int d) { return d == 32 || d == 64 || d == 128; }
+
+// The rotation's arguments; `freqs` null: none.
+int check_rotation(const double* freqs, int r, int d, float amplitude, int interleaved) {
+  if (interleaved != 0 && interleaved != 1) return ATTN_E_ARG;
+  if (!freqs) return ATTN_OK;
+  if (!std::isfinite(amplitude)) return ATTN_E_ARG;
+  if (r < 16 || r > d || r % 16 != 0) return ATTN_E_UNSUPPORTED;
+  return aligned(freqs, 8) ? ATTN_OK : ATTN_E_ALIGN;
+}
+attn::Rotation rotation(const double* freqs, int r, float amplitude) {
+  attn::Rotation rot{};
+  rot.freqs = freqs;
+  rot.r = freqs ? r : 0;
+  rot.amplitude = amplitude;
+  return rot;
+}
+
+// The caller's strides (sequence, head, token), or those of a dense [B, H, n, d].
+// That of an axis of one entry says nothing.
+Strides strides_of(const long long* s, int B, int H, int n, int d) {
+  Strides r = {(long long)H * n * d, (long long)n * d, d};
+  if (s) r = {s[0], s[1], s[2]};
+  if (B == 1) r.b = 0;
+  if (H == 1) r.h = 0;
+  if (n == 1) r.t = 0;
+  return r;
+}
+// Rows start at multiples of 16 bytes.
+bool aligned(const Strides& s, int elem) {
+  const int m = 16 / elem;
+  return s.b % m == 0 && s.h % m == 0 && s.t % m == 0;
+}
+// Rows of a written tensor must not overlap: from the smallest stride on, each
+// has to step over all that the smaller ones span.
+bool writable(const Strides& s, int B, int H, int n, int d) {
+  struct { long long step; int size; } dim[3] = {{s.b, B}, {s.h, H}, {s.t, n}};
+  std::sort(dim, dim + 3, [](const auto& x, const auto& y) { return x.step < y.step; });
+  __int128 span = d;
+  for (const auto& x : dim) {
+    if (x.size == 1) continue;
+    if (x.step < span) return false;
+    span += (__int128)x.step * (x.size - 1);
+  }
+  return true;
+}
+bool fits(const Strides& s, int B, int H, int n) {   // offsets in 62 bits
+  __int128 far = 0;
+  for (const auto& [step, size] : {std::pair<long long, int>{s.b, B}, {s.h, H}, {s.t, n}}) {
+    if (step < 0) return false;
+    far += (__int128)step * (size - 1);
+  }
+  return far < ((__int128)1 << 60);
+}
+
+// Heads per workgroup: a thread's sines and cosines serve all of them, so as many
+// as leave eight workgroups per compute unit.
+int heads_per_group(long long token_blocks, int heads) {
+  const long long want = attn::kXcds * attn::kCusPerXcd * 8;
+  return (int)std::max<long long>(1, std::min<long long>(heads, token_blocks * heads / want));
+}
+
+template <typename T> void launch_rope(attn::RopeArgs a, bool interleaved, hipStream_t st) {
+  const int per = 256 / (a.d / (2 * attn::Chunk<T>::N));
+  const unsigned blocks = (unsigned)((a.tokens + (long long)per - 1) / per);
+  a.hgroup = heads_per_group(blocks, a.Hq + a.Hk);
+  const dim3 grid(blocks, (a.Hq + a.Hk + a.hgroup - 1) / a.hgroup);
+  if (interleaved) hipLaunchKernelGGL((attn::rope_kernel<T, true>), grid, dim3(256), 0, st, a);
+  else hipLaunchKernelGGL((attn::rope_kernel<T, false>), grid, dim3(256), 0, st, a);
+}
+
+int rope(const void* q, const void* k, void* q_out, void* k_out, const long long* strides, const double* freqs,
+         const int* positions, long long pos_stride, int start, int B, int Hq, int Hk, int n, int d, int r,
+         float amplitude, int interleaved, int dtype, void* stream, float sign) {
+  if (!q || !q_out || !freqs || (k == nullptr) != (k_out == nullptr)) return ATTN_E_NULL;
+  if (!k) Hk = 0;
+  if (B < 1 || Hq < 1 || (k && Hk < 1) || n < 1) return ATTN_E_SHAPE;
+  if (dtype != ATTN_BF16 && dtype != ATTN_F32) return ATTN_E_UNSUPPORTED;
+  if (!good_d(d)) return ATTN_E_UNSUPPORTED;
+  if (const int rc = check_rotation(freqs, r, d, amplitude, interleaved)) return rc;
+  const int elem = dtype == ATTN_BF16 ? 2 : 4;
+  if ((long long)B * n > INT_MAX || (long long)Hq + Hk > 65535) return ATTN_E_SHAPE;
+  if (positions ? pos_stride < 0 || pos_stride > LLONG_MAX / B : start > INT_MAX - n) return ATTN_E_SHAPE;
+  attn::RopeArgs a{};
+  a.q = q; a.k = k; a.qo = q_out; a.ko = k_out;
+  a.qs = strides_of(strides, B, Hq, n, d);
+  a.qos = strides_of(strides ? strides + 6 : nullptr, B, Hq, n, d);
+  if (!fits(a.qs, B, Hq, n) || !fits(a.qos, B, Hq, n)) return ATTN_E_SHAPE;
+  if (!aligned(q, 16) || !aligned(q_out, 16) || !aligned(a.qs, elem) || !aligned(a.qos, elem) ||
+      (positions && !aligned(positions, 4)))
+    return ATTN_E_ALIGN;
+  if (!writable(a.qos, B, Hq, n, d)) return ATTN_E_ARG;
+  if (k) {
+    a.ks = strides_of(strides ? strides + 3 : nullptr, B, Hk, n, d);
+    a.kos = strides_of(strides ? strides + 9 : nullptr, B, Hk, n, d);
+    if (!fits(a.ks, B, Hk, n) || !fits(a.kos, B, Hk, n)) return ATTN_E_SHAPE;
+    if (!aligned(k, 16) || !aligned(k_out, 16) || !aligned(a.ks, elem) || !aligned(a.kos, elem)) return ATTN_E_ALIGN;
+    if (!writable(a.kos, B, Hk, n, d)) return ATTN_E_ARG;
+  }
+  a.pos = positions;
+  a.pos_stride = pos_stride;
+  a.start = start;
+  a.rot = rotation(freqs, r, amplitude);
+  a.Hq = Hq; a.Hk = Hk; a.n = n; a.d = d;
+  a.tokens = B * n;
+  a.sign = sign;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  (void)hipGetLastError();
+  if (dtype == ATTN_BF16) launch_rope<bf16>(a, interleaved, st);
+  else launch_rope<float>(a, interleaved, st);
+  return hipGetLastError() == hipSuccess ? ATTN_OK : ATTN_E_HIP;
+}
+
+// A pool and its tables.
+int check_pages(const void* kp, const void* vp, const void* ksc, const void* vsc, const int* table, const int* lens,
+                int B, int Hkv, int num_pages, int page_size, int width, int d, int dtype) {
+  if (!kp || !vp || !table || !lens || (ksc == nullptr) != (vsc == nullptr)) return ATTN_E_NULL;
+  if (B < 1 || Hkv < 1 || num_pages < 1 || width < 1) return ATTN_E_SHAPE;
+  if (dtype != ATTN_BF16 || !good_d(d)) return ATTN_E_UNSUPPORTED;
+  if (page_size < attn::kGranule || page_size > (1 << 20) || (page_size & (page_size - 1)) != 0) return ATTN_E_UNSUPPORTED;
+  if ((__int128)num_pages * Hkv * page_size * d > ((__int128)1 << 46)) return ATTN_E_SHAPE;
+  if (B > 65535 || Hkv > 65535) return ATTN_E_SHAPE;   // grid limits
+  if (!aligned(kp, 16) || !aligned(vp, 16) || !aligned(ksc, 16) || !aligned(vsc, 16) || !aligned(table, 4) ||
+      !aligned(lens, 4))
+    return ATTN_E_ALIGN;
+  return ATTN_OK;
+}
+attn::Pages pages_of(const int* table, int Hkv, int num_pages, int page_size, int width) {
+  attn::Pages p{};
+  p.table = table;
+  p.width = width;
+  p.num_pages = num_pages;
+  while ((1 << p.shift) < page_size) ++p.shift;
+  p.Hkv = Hkv;
+  return p;
+}
+
+void launch_append(attn::AppendArgs a, bool interleaved, hipStream_t st) {
+  const bool q4 = a.ksc != nullptr;
+  const int per = 256 / (a.d / (q4 ? 8 : 16));
+  const unsigned blocks = (unsigned)((a.tokens + (long long)per - 1) / per);
+  a.hgroup = heads_per_group(blocks, a.pg.Hkv);
+  const dim3 grid(blocks, (a.pg.Hkv + a.hgroup - 1) / a.hgroup);
+  if (q4) {
+    if (interleaved) hipLaunchKernelGGL(attn::append4_kernel<true>, grid, dim3(256), 0, st, a);
+    else hipLaunchKernelGGL(attn::append4_kernel<false>, grid, dim3(256), 0, st, a);
+  } else {
+    if (interleaved) hipLaunchKernelGGL(attn::append_kernel<true>, grid, dim3(256), 0, st, a);
+    else hipLaunchKernelGGL(attn::append_kernel<false>, grid, dim3(256), 0, st, a);
+  }
+}
+
+// Decode: a workgroup owns (sequence, cache head, up to 32 query heads, one split
+// of the keys); the keys are split, into whole tiles of four blocks, until there
+// are about two workgroups per compute unit.
+struct PagedPlan {
+  int nq;        // query columns of a workgroup / 16
+  int qchunks, nsplit;
+};
+PagedPlan paged_plan(int B, int Hq, int Hkv, int n, int append, bool q4) {
+  PagedPlan p;
+  const int G = Hq / Hkv, tile = q4 ? 256 : 128;
+  p.nq = G > 16 ? 2 : 1;
+  p.qchunks = (G + 16 * p.nq - 1) / (16 * p.nq);
+  const long long groups = (long long)B * Hkv * p.qchunks;
+  const long long tiles = std::max<long long>(1, ((long long)n + append + tile - 1) / tile);
+  long long ns = std::min(std::max<long long>(1, (512 + groups - 1) / groups), tiles);
+  const long long per = (tiles + ns - 1) / ns;
+  p.nsplit = (int)((tiles + per - 1) / per);
+  return p;
+}
+
+template <int D> void launch_decode(const attn::PagedArgs& a, const dim3& grid, int nq, hipStream_t st) {
+  const dim3 block(256);
+  if (a.ksc) {
+    if (nq == 1) hipLaunchKernelGGL((attn::paged_decode_kernel<D, 1, true>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((attn::paged_decode_kernel<D, 2, true>), grid, block, 0, st, a);
+  } else {
+    if (nq == 1) hipLaunchKernelGGL((attn::paged_decode_kernel<D, 1, false>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((attn::paged_decode_kernel<D, 2, false>), grid, block, 0, st, a);
+  }
+}
+
+}  // namespace
+
+extern "C" {
+
+int attn_rope(const void* q, const void* k, void* q_out, void* k_out, const long long* strides, const double* freqs,
+              const int* positions, long long pos_stride, int start, int B, int Hq, int Hk, int n, int d, int r,
+              float amplitude, int interleaved, int dtype, void* stream) {
+  return rope(q, k, q_out, k_out, strides, freqs, positions, pos_stride, start, B, Hq, Hk, n, d, r, amplitude,
+              interleaved, dtype, stream, 1.f);
+}
+
+int attn_rope_bwd(const void* dq, const void* dk, void* dq_in, void* dk_in, const long long* strides, const double* freqs,
+                  const int* positions, long long pos_stride, int start, int B, int Hq, int Hk, int n, int d, int r,
+                  float amplitude, int interleaved, int dtype, void* stream) {
+  return rope(dq, dk, dq_in, dk_in, strides, freqs, positions, pos_stride, start, B, Hq, Hk, n, d, r, amplitude,
+              interleaved, dtype, stream, -1.f);
+}
+
+int attn_paged_append(const void* k_new, const void* v_new, const long long* strides, void* k_pages, void* v_pages,
+                      void* k_scales, void* v_scales, const int* block_table, const int* lens, const int* new_lens,
+                      const double* freqs, const int* positions, int B, int Hkv, int T, int num_pages, int page_size,
+                      int table_width, int d, int r, float amplitude, int interleaved, int dtype, void* stream) {
+  if (!k_new || !v_new) return ATTN_E_NULL;
+  if (const int rc = check_pages(k_pages, v_pages, k_scales, v_scales, block_table, lens, B, Hkv, num_pages, page_size,
+                                 table_width, d, dtype))
+    return rc;
+  if (T < 1 || (long long)B * T > INT_MAX) return ATTN_E_SHAPE;
+  if (const int rc = check_rotation(freqs, r, d, amplitude, interleaved)) return rc;
+  attn::AppendArgs a{};
+  a.k_new = k_new; a.v_new = v_new;
+  a.ks = strides_of(strides, B, Hkv, T, d);
+  a.vs = strides_of(strides ? strides + 3 : nullptr, B, Hkv, T, d);
+  if (!fits(a.ks, B, Hkv, T) || !fits(a.vs, B, Hkv, T)) return ATTN_E_SHAPE;
+  if (!aligned(k_new, 16) || !aligned(v_new, 16) || !aligned(a.ks, 2) || !aligned(a.vs, 2) ||
+      !aligned(new_lens, 4) || !aligned(positions, 4))
+    return ATTN_E_ALIGN;
+  a.kp = k_pages; a.vp = v_pages;
+  a.ksc = static_cast<uint8_t*>(k_scales); a.vsc = static_cast<uint8_t*>(v_scales);
+  a.pg = pages_of(block_table, Hkv, num_pages, page_size, table_width);
+  a.lens = lens; a.new_lens = new_lens;
+  a.pos = positions;
+  a.rot = rotation(freqs, r, amplitude);
+  a.T = T; a.d = d; a.tokens = B * T;
+  a.limit = -1;
+  (void)hipGetLastError();
+  launch_append(a, interleaved, static_cast<hipStream_t>(stream));
+  return hipGetLastError() == hipSuccess ? ATTN_OK : ATTN_E_HIP;
+}
+
+int attn_paged_gather(const void* k_pages, const void* v_pages, const void* k_scales, const void* v_scales,
+                      const int* block_table, const int* lens, const int* starts, void* K, void* V, int B, int Hkv,
+                      int n, int num_pages, int page_size, int table_width, int d, int dtype, void* stream) {
+  if (!K || !V) return ATTN_E_NULL;
+  if (const int rc = check_pages(k_pages, v_pages, k_scales, v_scales, block_table, lens, B, Hkv, num_pages, page_size,
+                                 table_width, d, dtype))
+    return rc;
+  if (n < 1 || (__int128)B * Hkv * n * d > ((__int128)1 << 46)) return ATTN_E_SHAPE;
+  if (!aligned(K, 16) || !aligned(V, 16) || !aligned(starts, 4)) return ATTN_E_ALIGN;
+  attn::GatherArgs a{};
+  a.kp = k_pages; a.vp = v_pages;
+  a.ksc = static_cast<const uint8_t*>(k_scales); a.vsc = static_cast<const uint8_t*>(v_scales);
+  a.pg = pages_of(block_table, Hkv, num_pages, page_size, table_width);
+  a.lens = lens; a.starts = starts;
+  a.k = K; a.v = V;
+  a.n = n; a.d = d;
+  const int per = 256 / (d / 8);
+  const dim3 grid((unsigned)((n + (long long)per - 1) / per), Hkv, B);
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  (void)hipGetLastError();
+  if (k_scales) hipLaunchKernelGGL(attn::gather_kernel<true>, grid, dim3(256), 0, st, a);
+  else hipLaunchKernelGGL(attn::gather_kernel<false>, grid, dim3(256), 0, st, a);
+  return hipGetLastError() == hipSuccess ? ATTN_OK : ATTN_E_HIP;
+}
+
+size_t attn_paged_decode_workspace_bytes(int B, int Hq, int Hkv, int n, int d, int append, int bits) {
+  if (B < 1 || Hq < 1 || Hkv < 1 || Hq % Hkv != 0 || n < 0 || !good_d(d) || (bits != 16 && bits != 4)) return 0;
+  const PagedPlan p = paged_plan(B, Hq, Hkv, n, append ? 1 : 0, bits == 4);
+  if (p.nsplit == 1) return 0;
+  return (size_t)B * Hq * p.nsplit * (size_t)(d + 2) * sizeof(float);
+}
+
+int attn_paged_decode(const void* q, const void* k_new, const void* v_new, const long long* strides, void* k_pages,
+                      void* v_pages, void* k_scales, void* v_scales, const int* block_table, const int* lens,
+                      const double* freqs, const int* positions, void* O, float* L, void* workspace,
+                      size_t workspace_bytes, int B, int Hq, int Hkv, int n, int num_pages, int page_size,
+                      int table_width, int d, int r, float amplitude, int interleaved, float scale, int dtype,
+                      void* stream) {
+  if (!q || !O || (k_new == nullptr) != (v_new == nullptr)) return ATTN_E_NULL;
+  if (const int rc = check_pages(k_pages, v_pages, k_scales, v_scales, block_table, lens, B, Hkv, num_pages, page_size,
+                                 table_width, d, dtype))
+    return rc;
+  const int append = k_new ? 1 : 0;
+  const bool q4 = k_scales != nullptr;
+  if (Hq < 1 || Hq % Hkv != 0 || n < 0 || n > INT_MAX - 1024) return ATTN_E_SHAPE;
+  if ((long long)n + append > (long long)table_width * page_size) return ATTN_E_SHAPE;
+  if ((long long)B * Hq > INT_MAX) return ATTN_E_SHAPE;
+  if (!std::isfinite(scale)) return ATTN_E_ARG;
+  if (const int rc = check_rotation(freqs, r, d, amplitude, interleaved)) return rc;
+  // elements between sequences; with one of them the caller's say nothing
+  const bool given = strides && B > 1;
+  const long long row_q = given ? strides[0] : (long long)Hq * d, row_k = given ? strides[1] : (long long)Hkv * d,
+                  row_v = given ? strides[2] : (long long)Hkv * d;
+  for (const long long s : {row_q, row_k, row_v}) {
+    if (s < 0 || s > (1LL << 44)) return ATTN_E_SHAPE;
+    if (s % 8 != 0) return ATTN_E_ALIGN;
+  }
+  if (!aligned(q, 16) || !aligned(k_new, 16) || !aligned(v_new, 16) || !aligned(O, 16) || !aligned(L, 4) ||
+      !aligned(positions, 4))
+    return ATTN_E_ALIGN;
+  const PagedPlan plan = paged_plan(B, Hq, Hkv, n, append, q4);
+  if ((long long)B * Hkv * plan.qchunks > 65535) return ATTN_E_SHAPE;   // grid y limit
+  const size_t need = attn_paged_decode_workspace_bytes(B, Hq, Hkv, n, d, append, q4 ? 4 : 16);
+  if (need > 0) {
+    if (!workspace) return ATTN_E_NULL;
+    if (!aligned(workspace, 16)) return ATTN_E_ALIGN;
+    if (workspace_bytes < need) return ATTN_E_WORKSPACE;
+  }
+  attn::PagedArgs a{};
+  a.q = q; a.k_new = k_new; a.v_new = v_new;
+  a.q_b = row_q; a.k_b = row_k; a.v_b = row_v;
+  a.kp = k_pages; a.vp = v_pages;
+  a.ksc = static_cast<uint8_t*>(k_scales); a.vsc = static_cast<uint8_t*>(v_scales);
+  a.pg = pages_of(block_table, Hkv, num_pages, page_size, table_width);
+  a.lens = lens; a.pos = positions;
+  a.rot = rotation(freqs, r, amplitude);
+  a.part = static_cast<float*>(workspace);
+  a.o = O; a.lse = L;
+  a.Hq = Hq; a.G = Hq / Hkv; a.n = n; a.append = append; a.rows = B * Hq;
+  a.fuse_append = append && plan.qchunks == 1;
+  a.nsplit = plan.nsplit; a.qchunks = plan.qchunks;
+  // a zero scale would turn masked scores into NaN: see split_scale in attn.hip
+  a.sl2 = std::fmax(std::fabs(scale) * attn::kLog2e, 1e-30f);
+  a.interleaved = interleaved;
+  a.negate = scale < 0.f;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  (void)hipGetLastError();
+  if (append && !a.fuse_append) {   // several workgroups read the new row: it is written before them
+    attn::AppendArgs w{};
+    w.k_new = k_new; w.v_new = v_new;
+    w.ks = {row_k, d, 0}; w.vs = {row_v, d, 0};
+    w.kp = k_pages; w.vp = v_pages; w.ksc = a.ksc; w.vsc = a.vsc;
+    w.pg = a.pg; w.lens = lens; w.limit = n;
+    w.pos = positions; w.rot = a.rot;
+    w.T = 1; w.d = d; w.tokens = B;
+    launch_append(w, interleaved, st);
+  }
+  const dim3 grid(plan.nsplit, B * Hkv * plan.qchunks);
+  if (d == 32) launch_decode<32>(a, grid, plan.nq, st);
+  else if (d == 64) launch_decode<64>(a, grid, plan.nq, st);
+  else launch_decode<128>(a, grid, plan.nq, st);
+  if (plan.nsplit > 1) attn::launch_paged_combine(a.part, O, L, a.rows, plan.nsplit, d, st);
+  return hipGetLastError() == hipSuccess ? ATTN_OK : ATTN_E_HIP;
+}
+
+}  // extern "C"

@@ -1,0 +1,189 @@
+// Rotary positions: a head's columns are taken in pairs, and pair i of the token
+// at position p is turned by the angle p f_i and stretched by an amplitude a:
+//   u' = a (u cos t - w sin t),  w' = a (w cos t + u sin t),  t = p f_i.
+// The first r columns are paired, (x_i, x_{i + r/2}) or interleaved
+// (x_{2i}, x_{2i+1}); columns from r on stay as they are. The transpose of a
+// turn is the turn back, so the gradient is the same with sin t negated. A
+// scaling for long contexts is a choice of the f_i and of a, made by the caller.
+//
+// The f_i are float64 and the angle is reduced to a fraction of a circle in 64
+// bits: in 32 bits the angle of position 10^6 would be off by 0.03 radian. The
+// sine and cosine of the remaining fraction are float32 (within 2 units in the
+// last place, far below the rounding of a bfloat16 result and at that of a float32
+// one); where the result is rounded to 4 bits they are float64 (see Quant4).
+#pragma once
+
+#include "common.hpp"
+#include "pages.hpp"
+
+namespace attn {
+
+struct Rotation {
+  const double* freqs;   // [r / 2] radians per position
+  int r;                 // columns that turn (a multiple of 16), 0: none
+  float amplitude;
+};
+
+// p f, as a fraction of a circle in [-1/2, 1/2]
+__device__ __forceinline__ double turn(int p, double f) {
+  const double x = (double)p * f * 0.15915494309189535;   // 1 / (2 pi)
+  return x - rint(x);
+}
+__device__ __forceinline__ void turn_cs(int p, const Rotation& rot, int i, float& c, float& s) {
+  float c0, s0;
+  sincospif((float)(2.0 * turn(p, rot.freqs[i])), &s0, &c0);
+  c = c0 * rot.amplitude;
+  s = s0 * rot.amplitude;
+}
+__device__ __forceinline__ void turn_cs(int p, const Rotation& rot, int i, double& c, double& s) {
+  double c0, s0;
+  sincospi(2.0 * turn(p, rot.freqs[i]), &s0, &c0);
+  c = c0 * (double)rot.amplitude;
+  s = s0 * (double)rot.amplitude;
+}
+
+// 16 bytes of a row and its values
+template <typename T> struct Chunk;
+template <> struct Chunk<bf16> {
+  static constexpr int N = 8;
+  __device__ __forceinline__ static void get(u32x4 x, float (&v)[8]) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      v[2 * e] = __uint_as_float(x[e] << 16);
+      v[2 * e + 1] = __uint_as_float(x[e] & 0xffff0000u);
+    }
+  }
+  __device__ __forceinline__ static u32x4 put(const float (&v)[8]) {
+    u32x4 x;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = pack_bf16x2(v[2 * e], v[2 * e + 1]);
+    return x;
+  }
+};
+template <> struct Chunk<float> {
+  static constexpr int N = 4;
+  __device__ __forceinline__ static void get(u32x4 x, float (&v)[4]) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = __uint_as_float(x[e]);
+  }
+  __device__ __forceinline__ static u32x4 put(const float (&v)[4]) {
+    return (u32x4){__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+  }
+};
+
+// A thread's two 16-byte chunks of a row and the N pairs between them. Thread j
+// of the d / 2N that share a row takes chunk j of the first half of the pairs and
+// of the second, or (interleaved) chunks 2j and 2j + 1; past the rotated columns,
+// two neighbouring chunks to copy. Both loads of a wave then cover whole
+// 128-byte lines of a bf16 row, and a pair never leaves its thread, so a row
+// may be turned in place.
+template <typename T, bool INTER> struct PairChunks {
+  static constexpr int N = Chunk<T>::N;
+  int col[2];
+  bool turns;
+  float c[N], s[N];
+  __device__ __forceinline__ PairChunks(const Rotation& rot, int j, int p, float sign) {
+    const int nrot = rot.r / (2 * N);
+    turns = j < nrot;
+    if (turns && !INTER) {
+      col[0] = N * j;
+      col[1] = rot.r / 2 + N * j;
+    } else {
+      col[0] = 2 * N * j;
+      col[1] = 2 * N * j + N;
+    }
+#pragma unroll
+    for (int e = 0; e < N; ++e) c[e] = 1.f, s[e] = 0.f;
+    if (turns) {
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        turn_cs(p, rot, N * j + e, c[e], s[e]);
+        s[e] *= sign;
+      }
+    }
+  }
+  __device__ __forceinline__ void apply(u32x4& xa, u32x4& xb) const {
+    if (!turns) return;   // the copied columns keep their bits
+    float a[N], b[N];
+    Chunk<T>::get(xa, a);
+    Chunk<T>::get(xb, b);
+    if (INTER) {
+#pragma unroll
+      for (int e = 0; e < N / 2; ++e) {
+        const float u = a[2 * e], w = a[2 * e + 1], u2 = b[2 * e], w2 = b[2 * e + 1];
+        const int f = N / 2 + e;
+        a[2 * e] = u * c[e] - w * s[e];
+        a[2 * e + 1] = w * c[e] + u * s[e];
+        b[2 * e] = u2 * c[f] - w2 * s[f];
+        b[2 * e + 1] = w2 * c[f] + u2 * s[f];
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        const float u = a[e], w = b[e];
+        a[e] = u * c[e] - w * s[e];
+        b[e] = w * c[e] + u * s[e];
+      }
+    }
+    xa = Chunk<T>::put(a);
+    xb = Chunk<T>::put(b);
+  }
+};
+
+// ---------------------------------------------------------------- attn_rope --
+struct Strides {
+  long long b, h, t;   // elements between sequences, heads, tokens
+};
+struct RopeArgs {
+  const void *q, *k;
+  void *qo, *ko;
+  Strides qs, ks, qos, kos;
+  const int* pos;          // positions, or null: start + token
+  long long pos_stride;    // entries between sequences (0: shared)
+  int start;
+  Rotation rot;
+  int Hq, Hk, n, d;
+  int tokens;              // B n
+  int hgroup;              // heads (q's, then k's) per workgroup
+  float sign;              // of the sine: -1 for the gradient
+};
+
+// Bound by memory: every element is read and written once. The angles belong to a
+// token, not to a head, so a thread keeps its pairs' sines and cosines in registers
+// and walks over the heads, U at a time with all their loads in flight.
+template <typename T, bool INTER>
+__global__ void __launch_bounds__(256) rope_kernel(const RopeArgs a) {
+  constexpr int N = Chunk<T>::N, U = 4;
+  const int tpt = a.d / (2 * N);   // threads per token
+  const int j = threadIdx.x % tpt;
+  const int tok = blockIdx.x * (256 / tpt) + threadIdx.x / tpt;
+  if (tok >= a.tokens) return;
+  const int b = tok / a.n, i = tok - b * a.n;
+  const int p = a.pos ? a.pos[b * a.pos_stride + i] : a.start + i;
+  const PairChunks<T, INTER> pc(a.rot, j, p, a.sign);
+  const int h1 = min((int)(blockIdx.y + 1) * a.hgroup, a.Hq + a.Hk);
+  for (int h0 = blockIdx.y * a.hgroup; h0 < h1; h0 += U) {
+    u32x4 xa[U], xb[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (h0 + u < h1) {
+        const bool isk = h0 + u >= a.Hq;
+        const Strides& st = isk ? a.ks : a.qs;
+        const T* src = (const T*)(isk ? a.k : a.q) + b * st.b + (h0 + u - (isk ? a.Hq : 0)) * st.h + i * st.t;
+        xa[u] = *(const u32x4*)(src + pc.col[0]);
+        xb[u] = *(const u32x4*)(src + pc.col[1]);
+      }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (h0 + u < h1) {
+        const bool isk = h0 + u >= a.Hq;
+        const Strides& st = isk ? a.kos : a.qos;
+        T* dst = (T*)(isk ? a.ko : a.qo) + b * st.b + (h0 + u - (isk ? a.Hq : 0)) * st.h + i * st.t;
+        pc.apply(xa[u], xb[u]);
+        *(u32x4*)(dst + pc.col[0]) = xa[u];
+        *(u32x4*)(dst + pc.col[1]) = xb[u];
+      }
+  }
+}
+
+}  // namespace attn
