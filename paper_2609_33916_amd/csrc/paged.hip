@@ -174,22 +174,21 @@ void launch_append(attn::AppendArgs a, bool interleaved, hipStream_t st) {
 }
 
 // Decode: a workgroup owns (sequence, cache head, up to 32 query heads, one split
-// of the keys); the keys are split, into whole tiles of four blocks, until there
-// are about two workgroups per compute unit.
+// of the keys); the keys are split, a block for each of its four waves at
+// least, until there are about two workgroups per compute unit.
+constexpr long long kWorkgroups = 512;
 struct PagedPlan {
   int nq;        // query columns of a workgroup / 16
   int qchunks, nsplit;
 };
 PagedPlan paged_plan(int B, int Hq, int Hkv, int n, int append, bool q4) {
   PagedPlan p;
-  const int G = Hq / Hkv, tile = q4 ? 256 : 128;
+  const int G = Hq / Hkv, block = q4 ? 64 : 32;
   p.nq = G > 16 ? 2 : 1;
   p.qchunks = (G + 16 * p.nq - 1) / (16 * p.nq);
   const long long groups = (long long)B * Hkv * p.qchunks;
-  const long long tiles = std::max<long long>(1, ((long long)n + append + tile - 1) / tile);
-  long long ns = std::min(std::max<long long>(1, (512 + groups - 1) / groups), tiles);
-  const long long per = (tiles + ns - 1) / ns;
-  p.nsplit = (int)((tiles + per - 1) / per);
+  const long long blocks = ((long long)n + append + block - 1) / block;
+  p.nsplit = (int)std::max<long long>(1, std::min((kWorkgroups + groups - 1) / groups, blocks / 4));
   return p;
 }
 

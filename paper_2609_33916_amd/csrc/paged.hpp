@@ -286,106 +286,231 @@ struct PagedArgs {
 
 typedef const __attribute__((address_space(4))) int* ConstInt;   // uniform reads by the scalar unit
 
+// A barrier that orders LDS only: loads stay in flight across it.
+__device__ __forceinline__ void lds_barrier() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
+// A buffer of `bytes` bytes; W words of each lane at byte offset `off`, zeros
+// behind its end.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_rsrc(const void* base, int bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), (short)0, bytes, 0x00020000);
+}
+// The pages are read once per step, and between two steps a model reads far more
+// than the caches hold: 16 sequences of 8192 tokens, 64 heads, d = 128 82.4 us a
+// step, 93.5 with ordinary loads; one of 131072 in 4 bits 31.6, 33.7; small calls the
+// same to 1 %.
+constexpr int kNonTemporal = 2;
+template <int W> struct Words;
+template <> struct Words<1> {
+  typedef uint32_t type;
+  __device__ __forceinline__ static type load(__amdgpu_buffer_rsrc_t r, unsigned off) {
+    return __builtin_amdgcn_raw_buffer_load_b32(r, off, 0, kNonTemporal);
+  }
+};
+template <> struct Words<2> {
+  typedef u32x2 type;
+  __device__ __forceinline__ static type load(__amdgpu_buffer_rsrc_t r, unsigned off) {
+    return __builtin_amdgcn_raw_buffer_load_b64(r, off, 0, kNonTemporal);
+  }
+};
+template <> struct Words<4> {
+  typedef u32x4 type;
+  __device__ __forceinline__ static type load(__amdgpu_buffer_rsrc_t r, unsigned off) {
+    return __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, kNonTemporal);
+  }
+};
+__device__ __forceinline__ uint32_t word(uint32_t x, int) { return x; }
+template <typename V> __device__ __forceinline__ uint32_t word(V x, int i) { return x[i]; }
+// f(word, its index) of every word
+template <typename F> __device__ __forceinline__ uint32_t map_words(uint32_t x, F f) { return f(x, 0); }
+template <typename F> __device__ __forceinline__ u32x2 map_words(u32x2 x, F f) { return (u32x2){f(x[0], 0), f(x[1], 1)}; }
+template <typename F> __device__ __forceinline__ u32x4 map_words(u32x4 x, F f) {
+  return (u32x4){f(x[0], 0), f(x[1], 1), f(x[2], 2), f(x[3], 3)};
+}
+
 template <int D, int NQ, bool Q4>
 __global__ void __launch_bounds__(256, 2) paged_decode_kernel(const PagedArgs a) {
   constexpr int BK = Q4 ? 64 : 32, KB = BK / kGranule;   // keys of a block, in rows of 16
   constexpr int TD = D / 32, DB = D / 16;                // steps over d, output rows of 16
   constexpr int C = 16 * NQ;                             // query columns
-  constexpr int KW = Q4 ? TD : 4 * TD;                   // 32-bit words of K per lane and row of 16
   constexpr int RB = Q4 ? D / 2 : 2 * D;                 // bytes of a row
-  constexpr int NV = BK * RB / 1024;                     // 16-byte loads of V per lane
   constexpr int QS = D + 8;                              // row stride of the queries in LDS (elements)
-  constexpr int VBYTES = 4 * BK * RB, OBYTES = 4 * D * C * 4, QBYTES = 2 * C * QS * 2;
-  constexpr int BYTES = VBYTES > OBYTES ? VBYTES : OBYTES;
-  __shared__ __attribute__((aligned(16))) unsigned char smem[BYTES > QBYTES ? BYTES : QBYTES];
+  constexpr int VBYTES = 4 * BK * RB, OBYTES = 4 * D * C * 4;
+  constexpr int BYTES = VBYTES + 2 * C * QS * 2;
+  // the waves' stages of V and the queries; at the end the waves' O
+  __shared__ __attribute__((aligned(16))) unsigned char smem[BYTES > OBYTES ? BYTES : OBYTES];
   __shared__ float ml[2][4][C];
-  __shared__ __attribute__((aligned(16))) float nrow[2][D];   // 4 bits: the new key and value
+  // the new key and value as they are stored; 4 bits: their scales, and before that their values
+  __shared__ __attribute__((aligned(16))) uint32_t nrow[2][RB / 4];
+  __shared__ uint32_t nscale[2];
+  __shared__ float nval[2][Q4 ? D : 1];
 
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 4, c = lane & 15;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int split = (int)gridDim.x - 1 - (int)blockIdx.x;   // the one with the new row starts first
   const int qc = blockIdx.y % a.qchunks, bh = blockIdx.y / a.qchunks;
   const int b = bh / a.pg.Hkv, hk = bh - b * a.pg.Hkv;
-  const int len = min(max(a.lens[b], 0), a.n);
+  const int len = min(max(((ConstInt)(uintptr_t)a.lens)[b], 0), a.n);
   const int T_b = len + a.append;
-  const unsigned tiles = (unsigned)(T_b + 4 * BK - 1) / (4 * BK);
-  const int k_lo = 4 * BK * (int)(split * (size_t)tiles / a.nsplit);
-  const int k_hi = min(T_b, 4 * BK * (int)((split + 1) * (size_t)tiles / a.nsplit));
+  // the sequence's own blocks, evenly over the splits
+  const unsigned blocks = (unsigned)(T_b + BK - 1) / BK, ns = (unsigned)a.nsplit;
+  const unsigned per = blocks / ns, more = blocks - per * ns, us = (unsigned)split;
+  const int k_lo = BK * (int)(us * per + min(us, more));
+  const int k_hi = min(T_b, k_lo + BK * (int)(per + (us < more ? 1u : 0u)));
   const int h0 = hk * a.G + qc * C, nq = min(C, a.G - qc * C);
   const int* table = a.pg.table + (size_t)b * a.pg.width;
-  const int pos = a.pos ? a.pos[b] : T_b - 1;
+  const int pos = a.pos ? ((ConstInt)(uintptr_t)a.pos)[b] : T_b - 1;
+
+  // 4 bits: the byte, of the scales of 16 keys, of this lane's columns of its key
+  const int ksb = c * TD + g * TD / 4;
+  typedef Words<Q4 ? TD : 4> Part;   // of a row: a lane's loads
+  typedef typename Part::type part_t;
+  constexpr int NP = Q4 ? 1 : TD;
+  struct Block {
+    part_t k[KB][NP], v[KB][NP];
+    uint32_t ks[Q4 ? KB : 1];
+    part_t vs[Q4 ? KB : 1];
+    int lim[KB];   // keys of each row of 16 that take part
+  };
+  // page numbers of the block at key kv0 (a multiple of 16); behind the split, of its last key
+  struct Ids {
+    int page[KB];
+  };
+  auto fetch = [&](Ids& ids, int kv0) __attribute__((always_inline)) {
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+      ids.page[kb] = ((ConstInt)(uintptr_t)table)[min(kv0 + kGranule * kb, k_hi - 1) >> a.pg.shift];
+  };
+  // The block's loads. Each row of 16 has a buffer of its own that ends behind its last
+  // key, so what takes no part (keys behind the end, pages that are none, blocks
+  // behind the split) reads as zeros, without an access.
+  const unsigned koff = c * RB + (Q4 ? RB / 4 * g : 16 * g), voff = Q4 ? RB / 4 * lane : 16 * lane;
+  auto load = [&](Block& x, const Ids& ids, int kv0) __attribute__((always_inline)) {
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) {
+      const int p = kv0 + kGranule * kb;
+      const bool ok = p < k_hi && page_ok(a.pg, ids.page[kb]);
+      x.lim[kb] = ok ? min(k_hi - p, kGranule) : 0;
+      const long long row = ok ? (((long long)ids.page[kb] * a.pg.Hkv + hk) << a.pg.shift) + (p & ((1 << a.pg.shift) - 1)) : 0;
+      const auto kr = rows_rsrc((const unsigned char*)a.kp + row * RB, x.lim[kb] * RB);
+      const auto vr = rows_rsrc((const unsigned char*)a.vp + row * RB, x.lim[kb] * RB);
+      if constexpr (!Q4) {
+#pragma unroll
+        for (int t = 0; t < TD; ++t) x.k[kb][t] = Part::load(kr, koff + 64 * t);
+#pragma unroll
+        for (int t = 0; t < TD; ++t) x.v[kb][t] = Part::load(vr, voff + 1024 * t);
+      } else {
+        const int n = ok ? kGranule * TD : 0;
+        x.ks[kb] = Words<1>::load(rows_rsrc(a.ksc + row * TD, n), ksb & ~3);
+        x.k[kb][0] = Part::load(kr, koff);
+        x.v[kb][0] = Part::load(vr, voff);
+        x.vs[kb] = Part::load(rows_rsrc(a.vsc + row * TD, n), 4 * TD * g);
+      }
+    }
+  };
+  Block A, B2;
+  Ids ids;
+  int kv = k_lo + BK * w;
+  if (kv < k_hi) {   // in flight while the queries are made
+    fetch(ids, kv);
+    load(A, ids, kv);
+    fetch(ids, kv + 4 * BK);
+  }
+  // This split holds the new row: it writes it, and takes it from LDS itself.
+  const bool writes = a.fuse_append && T_b - 1 >= k_lo && T_b - 1 < k_hi;
 
   // ---- the queries, turned, as two bfloat16 each (their sum is 16 bits of the
   // result; one alone would cost L its last digits), and the new row
-  bf16* qh = (bf16*)smem;
-  bf16* ql = qh + C * QS;
+  bf16 *const qh = (bf16*)(smem + VBYTES), *const ql = qh + C * QS;
   {
     constexpr int P = D / 2;                    // pairs of a row, or neighbours that do not turn
     const int pr = tid % P, nrot = a.rot.r / 2;
-    const bool turns = pr < nrot;
-    const bool halves = turns && !a.interleaved;
+    const bool turns = pr < nrot, halves = turns && !a.interleaved;
     const int c0 = halves ? pr : 2 * pr, c1 = halves ? pr + nrot : 2 * pr + 1;
-    typedef typename std::conditional<Q4, double, float>::type R;
-    R cs = 1, sn = 0;
-    if (turns) turn_cs(pos, a.rot, pr, cs, sn);
-    for (int r = tid / P; r < C; r += 256 / P) {
-      float u = 0.f, x = 0.f;
-      if (r < nq) {
-        const bf16* src = (const bf16*)a.q + b * a.q_b + (size_t)(h0 + r) * D;
-        u = (float)src[c0];
-        x = (float)src[c1];
-      }
-      if (turns) {
-        const float u2 = u * (float)cs - x * (float)sn;
-        x = x * (float)cs + u * (float)sn;
-        u = u2;
-      }
-      if (a.negate) u = -u, x = -x;
-      const bf16 uh = (bf16)u, xh = (bf16)x;
-      qh[r * QS + c0] = uh;
-      qh[r * QS + c1] = xh;
-      ql[r * QS + c0] = (bf16)(u - (float)uh);
-      ql[r * QS + c1] = (bf16)(x - (float)xh);
+    float u[C * P / 256], x[C * P / 256];
+#pragma unroll
+    for (int i = 0; i < C * P / 256; ++i) {
+      const int r = tid / P + 256 / P * i;
+      const bf16* src = (const bf16*)a.q + b * a.q_b + (size_t)(h0 + min(r, nq - 1)) * D;
+      u[i] = (float)src[c0];
+      x[i] = (float)src[c1];
     }
-    // the split that holds the new row writes it; only this workgroup reads it,
-    // behind the barrier
-    const long long row = a.fuse_append && T_b - 1 >= k_lo && T_b - 1 < k_hi ? page_row(a.pg, table, T_b - 1) : -1;
-    if (row >= 0) {
-      const long long r = row + ((long long)hk << a.pg.shift);
-      const bf16* kn = (const bf16*)a.k_new + b * a.k_b + (size_t)hk * D;
-      const bf16* vn = (const bf16*)a.v_new + b * a.v_b + (size_t)hk * D;
+    float cs = 1.f, sn = 0.f;
+    if (turns) turn_cs(pos, a.rot, pr, cs, sn);
+#pragma unroll
+    for (int i = 0; i < C * P / 256; ++i) {
+      const int r = tid / P + 256 / P * i;
+      float y = u[i], z = x[i];
+      if (turns) {
+        y = u[i] * cs - x[i] * sn;
+        z = x[i] * cs + u[i] * sn;
+      }
+      if (r >= nq) y = z = 0.f;
+      if (a.negate) y = -y, z = -z;
+      const bf16 yh = (bf16)y, zh = (bf16)z;
+      qh[r * QS + c0] = yh;
+      qh[r * QS + c1] = zh;
+      ql[r * QS + c0] = (bf16)(turns ? y - (float)yh : 0.f);
+      ql[r * QS + c1] = (bf16)(turns ? z - (float)zh : 0.f);
+    }
+    if (writes) {
+      const long long at = page_row(a.pg, table, T_b - 1);
+      const long long r = at + ((long long)hk << a.pg.shift);
       if (tid < P) {
-        const R u = (R)(float)kn[c0], x = (R)(float)kn[c1];
-        const R u2 = turns ? u * cs - x * sn : u, x2 = turns ? x * cs + u * sn : x;
+        typedef typename std::conditional<Q4, double, float>::type R;
+        const bf16* kn = (const bf16*)a.k_new + b * a.k_b + (size_t)hk * D;
+        const bf16* vn = (const bf16*)a.v_new + b * a.v_b + (size_t)hk * D;
+        const bf16 v0 = vn[c0], v1 = vn[c1];
+        bf16 k0 = kn[c0], k1 = kn[c1];
+        R y = (R)(float)k0, z = (R)(float)k1;
+        if (turns) {
+          R rc, rs;
+          turn_cs(pos, a.rot, pr, rc, rs);
+          const R y2 = y * rc - z * rs;
+          z = z * rc + y * rs;
+          y = y2;
+          k0 = (bf16)y;
+          k1 = (bf16)z;
+        }
         if constexpr (Q4) {
-          nrow[0][c0] = Quant4::odd(u2);
-          nrow[0][c1] = Quant4::odd(x2);
-          nrow[1][c0] = (float)vn[c0];
-          nrow[1][c1] = (float)vn[c1];
+          nval[0][c0] = Quant4::odd(y);
+          nval[0][c1] = Quant4::odd(z);
+          nval[1][c0] = (float)v0;
+          nval[1][c1] = (float)v1;
         } else {
-          bf16 *kd = (bf16*)a.kp + r * D, *vd = (bf16*)a.vp + r * D;
-          kd[c0] = turns ? (bf16)u2 : kn[c0];
-          kd[c1] = turns ? (bf16)x2 : kn[c1];
-          vd[c0] = vn[c0];
-          vd[c1] = vn[c1];
+          bf16 *kd = (bf16*)nrow[0], *vd = (bf16*)nrow[1];
+          kd[c0] = k0, kd[c1] = k1;
+          vd[c0] = v0, vd[c1] = v1;
+          if (at >= 0) {
+            kd = (bf16*)a.kp + r * D, vd = (bf16*)a.vp + r * D;
+            kd[c0] = k0, kd[c1] = k1;
+            vd[c0] = v0, vd[c1] = v1;
+          }
         }
       }
       if constexpr (Q4) {
-        __syncthreads();   // row is the same for the whole workgroup
+        lds_barrier();   // the same for the whole workgroup
         if (tid < D / 4) {
           const int which = tid / (D / 8), ch = tid % (D / 8);
           float v[8];
 #pragma unroll
-          for (int e = 0; e < 8; ++e) v[e] = nrow[which][8 * ch + e];
+          for (int e = 0; e < 8; ++e) v[e] = nval[which][8 * ch + e];
           uint32_t sc;
-          const uint32_t x = Quant4::put(v, sc);
-          ((uint32_t*)(which ? a.vp : a.kp))[r * (D / 8) + ch] = x;
-          if (ch % 4 == 0) (which ? a.vsc : a.ksc)[r * (D / 32) + ch / 4] = (uint8_t)sc;
+          const uint32_t y = Quant4::put(v, sc);
+          nrow[which][ch] = y;
+          if (ch % 4 == 0) ((uint8_t*)&nscale[which])[ch / 4] = (uint8_t)sc;
+          if (at >= 0) {
+            ((uint32_t*)(which ? a.vp : a.kp))[r * (D / 8) + ch] = y;
+            if (ch % 4 == 0) (which ? a.vsc : a.ksc)[r * (D / 32) + ch / 4] = (uint8_t)sc;
+          }
         }
       }
     }
   }
-  __syncthreads();
+  lds_barrier();
   bf16x8 qf[NQ][TD], qr[NQ][TD];
 #pragma unroll
   for (int x = 0; x < NQ; ++x)
@@ -395,7 +520,6 @@ __global__ void __launch_bounds__(256, 2) paged_decode_kernel(const PagedArgs a)
       qf[x][t] = *(const bf16x8*)(qh + at);
       qr[x][t] = *(const bf16x8*)(ql + at);
     }
-  __syncthreads();   // the stages below take this memory
 
   f32x4 oacc[NQ][DB];
   float m_use[NQ], lsum[NQ];
@@ -407,106 +531,67 @@ __global__ void __launch_bounds__(256, 2) paged_decode_kernel(const PagedArgs a)
     for (int db = 0; db < DB; ++db) oacc[x][db] = (f32x4){0.f, 0.f, 0.f, 0.f};
   }
 
-  struct Block {
-    uint32_t k[KB][KW];
-    u32x4 v[NV];
-    uint32_t ks[Q4 ? KB : 1], vs[Q4 ? KB : 1][Q4 ? TD : 1];
-    int lim[KB];   // keys of each row of 16 that take part
-  };
-  // loads of the block at key kv0 (a multiple of 16, inside the table)
-  auto load = [&](Block& x, int kv0) __attribute__((always_inline)) {
-    long long row[KB];
+  unsigned char* vst = smem + w * (BK * RB);
+  const unsigned kshift = 8 * (ksb & 3);
+  const float sl2 = a.sl2;
+  // the new row in place of what its page held: lane (g, c) has a part of key c and,
+  // of V, 16 (bf16) or RB / 4 bytes at its place in the 16 rows
+  auto patch = [&](Block& x, int at) __attribute__((always_inline)) {
+    const int row = at & 15;
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) {
-      const int p = kv0 + kGranule * kb;
-      x.lim[kb] = 0;
-      row[kb] = 0;   // the first rows of page 0, which exist: never used
-      if (p < k_hi) {
-        const int page = ((ConstInt)(uintptr_t)table)[p >> a.pg.shift];
-        if (page_ok(a.pg, page)) {
-          row[kb] = (((long long)page * a.pg.Hkv + hk) << a.pg.shift) + (p & ((1 << a.pg.shift) - 1));
-          x.lim[kb] = min(k_hi - p, kGranule);
-        }
-      }
-    }
-#pragma unroll
-    for (int kb = 0; kb < KB; ++kb) {
-      const unsigned char* src = (const unsigned char*)a.kp + row[kb] * RB + c * RB + (Q4 ? RB / 4 * g : 16 * g);
+      const bool here = at >> 4 == kb;
+      const bool k_mine = here && c == row;
       if constexpr (!Q4) {
 #pragma unroll
         for (int t = 0; t < TD; ++t) {
-          const u32x4 y = *(const u32x4*)(src + 64 * t);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) x.k[kb][4 * t + e] = y[e];
+          if (k_mine) x.k[kb][t] = *(const u32x4*)&nrow[0][16 * t + 4 * g];
+          if (here && (1024 * t + voff) / RB == row) x.v[kb][t] = *(const u32x4*)&nrow[1][(1024 * t + voff) % RB / 4];
         }
       } else {
-        if constexpr (TD == 4) {
-          const u32x4 y = *(const u32x4*)src;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) x.k[kb][e] = y[e];
-        } else if constexpr (TD == 2) {
-          const u32x2 y = *(const u32x2*)src;
-          x.k[kb][0] = y[0];
-          x.k[kb][1] = y[1];
-        } else {
-          x.k[kb][0] = *(const uint32_t*)src;
+        if (k_mine) {
+          x.k[kb][0] = *(const part_t*)&nrow[0][TD * g];
+          x.ks[kb] = nscale[0] >> (8 * (g * TD / 4)) << kshift;
         }
-        x.ks[kb] = a.ksc[(row[kb] + c) * TD + g * TD / 4];
-        const unsigned char* vs = a.vsc + (row[kb] + 4 * g) * TD;
-        if constexpr (TD == 4) {
-          const u32x4 y = *(const u32x4*)vs;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) x.vs[kb][e] = y[e];
-        } else if constexpr (TD == 2) {
-          const u32x2 y = *(const u32x2*)vs;
-          x.vs[kb][0] = y[0];
-          x.vs[kb][1] = y[1];
-        } else {
-          x.vs[kb][0] = *(const uint32_t*)vs;
-        }
+        if (here && voff / RB == row) x.v[kb][0] = *(const part_t*)&nrow[1][voff % RB / 4];
+        // the row's TD bytes are bytes (row % 4) TD on of the 4 TD that lanes of its group hold
+        const unsigned first = (row & 3) * TD, shift = 8 * (first & 3);
+        const uint32_t mask = here && g == row >> 2 ? (TD == 4 ? ~0u : (1u << (8 * TD % 32)) - 1) << shift : 0u;
+        const uint32_t fresh = nscale[1] << shift;
+        x.vs[kb] = map_words(x.vs[kb], [=](uint32_t y, unsigned t) {
+          return first / 4 == t ? (y & ~mask) | (fresh & mask) : y;
+        });
       }
-    }
-    // V: 1 KB per load, the block's rows one after the other
-#pragma unroll
-    for (int m = 0; m < NV; ++m) {
-      constexpr int RPL = 1024 / RB;   // rows of a load
-      const int r = RPL * m + lane / (64 / RPL);
-      long long base = row[RPL * m / kGranule];
-      if constexpr (RPL > kGranule) {
-#pragma unroll
-        for (int kb = 1; kb < RPL / kGranule; ++kb)
-          base = r / kGranule == RPL * m / kGranule + kb ? row[RPL * m / kGranule + kb] : base;
-      }
-      x.v[m] = *(const u32x4*)((const unsigned char*)a.vp + (base + r % kGranule) * RB + 16 * (lane % (64 / RPL)));
     }
   };
-
-  unsigned char* vst = smem + w * (BK * RB);
-  const float sl2 = a.sl2;
-  auto step = [&](Block& x) __attribute__((always_inline)) {
+  auto step = [&](Block& x, int kv0) __attribute__((always_inline)) {
+    if (writes && T_b - 1 - kv0 < BK) patch(x, T_b - 1 - kv0);
     bool whole = true;
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) whole = whole && x.lim[kb] == kGranule;
-    // V to LDS; rows that take no part as zeros, so that P's zeros meet no NaN
 #pragma unroll
-    for (int m = 0; m < NV; ++m) {
-      constexpr int RPL = 1024 / RB, CPR = 64 / RPL;
-      const int r = RPL * m + lane / CPR, ch = lane % CPR;
-      u32x4 y = x.v[m];
+    for (int kb = 0; kb < KB; ++kb) {
       if constexpr (!Q4) {
-        if (!whole) {
-          int lim = x.lim[0];
 #pragma unroll
-          for (int kb = 1; kb < KB; ++kb) lim = r / kGranule == kb ? x.lim[kb] : lim;
-          if (r % kGranule >= lim) y = (u32x4){0u, 0u, 0u, 0u};
+        for (int t = 0; t < TD; ++t) {
+          constexpr int RPL = 1024 / RB, CPR = 64 / RPL;
+          const int r = kGranule * kb + RPL * t + lane / CPR, ch = lane % CPR;
+          *(part_t*)(vst + r * RB + 16 * (ch ^ swz16<D>(r))) = x.v[kb][t];
         }
-        *(u32x4*)(vst + r * RB + 16 * (ch ^ swz16<D>(r))) = y;
       } else {
-        // 8-byte pieces; the eight rows that a half-wave's transposed read takes
-        // at one place of a 256-byte line get different pieces of it
-        const int f = D == 128 ? ((r >> 4) & 3) * 2 + ((r >> 2) & 1) : D == 64 ? (r >> 4) & 3 : (r >> 4) & 1;
-        *(u32x2*)(vst + r * RB + 8 * ((2 * ch) ^ f)) = (u32x2){y[0], y[1]};
-        *(u32x2*)(vst + r * RB + 8 * ((2 * ch + 1) ^ f)) = (u32x2){y[2], y[3]};
+        // 8-byte pieces; the eight rows that a half-wave's transposed read takes at one
+        // place of a 256-byte line get different pieces of it
+        const int r = kGranule * kb + lane / 4;
+        if constexpr (TD == 4) {
+          const int p = 2 * (lane & 3), f = 2 * kb + ((r >> 2) & 1);
+          const part_t y = x.v[kb][0];
+          *(u32x2*)(vst + r * RB + 8 * (p ^ f)) = (u32x2){y[0], y[1]};
+          *(u32x2*)(vst + r * RB + 8 * ((p + 1) ^ f)) = (u32x2){y[2], y[3]};
+        } else if constexpr (TD == 2) {
+          *(part_t*)(vst + r * RB + 8 * ((lane & 3) ^ kb)) = x.v[kb][0];
+        } else {
+          *(part_t*)(vst + r * RB + 8 * ((lane >> 1 & 1) ^ (kb & 1)) + 4 * (lane & 1)) = x.v[kb][0];
+        }
       }
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -515,17 +600,22 @@ __global__ void __launch_bounds__(256, 2) paged_decode_kernel(const PagedArgs a)
     for (int q = 0; q < NQ; ++q)
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb) s[q][kb] = (f32x4){0.f, 0.f, 0.f, 0.f};
+    float unit[KB];
+    if constexpr (Q4) {
 #pragma unroll
-    for (int kb = 0; kb < KB; ++kb)
+      for (int kb = 0; kb < KB; ++kb) unit[kb] = __uint_as_float(((x.ks[kb] >> kshift) & 255u) << 23);
+    }
 #pragma unroll
-      for (int t = 0; t < TD; ++t) {
+    for (int t = 0; t < TD; ++t)   // the chains of the KB sums side by side
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb) {
         bf16x8 kf;
-        if constexpr (Q4) kf = Quant4::get(x.k[kb][t], __uint_as_float(x.ks[kb] << 23));
-        else kf = __builtin_bit_cast(bf16x8, (u32x4){x.k[kb][4 * t], x.k[kb][4 * t + 1], x.k[kb][4 * t + 2], x.k[kb][4 * t + 3]});
+        if constexpr (Q4) kf = Quant4::get(word(x.k[kb][0], t), unit[kb]);
+        else kf = __builtin_bit_cast(bf16x8, x.k[kb][t]);
 #pragma unroll
         for (int q = 0; q < NQ; ++q) {
           mma16(s[q][kb], kf, qf[q][t]);
-          if (a.rot.r) mma16(s[q][kb], kf, qr[q][t]);
+          mma16(s[q][kb], kf, qr[q][t]);
         }
       }
     if (!whole) {
@@ -579,13 +669,13 @@ __global__ void __launch_bounds__(256, 2) paged_decode_kernel(const PagedArgs a)
     } else {
       if (!whole) {   // scales of rows that take no part
 #pragma unroll
-        for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-          for (int t = 0; t < TD; ++t) {
-            // byte k of the words together is row k / TD, block k % TD
-            const int keep = max(0, min(x.lim[kb] - 4 * g, 4)) * TD - 4 * t;   // bytes of this word
-            x.vs[kb][t] &= keep >= 4 ? ~0u : keep <= 0 ? 0u : (1u << (8 * keep)) - 1;
-          }
+        for (int kb = 0; kb < KB; ++kb) {
+          const int bytes = max(0, min(x.lim[kb] - 4 * g, 4)) * TD;
+          x.vs[kb] = map_words(x.vs[kb], [&](uint32_t y, int t) {
+            const int keep = bytes - 4 * t;
+            return y & (keep >= 4 ? ~0u : keep <= 0 ? 0u : (1u << (8 * keep)) - 1);
+          });
+        }
       }
       const int rr = 16 * (c >> 2) + 4 * g + (c & 3);   // the row whose columns this lane fetches
       const int f = D == 128 ? ((rr >> 4) & 3) * 2 + ((rr >> 2) & 1) : D == 64 ? (rr >> 4) & 3 : (rr >> 4) & 1;
@@ -598,7 +688,7 @@ __global__ void __launch_bounds__(256, 2) paged_decode_kernel(const PagedArgs a)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const int k = i * TD + dg;
-            sc[kb][i] = __uint_as_float(((x.vs[kb][k / 4] >> (8 * (k % 4))) & 255u) << 23);
+            sc[kb][i] = __uint_as_float(((word(x.vs[kb], k / 4) >> (8 * (k % 4))) & 255u) << 23);
           }
 #pragma unroll
         for (int q = 0; q < NQ; ++q) {
@@ -622,23 +712,20 @@ __global__ void __launch_bounds__(256, 2) paged_decode_kernel(const PagedArgs a)
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   };
 
-  {
-    Block A, B2;
-    int kv = k_lo + BK * w;
-    if (kv < k_hi) load(A, kv);
-    while (kv < k_hi) {
-      const bool more = kv + 4 * BK < k_hi;
-      if (more) load(B2, kv + 4 * BK);
-      step(A);
-      if (!more) break;
-      kv += 8 * BK;
-      if (kv < k_hi) load(A, kv);
-      step(B2);
-    }
+  // The next block's loads are issued whether there is one or not (they are then those
+  // of page 0's first rows): behind a branch the compiler, counting the loads that are
+  // certainly in flight, would wait for them before it uses this block's.
+  for (; kv < k_hi; kv += 8 * BK) {
+    load(B2, ids, kv + 4 * BK);
+    fetch(ids, kv + 8 * BK);
+    step(A, kv);
+    load(A, ids, kv + 8 * BK);
+    fetch(ids, kv + 12 * BK);
+    if (kv + 4 * BK < k_hi) step(B2, kv + 4 * BK);
   }
 
   // ---- merge the waves through LDS: O parts [4][D][C], maxima and sums [4][C]
-  __syncthreads();
+  lds_barrier();
   float* ow = (float*)smem;
 #pragma unroll
   for (int q = 0; q < NQ; ++q) {
@@ -653,7 +740,7 @@ __global__ void __launch_bounds__(256, 2) paged_decode_kernel(const PagedArgs a)
 #pragma unroll
       for (int i = 0; i < 4; ++i) ow[(w * D + 16 * db + 4 * g + i) * C + 16 * q + c] = oacc[q][db][i];
   }
-  __syncthreads();
+  lds_barrier();
   for (int it = tid; it < C * (D / 4); it += 256) {
     const int col = it % C, d4 = it / C;
     if (col >= nq) continue;
