@@ -192,14 +192,24 @@ PagedPlan paged_plan(int B, int Hq, int Hkv, int n, int append, bool q4) {
   return p;
 }
 
+template <int D, int NQ, int REP, bool Q4> void launch_decode(const attn::PagedArgs& a, const dim3& grid, hipStream_t st) {
+  constexpr int block = Q4 ? 64 : 32;
+  if (1 << a.pg.shift >= block)
+    hipLaunchKernelGGL((attn::paged_decode_kernel<D, NQ, REP, Q4, block>), grid, dim3(256), 0, st, a);
+  else
+    hipLaunchKernelGGL((attn::paged_decode_kernel<D, NQ, REP, Q4, attn::kGranule>), grid, dim3(256), 0, st, a);
+}
 template <int D> void launch_decode(const attn::PagedArgs& a, const dim3& grid, int nq, hipStream_t st) {
-  const dim3 block(256);
-  if (a.ksc) {
-    if (nq == 1) hipLaunchKernelGGL((attn::paged_decode_kernel<D, 1, true>), grid, block, 0, st, a);
-    else hipLaunchKernelGGL((attn::paged_decode_kernel<D, 2, true>), grid, block, 0, st, a);
+  if (!a.ksc) {
+    nq == 1 ? launch_decode<D, 1, 1, false>(a, grid, st) : launch_decode<D, 2, 1, false>(a, grid, st);
+  } else if (nq == 2) {
+    launch_decode<D, 2, 1, true>(a, grid, st);
+  } else if (D == 128 && a.G <= 4) {   // as often in the 16 columns as the heads go into them
+    launch_decode<D, 1, D / 32, true>(a, grid, st);
+  } else if (D >= 64 && a.G <= 8) {
+    launch_decode<D, 1, D == 32 ? 1 : 2, true>(a, grid, st);
   } else {
-    if (nq == 1) hipLaunchKernelGGL((attn::paged_decode_kernel<D, 1, false>), grid, block, 0, st, a);
-    else hipLaunchKernelGGL((attn::paged_decode_kernel<D, 2, false>), grid, block, 0, st, a);
+    launch_decode<D, 1, 1, true>(a, grid, st);
   }
 }
 

@@ -293,8 +293,8 @@ __device__ __forceinline__ void lds_barrier() {
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
-// A buffer of `bytes` bytes; W words of each lane at byte offset `off`, zeros
-// behind its end.
+// A buffer of `bytes` bytes; W words of each lane at byte offset `off` + `at` (the
+// same for all lanes), zeros behind its end.
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_rsrc(const void* base, int bytes) {
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), (short)0, bytes, 0x00020000);
 }
@@ -306,20 +306,20 @@ constexpr int kNonTemporal = 2;
 template <int W> struct Words;
 template <> struct Words<1> {
   typedef uint32_t type;
-  __device__ __forceinline__ static type load(__amdgpu_buffer_rsrc_t r, unsigned off) {
-    return __builtin_amdgcn_raw_buffer_load_b32(r, off, 0, kNonTemporal);
+  __device__ __forceinline__ static type load(__amdgpu_buffer_rsrc_t r, unsigned off, int at) {
+    return __builtin_amdgcn_raw_buffer_load_b32(r, off, at, kNonTemporal);
   }
 };
 template <> struct Words<2> {
   typedef u32x2 type;
-  __device__ __forceinline__ static type load(__amdgpu_buffer_rsrc_t r, unsigned off) {
-    return __builtin_amdgcn_raw_buffer_load_b64(r, off, 0, kNonTemporal);
+  __device__ __forceinline__ static type load(__amdgpu_buffer_rsrc_t r, unsigned off, int at) {
+    return __builtin_amdgcn_raw_buffer_load_b64(r, off, at, kNonTemporal);
   }
 };
 template <> struct Words<4> {
   typedef u32x4 type;
-  __device__ __forceinline__ static type load(__amdgpu_buffer_rsrc_t r, unsigned off) {
-    return __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, kNonTemporal);
+  __device__ __forceinline__ static type load(__amdgpu_buffer_rsrc_t r, unsigned off, int at) {
+    return __builtin_amdgcn_raw_buffer_load_b128(r, off, at, kNonTemporal);
   }
 };
 __device__ __forceinline__ uint32_t word(uint32_t x, int) { return x; }
@@ -331,9 +331,29 @@ template <typename F> __device__ __forceinline__ u32x4 map_words(u32x4 x, F f) {
   return (u32x4){f(x[0], 0), f(x[1], 1), f(x[2], 2), f(x[3], 3)};
 }
 
-template <int D, int NQ, bool Q4>
+// 2^(byte B of w - 127), as the scales mean it, in one instruction
+template <int B> __device__ __forceinline__ float byte_power(uint32_t w) {
+  float r;
+  if constexpr (B == 0)
+    asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD src1_sel:BYTE_0" : "=v"(r) : "v"(23), "v"(w));
+  else if constexpr (B == 1)
+    asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD src1_sel:BYTE_1" : "=v"(r) : "v"(23), "v"(w));
+  else if constexpr (B == 2)
+    asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD src1_sel:BYTE_2" : "=v"(r) : "v"(23), "v"(w));
+  else
+    asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD src1_sel:BYTE_3" : "=v"(r) : "v"(23), "v"(w));
+  return r;
+}
+
+// REP: the query heads (at most 16 / REP of them) stand REP times in the 16 columns, and a
+// lane scales P for only 1 / REP of the 32-column blocks of d. PAGE: the least number
+// of keys that lie in one page, 16 or a whole block.
+template <int D, int NQ, int REP, bool Q4, int PAGE>
 __global__ void __launch_bounds__(256, 2) paged_decode_kernel(const PagedArgs a) {
   constexpr int BK = Q4 ? 64 : 32, KB = BK / kGranule;   // keys of a block, in rows of 16
+  constexpr int NG = BK / PAGE, GB = PAGE / kGranule;    // its pieces of pages, rows of 16 in one
+  constexpr int HR = 16 / REP;                           // heads side by side
+  static_assert(REP == 1 || (Q4 && NQ == 1 && D / 32 % REP == 0), "replicas share the blocks of d");
   constexpr int TD = D / 32, DB = D / 16;                // steps over d, output rows of 16
   constexpr int C = 16 * NQ;                             // query columns
   constexpr int RB = Q4 ? D / 2 : 2 * D;                 // bytes of a row
@@ -373,41 +393,49 @@ __global__ void __launch_bounds__(256, 2) paged_decode_kernel(const PagedArgs a)
     part_t k[KB][NP], v[KB][NP];
     uint32_t ks[Q4 ? KB : 1];
     part_t vs[Q4 ? KB : 1];
-    int lim[KB];   // keys of each row of 16 that take part
+    int lim[NG];   // keys of each piece that take part
+  };
+  auto limit = [](const Block& x, int kb) __attribute__((always_inline)) {   // of a row of 16
+    return GB == 1 ? x.lim[kb] : max(0, min(x.lim[kb / GB] - kb % GB * kGranule, kGranule));
   };
   // page numbers of the block at key kv0 (a multiple of 16); behind the split, of its last key
   struct Ids {
-    int page[KB];
+    int page[NG];
   };
   auto fetch = [&](Ids& ids, int kv0) __attribute__((always_inline)) {
 #pragma unroll
-    for (int kb = 0; kb < KB; ++kb)
-      ids.page[kb] = ((ConstInt)(uintptr_t)table)[min(kv0 + kGranule * kb, k_hi - 1) >> a.pg.shift];
+    for (int i = 0; i < NG; ++i)
+      ids.page[i] = ((ConstInt)(uintptr_t)table)[min(kv0 + PAGE * i, k_hi - 1) >> a.pg.shift];
   };
-  // The block's loads. Each row of 16 has a buffer of its own that ends behind its last
+  // The block's loads. Each piece has a buffer of its own that ends behind its last
   // key, so what takes no part (keys behind the end, pages that are none, blocks
   // behind the split) reads as zeros, without an access.
   const unsigned koff = c * RB + (Q4 ? RB / 4 * g : 16 * g), voff = Q4 ? RB / 4 * lane : 16 * lane;
   auto load = [&](Block& x, const Ids& ids, int kv0) __attribute__((always_inline)) {
 #pragma unroll
-    for (int kb = 0; kb < KB; ++kb) {
-      const int p = kv0 + kGranule * kb;
-      const bool ok = p < k_hi && page_ok(a.pg, ids.page[kb]);
-      x.lim[kb] = ok ? min(k_hi - p, kGranule) : 0;
-      const long long row = ok ? (((long long)ids.page[kb] * a.pg.Hkv + hk) << a.pg.shift) + (p & ((1 << a.pg.shift) - 1)) : 0;
-      const auto kr = rows_rsrc((const unsigned char*)a.kp + row * RB, x.lim[kb] * RB);
-      const auto vr = rows_rsrc((const unsigned char*)a.vp + row * RB, x.lim[kb] * RB);
-      if constexpr (!Q4) {
+    for (int i = 0; i < NG; ++i) {
+      const int p = kv0 + PAGE * i;
+      const bool ok = p < k_hi && page_ok(a.pg, ids.page[i]);
+      x.lim[i] = ok ? min(k_hi - p, PAGE) : 0;
+      const long long row = ok ? (((long long)ids.page[i] * a.pg.Hkv + hk) << a.pg.shift) + (p & ((1 << a.pg.shift) - 1)) : 0;
+      const auto kr = rows_rsrc((const unsigned char*)a.kp + row * RB, x.lim[i] * RB);
+      const auto vr = rows_rsrc((const unsigned char*)a.vp + row * RB, x.lim[i] * RB);
+      const int scales = Q4 && ok ? PAGE * TD : 0;
+      const auto ksr = rows_rsrc(a.ksc + row * TD, scales), vsr = rows_rsrc(a.vsc + row * TD, scales);
 #pragma unroll
-        for (int t = 0; t < TD; ++t) x.k[kb][t] = Part::load(kr, koff + 64 * t);
+      for (int j = 0; j < GB; ++j) {
+        const int kb = GB * i + j, at = kGranule * RB * j;
+        if constexpr (!Q4) {
 #pragma unroll
-        for (int t = 0; t < TD; ++t) x.v[kb][t] = Part::load(vr, voff + 1024 * t);
-      } else {
-        const int n = ok ? kGranule * TD : 0;
-        x.ks[kb] = Words<1>::load(rows_rsrc(a.ksc + row * TD, n), ksb & ~3);
-        x.k[kb][0] = Part::load(kr, koff);
-        x.v[kb][0] = Part::load(vr, voff);
-        x.vs[kb] = Part::load(rows_rsrc(a.vsc + row * TD, n), 4 * TD * g);
+          for (int t = 0; t < TD; ++t) x.k[kb][t] = Part::load(kr, koff + 64 * t, at);
+#pragma unroll
+          for (int t = 0; t < TD; ++t) x.v[kb][t] = Part::load(vr, voff + 1024 * t, at);
+        } else {
+          x.ks[kb] = Words<1>::load(ksr, ksb & ~3, kGranule * TD * j);
+          x.k[kb][0] = Part::load(kr, koff, at);
+          x.v[kb][0] = Part::load(vr, voff, at);
+          x.vs[kb] = Part::load(vsr, 4 * TD * g, kGranule * TD * j);
+        }
       }
     }
   };
@@ -434,7 +462,7 @@ __global__ void __launch_bounds__(256, 2) paged_decode_kernel(const PagedArgs a)
 #pragma unroll
     for (int i = 0; i < C * P / 256; ++i) {
       const int r = tid / P + 256 / P * i;
-      const bf16* src = (const bf16*)a.q + b * a.q_b + (size_t)(h0 + min(r, nq - 1)) * D;
+      const bf16* src = (const bf16*)a.q + b * a.q_b + (size_t)(h0 + min(REP == 1 ? r : r % HR, nq - 1)) * D;
       u[i] = (float)src[c0];
       x[i] = (float)src[c1];
     }
@@ -448,7 +476,7 @@ __global__ void __launch_bounds__(256, 2) paged_decode_kernel(const PagedArgs a)
         y = u[i] * cs - x[i] * sn;
         z = x[i] * cs + u[i] * sn;
       }
-      if (r >= nq) y = z = 0.f;
+      if ((REP == 1 ? r : r % HR) >= nq) y = z = 0.f;
       if (a.negate) y = -y, z = -z;
       const bf16 yh = (bf16)y, zh = (bf16)z;
       qh[r * QS + c0] = yh;
@@ -568,7 +596,7 @@ __global__ void __launch_bounds__(256, 2) paged_decode_kernel(const PagedArgs a)
     if (writes && T_b - 1 - kv0 < BK) patch(x, T_b - 1 - kv0);
     bool whole = true;
 #pragma unroll
-    for (int kb = 0; kb < KB; ++kb) whole = whole && x.lim[kb] == kGranule;
+    for (int i = 0; i < NG; ++i) whole = whole && x.lim[i] == PAGE;
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) {
       if constexpr (!Q4) {
@@ -624,7 +652,7 @@ __global__ void __launch_bounds__(256, 2) paged_decode_kernel(const PagedArgs a)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
 #pragma unroll
-          for (int q = 0; q < NQ; ++q) s[q][kb][i] = 4 * g + i < x.lim[kb] ? s[q][kb][i] : -INFINITY;
+          for (int q = 0; q < NQ; ++q) s[q][kb][i] = 4 * g + i < limit(x, kb) ? s[q][kb][i] : -INFINITY;
         }
     }
 #pragma unroll
@@ -670,7 +698,7 @@ __global__ void __launch_bounds__(256, 2) paged_decode_kernel(const PagedArgs a)
       if (!whole) {   // scales of rows that take no part
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb) {
-          const int bytes = max(0, min(x.lim[kb] - 4 * g, 4)) * TD;
+          const int bytes = max(0, min(limit(x, kb) - 4 * g, 4)) * TD;
           x.vs[kb] = map_words(x.vs[kb], [&](uint32_t y, int t) {
             const int keep = bytes - 4 * t;
             return y & (keep >= 4 ? ~0u : keep <= 0 ? 0u : (1u << (8 * keep)) - 1);
@@ -679,22 +707,29 @@ __global__ void __launch_bounds__(256, 2) paged_decode_kernel(const PagedArgs a)
       }
       const int rr = 16 * (c >> 2) + 4 * g + (c & 3);   // the row whose columns this lane fetches
       const int f = D == 128 ? ((rr >> 4) & 3) * 2 + ((rr >> 2) & 1) : D == 64 ? (rr >> 4) & 3 : (rr >> 4) & 1;
+      // P for this lane's blocks of d, those from DL c / HR on; of the products below a
+      // block's are right in the columns whose lanes scaled P for it
+      constexpr int DL = TD / REP;
+      bf16x8 pf[NQ][DL][2];
+      part_t vs[KB];
 #pragma unroll
-      for (int dg = 0; dg < TD; ++dg) {
-        bf16x8 pf[NQ][2];
+      for (int kb = 0; kb < KB; ++kb)
+        vs[kb] = map_words(x.vs[kb], [&](uint32_t y, int) { return REP == 1 ? y : y >> (8 * DL * (c / HR)); });
+      auto scaled = [&](auto dl) __attribute__((always_inline)) {
+        constexpr int B = decltype(dl)::value;
         f32x4 sc[KB];
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int k = i * TD + dg;
-            sc[kb][i] = __uint_as_float(((word(x.vs[kb], k / 4) >> (8 * (k % 4))) & 255u) << 23);
-          }
+          sc[kb] = (f32x4){byte_power<B>(word(vs[kb], 0)), byte_power<(TD + B) % 4>(word(vs[kb], TD / 4)),
+                           byte_power<(2 * TD + B) % 4>(word(vs[kb], 2 * TD / 4)),
+                           byte_power<(3 * TD + B) % 4>(word(vs[kb], 3 * TD / 4))};
 #pragma unroll
         for (int q = 0; q < NQ; ++q) {
-          pf[q][0] = frag16(s[q][0] * sc[0], s[q][1] * sc[1]);
-          pf[q][1] = frag16(s[q][2] * sc[2], s[q][3] * sc[3]);
+          pf[q][B][0] = frag16(s[q][0] * sc[0], s[q][1] * sc[1]);
+          pf[q][B][1] = frag16(s[q][2] * sc[2], s[q][3] * sc[3]);
         }
+      };
+      auto products = [&](int dg) __attribute__((always_inline)) {
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
           const int db = 2 * dg + e;
@@ -703,10 +738,21 @@ __global__ void __launch_bounds__(256, 2) paged_decode_kernel(const PagedArgs a)
           const bf16x8 v0 = Quant4::get((uint32_t)y[0], 1.f), v1 = Quant4::get((uint32_t)y[1], 1.f);
 #pragma unroll
           for (int q = 0; q < NQ; ++q) {
-            mma16(oacc[q][db], v0, pf[q][0]);
-            mma16(oacc[q][db], v1, pf[q][1]);
+            mma16(oacc[q][db], v0, pf[q][dg % DL][0]);
+            mma16(oacc[q][db], v1, pf[q][dg % DL][1]);
           }
         }
+      };
+      auto block = [&](auto dl) __attribute__((always_inline)) {
+        scaled(dl);
+#pragma unroll
+        for (int r = 0; r < REP; ++r) products(r * DL + decltype(dl)::value);
+      };
+      block(std::integral_constant<int, 0>{});
+      if constexpr (DL > 1) block(std::integral_constant<int, 1>{});
+      if constexpr (DL > 2) {
+        block(std::integral_constant<int, 2>{});
+        block(std::integral_constant<int, 3>{});
       }
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -741,8 +787,9 @@ __global__ void __launch_bounds__(256, 2) paged_decode_kernel(const PagedArgs a)
       for (int i = 0; i < 4; ++i) ow[(w * D + 16 * db + 4 * g + i) * C + 16 * q + c] = oacc[q][db][i];
   }
   lds_barrier();
-  for (int it = tid; it < C * (D / 4); it += 256) {
-    const int col = it % C, d4 = it / C;
+  constexpr int heads = C / REP;
+  for (int it = tid; it < heads * (D / 4); it += 256) {
+    const int col = it % heads, d4 = it / heads;
     if (col >= nq) continue;
     float M = -INFINITY, l = 0.f;
 #pragma unroll
@@ -753,7 +800,7 @@ __global__ void __launch_bounds__(256, 2) paged_decode_kernel(const PagedArgs a)
       const float f = M == -INFINITY ? 0.f : exp2_fast(ml[0][v][col] - M);
       l += f * ml[1][v][col];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) acc[i] += f * ow[(v * D + 4 * d4 + i) * C + col];
+      for (int i = 0; i < 4; ++i) acc[i] += f * ow[(v * D + 4 * d4 + i) * C + col + HR * (4 * d4 / (D / REP))];
     }
     const size_t row = (size_t)b * a.Hq + h0 + col;
     if (a.nsplit == 1) {

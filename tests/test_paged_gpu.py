@@ -266,6 +266,14 @@ def test_decode_groups(bits, d, Hq, Hkv):
 
 
 @pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("d", [32, 64, 128])
+@pytest.mark.parametrize("G", [1, 4, 5, 8, 9, 16, 20])
+def test_decode_groups_in_large_pages(bits, d, G):
+    """Blocks inside one page (64 tokens and more), ends at and beside its edges."""
+    decode_case([0, 63, 64, 65, 128, 200, 255, 256, 257], 2 * G, 2, 64 if G % 2 else 128, d, bits, r=d // 2, seed=G, spoil=[(5, 1)])
+
+
+@pytest.mark.parametrize("bits", [16, 4])
 @pytest.mark.parametrize("d", [64, 128])
 def test_decode_many_splits(bits, d):
     """One long sequence and short ones beside it: splits that hold nothing."""
