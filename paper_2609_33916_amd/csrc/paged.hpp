@@ -359,7 +359,7 @@ __global__ void __launch_bounds__(256, 2) paged_decode_kernel(const PagedArgs a)
   constexpr int RB = Q4 ? D / 2 : 2 * D;                 // bytes of a row
   constexpr int QS = D + 8;                              // row stride of the queries in LDS (elements)
   constexpr int VBYTES = 4 * BK * RB, OBYTES = 4 * D * C * 4;
-  constexpr int BYTES = VBYTES + 2 * C * QS * 2;
+  constexpr int BYTES = VBYTES + (REP == 1 ? 2 : 1) * C * QS * 2;
   // the waves' stages of V and the queries; at the end the waves' O
   __shared__ __attribute__((aligned(16))) unsigned char smem[BYTES > OBYTES ? BYTES : OBYTES];
   __shared__ float ml[2][4][C];
@@ -479,10 +479,17 @@ __global__ void __launch_bounds__(256, 2) paged_decode_kernel(const PagedArgs a)
       if ((REP == 1 ? r : r % HR) >= nq) y = z = 0.f;
       if (a.negate) y = -y, z = -z;
       const bf16 yh = (bf16)y, zh = (bf16)z;
-      qh[r * QS + c0] = yh;
-      qh[r * QS + c1] = zh;
-      ql[r * QS + c0] = (bf16)(turns ? y - (float)yh : 0.f);
-      ql[r * QS + c1] = (bf16)(turns ? z - (float)zh : 0.f);
+      const bf16 yl = (bf16)(turns ? y - (float)yh : 0.f), zl = (bf16)(turns ? z - (float)zh : 0.f);
+      if constexpr (REP == 1) {
+        qh[r * QS + c0] = yh;
+        qh[r * QS + c1] = zh;
+        ql[r * QS + c0] = yl;
+        ql[r * QS + c1] = zl;
+      } else {   // the two parts in replicas side by side
+        const bool low = r / HR & 1;
+        qh[r * QS + c0] = low ? yl : yh;
+        qh[r * QS + c1] = low ? zl : zh;
+      }
     }
     if (writes) {
       const long long at = page_row(a.pg, table, T_b - 1);
@@ -539,14 +546,14 @@ __global__ void __launch_bounds__(256, 2) paged_decode_kernel(const PagedArgs a)
     }
   }
   lds_barrier();
-  bf16x8 qf[NQ][TD], qr[NQ][TD];
+  bf16x8 qf[NQ][TD], qr[NQ][REP == 1 ? TD : 1];
 #pragma unroll
   for (int x = 0; x < NQ; ++x)
 #pragma unroll
     for (int t = 0; t < TD; ++t) {
       const int at = (16 * x + c) * QS + (Q4 ? D / 4 * g + 8 * t : 32 * t + 8 * g);
       qf[x][t] = *(const bf16x8*)(qh + at);
-      qr[x][t] = *(const bf16x8*)(ql + at);
+      if constexpr (REP == 1) qr[x][t] = *(const bf16x8*)(ql + at);
     }
 
   f32x4 oacc[NQ][DB];
@@ -643,9 +650,16 @@ __global__ void __launch_bounds__(256, 2) paged_decode_kernel(const PagedArgs a)
 #pragma unroll
         for (int q = 0; q < NQ; ++q) {
           mma16(s[q][kb], kf, qf[q][t]);
-          mma16(s[q][kb], kf, qr[q][t]);
+          if constexpr (REP == 1) mma16(s[q][kb], kf, qr[q][t]);
         }
       }
+    if constexpr (REP > 1) {   // the sum of the two parts, in both
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          s[0][kb][i] += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(s[0][kb][i]), 0x120 + HR, 0xf, 0xf, true));
+    }
     if (!whole) {
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb)
