@@ -29,17 +29,18 @@ __device__ __forceinline__ double turn(int p, double f) {
   const double x = (double)p * f * 0.15915494309189535;   // 1 / (2 pi)
   return x - rint(x);
 }
-__device__ __forceinline__ void turn_cs(int p, const Rotation& rot, int i, float& c, float& s) {
+// a cos(p f), a sin(p f)
+__device__ __forceinline__ void turn_cs(int p, double f, float a, float& c, float& s) {
   float c0, s0;
-  sincospif((float)(2.0 * turn(p, rot.freqs[i])), &s0, &c0);
-  c = c0 * rot.amplitude;
-  s = s0 * rot.amplitude;
+  sincospif((float)(2.0 * turn(p, f)), &s0, &c0);
+  c = c0 * a;
+  s = s0 * a;
 }
-__device__ __forceinline__ void turn_cs(int p, const Rotation& rot, int i, double& c, double& s) {
+__device__ __forceinline__ void turn_cs(int p, double f, float a, double& c, double& s) {
   double c0, s0;
-  sincospi(2.0 * turn(p, rot.freqs[i]), &s0, &c0);
-  c = c0 * (double)rot.amplitude;
-  s = s0 * (double)rot.amplitude;
+  sincospi(2.0 * turn(p, f), &s0, &c0);
+  c = c0 * (double)a;
+  s = s0 * (double)a;
 }
 
 // 16 bytes of a row and its values
@@ -97,7 +98,7 @@ template <typename T, bool INTER> struct PairChunks {
     if (turns) {
 #pragma unroll
       for (int e = 0; e < N; ++e) {
-        turn_cs(p, rot, N * j + e, c[e], s[e]);
+        turn_cs(p, rot.freqs[N * j + e], rot.amplitude, c[e], s[e]);
         s[e] *= sign;
       }
     }
