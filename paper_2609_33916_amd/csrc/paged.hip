@@ -76,11 +76,11 @@ bool fits(const Strides& s, int B, int H, int n) {   // offsets in 62 bits
   return far < ((__int128)1 << 60);
 }
 
-// Heads per workgroup: a thread's sines and cosines serve all of them, so as many
-// as leave eight workgroups per compute unit.
+// Heads per workgroup: a thread's sines and cosines serve all of them, so as many,
+// up to 8, as leave four workgroups per compute unit.
 int heads_per_group(long long token_blocks, int heads) {
-  const long long want = attn::kXcds * attn::kCusPerXcd * 8;
-  return (int)std::max<long long>(1, std::min<long long>(heads, token_blocks * heads / want));
+  const long long want = attn::kXcds * attn::kCusPerXcd * 4;
+  return (int)std::max<long long>(1, std::min<long long>({8, heads, token_blocks * heads / want}));
 }
 
 template <typename T> void launch_rope(attn::RopeArgs a, bool interleaved, hipStream_t st) {
@@ -158,6 +158,10 @@ attn::Pages pages_of(const int* table, int Hkv, int num_pages, int page_size, in
   return p;
 }
 
+template <int D> void launch_append4(const attn::AppendArgs& a, const dim3& grid, bool interleaved, hipStream_t st) {
+  if (interleaved) hipLaunchKernelGGL((attn::append4_kernel<D, true>), grid, dim3(256), 0, st, a);
+  else hipLaunchKernelGGL((attn::append4_kernel<D, false>), grid, dim3(256), 0, st, a);
+}
 void launch_append(attn::AppendArgs a, bool interleaved, hipStream_t st) {
   const bool q4 = a.ksc != nullptr;
   const int per = 256 / (a.d / (q4 ? 8 : 16));
@@ -165,8 +169,9 @@ void launch_append(attn::AppendArgs a, bool interleaved, hipStream_t st) {
   a.hgroup = heads_per_group(blocks, a.pg.Hkv);
   const dim3 grid(blocks, (a.pg.Hkv + a.hgroup - 1) / a.hgroup);
   if (q4) {
-    if (interleaved) hipLaunchKernelGGL(attn::append4_kernel<true>, grid, dim3(256), 0, st, a);
-    else hipLaunchKernelGGL(attn::append4_kernel<false>, grid, dim3(256), 0, st, a);
+    if (a.d == 32) launch_append4<32>(a, grid, interleaved, st);
+    else if (a.d == 64) launch_append4<64>(a, grid, interleaved, st);
+    else launch_append4<128>(a, grid, interleaved, st);
   } else {
     if (interleaved) hipLaunchKernelGGL(attn::append_kernel<true>, grid, dim3(256), 0, st, a);
     else hipLaunchKernelGGL(attn::append_kernel<false>, grid, dim3(256), 0, st, a);

@@ -26,18 +26,17 @@ namespace attn {
 
 // ------------------------------------------------------------ 4-bit values --
 struct Quant4 {
-  // A float that rounds to every shorter format as y does: y cut to 24 bits, the
-  // last one set if anything was lost. (A plain conversion could carry a value
-  // next to a border of the codes onto it. The rotation before it is in 64 bits
-  // for the same reason: a row's codes then do not depend on how 32-bit sums are
-  // ordered, and the pass is bound by memory either way.)
+  // A float that rounds to every shorter format as y does: y cut to 20 bits behind its
+  // first, the last bit of the float set if anything was lost. (A plain conversion
+  // could carry a value next to a border of the codes onto it. The rotation before it
+  // is in 64 bits for the same reason: a row's codes then do not depend on how 32-bit
+  // sums are ordered.) Below 2^-127 it is 0, from 2^128 on infinite, as is NaN.
   __device__ __forceinline__ static float odd(double y) {
-    const float f = (float)y;
-    const double d = (double)f;
-    if (d == y) return f;
-    uint32_t bits = __float_as_uint(f);
-    if (fabs(d) > fabs(y)) bits -= 1;
-    return __uint_as_float(bits | 1u);
+    const uint64_t bits = __builtin_bit_cast(uint64_t, y);
+    const uint32_t hi = (uint32_t)(bits >> 32), lo = (uint32_t)bits;
+    const uint32_t m = min(max(hi & 0x7fffffffu, 896u << 20), 1151u << 20);   // exponents 1 and 255 of a float, less 1 and 0
+    const uint32_t f = ((m << 3) - (896u << 23)) | min(lo, 1u);
+    return __uint_as_float(f | (hi & 0x80000000u));
   }
   // largest magnitude, as bits, of the four lanes of a quad
   __device__ __forceinline__ static uint32_t quad_max(uint32_t m) {
@@ -149,62 +148,88 @@ __global__ void __launch_bounds__(256) append_kernel(const AppendArgs a) {
 
 // 4-bit pages: a thread takes 8 consecutive columns, a quad a block of 32. The
 // other halves of its pairs are read too (by another thread as well: from
-// cache), so that the result is in the order it is stored in.
-template <bool INTER>
+// cache), so that the result is in the order it is stored in. The 64-bit sines and
+// cosines, a hundred instructions each, are made once per token and pair, in LDS.
+template <int D, bool INTER>
 __global__ void __launch_bounds__(256) append4_kernel(const AppendArgs a) {
-  const int tpt = a.d / 8;
-  const int ch = threadIdx.x % tpt, col = 8 * ch;
-  const int tok = blockIdx.x * (256 / tpt) + threadIdx.x / tpt;
-  if (tok >= a.tokens) return;
-  const int b = tok / a.T, t = tok - b * a.T;
-  int p = 0;
-  const long long row = append_row(a, b, t, p);
+  constexpr int TPT = D / 8, TOK = 256 / TPT;   // threads per token, tokens
+  __shared__ double tab[2][TOK][D / 2];
+  const int ch = threadIdx.x % TPT, col = 8 * ch, lt = threadIdx.x / TPT;
+  const int tok = blockIdx.x * TOK + lt;
+  int b = 0, t = 0, p = 0;
+  long long row = -1;
+  if (tok < a.tokens) {
+    b = tok / a.T;
+    t = tok - b * a.T;
+    row = append_row(a, b, t, p);
+  }
+  if (row >= 0)
+    for (int i = ch; i < a.rot.r / 2; i += TPT) turn_cs(p, a.rot.freqs[i], a.rot.amplitude, tab[0][lt][i], tab[1][lt][i]);
+  __syncthreads();
   if (row < 0) return;   // the same for the whole quad
   const bool turns = col < a.rot.r, second = col >= a.rot.r / 2;
   const int mate = INTER ? col : second ? col - a.rot.r / 2 : col + a.rot.r / 2;
   double c[8], s[8];
   if (turns) {
-    if (INTER) {
+    const int i0 = INTER ? col / 2 : second ? mate : col;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) turn_cs(p, a.rot.freqs[col / 2 + e], a.rot.amplitude, c[e], s[e]);
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        turn_cs(p, a.rot.freqs[(second ? mate : col) + e], a.rot.amplitude, c[e], s[e]);
-        if (second) s[e] = -s[e];   // w' = w c + u s, u' = u c - w s
-      }
+    for (int e = 0; e < (INTER ? 4 : 8); ++e) {
+      c[e] = tab[0][lt][i0 + e];
+      s[e] = second && !INTER ? -tab[1][lt][i0 + e] : tab[1][lt][i0 + e];   // w' = w c + u s, u' = u c - w s
     }
   }
   const bf16* ks = (const bf16*)a.k_new + b * a.ks.b + t * a.ks.t;
   const bf16* vs = (const bf16*)a.v_new + b * a.vs.b + t * a.vs.t;
   const int h1 = min((int)(blockIdx.y + 1) * a.hgroup, a.pg.Hkv);
-  for (int h = blockIdx.y * a.hgroup; h < h1; ++h) {
-    const u32x4 xk = *(const u32x4*)(ks + h * a.ks.h + col);
-    const u32x4 xv = *(const u32x4*)(vs + h * a.vs.h + col);
-    float k[8], v[8];
-    Chunk<bf16>::get(xk, k);
-    Chunk<bf16>::get(xv, v);
-    if (turns) {
-      if (INTER) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const double u = k[2 * e], w = k[2 * e + 1];
-          k[2 * e] = Quant4::odd(u * c[e] - w * s[e]);
-          k[2 * e + 1] = Quant4::odd(w * c[e] + u * s[e]);
-        }
-      } else {
-        float m[8];
-        Chunk<bf16>::get(*(const u32x4*)(ks + h * a.ks.h + mate), m);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) k[e] = Quant4::odd((double)k[e] * c[e] - (double)m[e] * s[e]);
-      }
+  // a row's scale bytes, one store
+  auto put_scales = [&](uint8_t* dst, uint32_t sc) __attribute__((always_inline)) {
+    if constexpr (D == 128) {   // the row's 16 lanes: a quad's byte to all of them
+      uint32_t y = sc << (8 * (ch / 4));
+      y |= (uint32_t)__builtin_amdgcn_mov_dpp((int)y, 0x124, 0xf, 0xf, true);
+      y |= (uint32_t)__builtin_amdgcn_mov_dpp((int)y, 0x128, 0xf, 0xf, true);
+      if (ch == 0) *(uint32_t*)dst = y;
+    } else {
+      if (ch % 4 == 0) dst[ch / 4] = (uint8_t)sc;
     }
-    const long long r = row + ((long long)h << a.pg.shift);
-    uint32_t sc;
-    ((uint32_t*)a.kp)[r * (a.d / 8) + ch] = Quant4::put(k, sc);
-    if (ch % 4 == 0) a.ksc[r * (a.d / 32) + ch / 4] = (uint8_t)sc;
-    ((uint32_t*)a.vp)[r * (a.d / 8) + ch] = Quant4::put(v, sc);
-    if (ch % 4 == 0) a.vsc[r * (a.d / 32) + ch / 4] = (uint8_t)sc;
+  };
+  constexpr int U = 2;
+  for (int h0 = blockIdx.y * a.hgroup; h0 < h1; h0 += U) {
+    u32x4 xk[U], xm[U], xv[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (h0 + u < h1) {
+        xk[u] = *(const u32x4*)(ks + (h0 + u) * a.ks.h + col);
+        if (!INTER && turns) xm[u] = *(const u32x4*)(ks + (h0 + u) * a.ks.h + mate);
+        xv[u] = *(const u32x4*)(vs + (h0 + u) * a.vs.h + col);
+      }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (h0 + u < h1) {
+        float k[8], v[8];
+        Chunk<bf16>::get(xk[u], k);
+        Chunk<bf16>::get(xv[u], v);
+        if (turns) {
+          if (INTER) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const double y = k[2 * e], z = k[2 * e + 1];
+              k[2 * e] = Quant4::odd(y * c[e] - z * s[e]);
+              k[2 * e + 1] = Quant4::odd(z * c[e] + y * s[e]);
+            }
+          } else {
+            float m[8];
+            Chunk<bf16>::get(xm[u], m);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) k[e] = Quant4::odd((double)k[e] * c[e] - (double)m[e] * s[e]);
+          }
+        }
+        const long long r = row + ((long long)(h0 + u) << a.pg.shift);
+        uint32_t sc;
+        ((uint32_t*)a.kp)[r * TPT + ch] = Quant4::put(k, sc);
+        put_scales(a.ksc + r * (D / 32), sc);
+        ((uint32_t*)a.vp)[r * TPT + ch] = Quant4::put(v, sc);
+        put_scales(a.vsc + r * (D / 32), sc);
+      }
   }
 }
 

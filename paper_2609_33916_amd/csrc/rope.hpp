@@ -72,33 +72,27 @@ template <> struct Chunk<float> {
   }
 };
 
-// A thread's two 16-byte chunks of a row and the N pairs between them. Thread j
-// of the d / 2N that share a row takes chunk j of the first half of the pairs and
-// of the second, or (interleaved) chunks 2j and 2j + 1; past the rotated columns,
-// two neighbouring chunks to copy. Both loads of a wave then cover whole
-// 128-byte lines of a bf16 row, and a pair never leaves its thread, so a row
-// may be turned in place.
+// A thread's two 16-byte chunks of a row and their N pairs. Thread j of the d / 2N
+// that share a row takes chunk j of each half of the rotated columns; past them, two
+// neighbouring chunks to copy. A pair of halves (i, i + r/2), or a neighbouring pair
+// inside a chunk, never leaves its thread, so a row may be turned in place, and
+// each load of a wave covers whole 64-byte pieces.
 template <typename T, bool INTER> struct PairChunks {
   static constexpr int N = Chunk<T>::N;
   int col[2];
   bool turns;
   float c[N], s[N];
   __device__ __forceinline__ PairChunks(const Rotation& rot, int j, int p, float sign) {
-    const int nrot = rot.r / (2 * N);
-    turns = j < nrot;
-    if (turns && !INTER) {
-      col[0] = N * j;
-      col[1] = rot.r / 2 + N * j;
-    } else {
-      col[0] = 2 * N * j;
-      col[1] = 2 * N * j + N;
-    }
+    turns = j < rot.r / (2 * N);
+    col[0] = turns ? N * j : 2 * N * j;
+    col[1] = turns ? rot.r / 2 + N * j : 2 * N * j + N;
 #pragma unroll
     for (int e = 0; e < N; ++e) c[e] = 1.f, s[e] = 0.f;
     if (turns) {
 #pragma unroll
       for (int e = 0; e < N; ++e) {
-        turn_cs(p, rot.freqs[N * j + e], rot.amplitude, c[e], s[e]);
+        const int i = !INTER ? N * j + e : (e < N / 2 ? N * j / 2 : rot.r / 4 + N * j / 2 - N / 2) + e;
+        turn_cs(p, rot.freqs[i], rot.amplitude, c[e], s[e]);
         s[e] *= sign;
       }
     }
