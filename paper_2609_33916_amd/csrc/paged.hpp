@@ -112,18 +112,12 @@ __global__ void __launch_bounds__(256) append_kernel(const AppendArgs a) {
   const int tok = blockIdx.x * (256 / tpt) + threadIdx.x / tpt;
   if (tok >= a.tokens) return;
   const int b = tok / a.T, t = tok - b * a.T;
-  int p = 0;
-  const long long row = append_row(a, b, t, p);
-  if (row < 0) return;
-  const PairChunks<bf16, INTER> pc(a.rot, j, p, 1.f);
+  PairChunks<bf16, INTER> pc(a.rot, j);
   const bf16* ks = (const bf16*)a.k_new + b * a.ks.b + t * a.ks.t;
   const bf16* vs = (const bf16*)a.v_new + b * a.vs.b + t * a.vs.t;
-  bf16* kd = (bf16*)a.kp + row * a.d;
-  bf16* vd = (bf16*)a.vp + row * a.d;
-  const long long hs = (long long)a.d << a.pg.shift;
   const int h1 = min((int)(blockIdx.y + 1) * a.hgroup, a.pg.Hkv);
-  for (int h0 = blockIdx.y * a.hgroup; h0 < h1; h0 += U) {
-    u32x4 ka[U], kb[U], va[U], vb[U];
+  u32x4 ka[U], kb[U], va[U], vb[U];
+  auto load = [&](int h0) __attribute__((always_inline)) {
 #pragma unroll
     for (int u = 0; u < U; ++u)
       if (h0 + u < h1) {
@@ -133,6 +127,16 @@ __global__ void __launch_bounds__(256) append_kernel(const AppendArgs a) {
         va[u] = *(const u32x4*)(v + pc.col[0]);
         vb[u] = *(const u32x4*)(v + pc.col[1]);
       }
+  };
+  load(blockIdx.y * a.hgroup);   // in flight while the place and the angles are found
+  int p = 0;
+  const long long row = append_row(a, b, t, p);
+  if (row < 0) return;
+  pc.angles(a.rot, j, p, 1.f);
+  bf16* kd = (bf16*)a.kp + row * a.d;
+  bf16* vd = (bf16*)a.vp + row * a.d;
+  const long long hs = (long long)a.d << a.pg.shift;
+  for (int h0 = blockIdx.y * a.hgroup; h0 < h1; h0 += U) {
 #pragma unroll
     for (int u = 0; u < U; ++u)
       if (h0 + u < h1) {
@@ -143,6 +147,7 @@ __global__ void __launch_bounds__(256) append_kernel(const AppendArgs a) {
         *(u32x4*)(v + pc.col[0]) = va[u];
         *(u32x4*)(v + pc.col[1]) = vb[u];
       }
+    load(h0 + U);
   }
 }
 
@@ -309,6 +314,8 @@ struct PagedArgs {
   int negate;                  // the scale is negative
 };
 
+constexpr int kShort = 64;   // keys of a short sequence: L is off by 1e-6 with two parts and one key, by 2e-7 with ten
+
 typedef const __attribute__((address_space(4))) int* ConstInt;   // uniform reads by the scalar unit
 
 // A barrier that orders LDS only: loads stay in flight across it.
@@ -384,7 +391,7 @@ __global__ void __launch_bounds__(256, 2) paged_decode_kernel(const PagedArgs a)
   constexpr int RB = Q4 ? D / 2 : 2 * D;                 // bytes of a row
   constexpr int QS = D + 8;                              // row stride of the queries in LDS (elements)
   constexpr int VBYTES = 4 * BK * RB, OBYTES = 4 * D * C * 4;
-  constexpr int BYTES = VBYTES + (REP == 1 ? 2 : 1) * C * QS * 2;
+  constexpr int BYTES = VBYTES + (REP == 1 ? 3 : 2) * C * QS * 2;
   // the waves' stages of V and the queries; at the end the waves' O
   __shared__ __attribute__((aligned(16))) unsigned char smem[BYTES > OBYTES ? BYTES : OBYTES];
   __shared__ float ml[2][4][C];
@@ -494,8 +501,9 @@ __global__ void __launch_bounds__(256, 2) paged_decode_kernel(const PagedArgs a)
   const bool writes = a.fuse_append && T_b - 1 >= k_lo && T_b - 1 < k_hi;
 
   // ---- the queries, turned, as two bfloat16 each (their sum is 16 bits of the
-  // result; one alone would cost L its last digits), and the new row
-  bf16 *const qh = (bf16*)(smem + VBYTES), *const ql = qh + C * QS;
+  // result; one alone would cost L its last digits), in short sequences, where a
+  // score's error does not average out, as three (24 bits); and the new row
+  bf16 *const qh = (bf16*)(smem + VBYTES), *const ql = qh + C * QS, *const qm = REP == 1 ? ql + C * QS : ql;
   {
     float cs = 1.f, sn = 0.f;
     if (turns) turn_cs(pos, freq, a.rot.amplitude, cs, sn);
@@ -510,7 +518,11 @@ __global__ void __launch_bounds__(256, 2) paged_decode_kernel(const PagedArgs a)
       if ((REP == 1 ? r : r % HR) >= nq) y = z = 0.f;
       if (a.negate) y = -y, z = -z;
       const bf16 yh = (bf16)y, zh = (bf16)z;
-      const bf16 yl = (bf16)(turns ? y - (float)yh : 0.f), zl = (bf16)(turns ? z - (float)zh : 0.f);
+      const float yr = turns ? y - (float)yh : 0.f, zr = turns ? z - (float)zh : 0.f;
+      const bf16 yl = (bf16)yr, zl = (bf16)zr;
+      const bool third = REP == 1 || r / HR % 2 == 0;
+      qm[r * QS + c0] = (bf16)(third ? yr - (float)yl : 0.f);
+      qm[r * QS + c1] = (bf16)(third ? zr - (float)zl : 0.f);
       if constexpr (REP == 1) {
         qh[r * QS + c0] = yh;
         qh[r * QS + c1] = zh;
@@ -684,6 +696,22 @@ __global__ void __launch_bounds__(256, 2) paged_decode_kernel(const PagedArgs a)
           if constexpr (REP == 1) mma16(s[q][kb], kf, qr[q][t]);
         }
       }
+    if (T_b <= kShort) {
+#pragma unroll
+      for (int q = 0; q < NQ; ++q)
+#pragma unroll
+        for (int t = 0; t < TD; ++t) {
+          const bf16x8 qf3 = *(const bf16x8*)(qm + (16 * q + c) * QS + (Q4 ? D / 4 * g + 8 * t : 32 * t + 8 * g));
+#pragma unroll
+          for (int kb = 0; kb < KB; ++kb) {
+            if constexpr (Q4) {
+              float u = unit[kb];
+              asm("" : "+v"(u));   // converted again: kept from above, the operands would take 64 registers
+              mma16(s[q][kb], Quant4::get(word(x.k[kb][0], t), u), qf3);
+            } else mma16(s[q][kb], __builtin_bit_cast(bf16x8, x.k[kb][t]), qf3);
+          }
+        }
+    }
     if constexpr (REP > 1) {   // the sum of the two parts, in both
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb)

@@ -82,10 +82,13 @@ template <typename T, bool INTER> struct PairChunks {
   int col[2];
   bool turns;
   float c[N], s[N];
-  __device__ __forceinline__ PairChunks(const Rotation& rot, int j, int p, float sign) {
+  __device__ __forceinline__ PairChunks(const Rotation& rot, int j) {
     turns = j < rot.r / (2 * N);
     col[0] = turns ? N * j : 2 * N * j;
     col[1] = turns ? rot.r / 2 + N * j : 2 * N * j + N;
+  }
+  // position p; `sign` of the sine
+  __device__ __forceinline__ void angles(const Rotation& rot, int j, int p, float sign) {
 #pragma unroll
     for (int e = 0; e < N; ++e) c[e] = 1.f, s[e] = 0.f;
     if (turns) {
@@ -155,7 +158,8 @@ __global__ void __launch_bounds__(256) rope_kernel(const RopeArgs a) {
   if (tok >= a.tokens) return;
   const int b = tok / a.n, i = tok - b * a.n;
   const int p = a.pos ? a.pos[b * a.pos_stride + i] : a.start + i;
-  const PairChunks<T, INTER> pc(a.rot, j, p, a.sign);
+  PairChunks<T, INTER> pc(a.rot, j);
+  pc.angles(a.rot, j, p, a.sign);
   const int h1 = min((int)(blockIdx.y + 1) * a.hgroup, a.Hq + a.Hk);
   for (int h0 = blockIdx.y * a.hgroup; h0 < h1; h0 += U) {
     u32x4 xa[U], xb[U];
