@@ -589,15 +589,21 @@ __global__ void __launch_bounds__(256, 2) paged_decode_kernel(const PagedArgs a)
     }
   }
   lds_barrier();
-  bf16x8 qf[NQ][TD], qr[NQ][REP == 1 ? TD : 1];
+  // With two columns of queries at d = 128 their operands stay in LDS (64 registers).
+  constexpr bool QLDS = NQ == 2 && D == 128;
+  auto query = [&](const bf16* part, int x, int t) __attribute__((always_inline)) {
+    return *(const bf16x8*)(part + (16 * x + c) * QS + (Q4 ? D / 4 * g + 8 * t : 32 * t + 8 * g));
+  };
+  bf16x8 qf[NQ][TD], qr[NQ][TD];
+  if constexpr (!QLDS) {
 #pragma unroll
-  for (int x = 0; x < NQ; ++x)
+    for (int x = 0; x < NQ; ++x)
 #pragma unroll
-    for (int t = 0; t < TD; ++t) {
-      const int at = (16 * x + c) * QS + (Q4 ? D / 4 * g + 8 * t : 32 * t + 8 * g);
-      qf[x][t] = *(const bf16x8*)(qh + at);
-      if constexpr (REP == 1) qr[x][t] = *(const bf16x8*)(ql + at);
-    }
+      for (int t = 0; t < TD; ++t) {
+        qf[x][t] = query(qh, x, t);
+        if constexpr (REP == 1) qr[x][t] = query(ql, x, t);
+      }
+  }
 
   f32x4 oacc[NQ][DB];
   float m_use[NQ], lsum[NQ];
@@ -684,7 +690,14 @@ __global__ void __launch_bounds__(256, 2) paged_decode_kernel(const PagedArgs a)
       for (int kb = 0; kb < KB; ++kb) unit[kb] = __uint_as_float(((x.ks[kb] >> kshift) & 255u) << 23);
     }
 #pragma unroll
-    for (int t = 0; t < TD; ++t)   // the chains of the KB sums side by side
+    for (int t = 0; t < TD; ++t) {   // the chains of the KB sums side by side
+      if constexpr (QLDS) {
+#pragma unroll
+        for (int q = 0; q < NQ; ++q) {
+          qf[q][t] = query(qh, q, t);
+          qr[q][t] = query(ql, q, t);
+        }
+      }
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb) {
         bf16x8 kf;
@@ -696,12 +709,13 @@ __global__ void __launch_bounds__(256, 2) paged_decode_kernel(const PagedArgs a)
           if constexpr (REP == 1) mma16(s[q][kb], kf, qr[q][t]);
         }
       }
+    }
     if (T_b <= kShort) {
 #pragma unroll
       for (int q = 0; q < NQ; ++q)
 #pragma unroll
         for (int t = 0; t < TD; ++t) {
-          const bf16x8 qf3 = *(const bf16x8*)(qm + (16 * q + c) * QS + (Q4 ? D / 4 * g + 8 * t : 32 * t + 8 * g));
+          const bf16x8 qf3 = query(qm, q, t);
 #pragma unroll
           for (int kb = 0; kb < KB; ++kb) {
             if constexpr (Q4) {
@@ -817,6 +831,7 @@ __global__ void __launch_bounds__(256, 2) paged_decode_kernel(const PagedArgs a)
         }
       };
       auto block = [&](auto dl) __attribute__((always_inline)) {
+        if constexpr (NQ == 2) __builtin_amdgcn_sched_barrier(0);   // one block's operands at a time: registers
         scaled(dl);
 #pragma unroll
         for (int r = 0; r < REP; ++r) products(r * DL + decltype(dl)::value);
