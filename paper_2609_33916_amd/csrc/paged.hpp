@@ -390,7 +390,7 @@ __global__ void __launch_bounds__(256, 2) paged_decode_kernel(const PagedArgs a)
   constexpr int C = 16 * NQ;                             // query columns
   constexpr int RB = Q4 ? D / 2 : 2 * D;                 // bytes of a row
   constexpr int QS = D + 8;                              // row stride of the queries in LDS (elements)
-  constexpr int VBYTES = 4 * BK * RB, OBYTES = 4 * D * C * 4;
+  constexpr int VBYTES = 4 * BK * RB, OS = D + 4, OBYTES = 4 * C * OS * 4;
   constexpr int BYTES = VBYTES + (REP == 1 ? 3 : 2) * C * QS * 2;
   // the waves' stages of V and the queries; at the end the waves' O
   __shared__ __attribute__((aligned(16))) unsigned char smem[BYTES > OBYTES ? BYTES : OBYTES];
@@ -859,7 +859,8 @@ __global__ void __launch_bounds__(256, 2) paged_decode_kernel(const PagedArgs a)
     if (kv + 4 * BK < k_hi) step(B2, kv + 4 * BK);
   }
 
-  // ---- merge the waves through LDS: O parts [4][D][C], maxima and sums [4][C]
+  // ---- merge the waves through LDS: O parts [4][C][D] (rows padded by 16 bytes), maxima
+  // and sums [4][C]
   lds_barrier();
   float* ow = (float*)smem;
 #pragma unroll
@@ -871,9 +872,7 @@ __global__ void __launch_bounds__(256, 2) paged_decode_kernel(const PagedArgs a)
       ml[1][w][16 * q + c] = l;
     }
 #pragma unroll
-    for (int db = 0; db < DB; ++db)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) ow[(w * D + 16 * db + 4 * g + i) * C + 16 * q + c] = oacc[q][db][i];
+    for (int db = 0; db < DB; ++db) *(f32x4*)(ow + (w * C + 16 * q + c) * OS + 16 * db + 4 * g) = oacc[q][db];
   }
   lds_barrier();
   constexpr int heads = C / REP;
@@ -888,8 +887,7 @@ __global__ void __launch_bounds__(256, 2) paged_decode_kernel(const PagedArgs a)
     for (int v = 0; v < 4; ++v) {
       const float f = M == -INFINITY ? 0.f : exp2_fast(ml[0][v][col] - M);
       l += f * ml[1][v][col];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) acc[i] += f * ow[(v * D + 4 * d4 + i) * C + col + HR * (4 * d4 / (D / REP))];
+      acc += f * *(const f32x4*)(ow + (v * C + col + HR * (4 * d4 / (D / REP))) * OS + 4 * d4);
     }
     const size_t row = (size_t)b * a.Hq + h0 + col;
     if (a.nsplit == 1) {
