@@ -76,6 +76,11 @@ bool fits(const Strides& s, int B, int H, int n) {   // offsets in 62 bits
   return far < ((__int128)1 << 60);
 }
 
+// Workgroups of 256 threads for `rows` rows, `per` to a workgroup; a launch has fewer
+// than 2^32 threads along an axis.
+long long blocks_for(long long rows, int per) { return (rows + per - 1) / per; }
+bool launches(long long rows, int per) { return blocks_for(rows, per) < 1LL << 24; }
+
 // Heads per workgroup: a thread's sines and cosines serve all of them, so as many,
 // up to 8, as leave four workgroups per compute unit.
 int heads_per_group(long long token_blocks, int heads) {
@@ -84,8 +89,7 @@ int heads_per_group(long long token_blocks, int heads) {
 }
 
 template <typename T> void launch_rope(attn::RopeArgs a, bool interleaved, hipStream_t st) {
-  const int per = 256 / (a.d / (2 * attn::Chunk<T>::N));
-  const unsigned blocks = (unsigned)((a.tokens + (long long)per - 1) / per);
+  const unsigned blocks = (unsigned)blocks_for(a.tokens, 512 * attn::Chunk<T>::N / a.d);
   a.hgroup = heads_per_group(blocks, a.Hq + a.Hk);
   const dim3 grid(blocks, (a.Hq + a.Hk + a.hgroup - 1) / a.hgroup);
   if (interleaved) hipLaunchKernelGGL((attn::rope_kernel<T, true>), grid, dim3(256), 0, st, a);
@@ -102,7 +106,8 @@ int rope(const void* q, const void* k, void* q_out, void* k_out, const long long
   if (!good_d(d)) return ATTN_E_UNSUPPORTED;
   if (const int rc = check_rotation(freqs, r, d, amplitude, interleaved)) return rc;
   const int elem = dtype == ATTN_BF16 ? 2 : 4;
-  if ((long long)B * n > INT_MAX || (long long)Hq + Hk > 65535) return ATTN_E_SHAPE;
+  if ((long long)B * n > INT_MAX || !launches((long long)B * n, 8192 / elem / d) || (long long)Hq + Hk > 65535)
+    return ATTN_E_SHAPE;
   if (positions ? pos_stride < 0 || pos_stride > LLONG_MAX / B : start > INT_MAX - n) return ATTN_E_SHAPE;
   attn::RopeArgs a{};
   a.q = q; a.k = k; a.qo = q_out; a.ko = k_out;
@@ -162,10 +167,10 @@ template <int D> void launch_append4(const attn::AppendArgs& a, const dim3& grid
   if (interleaved) hipLaunchKernelGGL((attn::append4_kernel<D, true>), grid, dim3(256), 0, st, a);
   else hipLaunchKernelGGL((attn::append4_kernel<D, false>), grid, dim3(256), 0, st, a);
 }
+int append_tokens(int d, bool q4) { return 256 / (d / (q4 ? 8 : 16)); }   // per workgroup
 void launch_append(attn::AppendArgs a, bool interleaved, hipStream_t st) {
   const bool q4 = a.ksc != nullptr;
-  const int per = 256 / (a.d / (q4 ? 8 : 16));
-  const unsigned blocks = (unsigned)((a.tokens + (long long)per - 1) / per);
+  const unsigned blocks = (unsigned)blocks_for(a.tokens, append_tokens(a.d, q4));
   a.hgroup = heads_per_group(blocks, a.pg.Hkv);
   const dim3 grid(blocks, (a.pg.Hkv + a.hgroup - 1) / a.hgroup);
   if (q4) {
@@ -244,7 +249,8 @@ int attn_paged_append(const void* k_new, const void* v_new, const long long* str
   if (const int rc = check_pages(k_pages, v_pages, k_scales, v_scales, block_table, lens, B, Hkv, num_pages, page_size,
                                  table_width, d, dtype))
     return rc;
-  if (T < 1 || (long long)B * T > INT_MAX) return ATTN_E_SHAPE;
+  if (T < 1 || (long long)B * T > INT_MAX || !launches((long long)B * T, append_tokens(d, k_scales != nullptr)))
+    return ATTN_E_SHAPE;
   if (const int rc = check_rotation(freqs, r, d, amplitude, interleaved)) return rc;
   attn::AppendArgs a{};
   a.k_new = k_new; a.v_new = v_new;
@@ -274,7 +280,8 @@ int attn_paged_gather(const void* k_pages, const void* v_pages, const void* k_sc
   if (const int rc = check_pages(k_pages, v_pages, k_scales, v_scales, block_table, lens, B, Hkv, num_pages, page_size,
                                  table_width, d, dtype))
     return rc;
-  if (n < 1 || (__int128)B * Hkv * n * d > ((__int128)1 << 46)) return ATTN_E_SHAPE;
+  const int per = 256 / (d / 8);
+  if (n < 1 || !launches(n, per) || (__int128)B * Hkv * n * d > ((__int128)1 << 46)) return ATTN_E_SHAPE;
   if (!aligned(K, 16) || !aligned(V, 16) || !aligned(starts, 4)) return ATTN_E_ALIGN;
   attn::GatherArgs a{};
   a.kp = k_pages; a.vp = v_pages;
@@ -283,8 +290,7 @@ int attn_paged_gather(const void* k_pages, const void* v_pages, const void* k_sc
   a.lens = lens; a.starts = starts;
   a.k = K; a.v = V;
   a.n = n; a.d = d;
-  const int per = 256 / (d / 8);
-  const dim3 grid((unsigned)((n + (long long)per - 1) / per), Hkv, B);
+  const dim3 grid((unsigned)blocks_for(n, per), Hkv, B);
   hipStream_t st = static_cast<hipStream_t>(stream);
   (void)hipGetLastError();
   if (k_scales) hipLaunchKernelGGL(attn::gather_kernel<true>, grid, dim3(256), 0, st, a);

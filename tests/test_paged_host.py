@@ -171,6 +171,19 @@ class Fake(FakeLib):
         return 4096
 
 
+@pytest.mark.parametrize("elem,d", [(2, 128), (2, 64), (2, 32), (4, 128), (4, 32)])
+def test_launches_past_32_bits(L, elem, d):
+    """More threads than a launch can have (2^32 along an axis): refused, not launched."""
+    n = min(2**32 * 8 * 4 // elem // d, 2**31 - 1)   # a thread per 32 bytes
+    for fn in ("attn_rope", "attn_rope_bwd"):
+        assert _rope(L, fn, B=1, n=n, start=-n, d=d, r=16, dtype=0 if elem == 2 else 1) == -2
+    if elem == 2:
+        for four in (False, True):
+            sc = dict(ks=FAKE, vs=FAKE) if four else {}
+            assert _append(L, B=1, T=min(2**32 * (8 if four else 16) // d, 2**31 - 1), d=d, **sc) == -2
+            assert _gather(L, B=1, Hkv=1, n=min(2**32 * 8 // d, 2**31 - 1), d=d, **sc) == -2
+
+
 @pytest.fixture
 def fake(monkeypatch):
     f = Fake()
