@@ -619,12 +619,13 @@ __global__ void __launch_bounds__(256, 2) paged_decode_kernel(const PagedArgs a)
   const unsigned kshift = 8 * (ksb & 3);
   const float sl2 = a.sl2;
   // the new row in place of what its page held: lane (g, c) has a part of key c and,
-  // of V, 16 (bf16) or RB / 4 bytes at its place in the 16 rows
+  // of V, 16 (bf16) or RB / 4 bytes at its place in the 16 rows. Without a page it takes
+  // no part: its values stay out, for 0 times one that is not finite is not 0.
   auto patch = [&](Block& x, int at) __attribute__((always_inline)) {
     const int row = at & 15;
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) {
-      const bool here = at >> 4 == kb;
+      const bool here = at >> 4 == kb && limit(x, kb) > 0;
       const bool k_mine = here && c == row;
       if constexpr (!Q4) {
 #pragma unroll

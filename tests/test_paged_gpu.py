@@ -289,6 +289,22 @@ def test_decode_bad_pages(bits):
 
 
 @pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("page", [16, 64])
+@pytest.mark.parametrize("bad", [float("inf"), NAN])
+def test_new_row_without_a_page_stays_out(bits, page, bad):
+    """The newest token has no page: its values, finite or not, do not touch the result,
+    which is that of the tokens before it."""
+    pool = Pool([page + 1, 1], 1, page, 64, bits).fill([page, 0])
+    pool.t_table[0, 1] = pool.t_table[1, 0] = -1
+    q = torch.randn(2, 4, 64, device="cuda").to(BF16)
+    new = torch.full((2, 1, 64), bad, device="cuda").to(BF16)
+    want = lib.attn_paged_decode(q, lens=ints([page, 0]), **pool.args())
+    for k, v in ((q[:, :1], new), (new, q[:, :1]), (new, new)):
+        got = lib.attn_paged_decode(q, lens=ints([page, 0]), k_new=k.contiguous(), v_new=v.contiguous(), **pool.args())
+        assert all(torch.equal(x, y) for x, y in zip(got, want))
+
+
+@pytest.mark.parametrize("bits", [16, 4])
 @pytest.mark.parametrize("scale", [-0.2, 0.0, 0.5, 3.0])
 def test_decode_scales(bits, scale):
     decode_case([300, 20], 8, 2, 16, 64, bits, r=32, scale=scale, seed=8)
