@@ -294,15 +294,6 @@ long long mat_lda(int n) { return ((long long)n + 127) / 128 * 128; }
 
 }  // namespace
 
-namespace attn {
-void launch_paged_combine(const float* part, void* o, float* lse, int rows, int nsplit, int d, hipStream_t st) {
-  const dim3 grid((unsigned)rows), block(256);
-  if (d == 32) hipLaunchKernelGGL((decode_combine_kernel<bf16, 32, true>), grid, block, 0, st, part, o, lse, rows, nsplit);
-  else if (d == 64) hipLaunchKernelGGL((decode_combine_kernel<bf16, 64, true>), grid, block, 0, st, part, o, lse, rows, nsplit);
-  else hipLaunchKernelGGL((decode_combine_kernel<bf16, 128, true>), grid, block, 0, st, part, o, lse, rows, nsplit);
-}
-}  // namespace attn
-
 extern "C" {
 
 size_t attn_workspace_bytes(int B, int H, int n, int d) {

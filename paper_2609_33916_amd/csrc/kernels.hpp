@@ -1789,8 +1789,7 @@ __global__ void __launch_bounds__(256) decode_kernel(const DecArgs a) {
 // O_s / sum_s 2^(m_s - M) l_s and L = (M + log2 l) ln 2. One workgroup per
 // row: thread t takes 4 consecutive d values (t % (D/4)) of the splits
 // s = t / (D/4) + k * SL, and the SL partial sums are added through LDS.
-// NANS: a split whose scores were all NaN, and which so has no maximum, counts.
-template <typename T, int D, bool NANS = false>
+template <typename T, int D>
 __global__ void __launch_bounds__(256) decode_combine_kernel(const float* part, void* o, float* lse, int rows,
                                                              int nsplit) {
   // one workgroup per query row; thread t takes 4 of the d values (dl) of
@@ -1808,7 +1807,7 @@ __global__ void __launch_bounds__(256) decode_combine_kernel(const float* part, 
   f32x4 acc = (f32x4){0.f, 0.f, 0.f, 0.f};
   // fold one partial state (m: base-2 max, l: sum, v: unnormalised O) into (mt, lt, acc)
   auto fold = [&](float m, float l, f32x4 v) __attribute__((always_inline)) {
-    if (m == -INFINITY && !(NANS && l != l)) return;   // an empty split
+    if (m == -INFINITY) return;   // an empty split
     const float nm = fmaxf(mt, m);
     const float a = (mt == -INFINITY) ? 0.f : exp2_fast(mt - nm), b = exp2_fast(m - nm);
     lt = lt * a + l * b;
@@ -1841,10 +1840,9 @@ __global__ void __launch_bounds__(256) decode_combine_kernel(const float* part, 
     acc = (f32x4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int k = 0; k < SL; ++k) fold(smax[k][t], ssum[k][t], sacc[k][t]);
-    const bool any = NANS ? lt != 0.f : lt > 0.f;
-    const float inv = any ? 1.f / lt : 0.f;
+    const float inv = lt > 0.f ? 1.f / lt : 0.f;
     Quad<T>::store((T*)o + (size_t)row * D + 4 * t, acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
-    if (lse && t == 0) lse[row] = any ? (mt + log2f(lt)) * kLn2 : -INFINITY;
+    if (lse && t == 0) lse[row] = lt > 0.f ? (mt + log2f(lt)) * kLn2 : -INFINITY;
   }
 }
 

@@ -54,7 +54,4 @@ template <int D, bool CAUSAL> void launch_fwd_x3(FwdArgs a, int heads, hipStream
 template <int D, bool CAUSAL> void launch_dkdv_x3(BwdArgs a, int heads, hipStream_t st);
 template <int D, bool CAUSAL> void launch_dq_x3(BwdArgs a, int heads, hipStream_t st);
 
-// Merges the splits of a paged decode step (attn.hip).
-void launch_paged_combine(const float* part, void* o, float* lse, int rows, int nsplit, int d, hipStream_t st);
-
 }  // namespace attn

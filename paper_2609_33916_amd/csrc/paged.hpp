@@ -304,7 +304,7 @@ struct PagedArgs {
   const int* lens;
   const int* pos;              // [B] positions of the queries (and new keys), or null: T_b - 1
   Rotation rot;
-  float* part;                 // nsplit > 1: as decode_kernel's
+  float* part;                 // nsplit > 1: [rows][nsplit][d] unnormalised O, then [rows][nsplit] (max2, sum)
   void* o;
   float* lse;
   int Hq, G, n, append, fuse_append, rows;
@@ -903,6 +903,75 @@ __global__ void __launch_bounds__(256, 2) paged_decode_kernel(const PagedArgs a)
         pml[1] = l;
       }
     }
+  }
+}
+
+// O = sum_s 2^(m_s - M) O_s / l and L = (M + log2 l) ln 2 with M = max_s m_s, l =
+// sum_s 2^(m_s - M) l_s over the splits of a query row: W waves per row, 64 / (D / 4)
+// splits of a wave side by side, U loads of each in flight.
+template <int D, int W>
+__global__ void __launch_bounds__(64 * W) paged_combine_kernel(const float* part, void* o, float* lse, int rows, int nsplit) {
+  constexpr int DL = D / 4, SL = 64 / DL, U = 8;
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, dl = lane % DL, row = blockIdx.x;
+  const float* po = part + (size_t)row * nsplit * D + 4 * dl;
+  const f32x2* pml = (const f32x2*)(part + (size_t)rows * nsplit * D + (size_t)row * nsplit * 2);
+  float m = -INFINITY, l = 0.f;
+  f32x4 acc = (f32x4){0.f, 0.f, 0.f, 0.f};
+  // to the maximum `to`; an empty part (maximum -inf) counts 0 times, so that a NaN in it stays
+  auto weight = [](float from, float to) __attribute__((always_inline)) { return from == -INFINITY ? 0.f : exp2_fast(from - to); };
+  for (int s0 = w * SL + lane / DL; s0 < nsplit; s0 += W * SL * U) {
+    f32x2 ml[U];
+    f32x4 v[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int s = s0 + W * SL * u;
+      ml[u] = (f32x2){-INFINITY, 0.f};
+      v[u] = (f32x4){0.f, 0.f, 0.f, 0.f};
+      if (s < nsplit) {
+        ml[u] = pml[s];
+        v[u] = *(const f32x4*)(po + (size_t)s * D);
+      }
+    }
+    float M = m;
+#pragma unroll
+    for (int u = 0; u < U; ++u) M = fmaxf(M, ml[u][0]);
+    const float f = weight(m, M);
+    l *= f;
+    acc *= f;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const float fu = weight(ml[u][0], M);
+      l += fu * ml[u][1];
+      acc += fu * v[u];
+    }
+    m = M;
+  }
+  auto join = [&](float m2, float l2, f32x4 a2) __attribute__((always_inline)) {
+    const float M = fmaxf(m, m2), f = weight(m, M), f2 = weight(m2, M);
+    l = f * l + f2 * l2;
+    acc = f * acc + f2 * a2;
+    m = M;
+  };
+#pragma unroll
+  for (int k = DL; k < 64; k *= 2)
+    join(__shfl_xor(m, k), __shfl_xor(l, k),
+         (f32x4){__shfl_xor(acc[0], k), __shfl_xor(acc[1], k), __shfl_xor(acc[2], k), __shfl_xor(acc[3], k)});
+  if constexpr (W > 1) {
+    __shared__ float sm[W - 1], sl[W - 1];
+    __shared__ __attribute__((aligned(16))) f32x4 sa[W - 1][DL];
+    if (w && lane < DL) {
+      if (lane == 0) sm[w - 1] = m, sl[w - 1] = l;
+      sa[w - 1][lane] = acc;
+    }
+    __syncthreads();
+    if (w) return;
+#pragma unroll
+    for (int k = 0; k < W - 1; ++k) join(sm[k], sl[k], sa[k][dl]);
+  }
+  if (lane < DL) {
+    const float inv = l == 0.f ? 0.f : 1.f / l;   // NaN stays
+    Quad<bf16>::store((bf16*)o + (size_t)row * D + 4 * lane, acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
+    if (lse && lane == 0) lse[row] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
   }
 }
 

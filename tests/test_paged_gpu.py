@@ -281,6 +281,15 @@ def test_decode_many_splits(bits, d):
 
 
 @pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("d", [32, 64, 128])
+def test_decode_joins_hundreds_of_splits(bits, d):
+    """One cache head; the lengths fill all of the splits, a few, one, none but the new row's."""
+    for x, n in ((40000, 40000), (19000, 40000), (70, 40000), (0, 40000)):
+        decode_case([x], 3, 1, 16, d, bits, r=32, n=n, width=2501, seed=x + 1)
+    decode_case([0], 3, 1, 16, d, bits, append=False, n=40000, width=2501)
+
+
+@pytest.mark.parametrize("bits", [16, 4])
 def test_decode_bad_pages(bits):
     """Numbers outside the pool inside a sequence: those tokens do not take part, the
     new row among them is not written; a sequence with none left."""
