@@ -184,21 +184,40 @@ void launch_append(attn::AppendArgs a, bool interleaved, hipStream_t st) {
 }
 
 // Decode: a workgroup owns (sequence, cache head, up to 32 query heads, one split
-// of the keys); the keys are split, a block for each of its four waves at
-// least, until there are about two workgroups per compute unit.
-constexpr long long kWorkgroups = 512;
+// of the keys). The keys are split, a block for each of its four waves at least,
+// into as many parts as leave no more than two workgroups per compute unit, so that
+// all run at once (160 groups of 1900 tokens in 4 bits 14.8 us in three parts, 18.3 in
+// four, 640 workgroups; one sequence of 131072 tokens in 4 bits 31, up to 768 workgroups
+// 36); from 257 groups on in two, which then even each other out (384 groups of 2000
+// tokens 66 us, undivided 72).
+//
+// Merging the splits costs a launch and 2.5 to 4 us, so up to a number of blocks
+// the keys stay undivided: few where many parts would share them (d = 128, 600 tokens in
+// 4 bits, 64 groups: 8.6 us, in two parts 9.8), more for three (160 groups of 1200
+// tokens in 4 bits 11.4, 12.8) and most where two workgroups of a compute unit would
+// only halve what one has to itself (256 groups of 1900 tokens in 4 bits 15.9, 18.4;
+// bfloat16, 1500: 34.3, 37.5). Beyond, sequences of different lengths need the
+// splits (176 groups of 8000 to 16000 tokens in 4 bits 55 us, undivided 63). In 4 bits
+// with two query columns at d = 128 (registers spill) a block takes several times as
+// long, and the limits are lower (2 groups of 1000 tokens 12.5 us, undivided 20.0; 220 of
+// 4096 62.7, 73.8; but 300 of 1000 undivided 31.7, in two 41.1).
+constexpr long long kWorkgroups = 2 * attn::kXcds * attn::kCusPerXcd;
 struct PagedPlan {
   int nq;        // query columns of a workgroup / 16
   int qchunks, nsplit;
 };
-PagedPlan paged_plan(int B, int Hq, int Hkv, int n, int append, bool q4) {
+PagedPlan paged_plan(int B, int Hq, int Hkv, int n, int d, int append, bool q4) {
   PagedPlan p;
   const int G = Hq / Hkv, block = q4 ? 64 : 32;
   p.nq = G > 16 ? 2 : 1;
   p.qchunks = (G + 16 * p.nq - 1) / (16 * p.nq);
   const long long groups = (long long)B * Hkv * p.qchunks;
   const long long blocks = ((long long)n + append + block - 1) / block;
-  p.nsplit = (int)std::max<long long>(1, std::min((kWorkgroups + groups - 1) / groups, blocks / 4));
+  const bool crowded = 2 * groups > kWorkgroups;
+  const long long parts = groups >= kWorkgroups ? 1 : crowded ? 2 : kWorkgroups / groups;
+  long long undivided = parts > 3 ? (q4 ? 16 : 12) : parts == 3 || crowded ? (q4 ? 32 : 16) : (q4 ? 128 : 64);
+  if (q4 && p.nq == 2 && d == 128) undivided = parts > 3 ? 4 : 32;
+  p.nsplit = blocks <= undivided ? 1 : (int)std::min(parts, blocks / 4);
   return p;
 }
 
@@ -310,7 +329,7 @@ int attn_paged_gather(const void* k_pages, const void* v_pages, const void* k_sc
 
 size_t attn_paged_decode_workspace_bytes(int B, int Hq, int Hkv, int n, int d, int append, int bits) {
   if (B < 1 || Hq < 1 || Hkv < 1 || Hq % Hkv != 0 || n < 0 || !good_d(d) || (bits != 16 && bits != 4)) return 0;
-  const PagedPlan p = paged_plan(B, Hq, Hkv, n, append ? 1 : 0, bits == 4);
+  const PagedPlan p = paged_plan(B, Hq, Hkv, n, d, append ? 1 : 0, bits == 4);
   if (p.nsplit == 1) return 0;
   return (size_t)B * Hq * p.nsplit * (size_t)(d + 2) * sizeof(float);
 }
@@ -343,7 +362,7 @@ int attn_paged_decode(const void* q, const void* k_new, const void* v_new, const
   if (!aligned(q, 16) || !aligned(k_new, 16) || !aligned(v_new, 16) || !aligned(O, 16) || !aligned(L, 4) ||
       !aligned(positions, 4))
     return ATTN_E_ALIGN;
-  const PagedPlan plan = paged_plan(B, Hq, Hkv, n, append, q4);
+  const PagedPlan plan = paged_plan(B, Hq, Hkv, n, d, append, q4);
   if ((long long)B * Hkv * plan.qchunks > 65535) return ATTN_E_SHAPE;   // grid y limit
   const size_t need = attn_paged_decode_workspace_bytes(B, Hq, Hkv, n, d, append, q4 ? 4 : 16);
   if (need > 0) {
