@@ -217,15 +217,20 @@ __global__ void __launch_bounds__(256) append4_kernel(const AppendArgs a) {
           if (INTER) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-              const double y = k[2 * e], z = k[2 * e + 1];
-              k[2 * e] = Quant4::odd(y * c[e] - z * s[e]);
-              k[2 * e + 1] = Quant4::odd(z * c[e] + y * s[e]);
+              double y = k[2 * e], z = k[2 * e + 1];
+              turn_pair(y, z, c[e], s[e]);
+              k[2 * e] = Quant4::odd(y);
+              k[2 * e + 1] = Quant4::odd(z);
             }
           } else {
             float m[8];
             Chunk<bf16>::get(xm[u], m);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) k[e] = Quant4::odd((double)k[e] * c[e] - (double)m[e] * s[e]);
+            for (int e = 0; e < 8; ++e) {   // s is negated in the second half
+              double y = k[e], z = m[e];
+              turn_pair(y, z, c[e], s[e]);
+              k[e] = Quant4::odd(y);
+            }
           }
         }
         const long long r = row + ((long long)(h0 + u) << a.pg.shift);
@@ -511,10 +516,7 @@ __global__ void __launch_bounds__(256, 2) paged_decode_kernel(const PagedArgs a)
     for (int i = 0; i < C * P / 256; ++i) {
       const int r = tid / P + 256 / P * i;
       float y = u[i], z = x[i];
-      if (turns) {
-        y = u[i] * cs - x[i] * sn;
-        z = x[i] * cs + u[i] * sn;
-      }
+      if (turns) turn_pair(y, z, cs, sn);
       if ((REP == 1 ? r : r % HR) >= nq) y = z = 0.f;
       if (a.negate) y = -y, z = -z;
       const bf16 yh = (bf16)y, zh = (bf16)z;
@@ -547,9 +549,7 @@ __global__ void __launch_bounds__(256, 2) paged_decode_kernel(const PagedArgs a)
         if (turns) {
           R rc, rs;
           turn_cs(pos, freq, a.rot.amplitude, rc, rs);
-          const R y2 = y * rc - z * rs;
-          z = z * rc + y * rs;
-          y = y2;
+          turn_pair(y, z, rc, rs);
           k0 = (bf16)y;
           k1 = (bf16)z;
         }

@@ -24,8 +24,12 @@ struct Rotation {
   float amplitude;
 };
 
+// Every operation here is rounded as written (no contraction of the compiler's choice),
+// so that all kernels turn a row to the same bits.
+
 // p f, as a fraction of a circle in [-1/2, 1/2]
 __device__ __forceinline__ double turn(int p, double f) {
+#pragma clang fp contract(off)
   const double x = (double)p * f * 0.15915494309189535;   // 1 / (2 pi)
   return x - rint(x);
 }
@@ -36,6 +40,7 @@ __device__ __forceinline__ double turn(int p, double f) {
 // (a = 1), the device library's sine and cosine of a fraction in 32 bits by 1.1e-7; a
 // turned float32 row's error is 3.9e-8 of its length, with those 5.2e-8.
 __device__ __forceinline__ void turn_cs(int p, double f, float a, float& c, float& s) {
+#pragma clang fp contract(off)
   const double y = 4.0 * turn(p, f), q = rint(y), r = y - q;
   const float z = (float)(r * 1.5707963267948966), az = (float)(r * (1.5707963267948966 * (double)a)), z2 = z * z;
   const float e = fmaf(z2, fmaf(z2, fmaf(z2, 1.f / 362880, -1.f / 5040), 1.f / 120), -1.f / 6) * z2;
@@ -48,10 +53,19 @@ __device__ __forceinline__ void turn_cs(int p, double f, float a, float& c, floa
   s = k & 2 ? -s : s;
 }
 __device__ __forceinline__ void turn_cs(int p, double f, float a, double& c, double& s) {
+#pragma clang fp contract(off)
   double c0, s0;
   sincospi(2.0 * turn(p, f), &s0, &c0);
   c = c0 * (double)a;
   s = s0 * (double)a;
+}
+
+// (u, w) turned by the angle of (c, s)
+template <typename R> __device__ __forceinline__ void turn_pair(R& u, R& w, R c, R s) {
+#pragma clang fp contract(off)
+  const R x = u, y = w, ys = y * s, xs = x * s;
+  u = __builtin_elementwise_fma(x, c, -ys);
+  w = __builtin_elementwise_fma(y, c, xs);
 }
 
 // 16 bytes of a row and its values
@@ -119,20 +133,12 @@ template <typename T, bool INTER> struct PairChunks {
     if (INTER) {
 #pragma unroll
       for (int e = 0; e < N / 2; ++e) {
-        const float u = a[2 * e], w = a[2 * e + 1], u2 = b[2 * e], w2 = b[2 * e + 1];
-        const int f = N / 2 + e;
-        a[2 * e] = u * c[e] - w * s[e];
-        a[2 * e + 1] = w * c[e] + u * s[e];
-        b[2 * e] = u2 * c[f] - w2 * s[f];
-        b[2 * e + 1] = w2 * c[f] + u2 * s[f];
+        turn_pair(a[2 * e], a[2 * e + 1], c[e], s[e]);
+        turn_pair(b[2 * e], b[2 * e + 1], c[N / 2 + e], s[N / 2 + e]);
       }
     } else {
 #pragma unroll
-      for (int e = 0; e < N; ++e) {
-        const float u = a[e], w = b[e];
-        a[e] = u * c[e] - w * s[e];
-        b[e] = w * c[e] + u * s[e];
-      }
+      for (int e = 0; e < N; ++e) turn_pair(a[e], b[e], c[e], s[e]);
     }
     xa = Chunk<T>::put(a);
     xb = Chunk<T>::put(b);

@@ -167,6 +167,30 @@ def test_append_given_positions_and_defaults():
     assert torch.equal(K, want) and torch.equal(V, v)
 
 
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_one_rotation_for_all(interleaved):
+    """attn_rope, an append and a decode step's append turn a key to the same bits, so a
+    cache does not depend on how its rows came in."""
+    B, T, d = 64, 80, 128
+    g = torch.Generator(device="cuda").manual_seed(5)
+    k = torch.randn(B, 2, T, d, device="cuda", generator=g).to(BF16)
+    freqs, a = lib.attn_rope_freqs(d, scaling="ramp", factor=3.0, original_length=100)
+    pos = torch.randint(0, 10**6, (B, T), device="cuda", generator=g).int()
+    rot = dict(freqs=freqs, amplitude=a, interleaved=interleaved)
+    want = lib.attn_rope(k, None, freqs, a, interleaved, positions=pos)[0]
+    rows = []
+    for bits in (16, 4):
+        one, all_ = (Pool([T] * B, 2, 16, d, bits, seed=2) for _ in range(2))
+        lib.attn_paged_append(k, k, lens=ints([0] * B), positions=pos, **rot, **all_.args())
+        for t in range(T):
+            new = k[:, :, t].contiguous()
+            lib.attn_paged_decode(new, lens=ints([t] * B), k_new=new, v_new=new, n=T - 1, positions=pos[:, t].contiguous(),
+                                  **rot, **one.args())
+        assert all(torch.equal(x.view(torch.uint8), y.view(torch.uint8)) for x, y in zip(one.state(), all_.state()))
+        rows.append(lib.attn_paged_gather(lens=ints([T] * B), n=T, **all_.args())[0])
+    assert torch.equal(rows[0], want)
+
+
 def test_4bit_extremes():
     """Zeros, infinities, NaN, the ends of the bfloat16 range and values on the borders of
     the codes, block by block, against the oracle; a block's neighbours are not touched."""
