@@ -311,7 +311,8 @@ int attn_rope_bwd(const void* dq, const void* dk, void* dq_in, void* dk_in, cons
  * never used. A page number outside [0, num_pages) that a call does meet is
  * skipped: tokens there are not written, read back as zeros and take no part
  * in attention. Pages may be shared between sequences for reading; a row that
- * one call writes twice holds either value.
+ * one call writes twice holds either value, and one that it writes for a sequence and
+ * reads for another is read before or after.
  *
  * Pages are bfloat16 (dtype; ATTN_E_UNSUPPORTED otherwise), or, with k_scales and
  * v_scales given, 4 bits: pools of bytes [num_pages, Hkv, page_size, d/2] (column
@@ -349,7 +350,9 @@ int attn_paged_gather(const void* k_pages, const void* v_pages, const void* k_sc
  * without an append), with len_b = lens[b] clamped to [0, n]; grouped heads, O, L,
  * empty sequences and the workspace as in attn_decode. With freqs, q and k_new are
  * rotated on the way, to position positions[b] (device int32 [B]) or T_b - 1; the
- * rotated query keeps 16 bits. `strides`: host array, the elements between
+ * rotated query keeps 16 bits, 24 up to 64 tokens. A key that is not finite makes its
+ * score one of its sign, or NaN. Sums are float32 before the division, so values
+ * beyond 2^100 may overflow. `strides`: host array, the elements between
  * sequences of q, k_new and v_new, or NULL (dense; a row [H, d] is always dense).
  * n + 1 tokens (n without an append) have to fit table_width pages. With more
  * than 32 query heads per cache head the append is a launch of its own before

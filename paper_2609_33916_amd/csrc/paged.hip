@@ -82,7 +82,9 @@ long long blocks_for(long long rows, int per) { return (rows + per - 1) / per; }
 bool launches(long long rows, int per) { return blocks_for(rows, per) < 1LL << 24; }
 
 // Heads per workgroup: a thread's sines and cosines serve all of them, so as many,
-// up to 8, as leave four workgroups per compute unit.
+// up to 8, as leave four workgroups per compute unit (rotation of 2 x 64 heads, n = 16384:
+// 196 us; up to 4 heads 211, up to 16 207. Append of 8192 tokens of 8 heads in bfloat16
+// 11.6, a workgroup per head 15.8).
 int heads_per_group(long long token_blocks, int heads) {
   const long long want = attn::kXcds * attn::kCusPerXcd * 4;
   return (int)std::max<long long>(1, std::min<long long>({8, heads, token_blocks * heads / want}));
