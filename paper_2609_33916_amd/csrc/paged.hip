@@ -83,8 +83,8 @@ bool launches(long long rows, int per) { return blocks_for(rows, per) < 1LL << 2
 
 // Heads per workgroup: a thread's sines and cosines serve all of them, so as many,
 // up to 8, as leave four workgroups per compute unit (rotation of 2 x 64 heads, n = 16384:
-// 196 us; up to 4 heads 211, up to 16 207. Append of 8192 tokens of 8 heads in bfloat16
-// 11.6, a workgroup per head 15.8).
+// 196 us, one head each 240, up to 16 207; append of 16000 tokens of 8 heads in 4 bits 21.3,
+// one head each 38.7, up to 4 22.2).
 int heads_per_group(long long token_blocks, int heads) {
   const long long want = attn::kXcds * attn::kCusPerXcd * 4;
   return (int)std::max<long long>(1, std::min<long long>({8, heads, token_blocks * heads / want}));
