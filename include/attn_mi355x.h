@@ -354,9 +354,8 @@ int attn_paged_gather(const void* k_pages, const void* v_pages, const void* k_sc
  * score one of its sign, or NaN. Sums are float32 before the division, so values
  * beyond 2^100 may overflow. `strides`: host array, the elements between
  * sequences of q, k_new and v_new, or NULL (dense; a row [H, d] is always dense).
- * n + 1 tokens (n without an append) have to fit table_width pages. With more
- * than 32 query heads per cache head the append is a launch of its own before
- * the attention. Positions only turn: which keys are seen goes by the lengths. */
+ * n + 1 tokens (n without an append) have to fit table_width pages. Positions
+ * only turn: which keys are seen goes by the lengths. */
 size_t attn_paged_decode_workspace_bytes(int B, int Hq, int Hkv, int n, int d, int append, int bits);
 
 int attn_paged_decode(const void* q, const void* k_new, const void* v_new, const long long* strides,

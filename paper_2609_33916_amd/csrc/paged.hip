@@ -199,10 +199,15 @@ void launch_append(attn::AppendArgs a, bool interleaved, hipStream_t st) {
 // tokens in 4 bits 11.4, 12.8) and most where two workgroups of a compute unit would
 // only halve what one has to itself (256 groups of 1900 tokens in 4 bits 15.9, 18.4;
 // bfloat16, 1500: 34.3, 37.5). Beyond, sequences of different lengths need the
-// splits (176 groups of 8000 to 16000 tokens in 4 bits 55 us, undivided 63). In 4 bits
-// with two query columns at d = 128 (registers spill) a block takes several times as
-// long, and the limits are lower (2 groups of 1000 tokens 12.5 us, undivided 20.0; 220 of
-// 4096 62.7, 73.8; but 300 of 1000 undivided 31.7, in two 41.1).
+// splits (176 groups of 8000 to 16000 tokens in 4 bits 55 us, undivided 63).
+//
+// More than 16 query heads of a cache head are two columns of 16, which read the keys
+// once (220 groups of 8000 tokens, 32 heads, d = 64: 46.6 us in 4 bits, 58.7 by workgroups
+// of one column; bfloat16 85, 158), or, with so few blocks that latency counts, workgroups
+// of one column each (2 groups of 1500 tokens 8.5 us, two columns 9.4; bfloat16, 500
+// tokens 7.2, 8.1). In 4 bits at d = 128 always the latter: two columns need more
+// registers than there are, and what is spilled comes back behind the next block's
+// loads (16 groups of 8000 tokens 15.1 us, 24.2; 220 of 1500 23.1, 32.1).
 constexpr long long kWorkgroups = 2 * attn::kXcds * attn::kCusPerXcd;
 struct PagedPlan {
   int nq;        // query columns of a workgroup / 16
@@ -211,14 +216,14 @@ struct PagedPlan {
 PagedPlan paged_plan(int B, int Hq, int Hkv, int n, int d, int append, bool q4) {
   PagedPlan p;
   const int G = Hq / Hkv, block = q4 ? 64 : 32;
-  p.nq = G > 16 ? 2 : 1;
+  const long long blocks = ((long long)n + append + block - 1) / block;
+  const long long pairs = (long long)B * Hkv * ((G + 31) / 32);
+  p.nq = G > 16 && !(q4 && d == 128) && pairs * blocks > (q4 ? 2048 : 512) ? 2 : 1;
   p.qchunks = (G + 16 * p.nq - 1) / (16 * p.nq);
   const long long groups = (long long)B * Hkv * p.qchunks;
-  const long long blocks = ((long long)n + append + block - 1) / block;
   const bool crowded = 2 * groups > kWorkgroups;
   const long long parts = groups >= kWorkgroups ? 1 : crowded ? 2 : kWorkgroups / groups;
-  long long undivided = parts > 3 ? (q4 ? 16 : 12) : parts == 3 || crowded ? (q4 ? 32 : 16) : (q4 ? 128 : 64);
-  if (q4 && p.nq == 2 && d == 128) undivided = parts > 3 ? 4 : 32;
+  const long long undivided = parts > 3 ? (q4 ? 16 : 12) : parts == 3 || crowded ? (q4 ? 32 : 16) : (q4 ? 128 : 64);
   p.nsplit = blocks <= undivided ? 1 : (int)std::min(parts, blocks / 4);
   return p;
 }
@@ -233,8 +238,8 @@ template <int D, int NQ, int REP, bool Q4> void launch_decode(const attn::PagedA
 template <int D> void launch_decode(const attn::PagedArgs& a, const dim3& grid, int nq, hipStream_t st) {
   if (!a.ksc) {
     nq == 1 ? launch_decode<D, 1, 1, false>(a, grid, st) : launch_decode<D, 2, 1, false>(a, grid, st);
-  } else if (nq == 2) {
-    launch_decode<D, 2, 1, true>(a, grid, st);
+  } else if (D < 128 && nq == 2) {
+    launch_decode<D < 128 ? D : 64, 2, 1, true>(a, grid, st);
   } else if (D == 128 && a.G <= 4) {   // as often in the 16 columns as the heads go into them
     launch_decode<D, 1, D / 32, true>(a, grid, st);
   } else if (D >= 64 && a.G <= 8) {
@@ -298,7 +303,6 @@ int attn_paged_append(const void* k_new, const void* v_new, const long long* str
   a.pos = positions;
   a.rot = rotation(freqs, r, amplitude);
   a.T = T; a.d = d; a.tokens = B * T;
-  a.limit = -1;
   (void)hipGetLastError();
   launch_append(a, interleaved, static_cast<hipStream_t>(stream));
   return hipGetLastError() == hipSuccess ? ATTN_OK : ATTN_E_HIP;
@@ -383,7 +387,6 @@ int attn_paged_decode(const void* q, const void* k_new, const void* v_new, const
   a.part = static_cast<float*>(workspace);
   a.o = O; a.lse = L;
   a.Hq = Hq; a.G = Hq / Hkv; a.n = n; a.append = append; a.rows = B * Hq;
-  a.fuse_append = append && plan.qchunks == 1;
   a.nsplit = plan.nsplit; a.qchunks = plan.qchunks;
   // a zero scale would turn masked scores into NaN: see split_scale in attn.hip
   a.sl2 = std::fmax(std::fabs(scale) * attn::kLog2e, 1e-30f);
@@ -391,16 +394,6 @@ int attn_paged_decode(const void* q, const void* k_new, const void* v_new, const
   a.negate = scale < 0.f;
   hipStream_t st = static_cast<hipStream_t>(stream);
   (void)hipGetLastError();
-  if (append && !a.fuse_append) {   // several workgroups read the new row: it is written before them
-    attn::AppendArgs w{};
-    w.k_new = k_new; w.v_new = v_new;
-    w.ks = {row_k, d, 0}; w.vs = {row_v, d, 0};
-    w.kp = k_pages; w.vp = v_pages; w.ksc = a.ksc; w.vsc = a.vsc;
-    w.pg = a.pg; w.lens = lens; w.limit = n;
-    w.pos = positions; w.rot = a.rot;
-    w.T = 1; w.d = d; w.tokens = B;
-    launch_append(w, interleaved, st);
-  }
   const dim3 grid(plan.nsplit, B * Hkv * plan.qchunks);
   if (d == 32) launch_decode<32>(a, grid, plan.nq, st);
   else if (d == 64) launch_decode<64>(a, grid, plan.nq, st);

@@ -90,14 +90,13 @@ struct AppendArgs {
   const int* pos;              // positions [B, T], or null: the token's place in the sequence
   Rotation rot;
   int T, d, tokens;            // tokens: B T
-  int limit;                   // lengths are clamped to [0, limit], as in the decode step; -1: not
   int hgroup;                  // heads per workgroup
 };
 
 // Where a thread's token goes: the pool's row, -1 where it has none (past the
 // sequence's count, behind its table, no page), and its position.
 __device__ __forceinline__ long long append_row(const AppendArgs& a, int b, int t, int& p) {
-  const int len = a.limit >= 0 ? min(max(a.lens[b], 0), a.limit) : a.lens[b];
+  const int len = a.lens[b];
   if (t >= (a.new_lens ? a.new_lens[b] : a.T) || len < 0 || len > INT_MAX - t) return -1;
   p = a.pos ? a.pos[(long long)b * a.T + t] : len + t;
   return page_row(a.pg, a.pg.table + (long long)b * a.pg.width, len + t);
@@ -327,7 +326,7 @@ struct PagedArgs {
   float* part;                 // nsplit > 1: [rows][nsplit][d] unnormalised O, then [rows][nsplit] (max2, sum)
   void* o;
   float* lse;
-  int Hq, G, n, append, fuse_append, rows;
+  int Hq, G, n, append, rows;
   int nsplit, qchunks;
   float sl2;
   int interleaved;
@@ -520,8 +519,9 @@ __global__ void __launch_bounds__(256, 2) paged_decode_kernel(const PagedArgs a)
     load(A, ids, kv);
     fetch(ids, kv + 4 * BK);
   }
-  // This split holds the new row: it writes it, and takes it from LDS itself.
-  const bool writes = a.fuse_append && T_b - 1 >= k_lo && T_b - 1 < k_hi;
+  // This split holds the new row: it takes it from LDS, and the first of the query
+  // chunks writes it.
+  const bool fresh = a.append && T_b - 1 >= k_lo && T_b - 1 < k_hi;
 
   // ---- the queries, turned, as two bfloat16 each (their sum is 16 bits of the
   // result; one alone would cost L its last digits), in short sequences, where a
@@ -554,8 +554,8 @@ __global__ void __launch_bounds__(256, 2) paged_decode_kernel(const PagedArgs a)
         qh[r * QS + c1] = low ? zl : zh;
       }
     }
-    if (writes) {
-      const long long at = page_row(a.pg, table, T_b - 1);
+    if (fresh) {
+      const long long at = qc == 0 ? page_row(a.pg, table, T_b - 1) : -1;
       const long long r = at + ((long long)hk << a.pg.shift);
       if (tid < P) {
         typedef typename std::conditional<Q4, double, float>::type R;
@@ -668,7 +668,7 @@ __global__ void __launch_bounds__(256, 2) paged_decode_kernel(const PagedArgs a)
     }
   };
   auto step = [&](Block& x, int kv0) __attribute__((always_inline)) {
-    if (writes && T_b - 1 - kv0 < BK) patch(x, T_b - 1 - kv0);
+    if (fresh && T_b - 1 - kv0 < BK) patch(x, T_b - 1 - kv0);
     bool whole = true;
 #pragma unroll
     for (int i = 0; i < NG; ++i) whole = whole && x.lim[i] == PAGE;
@@ -850,7 +850,6 @@ __global__ void __launch_bounds__(256, 2) paged_decode_kernel(const PagedArgs a)
         }
       };
       auto block = [&](auto dl) __attribute__((always_inline)) {
-        if constexpr (NQ == 2) __builtin_amdgcn_sched_barrier(0);   // one block's operands at a time: registers
         scaled(dl);
 #pragma unroll
         for (int r = 0; r < REP; ++r) products(r * DL + decltype(dl)::value);

@@ -306,6 +306,17 @@ def test_decode_many_splits(bits, d):
 
 @pytest.mark.parametrize("bits", [16, 4])
 @pytest.mark.parametrize("d", [32, 64, 128])
+@pytest.mark.parametrize("G", [17, 32, 33])
+@pytest.mark.parametrize("page", [16, 64])
+def test_decode_groups_in_large_batches(bits, d, G, page):
+    """Enough keys for two columns of query heads in a workgroup: split, and in one part."""
+    decode_case([0, 300, 64, 33], G, 1, page, d, bits, r=32, n=40000, width=40000 // page + 1, seed=G)
+    lens = [int(x) for x in np.random.default_rng(G).integers(0, 701, 200)]
+    decode_case(lens, G, 1, page, d, bits, r=32, n=700, width=701 // page + 1, seed=G, packed=True)
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("d", [32, 64, 128])
 def test_decode_joins_hundreds_of_splits(bits, d):
     """One cache head; the lengths fill all of the splits, a few, one, none but the new row's."""
     for x, n in ((40000, 40000), (19000, 40000), (70, 40000), (0, 40000)):
