@@ -288,8 +288,8 @@ __global__ void __launch_bounds__(256) gather_kernel(const GatherArgs a) {
 // ------------------------------------------------------------------- decode --
 // One new query token per head against the pages. As in decode_kernel a
 // workgroup owns one cache head, one split of its keys and up to 16 NQ of the
-// query heads that share it (the columns of S^T = K Q^T), so each cached row is
-// read once per step. Its four waves take blocks of BK keys in turn, each with
+// query heads that share it (the columns of S^T = K Q^T), so a cached row is read
+// once for all of these. Its four waves take blocks of BK keys in turn, each with
 // its own running (maximum, sum, O) and its own part of LDS: there is no barrier
 // in the loop, and a block's loads are in flight while the previous one is worked
 // on. Products are 16x16x32 (a lane of group g = lane / 16, column c = lane % 16):
@@ -893,10 +893,8 @@ __global__ void __launch_bounds__(256, 2) paged_decode_kernel(const PagedArgs a)
     for (int db = 0; db < DB; ++db) *(f32x4*)(ow + (w * C + 16 * q + c) * OS + 16 * db + 4 * g) = oacc[q][db];
   }
   lds_barrier();
-  constexpr int heads = C / REP;
-  for (int it = tid; it < heads * (D / 4); it += 256) {
-    const int col = it % heads, d4 = it / heads;
-    if (col >= nq) continue;
+  for (int it = tid; it < nq * (D / 4); it += 256) {
+    const int col = it / (D / 4), d4 = it % (D / 4);
     float M = -INFINITY, l = 0.f;
 #pragma unroll
     for (int v = 0; v < 4; ++v) M = fmaxf(M, ml[0][v][col]);
