@@ -533,9 +533,9 @@ __global__ void __launch_bounds__(256, 2) paged_decode_kernel(const PagedArgs a)
 #pragma unroll
     for (int i = 0; i < C * P / 256; ++i) {
       const int r = tid / P + 256 / P * i;
+      if ((REP == 1 ? r : r % HR) >= nq) continue;   // columns without a head repeat the last one's query
       float y = u[i], z = x[i];
       if (turns) turn_pair(y, z, cs, sn);
-      if ((REP == 1 ? r : r % HR) >= nq) y = z = 0.f;
       if (a.negate) y = -y, z = -z;
       const bf16 yh = (bf16)y, zh = (bf16)z;
       const float yr = turns ? y - (float)yh : 0.f, zr = turns ? z - (float)zh : 0.f;
@@ -609,8 +609,9 @@ __global__ void __launch_bounds__(256, 2) paged_decode_kernel(const PagedArgs a)
   lds_barrier();
   // With two columns of queries at d = 128 their operands stay in LDS (64 registers).
   constexpr bool QLDS = NQ == 2 && D == 128;
+  const int qrow = REP == 1 ? 0 : c / HR * HR + min(c % HR, nq - 1);
   auto query = [&](const bf16* part, int x, int t) __attribute__((always_inline)) {
-    return *(const bf16x8*)(part + (16 * x + c) * QS + (Q4 ? D / 4 * g + 8 * t : 32 * t + 8 * g));
+    return *(const bf16x8*)(part + (REP == 1 ? min(16 * x + c, nq - 1) : qrow) * QS + (Q4 ? D / 4 * g + 8 * t : 32 * t + 8 * g));
   };
   bf16x8 qf[NQ][TD], qr[NQ][TD];
   if constexpr (!QLDS) {
