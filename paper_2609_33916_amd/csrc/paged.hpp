@@ -310,9 +310,9 @@ __global__ void __launch_bounds__(256) gather_kernel(const GatherArgs a) {
 // frequencies' turn, cold loads behind each other) and the end of the last wave. In
 // 4 bits the conversions and the softmax would bound it, with two waves per SIMD 5
 // clocks an instruction: hence the transposed reads of codes, the replicas below, and
-// the maximum that rarely moves. Short caches are that fixed part: 1000 tokens 7.2 us.
+// the maximum that rarely moves. Short caches are that fixed part: 1000 tokens 6.65 us.
 // Not faster: three waves per SIMD (registers spill, 43 us where two took 25), eight
-// waves in a workgroup (1000 tokens 9.4 us, 7.2), two blocks loaded ahead (below).
+// waves in a workgroup (1000 tokens 9.4 us where four took 7.2), two blocks loaded ahead (below).
 struct PagedArgs {
   const void* q;               // bf16 [B, Hq, d], sequences q_b elements apart
   const void *k_new, *v_new;   // bf16 [B, Hkv, d], or null
