@@ -350,7 +350,7 @@ int attn_paged_gather(const void* k_pages, const void* v_pages, const void* k_sc
  * without an append), with len_b = lens[b] clamped to [0, n]; grouped heads, O, L,
  * empty sequences and the workspace as in attn_decode. With freqs, q and k_new are
  * rotated on the way, to position positions[b] (device int32 [B]) or T_b - 1; the
- * rotated query keeps 16 bits, 24 up to 64 tokens. A key that is not finite makes its
+ * rotated query keeps 16 bits, 24 up to 64 tokens, a probability 15. A key that is not finite makes its
  * score one of its sign, or NaN. Sums are float32 before the division, so values
  * beyond 2^100 may overflow. `strides`: host array, the elements between
  * sequences of q, k_new and v_new, or NULL (dense; a row [H, d] is always dense).

@@ -396,6 +396,29 @@ template <int B> __device__ __forceinline__ float byte_power(uint32_t w) {
   return r;
 }
 
+// P in two bfloat16: the float cut to its first 16 bits, and the rest rounded, so that 15
+// bits of the factor stay. (With P in one, O was off by 2.0e-3 to 2.4e-3 of its length,
+// with two by the 1.6e-3 of its own last rounding. A step costs nothing more in bf16, and
+// in 4 bits 28.8 us where one part took 28.0 (32 ragged sequences up to 4096, 4 heads per
+// cache head), 34.8 for 33.2 (one of 131072, 8 heads), 60 for 48.5 where instructions
+// bound it (220 of 8000, d = 64, 32 heads).) Infinite values of V need a rest above 0, for
+// 0 times infinity is not a number.
+constexpr float kLeastRest = 0x1p-100f;
+template <bool Q4> __device__ __forceinline__ void two_parts(const f32x4& a, const f32x4& b, bf16x8& first, bf16x8& rest) {
+  f32x4 ra, rb;
+  u32x4 f;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const f32x4& x = i < 2 ? a : b;
+    f[i] = __builtin_amdgcn_perm(__float_as_uint(x[2 * i % 4 + 1]), __float_as_uint(x[2 * i % 4]), 0x07060302u);
+    ra[i] = a[i] - __uint_as_float(__float_as_uint(a[i]) & 0xffff0000u);
+    rb[i] = b[i] - __uint_as_float(__float_as_uint(b[i]) & 0xffff0000u);
+    if constexpr (!Q4) ra[i] = fmaxf(ra[i], kLeastRest), rb[i] = fmaxf(rb[i], kLeastRest);
+  }
+  first = __builtin_bit_cast(bf16x8, f);
+  rest = frag16(ra, rb);
+}
+
 // REP: the query heads (at most 16 / REP of them) stand REP times in the 16 columns, and a
 // lane scales P for only 1 / REP of the 32-column blocks of d; the two parts of the
 // query are then columns, not products of their own (131072 tokens, 8 heads per cache
@@ -792,14 +815,17 @@ __global__ void __launch_bounds__(256, 2) paged_decode_kernel(const PagedArgs a)
         }
     }
     if constexpr (!Q4) {
-      bf16x8 pf[NQ];
+      bf16x8 pf[NQ], pr[NQ];
 #pragma unroll
-      for (int q = 0; q < NQ; ++q) pf[q] = frag16(s[q][0], s[q][1]);
+      for (int q = 0; q < NQ; ++q) two_parts<false>(s[q][0], s[q][1], pf[q], pr[q]);
 #pragma unroll
       for (int db = 0; db < DB; ++db) {
         const bf16x8 vf = tr_read16<D, BK>((const bf16*)vst, 0, db, g, c);
 #pragma unroll
-        for (int q = 0; q < NQ; ++q) mma16(oacc[q][db], vf, pf[q]);
+        for (int q = 0; q < NQ; ++q) {
+          mma16(oacc[q][db], vf, pf[q]);
+          mma16(oacc[q][db], vf, pr[q]);
+        }
       }
     } else {
       if (!whole) {   // scales of rows that take no part
@@ -817,7 +843,7 @@ __global__ void __launch_bounds__(256, 2) paged_decode_kernel(const PagedArgs a)
       // P for this lane's blocks of d, those from DL c / HR on; of the products below a
       // block's are right in the columns whose lanes scaled P for it
       constexpr int DL = TD / REP;
-      bf16x8 pf[NQ][DL][2];
+      bf16x8 pf[NQ][2], pr[NQ][2];
       part_t vs[KB];
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb)
@@ -832,8 +858,8 @@ __global__ void __launch_bounds__(256, 2) paged_decode_kernel(const PagedArgs a)
                            byte_power<(3 * TD + B) % 4>(word(vs[kb], 3 * TD / 4))};
 #pragma unroll
         for (int q = 0; q < NQ; ++q) {
-          pf[q][B][0] = frag16(s[q][0] * sc[0], s[q][1] * sc[1]);
-          pf[q][B][1] = frag16(s[q][2] * sc[2], s[q][3] * sc[3]);
+          two_parts<true>(s[q][0] * sc[0], s[q][1] * sc[1], pf[q][0], pr[q][0]);
+          two_parts<true>(s[q][2] * sc[2], s[q][3] * sc[3], pf[q][1], pr[q][1]);
         }
       };
       auto products = [&](int dg) __attribute__((always_inline)) {
@@ -845,8 +871,10 @@ __global__ void __launch_bounds__(256, 2) paged_decode_kernel(const PagedArgs a)
           const bf16x8 v0 = Quant4::get((uint32_t)y[0], 1.f), v1 = Quant4::get((uint32_t)y[1], 1.f);
 #pragma unroll
           for (int q = 0; q < NQ; ++q) {
-            mma16(oacc[q][db], v0, pf[q][dg % DL][0]);
-            mma16(oacc[q][db], v1, pf[q][dg % DL][1]);
+            mma16(oacc[q][db], v0, pf[q][0]);
+            mma16(oacc[q][db], v1, pf[q][1]);
+            mma16(oacc[q][db], v0, pr[q][0]);
+            mma16(oacc[q][db], v1, pr[q][1]);
           }
         }
       };
