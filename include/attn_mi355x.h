@@ -319,10 +319,12 @@ int attn_rope_bwd(const void* dq, const void* dk, void* dq_in, void* dk_in, cons
  * 2i in the low half of byte i) and scales [num_pages, Hkv, page_size, d/32], the
  * microscaling format with E2M1 elements and one E8M0 scale per 32 columns.
  * A code is a sign and one of 0, .5, 1, 1.5, 2, 3, 4, 6, scale byte x stands for
- * 2^(x-127), 255 for "not a number". Written blocks take the smallest power
- * 2^e >= 2^-125 with every magnitude below 7 2^e, each value the nearest code (ties to
- * the even one) that stands for a finite bfloat16; rotated keys are rounded once, from 64 bits. A block with a
- * value that is not finite is stored as not-a-number. All four pools are 16-byte
+ * 2^(x-127), and 255 makes its 32 columns "not a number" whatever their codes. (Of
+ * pages that another writer filled, magnitudes from 2^128 on are read as infinite, and
+ * attention takes V's byte 0 as zero.) Written blocks take the smallest power 2^e >=
+ * 2^-125 with every magnitude below 7 2^e, each value the nearest code (ties to the even
+ * one) that stands for a finite bfloat16; rotated keys are rounded once, from 64 bits. A
+ * block with a value that is not finite is stored as not-a-number. All four pools are 16-byte
  * aligned. */
 
 /* Appends T tokens per sequence: token t < new_lens[b] (device int32 [B]; NULL:
@@ -350,9 +352,9 @@ int attn_paged_gather(const void* k_pages, const void* v_pages, const void* k_sc
  * without an append), with len_b = lens[b] clamped to [0, n]; grouped heads, O, L,
  * empty sequences and the workspace as in attn_decode. With freqs, q and k_new are
  * rotated on the way, to position positions[b] (device int32 [B]) or T_b - 1; the
- * rotated query keeps 16 bits, 24 up to 64 tokens, a probability 15. A key that is not finite makes its
- * score one of its sign, or NaN. Sums are float32 before the division, so values
- * beyond 2^100 may overflow. `strides`: host array, the elements between
+ * rotated query keeps 16 bits, 24 up to 64 tokens, a probability 15. A key that is not
+ * finite makes its score one of its sign, or NaN. Sums are float32 before the division, so
+ * values beyond 2^100 may overflow. `strides`: host array, the elements between
  * sequences of q, k_new and v_new, or NULL (dense; a row [H, d] is always dense).
  * n + 1 tokens (n without an append) have to fit table_width pages. Positions
  * only turn: which keys are seen goes by the lengths. */

@@ -382,7 +382,9 @@ template <typename F> __device__ __forceinline__ u32x4 map_words(u32x4 x, F f) {
   return (u32x4){f(x[0], 0), f(x[1], 1), f(x[2], 2), f(x[3], 3)};
 }
 
-// 2^(byte B of w - 127), as the scales mean it, in one instruction
+// 2^(byte B of w - 127), the scale that the byte means, in one instruction: but 0 for
+// byte 0 (2^-127; no writer here stores it) and infinite for 255, of which two_parts makes
+// not a number whatever the code and the probability
 template <int B> __device__ __forceinline__ float byte_power(uint32_t w) {
   float r;
   if constexpr (B == 0)
@@ -402,7 +404,8 @@ template <int B> __device__ __forceinline__ float byte_power(uint32_t w) {
 // in 4 bits 28.8 us where one part took 28.0 (32 ragged sequences up to 4096, 4 heads per
 // cache head), 34.8 for 33.2 (one of 131072, 8 heads), 60 for 48.5 where instructions
 // bound it (220 of 8000, d = 64, 32 heads).) Infinite values of V need a rest above 0, for
-// 0 times infinity is not a number.
+// 0 times infinity is not a number; in 4 bits the rest of a product with a scale of 255 has to
+// be not a number, as infinity less infinity is.
 constexpr float kLeastRest = 0x1p-100f;
 template <bool Q4> __device__ __forceinline__ void two_parts(const f32x4& a, const f32x4& b, bf16x8& first, bf16x8& rest) {
   f32x4 ra, rb;

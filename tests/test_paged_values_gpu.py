@@ -51,3 +51,81 @@ def test_infinite_values(n, G):
     assert bool((O[..., 9] == float("inf")).all()) and bool((O[..., 11] == -float("inf")).all())
     O[..., 9] = O[..., 11] = 0
     assert bool(torch.isfinite(O).all()) and bool(torch.isfinite(L).all())
+
+
+# --------------------------------------------- pages of another writer of the format --
+def all_codes(rows, d):
+    """[rows, d/2] bytes in which every code stands at every scale."""
+    c = (np.arange(d)[None] * 5 + np.arange(rows)[:, None]) % 16
+    return torch.from_numpy((c[:, 0::2] | c[:, 1::2] << 4).astype(np.uint8)).cuda()
+
+
+@pytest.mark.parametrize("d", [32, 64, 128])
+def test_gather_every_scale(d):
+    """All 256 scale bytes with all codes: what bfloat16 holds exactly, infinities behind
+    its range, NaN for 255."""
+    pool = Pool([256], 1, 16, d, 4)
+    for p in range(256):
+        at, r = int(pool.table[0, p // 16]), p % 16
+        pool.k[at, 0, r] = all_codes(256, d)[p]
+        pool.v[at, 0, r] = all_codes(256, d)[255 - p]
+        pool.scales["k_scales"][at, 0, r] = pool.scales["v_scales"][at, 0, r] = p
+    ref = pool.oracle()
+    K, V = lib.attn_paged_gather(lens=ints([256]), n=256, **pool.args())
+    for got, x in ((K, ref.k), (V, ref.v)):
+        want = ref.rows(0, range(256))[1 if x is ref.k else 2][0]
+        want = np.where(np.abs(want) >= 2.0 ** 128, np.copysign(np.inf, want), want)
+        assert same(to_host64(got)[0, 0], want)
+
+
+@pytest.mark.parametrize("n", [5, 100, 5000])
+@pytest.mark.parametrize("d,G", [(32, 2), (64, 1), (64, 20), (128, 3), (128, 8), (128, 12)])
+def test_a_scale_that_is_not_a_number(n, d, G):
+    """255 makes a block not a number whatever its codes: of V its 32 columns of O, of K
+    everything of its heads."""
+    pool = Pool([n], 2, 16, d, 4, seed=G).fill([n])
+    q = torch.randn(1, 2 * G, d, device="cuda").to(BF16)
+    at = int(pool.table[0, 0])
+    pool.v[at, 1, 3] = torch.randint(1, 8, (d // 2,), device="cuda").to(torch.uint8) * 17   # no code is 0
+    pool.scales["v_scales"][at, 1, 3, d // 32 - 1] = 255
+    O, L = lib.attn_paged_decode(q, lens=ints([n]), **pool.args())
+    bad = torch.zeros_like(O, dtype=torch.bool)
+    bad[0, G:, d - 32:] = True
+    assert torch.equal(torch.isnan(O), bad) and bool(torch.isfinite(O[~bad]).all()) and bool(torch.isfinite(L).all())
+    pool.k[at, 0, 3] = pool.v[at, 1, 3]
+    pool.scales["k_scales"][at, 0, 3, 0] = 255
+    O, L = lib.attn_paged_decode(q, lens=ints([n]), **pool.args())
+    assert bool(torch.isnan(O[0, :G]).all()) and bool(torch.isnan(L[0, :G]).all()) and bool(torch.isfinite(L[0, G:]).all())
+
+
+@pytest.mark.parametrize("d,G", [(32, 2), (64, 20), (128, 3), (128, 8), (128, 12)])
+@pytest.mark.parametrize("byte", [0, 1, 2, 3, 30, 100, 126, 160, 200, 220])
+def test_decode_other_scales(byte, d, G):
+    """Scales far from 1, of V, then of K. V's byte 0 counts as zero (6 2^-127 at most);
+    a sum of products loses what is below 2^-133, a bfloat16's last bit, per token."""
+    n = 40
+    pool = Pool([n], 1, 16, d, 4, seed=byte).fill([n], seed=byte)
+    for i in range(3):
+        at = int(pool.table[0, i])
+        pool.k[at, 0], pool.v[at, 0] = all_codes(16, d), all_codes(16, d) + 16 * (i % 2)
+        pool.scales["v_scales"][at] = byte
+    q = torch.randn(1, G, d, device="cuda").to(BF16)
+    ref = pool.oracle()
+    O, L = lib.attn_paged_decode(q, lens=ints([n]), **pool.args())
+    want, lse, A, S = ref.attend(to_host64(q), [n], d ** -0.5)
+    D = S * d * 2.0 ** -24 + (4 * S + 8) * 2.0 ** -23
+    top = 6 * 2.0 ** (byte - 127)
+    tol = 2.0 ** -8 * np.abs(want) + A * (2.0 ** -15 + n * 2.0 ** -24 + 2.0 ** -21) * 1.01 + (2 * D * top)[..., None] + 2 * n * 2.0 ** -133
+    tol += 6 * 2.0 ** -127 if byte == 0 else 0
+    err = np.abs(to_host64(O) - want)
+    assert np.all(err <= tol), (err / tol).max()
+    for i in range(3):   # scores of the same size whatever the scale
+        at = int(pool.table[0, i])
+        pool.scales["k_scales"][at], pool.scales["v_scales"][at] = byte, 126
+    ref, scale = pool.oracle(), 0.1 * 2.0 ** min(127 - byte, 100)
+    O, L = lib.attn_paged_decode(q, lens=ints([n]), scale=scale, **pool.args())
+    want, lse, A, S = ref.attend(to_host64(q), [n], scale)
+    D = S * d * 2.0 ** -24 + (4 * S + 8) * 2.0 ** -23
+    assert np.all(np.abs(to_host64(L) - lse) <= D + np.abs(lse) * 2.0 ** -22 + 2.0 ** -22)
+    err, tol = np.abs(to_host64(O) - want), 2.0 ** -8 * np.abs(want) + 4 * A * (2.0 ** -15 + n * 2.0 ** -24 + 2.0 ** -21) + (6 * D)[..., None]
+    assert np.all(err <= tol), (err / tol).max()
