@@ -26,17 +26,18 @@ namespace attn {
 
 // ------------------------------------------------------------ 4-bit values --
 struct Quant4 {
-  // A float that rounds to every shorter format as y does: y cut to 20 bits behind its
-  // first, the last bit of the float set if anything was lost. (A plain conversion
-  // could carry a value next to a border of the codes onto it. The rotation before it
-  // is in 64 bits for the same reason: a row's codes then do not depend on how 32-bit
-  // sums are ordered.) Below 2^-127 it is 0, from 2^128 on infinite, as is NaN.
+  // A float that rounds to the codes as y does: y cut to 20 bits behind its first, the last
+  // of them set if anything was lost. (A plain conversion could carry a value next to a
+  // border of the codes onto it. The rotation before it is in 64 bits for the same reason:
+  // a row's codes then do not depend on how 32-bit sums are ordered.) From 2^128 on it is
+  // infinite, as is NaN; up to 2^-127 it is 0; between 2^-127 and 2^-126, where a float's bits
+  // have no room for the first, they are those behind it, which put() sets right.
   __device__ __forceinline__ static float odd(double y) {
     const uint64_t bits = __builtin_bit_cast(uint64_t, y);
     const uint32_t hi = (uint32_t)(bits >> 32), lo = (uint32_t)bits;
-    const uint32_t m = min(max(hi & 0x7fffffffu, 896u << 20), 1151u << 20);   // exponents 1 and 255 of a float, less 1 and 0
-    const uint32_t f = ((m << 3) - (896u << 23)) | min(lo, 1u);
-    return __uint_as_float(f | (hi & 0x80000000u));
+    const uint32_t mag = (hi & 0x7fffffffu) | min(lo, 1u);
+    const uint32_t m = min(max(mag, 896u << 20), 1151u << 20);   // exponents 0 and 255 of a float
+    return __uint_as_float(((m << 3) - (896u << 23)) | (hi & 0x80000000u));
   }
   // largest magnitude, as bits, of the four lanes of a quad
   __device__ __forceinline__ static uint32_t quad_max(uint32_t m) {
@@ -44,8 +45,9 @@ struct Quant4 {
     return max(m, (uint32_t)__builtin_amdgcn_mov_dpp((int)m, 0x4E, 0xf, 0xf, true));   // lanes 2 3 0 1
   }
   // Eight values of each lane of a quad (a block of 32): the lane's four bytes
-  // of codes and the block's scale. All four lanes have to be active.
-  __device__ __forceinline__ static uint32_t put(float (&v)[8], uint32_t& scale) {
+  // of codes and the block's scale. All four lanes have to be active. ODD: the values may
+  // come from odd() (`from_odd`: they do).
+  template <bool ODD> __device__ __forceinline__ static uint32_t put(float (&v)[8], uint32_t& scale, bool from_odd = false) {
     uint32_t m = 0;
 #pragma unroll
     for (int e = 0; e < 8; ++e) m = max(m, __float_as_uint(v[e]) & 0x7fffffffu);
@@ -56,6 +58,13 @@ struct Quant4 {
     }
     scale = (uint32_t)max((int)((m + 0x200000u) >> 23) - 2, 2);   // 1.75 2^k carries into the next exponent
     const float unit = __uint_as_float(scale << 23);
+    if (ODD && scale == 2 && from_odd) {   // above 2^-127, a quarter of the unit and a border of the codes, not yet above 2^-126
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const uint32_t y = __float_as_uint(v[e]) & 0x7fffffffu;
+        if (y) v[e] = copysignf(__uint_as_float(max(y, 0x600000u)), v[e]);
+      }
+    }
     if (scale == 253) {   // 4 2^126 would be infinite in bfloat16
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] = fminf(fmaxf(v[e], -3.f * unit), 3.f * unit);
@@ -237,9 +246,9 @@ __global__ void __launch_bounds__(256) append4_kernel(const AppendArgs a) {
         }
         const long long r = row + ((long long)(h0 + u) << a.pg.shift);
         uint32_t sc;
-        ((uint32_t*)a.kp)[r * TPT + ch] = Quant4::put(k, sc);
+        ((uint32_t*)a.kp)[r * TPT + ch] = Quant4::put<true>(k, sc, turns);
         put_scales(a.ksc + r * (D / 32), sc);
-        ((uint32_t*)a.vp)[r * TPT + ch] = Quant4::put(v, sc);
+        ((uint32_t*)a.vp)[r * TPT + ch] = Quant4::put<false>(v, sc);
         put_scales(a.vsc + r * (D / 32), sc);
       }
   }
@@ -621,7 +630,7 @@ __global__ void __launch_bounds__(256, 2) paged_decode_kernel(const PagedArgs a)
 #pragma unroll
           for (int e = 0; e < 8; ++e) v[e] = nval[which][8 * ch + e];
           uint32_t sc;
-          const uint32_t y = Quant4::put(v, sc);
+          const uint32_t y = Quant4::put<true>(v, sc, which == 0);
           nrow[which][ch] = y;
           if (ch % 4 == 0) ((uint8_t*)&nscale[which])[ch / 4] = (uint8_t)sc;
           if (at >= 0) {

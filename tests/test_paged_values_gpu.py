@@ -129,3 +129,33 @@ def test_decode_other_scales(byte, d, G):
     assert np.all(np.abs(to_host64(L) - lse) <= D + np.abs(lse) * 2.0 ** -22 + 2.0 ** -22)
     err, tol = np.abs(to_host64(O) - want), 2.0 ** -8 * np.abs(want) + 4 * A * (2.0 ** -15 + n * 2.0 ** -24 + 2.0 ** -21) + (6 * D)[..., None]
     assert np.all(err <= tol), (err / tol).max()
+
+
+# ------------------------------------------------------- the ends of what is written --
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("amplitude", [1.0, 1.25, 0.75])
+@pytest.mark.parametrize("d,r", [(32, 32), (64, 32), (128, 128), (128, 16)])
+def test_smallest_values(interleaved, amplitude, d, r):
+    """Every bfloat16 below 2^-125, where blocks have the smallest scale: codes of the
+    rotated and of the other columns against the oracle, at position 0 (products are
+    exact) and elsewhere; an append and a decode step's append store the same bytes."""
+    steps = torch.arange(512, dtype=torch.int16)   # bits: 0 .. 2^-124
+    g = torch.Generator().manual_seed(d + r)
+    rows = torch.stack([steps[torch.randperm(512, generator=g)[:d]] for _ in range(96)])
+    rows[:32] %= 256      # below 2^-125
+    rows[32:64] %= 128    # below 2^-126
+    x = rows.view(BF16) * torch.where(torch.rand(96, d, generator=g) < 0.5, -1, 1)
+    k = x.view(1, 1, 96, d).cuda()
+    freqs, _ = lib.attn_rope_freqs(r)
+    for at in (0, 77):
+        pos = ints([at] * 96)[None]
+        rot = dict(freqs=freqs, amplitude=amplitude, interleaved=interleaved)
+        pool, one = Pool([96], 1, 16, d, 4), Pool([96], 1, 16, d, 4)
+        lib.attn_paged_append(k, k, lens=ints([0]), positions=pos, **rot, **pool.args())
+        ref = pool.oracle().rows(0, range(96))
+        y = paged.rotate(to_host64(k)[0, 0], np.full(96, at), freqs.cpu().numpy(), amplitude, interleaved)
+        assert same(ref[1][0], stored(y, 4)) and same(ref[2][0], stored(to_host64(k)[0, 0], 4))
+        for t in range(96):
+            new = k[:, :, t].contiguous()
+            lib.attn_paged_decode(new, lens=ints([t]), k_new=new, v_new=new, positions=pos[:, t].contiguous(), **rot, **one.args())
+        assert all(torch.equal(a, b) for a, b in zip(pool.state(), one.state()))
