@@ -83,7 +83,7 @@ enum {
                               p_bytes < attn_mat_bytes(B, H, n, dtype) */
   ATTN_E_HIP = -6,         /* the HIP runtime rejected a kernel launch */
   ATTN_E_ARG = -7,         /* scale or amplitude not finite, causal or interleaved not 0/1,
-                              or an output whose rows overlap */
+                              or outputs whose rows overlap */
   ATTN_E_SCRATCH = -8      /* attn_fwd_bwd_noalloc: B*H*n > attn_noalloc_max_rows() */
 };
 
@@ -284,12 +284,14 @@ int attn_decode(const void* q, const void* k_new, const void* v_new, void* k_cac
  * tokens, three each for q, k, q_out, k_out, or is NULL for dense tensors: views
  * of a fused projection [B, n, Hq + 2 Hk, d] and of its gradient need no
  * copy. Strides are not negative, rows start at multiples of 16 bytes, and the rows
- * of an output must not overlap (ATTN_E_ARG). A tensor may be rotated in place
- * (same pointer and strides); otherwise outputs must not overlap inputs.
+ * of an output must not overlap each other or the other output's (ATTN_E_ARG; between two
+ * outputs of different strides that reach into each other the caller has to see to it). A
+ * tensor may be rotated in place (same pointer and strides); otherwise outputs must not
+ * overlap inputs.
  *
  * Positions: token i of sequence b is at positions[b * pos_stride + i] (device
  * int32; pos_stride 0: shared by all sequences), or at start + i where positions
- * is NULL. Positions may be negative. */
+ * is NULL. Positions may be negative; start + n is at most 2^31 - 1. */
 int attn_rope(const void* q, const void* k, void* q_out, void* k_out, const long long* strides,
               const double* freqs, const int* positions, long long pos_stride, int start,
               int B, int Hq, int Hk, int n, int d, int r, float amplitude, int interleaved, int dtype,

@@ -719,7 +719,7 @@ const char* attn_strerror(int code) {
     case ATTN_E_ALIGN: return "a tensor or its strides are not 16-byte aligned (L and workspace: 4-byte)";
     case ATTN_E_WORKSPACE: return "workspace smaller than attn_workspace_bytes(), or P smaller than attn_mat_bytes()";
     case ATTN_E_HIP: return "the HIP runtime rejected a kernel launch";
-    case ATTN_E_ARG: return "scale or amplitude not finite, a flag not 0 or 1, or an output whose rows overlap";
+    case ATTN_E_ARG: return "scale or amplitude not finite, a flag not 0 or 1, or outputs whose rows overlap";
     case ATTN_E_SCRATCH:
       return "B * H * n exceeds attn_noalloc_max_rows(), the rows the fixed scratch of attn_fwd_bwd_noalloc holds";
     default: return "unknown attn status code";

@@ -18,6 +18,7 @@ namespace {
 
 using attn::bf16;
 using attn::Strides;
+using attn::writable;
 
 bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 
@@ -53,19 +54,6 @@ Strides strides_of(const long long* s, int B, int H, int n, int d) {
 bool aligned(const Strides& s, int elem) {
   const int m = 16 / elem;
   return s.b % m == 0 && s.h % m == 0 && s.t % m == 0;
-}
-// Rows of a written tensor must not overlap: from the smallest stride on, each
-// has to step over all that the smaller ones span.
-bool writable(const Strides& s, int B, int H, int n, int d) {
-  struct { long long step; int size; } dim[3] = {{s.b, B}, {s.h, H}, {s.t, n}};
-  std::sort(dim, dim + 3, [](const auto& x, const auto& y) { return x.step < y.step; });
-  __int128 span = d;
-  for (const auto& x : dim) {
-    if (x.size == 1) continue;
-    if (x.step < span) return false;
-    span += (__int128)x.step * (x.size - 1);
-  }
-  return true;
 }
 bool fits(const Strides& s, int B, int H, int n) {   // offsets in 62 bits
   __int128 far = 0;
@@ -126,6 +114,8 @@ int rope(const void* q, const void* k, void* q_out, void* k_out, const long long
     if (!fits(a.ks, B, Hk, n) || !fits(a.kos, B, Hk, n)) return ATTN_E_SHAPE;
     if (!aligned(k, 16) || !aligned(k_out, 16) || !aligned(a.ks, elem) || !aligned(a.kos, elem)) return ATTN_E_ALIGN;
     if (!writable(a.kos, B, Hk, n, d)) return ATTN_E_ARG;
+    const long long apart = (reinterpret_cast<intptr_t>(k_out) - reinterpret_cast<intptr_t>(q_out)) / elem;
+    if (attn::rows_meet(a.qos, Hq, a.kos, Hk, B, n, d, apart)) return ATTN_E_ARG;
   }
   a.pos = positions;
   a.pos_stride = pos_stride;

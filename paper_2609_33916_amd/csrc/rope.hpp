@@ -15,6 +15,7 @@
 
 #include "common.hpp"
 #include "pages.hpp"
+#include "strides.hpp"
 
 namespace attn {
 
@@ -146,9 +147,6 @@ template <typename T, bool INTER> struct PairChunks {
 };
 
 // ---------------------------------------------------------------- attn_rope --
-struct Strides {
-  long long b, h, t;   // elements between sequences, heads, tokens
-};
 struct RopeArgs {
   const void *q, *k;
   void *qo, *ko;
