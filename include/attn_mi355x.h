@@ -284,8 +284,8 @@ int attn_decode(const void* q, const void* k_new, const void* v_new, void* k_cac
  * tokens, three each for q, k, q_out, k_out, or is NULL for dense tensors: views
  * of a fused projection [B, n, Hq + 2 Hk, d] and of its gradient need no
  * copy. Strides are not negative, rows start at multiples of 16 bytes, and the rows
- * of an output must not overlap each other or the other output's (ATTN_E_ARG; between two
- * outputs of different strides that reach into each other the caller has to see to it). A
+ * of an output must not overlap each other or the other output's (ATTN_E_ARG; with
+ * different strides and gaps between an output's rows the caller has to see to it). A
  * tensor may be rotated in place (same pointer and strides); otherwise outputs must not
  * overlap inputs.
  *

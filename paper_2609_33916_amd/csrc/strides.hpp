@@ -28,8 +28,9 @@ inline bool writable(const Strides& s, int B, int H, int n, int d) {
 // Whether a row of x [B, Hx, n, d] and one of y [B, Hy, n, d], both writable, have an element in
 // common; y starts `delta` elements behind x. Tensors that step alike (views of one buffer)
 // are told exactly: along an axis rows differ by a number i of steps, and from the largest
-// step on only those i matter that the smaller steps can still make up for. Of others that
-// reach into each other only the first rows are compared.
+// step on only those i matter that the smaller steps can still make up for. Of others the
+// first rows are compared, and the first and last of one with all of the other if that has no
+// gaps: any two tensors without gaps that reach into each other are found.
 inline bool rows_meet(const Strides& x, int Hx, const Strides& y, int Hy, int B, int n, int d, __int128 delta) {
   struct Axis { __int128 step, lo, hi; };
   Axis axis[3] = {{x.b, 1 - B, B - 1}, {std::max(x.h, y.h), 1 - Hx, Hy - 1}, {x.t, 1 - n, n - 1}};
@@ -39,7 +40,11 @@ inline bool rows_meet(const Strides& x, int Hx, const Strides& y, int Hy, int B,
     ends_y += (__int128)sy * (ny - 1);
   }
   if (delta >= ends_x || -delta >= ends_y) return false;
-  if (x.b != y.b || x.t != y.t || (x.h != y.h && Hx > 1 && Hy > 1)) return delta < d && -delta < d;
+  if (x.b != y.b || x.t != y.t || (x.h != y.h && Hx > 1 && Hy > 1)) {
+    if (delta < d && -delta < d) return true;
+    const bool dense_x = ends_x == (__int128)B * Hx * n * d, dense_y = ends_y == (__int128)B * Hy * n * d;
+    return (dense_x && (delta > -d || delta + ends_y < ends_x + d)) || (dense_y && (delta < d || delta + ends_y > ends_x - d));
+  }
   std::sort(axis, axis + 3, [](const Axis& p, const Axis& q) { return p.step > q.step; });
   const auto meet = [&](const auto& self, int k, __int128 at) -> bool {
     if (k == 3) return at < d && -at < d;

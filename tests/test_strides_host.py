@@ -50,8 +50,29 @@ int main() {
   const Strides far{1LL << 50, 128, 1LL << 20};
   if (!attn::rows_meet(far, 64, far, 64, 1 << 9, 1 << 20, 128, 128) || attn::rows_meet(far, 64, far, 64, 1 << 9, 1 << 20, 128, 64 * 128))
     return 1;
-  // other strides: the first rows
-  if (!attn::rows_meet({512, 64, 128}, 2, {512, 128, 64}, 2, 2, 2, 64, 0) || refused || met < 1000 || apart < 1000) return 1;
+  // other strides, two without gaps (all are told), then one with (none is called apart or met wrongly
+  // where its first or last row decides)
+  for (int it = 0; it < 100000; ++it) {
+    const int d = 4, B = pick(1, 3), n = pick(1, 4), Hx = pick(1, 4), Hy = pick(1, 4), gap = it % 2 ? 4 * pick(0, 3) : 0;
+    const Strides x{B > 1 ? Hx * n * d : 0, Hx > 1 ? n * d : 0, n > 1 ? d : 0};
+    const long long row = Hy * d + gap;
+    const Strides y{B > 1 ? n * row : 0, Hy > 1 ? d : 0, n > 1 ? row : 0};
+    const long long delta = pick(-200, 200);
+    bool want = false, edge = std::llabs(delta) < d;
+    const long long end = delta + (B * n - 1) * row + Hy * d;   // of y's last row
+    for (int k = 0; k < B * Hx * n; ++k) {
+      for (int c = 0; c < B * n; ++c) for (int j = 0; j < Hy; ++j) want = want || std::llabs(delta + c * row + j * d - k * d) < d;
+      edge = edge || std::llabs(delta - k * d) < d || std::llabs(end - d - k * d) < d;
+    }
+    for (int swap = 0; swap < 2; ++swap) {
+      const bool got = swap ? attn::rows_meet(y, Hy, x, Hx, B, n, d, -delta) : attn::rows_meet(x, Hx, y, Hy, B, n, d, delta);
+      if ((got && !want) || (!got && (gap == 0 ? want : edge))) {
+        std::printf("B %d n %d H %d %d gap %d delta %lld: %d, not %d\n", B, n, Hx, Hy, gap, delta, got, want);
+        return 1;
+      }
+    }
+  }
+  if (refused || met < 1000 || apart < 1000) return 1;
   std::printf("ok\n");
   return 0;
 }
