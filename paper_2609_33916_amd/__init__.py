@@ -591,6 +591,7 @@ def _rotation(freqs, d: int, ref: torch.Tensor):
     _need(isinstance(freqs, torch.Tensor) and freqs.is_cuda and freqs.device == ref.device
           and freqs.dtype == torch.float64 and freqs.dim() == 1 and freqs.is_contiguous(),
           "freqs must be a contiguous float64 GPU tensor of one axis")
+    _need(freqs.numel() > 0, "freqs is empty (None: no rotation)")
     _need(2 * freqs.numel() <= d, f"freqs holds {freqs.numel()} frequencies, {d} columns have {d // 2} pairs")
     return freqs.data_ptr(), 2 * freqs.numel()
 

@@ -330,7 +330,8 @@ bool get_rotation(PyObject* o, int64_t d, const at::Tensor& ref, const double*& 
   r = 0;
   if (o == Py_None) return true;
   const at::Tensor* t = plain(o);
-  if (!t || t->scalar_type() != at::kDouble || t->device() != ref.device() || t->dim() != 1 || 2 * t->numel() > d) return false;
+  if (!t || t->scalar_type() != at::kDouble || t->device() != ref.device() || t->dim() != 1 || t->numel() == 0 || 2 * t->numel() > d)
+    return false;
   p = (const double*)t->data_ptr();
   r = (int)(2 * t->numel());
   return true;
