@@ -312,9 +312,10 @@ int attn_rope_bwd(const void* dq, const void* dk, void* dq_in, void* dk_in, cons
  * cached before the call; no call changes it. Entries behind a sequence's pages are
  * never used. A page number outside [0, num_pages) that a call does meet is
  * skipped: tokens there are not written, read back as zeros and take no part
- * in attention. Pages may be shared between sequences for reading; a row that
- * one call writes twice holds either value, and one that it writes for a sequence and
- * reads for another is read before or after.
+ * in attention. Pages may be shared between sequences for reading. Rows are written in
+ * pieces of 2 to 16 bytes and in no order: one that a call writes for two sequences holds
+ * pieces of either (in 4 bits perhaps the codes of one with a scale of the other), and one
+ * that it writes for a sequence and reads for another may be read as such a mixture.
  *
  * Pages are bfloat16 (dtype; ATTN_E_UNSUPPORTED otherwise), or, with k_scales and
  * v_scales given, 4 bits: pools of bytes [num_pages, Hkv, page_size, d/2] (column
@@ -358,8 +359,9 @@ int attn_paged_gather(const void* k_pages, const void* v_pages, const void* k_sc
  * finite makes its score one of its sign, or NaN. Sums are float32 before the division, so
  * values beyond 2^100 may overflow. `strides`: host array, the elements between
  * sequences of q, k_new and v_new, or NULL (dense; a row [H, d] is always dense).
- * n + 1 tokens (n without an append) have to fit table_width pages. Positions
- * only turn: which keys are seen goes by the lengths. */
+ * n + 1 tokens (n without an append) have to fit table_width pages, and B Hkv ceil(Hq /
+ * Hkv / c) may be 65535 at most, c being the query heads of a workgroup: 16, in long caches
+ * up to 32 (ATTN_E_SHAPE). Positions only turn: which keys are seen goes by the lengths. */
 size_t attn_paged_decode_workspace_bytes(int B, int Hq, int Hkv, int n, int d, int append, int bits);
 
 int attn_paged_decode(const void* q, const void* k_new, const void* v_new, const long long* strides,
