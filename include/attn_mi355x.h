@@ -276,8 +276,8 @@ int attn_decode(const void* q, const void* k_new, const void* v_new, void* k_cac
  * with sin t negated (from dq, dk of the rotated tensors to those of the
  * originals). r is a multiple of 16, 16 <= r <= d. freqs is a device array of r/2
  * float64 (radians per position) and a the amplitude: every scaling for long
- * contexts is a choice of these two. Angles are reduced in 64 bits, so far
- * positions are as exact as near ones.
+ * contexts is a choice of these two. Angles are reduced in 64 bits: off by |t| 2^-52,
+ * so that positions up to 2^27 are as exact as near ones even in float32.
  *
  * Layout: q, q_out [B, Hq, n, d], k, k_out [B, Hk, n, d] (k and k_out NULL: q
  * alone). `strides` (a host array) holds the elements between sequences, heads and

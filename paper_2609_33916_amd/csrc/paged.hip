@@ -71,8 +71,8 @@ bool launches(long long rows, int per) { return blocks_for(rows, per) < 1LL << 2
 
 // Heads per workgroup: a thread's sines and cosines serve all of them, so as many,
 // up to 8, as leave four workgroups per compute unit (rotation of 2 x 64 heads, n = 16384:
-// 196 us, one head each 240, up to 16 207; append of 16000 tokens of 8 heads in 4 bits 21.3,
-// one head each 38.7, up to 4 22.2).
+// 197 us, one head each 228, up to 16 211; append of 16000 tokens of 8 heads in 4 bits 23.8,
+// one head each 42.6, up to 4 24.4).
 int heads_per_group(long long token_blocks, int heads) {
   const long long want = attn::kXcds * attn::kCusPerXcd * 4;
   return (int)std::max<long long>(1, std::min<long long>({8, heads, token_blocks * heads / want}));
@@ -176,28 +176,38 @@ void launch_append(attn::AppendArgs a, bool interleaved, hipStream_t st) {
 }
 
 // Decode: a workgroup owns (sequence, cache head, up to 32 query heads, one split
-// of the keys). The keys are split, a block for each of its four waves at least,
-// into as many parts as leave no more than two workgroups per compute unit, so that
-// all run at once (160 groups of 1900 tokens in 4 bits 14.8 us in three parts, 18.3 in
-// four, 640 workgroups; one sequence of 131072 tokens in 4 bits 31, up to 768 workgroups
-// 36); from 257 groups on in two, which then even each other out (384 groups of 2000
-// tokens 66 us, undivided 72).
+// of the keys). Times are a step's, merge included, back to back in a captured graph.
 //
-// Merging the splits costs a launch and 2.5 to 4 us, so up to a number of blocks
+// Up to 256 groups the keys are split, a block for each of its four waves at least, into as
+// many parts as leave no more than two workgroups per compute unit, so that all run at once
+// (160 groups of 1900 tokens in 4 bits 15.9 us in three parts, 19.3 in four, 640
+// workgroups; one sequence of 131072 tokens in 4 bits 33, up to 768 workgroups 37). From 257
+// to 511 groups they are split in two, up to 1022 workgroups, which even each other out
+// (384 groups of 2000 tokens, bfloat16, 68.5 us, undivided 77). From 512 on they are not
+// split: two parts cost 2 to 10 % where the lengths are alike (512 groups of 4096 tokens,
+// bfloat16 169 us, 172 in two; 4 bits 54 and 58). The price is a batch of which one sequence
+// is far longer than the rest, whose step takes as long as that one's workgroup (64
+// sequences of 8 heads, one of 16000 tokens, the others of 500: bfloat16 222 us, 119 in two
+// parts; 4 bits 76, 46).
+//
+// Merging the splits costs a launch and 2.7 to 4.7 us, so up to a number of blocks
 // the keys stay undivided: few where many parts would share them (d = 128, 600 tokens in
-// 4 bits, 64 groups: 8.6 us, in two parts 9.8), more for three (160 groups of 1200
-// tokens in 4 bits 11.4, 12.8) and most where two workgroups of a compute unit would
-// only halve what one has to itself (256 groups of 1900 tokens in 4 bits 15.9, 18.4;
-// bfloat16, 1500: 34.3, 37.5). Beyond, sequences of different lengths need the
-// splits (176 groups of 8000 to 16000 tokens in 4 bits 55 us, undivided 63).
+// 4 bits, 64 groups: 9.4 us, in two parts 10.5), more for three (160 groups of 1200
+// tokens in 4 bits 12.2, 13.7) and most where two workgroups of a compute unit would
+// only halve what one has to itself (256 groups of 1900 tokens in 4 bits 17.4, 20.1;
+// bfloat16, 1500: 35.1, 37.2). Beyond, sequences of different lengths need the
+// splits (176 groups of 8000 to 16000 tokens in 4 bits 74 us, undivided 78). At d = 64 and 32
+// the numbers of blocks are those of d = 128: they save less there (256 groups of 1500
+// tokens, bfloat16: d = 64 18.5 us, 20.8 in two parts, d = 32 11.7, 14.0), and in few groups of
+// bfloat16 they split too early (16 groups of 600 tokens, d = 32: 6.6 us, undivided 6.0).
 //
 // More than 16 query heads of a cache head are two columns of 16, which read the keys
-// once (220 groups of 8000 tokens, 32 heads, d = 64: 46.6 us in 4 bits, 58.7 by workgroups
-// of one column; bfloat16 85, 158), or, with so few blocks that latency counts, workgroups
-// of one column each (2 groups of 1500 tokens 8.5 us, two columns 9.4; bfloat16, 500
-// tokens 7.2, 8.1). In 4 bits at d = 128 always the latter: two columns need more
-// registers than there are, and what is spilled comes back behind the next block's
-// loads (16 groups of 8000 tokens 15.1 us, 24.2; 220 of 1500 23.1, 32.1).
+// once (220 groups of 8000 tokens, 32 heads, d = 64: 60.5 us in 4 bits, 68.0 by workgroups
+// of one column; bfloat16 84, 159), or, with so few blocks that latency counts, workgroups
+// of one column each (2 groups of 1500 tokens, d = 64, 4 bits 8.8 us, two columns 9.9;
+// bfloat16, d = 128, 500 tokens 9.1, 10.6). In 4 bits at d = 128 always the latter: two
+// columns need more registers than there are, and what is spilled comes back behind the next
+// block's loads (16 groups of 8000 tokens 16.9 us, 27.1; 220 of 1500 28.3, 38.2).
 constexpr long long kWorkgroups = 2 * attn::kXcds * attn::kCusPerXcd;
 struct PagedPlan {
   int nq;        // query columns of a workgroup / 16
@@ -240,8 +250,8 @@ template <int D> void launch_decode(const attn::PagedArgs& a, const dim3& grid, 
 }
 
 // One wave per row while it can have the loads of all splits in flight at once, otherwise
-// eight (512 splits at d = 128: 6.1 us, with four waves 9.0; 8 splits: 2.6 with one wave,
-// 3.4 with four and their join through LDS).
+// eight (a step of 3 heads in 512 splits at d = 128: 15.1 us, with one wave 32.6; of 32 heads
+// in 8 splits 9.0, with eight waves and their join through LDS 9.6).
 template <int D> void launch_combine(const attn::PagedArgs& a, hipStream_t st) {
   if (a.nsplit <= 8 * 256 / D)
     hipLaunchKernelGGL((attn::paged_combine_kernel<D, 1>), dim3(a.rows), dim3(64), 0, st, a.part, a.o, a.lse, a.rows, a.nsplit);

@@ -112,7 +112,8 @@ __device__ __forceinline__ long long append_row(const AppendArgs& a, int b, int 
 }
 
 // bf16 pages: as rope_kernel, the values copied beside the keys. 8 x 1024 tokens of 8
-// heads, d = 128: 12.6 us, 5.3 TB/s.
+// heads, d = 128: 12.9 us (67 MB, 5.2 TB/s). The first rows are read before the counts are
+// known: where sequences bring 512 to 1024 of the 1024 tokens 33.7 MB for 26.2, 14.9 us.
 template <bool INTER>
 __global__ void __launch_bounds__(256) append_kernel(const AppendArgs a) {
   constexpr int U = 4;
@@ -164,8 +165,8 @@ __global__ void __launch_bounds__(256) append_kernel(const AppendArgs a) {
 // other halves of its pairs are read too (by another thread as well: from
 // cache), so that the result is in the order it is stored in. The 64-bit sines and
 // cosines, a hundred instructions each, are made once per token and pair, in LDS.
-// 4 x 4000 tokens of 8 heads, d = 128: 21.3 us (84 MB, 3.9 TB/s), 18.2 with 64
-// interleaved columns turned; without the 64-bit rotation it would take 17.
+// 4 x 4000 tokens of 8 heads, d = 128: 23.8 us (83 MB, 3.5 TB/s), 17.5 with 64
+// interleaved columns turned; with the rotation in 32 bits a fifth less.
 template <int D, bool INTER>
 __global__ void __launch_bounds__(256) append4_kernel(const AppendArgs a) {
   constexpr int TPT = D / 8, TOK = 256 / TPT;   // threads per token, tokens
@@ -266,7 +267,7 @@ struct GatherArgs {
 
 // Rows starts[b] + [0, n) of every cache head, zeros where the sequence has no
 // such token (or no page for it). A thread moves 16 bytes of K and of V: 8 sequences of
-// about 2300 tokens, 8 heads, d = 128 28.4 us (179 MB, 6.3 TB/s), one row 2.5 to 4.6.
+// 2300 tokens, 8 heads, d = 128 23.9 us (151 MB, 6.3 TB/s), one row 2.9 to 4.5.
 template <bool Q4>
 __global__ void __launch_bounds__(256) gather_kernel(const GatherArgs a) {
   const int tpr = a.d / 8;
@@ -313,15 +314,16 @@ __global__ void __launch_bounds__(256) gather_kernel(const GatherArgs a) {
 // 32 columns.
 //
 // Bound by the pages' bytes where there are many: 16 sequences of 8192 tokens, 64
-// heads on 8, d = 128 83.6 us (537 MB, 6.4 TB/s); a sequence of 131072 in 4 bits 26.5 to 28
-// (143 MB, 5.2 TB/s), where one more microsecond of keys costs 7.1 TB/s' worth and the
-// rest, some 7 us, is the way to the first key (lengths, page numbers, the
-// frequencies' turn, cold loads behind each other) and the end of the last wave. In
-// 4 bits the conversions and the softmax would bound it, with two waves per SIMD 5
+// heads on 8, d = 128 84.8 us (537 MB, 6.3 TB/s); a sequence of 131072 in 4 bits 30.0
+// (143 MB, 4.8 TB/s), of which some 7 us are the way to the first key (lengths, page
+// numbers, the frequencies' turn, cold loads behind each other) and the end of the last
+// wave. In 4 bits the conversions and the softmax would bound it, with two waves per SIMD 5
 // clocks an instruction: hence the transposed reads of codes, the replicas below, and
-// the maximum that rarely moves. Short caches are that fixed part: 1000 tokens 6.65 us.
-// Not faster: three waves per SIMD (registers spill, 43 us where two took 25), eight
-// waves in a workgroup (1000 tokens 9.4 us where four took 7.2), two blocks loaded ahead (below).
+// the maximum that rarely moves; from 9 query heads per cache head on they do. Short caches
+// are that fixed part: 1000 tokens 7.2 us. (These are the kernel's times alone.)
+// Not faster, by the ratio of two runs in turn: three waves per SIMD (registers spill, 1.7
+// times as long), eight waves in a workgroup (1000 tokens 1.3 times), two blocks loaded
+// ahead (below).
 struct PagedArgs {
   const void* q;               // bf16 [B, Hq, d], sequences q_b elements apart
   const void *k_new, *v_new;   // bf16 [B, Hkv, d], or null
@@ -409,12 +411,12 @@ template <int B> __device__ __forceinline__ float byte_power(uint32_t w) {
 
 // P in two bfloat16: the float cut to its first 16 bits, and the rest rounded, so that 15
 // bits of the factor stay. (With P in one, O was off by 2.0e-3 to 2.4e-3 of its length,
-// with two by the 1.6e-3 of its own last rounding. A step costs nothing more in bf16, and
-// in 4 bits 28.8 us where one part took 28.0 (32 ragged sequences up to 4096, 4 heads per
-// cache head), 34.8 for 33.2 (one of 131072, 8 heads), 60 for 48.5 where instructions
-// bound it (220 of 8000, d = 64, 32 heads).) Infinite values of V need a rest above 0, for
-// 0 times infinity is not a number; in 4 bits the rest of a product with a scale of 255 has to
-// be not a number, as infinity less infinity is.
+// with two by the 1.6e-3 of its own last rounding. A step takes no longer in bf16; in 4
+// bits 3 % longer (32 ragged sequences up to 4096, 4 heads per cache head), 5 % (one of
+// 131072, 8 heads), 24 % where instructions bound it (220 of 8000, d = 64, 32 heads).)
+// Infinite values of V need a rest above 0, for 0 times infinity is not a number; in 4 bits
+// the rest of a product with a scale of 255 has to be not a number, as infinity less infinity
+// is.
 constexpr float kLeastRest = 0x1p-100f;
 template <bool Q4> __device__ __forceinline__ void two_parts(const f32x4& a, const f32x4& b, bf16x8& first, bf16x8& rest) {
   f32x4 ra, rb;
@@ -434,8 +436,8 @@ template <bool Q4> __device__ __forceinline__ void two_parts(const f32x4& a, con
 // REP: the query heads (at most 16 / REP of them) stand REP times in the 16 columns, and a
 // lane scales P for only 1 / REP of the 32-column blocks of d; the two parts of the
 // query are then columns, not products of their own (131072 tokens, 8 heads per cache
-// head: REP = 2 28.2 us, without 31.7; 32 ragged sequences, 4 heads: REP = 4 25.6, without
-// 30.0). PAGE: the least number of keys that lie in one page, 16 or a whole block, which
+// head: REP = 2 33.6 us a step, without 37; 32 ragged sequences, 4 heads: REP = 4 28.3, without
+// 36.7). PAGE: the least number of keys that lie in one page, 16 or a whole block, which
 // then has one page number and one buffer (part of the same figures).
 template <int D, int NQ, int REP, bool Q4, int PAGE>
 __global__ void __launch_bounds__(256, 2) paged_decode_kernel(const PagedArgs a) {
@@ -908,7 +910,7 @@ __global__ void __launch_bounds__(256, 2) paged_decode_kernel(const PagedArgs a)
   // The next block's loads are issued whether there is one or not (they then end before
   // memory): behind a branch the compiler, counting the loads that are certainly in
   // flight, would wait for them before it uses this block's. (Two blocks ahead, both
-  // from the start, short caches were slower: 256 groups, 512 tokens 14.2 us for 12.7.)
+  // from the start, short caches were slower: 256 groups, 512 tokens by an eighth.)
   for (; kv < k_hi; kv += 8 * BK) {
     load(B2, ids, kv + 4 * BK);
     fetch(ids, kv + 8 * BK);

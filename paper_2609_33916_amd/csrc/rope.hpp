@@ -164,8 +164,8 @@ struct RopeArgs {
 // Bound by memory: every element is read and written once. The angles belong to a
 // token, not to a head, so a thread keeps its pairs' sines and cosines in registers
 // and walks over the heads, U at a time with all their loads in flight. 2 sequences
-// of 16384 tokens, 64 heads, d = 128, bfloat16: 196 us, 5.5 TB/s (a large copy on the
-// same card 4.9); a short call is one launch (333 tokens, 10 heads: 3.7 us). Loads before
+// of 16384 tokens, 64 heads, d = 128, bfloat16: 195 us, 5.5 TB/s (a large copy on the
+// same card 4.9); a short call is one launch (333 tokens, 10 heads: 3.9 us). Loads before
 // the angles, and non-temporal loads or stores, were no faster.
 template <typename T, bool INTER>
 __global__ void __launch_bounds__(256) rope_kernel(const RopeArgs a) {
