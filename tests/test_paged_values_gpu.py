@@ -15,7 +15,7 @@ import torch
 import paper_2609_33916_amd as lib
 from helpers import gpu_available, to_host64
 from oracle import paged
-from test_paged_gpu import BF16, NAN, Pool, ints, same, stored
+from test_paged_gpu import BF16, Pool, ints, same, stored
 
 pytestmark = [pytest.mark.gpu, pytest.mark.skipif(not gpu_available(), reason="needs a GPU")]
 

@@ -1,6 +1,5 @@
 """Overlapping outputs of the rotation: the check (csrc/strides.hpp, compiled for the CPU)
 against all pairs of rows, and the refusal of the C ABI and the Python form."""
-import ctypes
 import os
 import shutil
 import subprocess
