@@ -371,6 +371,77 @@ int attn_paged_decode(const void* q, const void* k_new, const void* v_new, const
                       int B, int Hq, int Hkv, int n, int num_pages, int page_size, int table_width, int d,
                       int r, float amplitude, int interleaved, float scale, int dtype, void* stream);
 
+/* ---- Keys of another length -------------------------------------------------
+ * Not operations of the paper: the attention above between nq queries and nk keys, as
+ * a decoder's attention to the states of an encoder, or to a cache longer than
+ * the chunk of queries at hand, needs it, and with the bias by relative position that
+ * models of that kind learn. With r = j - (start_b + i), the place of key j relative to
+ * query i, and g = h / (Hq / Hkv):
+ *   x_ij = scale Q[b,h,i] . K[b,g,j] + bias[rows[min(max(r - first, 0), R - 1)], h],
+ *          masked to -inf where j >= len_b or (causal) r > 0
+ *   P = softmax_rows(x), L_i = ln sum_j exp(x_ij), O = P V
+ * and, from dO: dV, dP, D, dS, dQ, dK as above (dK and dV of a cache head being the sums over
+ * its query heads), dbias[c, h] = sum of dS_ij over all b, i and j with row c. A query that
+ * sees no key has O = 0, L = -inf and no gradient.
+ *
+ * Layout: Q, O, dO, dQ [B, Hq, nq, d], K, V, dK, dV [B, Hkv, nk, d] (Hq a multiple of Hkv),
+ * L float32 [B, Hq, nq], dense. `strides` (a host array) holds the elements between
+ * sequences, heads and tokens, three for each tensor in the order of the arguments, or is
+ * NULL for dense tensors: views of fused projections need no copy. Strides are not
+ * negative, a token's at most 2^22, rows start at multiples of 16 bytes, and the rows of an output
+ * must not overlap each other (ATTN_E_ARG), nor another tensor's. (An input may have
+ * strides of 0; its gradient still comes for every entry.)
+ *
+ * k_lens: device int32 [B] (clamped to [0, nk]) or NULL (nk). Keys from len_b on are never
+ * read, and dK and dV are 0 there. starts: device int32 [B] (clamped to [-2^30, 2^30]), or NULL:
+ * `start` for all, within these bounds: the place of the first query among the keys. It may be
+ * negative. Under the causal mask keys after a query take no part in its sums, except that
+ * a value (V) which is not finite may also reach the queries up to 127 places before its
+ * own.
+ *
+ * bias: [buckets, Hq] in dtype, or NULL (none, no gradient). rows: device int32 [R], 2 <= R <=
+ * 2048, the bucket of relative position first + t; nearer and farther positions take the first
+ * and last entry, and a bucket outside [0, buckets) stands for no bias. dbias: like bias,
+ * or NULL. An entry below -2^16 (-inf, a type's lowest value) masks its positions.
+ *
+ * Sums, softmax and gradients are float32 inside; with bfloat16 tensors P and dS are rounded
+ * to bfloat16 once before they multiply (P keeps 15 bits where there are few queries). No atomics
+ * whose order could change a result are issued: repeated calls give the same bits.
+ * Workspaces (16-byte aligned, contents ignored) hold the functions' bytes; 0 needs none.
+ * nq and nk are at most 2^29, B Hq nq and B Hkv nk below 2^26, and a call is cut into fewer than 2^24
+ * workgroups (ATTN_E_SHAPE). bias_positions: R, 0 without a bias (in the backward: without dbias). */
+size_t attn_cross_fwd_workspace_bytes(int B, int Hq, int Hkv, int nq, int nk, int d, int dtype, int bias_positions);
+
+int attn_cross_fwd(const void* Q, const void* K, const void* V, void* O, float* L, const long long* strides,
+                   const int* k_lens, const int* starts, int start, const void* bias, const int* rows, int first, int R,
+                   int buckets, void* workspace, size_t workspace_bytes, int B, int Hq, int Hkv, int nq, int nk, int d,
+                   float scale, int causal, int dtype, void* stream);
+
+/* O and L must be attn_cross_fwd's for the same arguments. strides: Q, K, V, O, dO, dQ, dK, dV. */
+size_t attn_cross_bwd_workspace_bytes(int B, int Hq, int Hkv, int nq, int nk, int d, int dtype, int bias_positions);
+
+int attn_cross_bwd(const void* Q, const void* K, const void* V, const void* O, const float* L, const void* dO,
+                   void* dQ, void* dK, void* dV, void* dbias, const long long* strides, const int* k_lens,
+                   const int* starts, int start, const void* bias, const int* rows, int first, int R, int buckets,
+                   void* workspace, size_t workspace_bytes, int B, int Hq, int Hkv, int nq, int nk, int d, float scale,
+                   int causal, int dtype, void* stream);
+
+/* ---- Decode behind a shared prefix --------------------------------------------
+ * attn_decode for a batch whose sequences all begin with the same np tokens: K and V of
+ * those are kept once, k_prefix, v_prefix [Hkv, np, d], and read once for the whole batch; what
+ * follows is in the caches of attn_decode, k_cache, v_cache [B, Hkv, n_cap, d]. k_new, v_new [B,
+ * Hkv, d] (both NULL: no append) go to row len_b of the caches, and q [B, Hq, d] attends to the
+ * prefix, to rows [0, len_b) and to the new token. len_b = cache_lens[b] (device int32 [B])
+ * clamped to [0, n], or n for all where NULL; n may be 0, n_cap >= n + 1 with an append, >= n
+ * without. Tensors are dense, bfloat16 only, 16-byte aligned; O [B, Hq, d], L float32 [B, Hq] or NULL.
+ * B Hq, B Hkv n and Hkv np are below 2^26. P keeps 15 bits. */
+size_t attn_prefix_decode_workspace_bytes(int B, int Hq, int Hkv, int np, int n, int d);
+
+int attn_prefix_decode(const void* q, const void* k_new, const void* v_new, const void* k_prefix, const void* v_prefix,
+                       void* k_cache, void* v_cache, const int* cache_lens, void* O, float* L, void* workspace,
+                       size_t workspace_bytes, int B, int Hq, int Hkv, int np, int n, int n_cap, int d, float scale,
+                       int dtype, void* stream);
+
 /* Not an operation of the paper: error reporting of this interface.
  * Static, NUL-terminated description of a status code (never NULL). */
 const char* attn_strerror(int code);

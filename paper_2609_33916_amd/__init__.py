@@ -20,6 +20,15 @@ Rotary positions and a paged key/value cache, in bfloat16 or 4 bits, stand besid
     O, L = attn_paged_decode(q, k_pages, v_pages, block_table, lens, k_new, v_new, freqs=freqs)
     K, V = attn_paged_gather(k_pages, v_pages, block_table, lens, n)
 
+So do attention to keys of another length, with a bias by relative position if asked, and
+a decode step behind a prefix that the batch shares:
+
+    O, L = attn_cross_fwd(q, k, v, k_lens=lens)             # strided views, grouped heads
+    dQ, dK, dV = attn_cross_bwd(q, k, v, O, L, do, k_lens=lens)
+    rows, first = attn_bias_buckets(32, 128)
+    O, L = attn_cross_fwd(q, k, v, bias=table, bias_rows=rows, bias_first=first)
+    O, L = attn_prefix_decode(q, k_prefix, v_prefix, k_cache, v_cache, k_new, v_new, cache_lens)
+
 There is no fallback: if the library is missing or the device is not a GPU,
 the call raises.
 """
@@ -39,7 +48,8 @@ __all__ = ["attn_fwd", "attn_fwd_bwd", "attn_fwd_bwd_timed", "attn_fwd_bwd_noall
            "attn_mat_bytes", "attn_mat_lda", "attn_mat_fwd", "attn_mat_bwd", "attn_mat_fwd_bwd",
            "attn_fwd_bwd_atomic", "attn_workspace_bytes_atomic", "attn_decode", "attn_decode_workspace_bytes",
            "attn_rope", "attn_rope_bwd", "attn_rope_freqs", "attn_paged_append", "attn_paged_gather",
-           "attn_paged_decode", "attn_paged_decode_workspace_bytes",
+           "attn_paged_decode", "attn_paged_decode_workspace_bytes", "attn_cross_fwd", "attn_cross_bwd",
+           "attn_bias_buckets", "attn_prefix_decode", "attn_prefix_decode_workspace_bytes",
            "AttnError", "lib", "LIB_PATH", "ATTN_BF16", "ATTN_F32"]
 
 # ATTN_MI355X_LIB may name another build of the same library (A/B comparison
@@ -117,6 +127,19 @@ def lib() -> ctypes.CDLL:
     L.attn_paged_decode.argtypes = [vp, vp, vp, ctypes.POINTER(ll), vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz,
                                     i, i, i, i, i, i, i, i, i, f, i, f, i, vp]
     L.attn_paged_decode.restype = i
+    mask = [vp, vp, i, vp, vp, i, i, i, vp, sz, i, i, i, i, i, i, f, i, i, vp]   # k_lens to stream
+    L.attn_cross_fwd_workspace_bytes.argtypes = [i] * 8
+    L.attn_cross_fwd_workspace_bytes.restype = sz
+    L.attn_cross_fwd.argtypes = [vp] * 5 + [ctypes.POINTER(ll)] + mask
+    L.attn_cross_fwd.restype = i
+    L.attn_cross_bwd_workspace_bytes.argtypes = [i] * 8
+    L.attn_cross_bwd_workspace_bytes.restype = sz
+    L.attn_cross_bwd.argtypes = [vp] * 10 + [ctypes.POINTER(ll)] + mask
+    L.attn_cross_bwd.restype = i
+    L.attn_prefix_decode_workspace_bytes.argtypes = [i] * 6
+    L.attn_prefix_decode_workspace_bytes.restype = sz
+    L.attn_prefix_decode.argtypes = [vp] * 11 + [sz] + [i] * 7 + [f, i, vp]
+    L.attn_prefix_decode.restype = i
     L.attn_strerror.argtypes = [i]
     L.attn_strerror.restype = ctypes.c_char_p
     _lib = L
@@ -808,4 +831,178 @@ def attn_paged_decode(q, k_pages, v_pages, block_table, lens, k_new=None, v_new=
           v_new.data_ptr() if append else None, strides, *ptr, f_ptr, p_ptr, O.data_ptr(),
           L.data_ptr() if L is not None else None, ws_ptr, ws_len, B, Hq, Hkv, n, P, ps, width, d, r, float(amplitude),
           int(bool(interleaved)), _scale(scale, d), ATTN_BF16)
+    return O, L
+
+
+# ------------------------------------------------------ keys of another length --
+def attn_bias_buckets(num_buckets: int, max_distance: int, bidirectional: bool = True, device="cuda") -> Tuple[torch.Tensor, int]:
+    """The buckets of relative positions (key less query) as attn_cross_fwd and attn_cross_bwd
+    take them: (rows, first), rows an int32 tensor on `device`, the bucket of relative position
+    first + t, of which the first and the last stand for all beyond. Of the buckets of a
+    direction (half of them each with ``bidirectional``, later keys in the upper half;
+    else all for earlier keys, and later ones count as distance 0) one half is for
+    the nearest positions, one each; the others end at equal ratios up to
+    ``max_distance``, from which on all share the last (arXiv:1910.10683, section 2.1). Borders are
+    computed in whole numbers, so that a position on one is where it belongs."""
+    _need(isinstance(num_buckets, int) and isinstance(max_distance, int), "num_buckets and max_distance must be integers")
+    _need(num_buckets % 2 == 0 or not bidirectional, "num_buckets must be even: half of them for each direction")
+    side = num_buckets // 2 if bidirectional else num_buckets
+    near = side // 2
+    _need(near >= 1, "too few buckets")
+    _need(max_distance > near, f"max_distance must be above the {near} nearest positions")
+    far = side - near
+    borders = []   # the first position of bucket near + k, k = 1, ...: the least p with p >= near (max_distance / near)^(k / far)
+    for k in range(1, far):
+        p, least = int(near * (max_distance / near) ** (k / far)), near ** (far - k) * max_distance ** k
+        while p ** far >= least:
+            p -= 1
+        while p ** far < least:
+            p += 1
+        borders.append(p)
+    last = borders[-1] if borders else near
+
+    def bucket(p: int) -> int:
+        return p if p < near else near + sum(p >= x for x in borders)
+    back = [bucket(p) for p in range(last, -1, -1)]
+    rows = back + ([side + bucket(p) for p in range(1, last + 1)] if bidirectional else [])
+    _need(len(rows) <= 2048, "max_distance is too large: more than 2048 positions have a bias of their own")
+    return torch.tensor(rows, dtype=torch.int32, device=device), -last
+
+
+def _cross_args(q, k, v, starts, start, k_lens, bias, bias_rows, bias_first):
+    """Checks what attn_cross_fwd and attn_cross_bwd share: (B, Hq, Hkv, nq, nk, d), the library's
+    arguments from k_lens to buckets, R."""
+    _need(isinstance(q, torch.Tensor) and q.dim() == 4 and q.is_cuda, "q must be a GPU tensor [B, Hq, nq, d]")
+    _need(isinstance(k, torch.Tensor) and k.dim() == 4, "k must be [B, Hkv, nk, d]")
+    B, Hq, nq, d = q.shape
+    Hkv, nk = k.shape[1], k.shape[2]
+    _rows("q", q, q.shape, q)
+    for name, t in (("k", k), ("v", v)):
+        _rows(name, t, (B, Hkv, nk, d), q)
+    _need(min(B, Hq, Hkv, nq, nk) > 0, "tensors must not be empty")
+    _need(-2**31 <= start < 2**31 and -2**31 <= bias_first < 2**31, "start and bias_first must fit 32 bits")
+    if bias is None:
+        _need(bias_rows is None, "bias_rows needs bias")
+        b_args, R = (None, None, 0, 0, 0), 0
+    else:
+        _need(isinstance(bias, torch.Tensor) and bias.dim() == 2, "bias must be [buckets, Hq]")
+        _check_out("bias", bias, (bias.shape[0], Hq), q.dtype, q)
+        _need(isinstance(bias_rows, torch.Tensor) and bias_rows.dim() == 1, "bias needs bias_rows, int32 [R]")
+        R = bias_rows.shape[0]
+        b_args = (bias.data_ptr(), _ints("bias_rows", bias_rows, ((R,),), q), int(bias_first), R, bias.shape[0])
+    args = (_ints("k_lens", k_lens, ((B,),), q), _ints("starts", starts, ((B,),), q), 0 if starts is not None else int(start)) + b_args
+    return (B, Hq, Hkv, nq, nk, d), args, R
+
+
+def _cross_strides(*tensors):
+    return (ctypes.c_longlong * (3 * len(tensors)))(*(s for t in tensors for s in t.stride()[:3]))
+
+
+def _cross_workspace(workspace, nbytes: int, ref: torch.Tensor):
+    """The tensor that holds it, its address and size."""
+    if workspace is None and nbytes > 0:
+        workspace = torch.empty(nbytes, dtype=torch.uint8, device=ref.device)
+    return (workspace, None, 0) if workspace is None else (workspace, *_check_workspace(workspace, nbytes, ref))
+
+
+def attn_cross_fwd(q, k, v, scale: Optional[float] = None, causal: bool = False, start: int = 0, starts=None, k_lens=None,
+                   bias=None, bias_rows=None, bias_first: int = 0, out=None, workspace=None):
+    """Attention of q [B, Hq, nq, d] to k, v [B, Hkv, nk, d]: returns (O, L). Any views whose last
+    axis is dense are taken as they are. k_lens (int32 [B] on the GPU): the keys of each sequence,
+    those behind are not read. Query i stands at place start + i among the keys, or starts[b] + i
+    (int32 [B]): ``causal`` hides later keys, and bias [buckets, Hq] (q's dtype) adds
+    bias[bias_rows[r - bias_first], h] to the scores of the pairs at relative position r = key -
+    query, positions beyond taking bias_rows' first and last entries (attn_bias_buckets).
+    A query without keys has O = 0, L = -inf."""
+    (B, Hq, Hkv, nq, nk, d), args, R = _cross_args(q, k, v, starts, start, k_lens, bias, bias_rows, bias_first)
+    code = _dtype_code(q)
+    if out is None:
+        O = torch.empty((B, Hq, nq, d), dtype=q.dtype, device=q.device)
+        L = torch.empty((B, Hq, nq), dtype=torch.float32, device=q.device)
+    else:
+        _need(len(out) == 2, "out must hold (O, L)")
+        O, L = out
+        _rows("O", O, q.shape, q)
+        _check_out("L", L, (B, Hq, nq), torch.float32, q)
+    workspace, ws_ptr, ws_len = _cross_workspace(
+        workspace, int(lib().attn_cross_fwd_workspace_bytes(B, Hq, Hkv, nq, nk, d, code, R)), q)
+    _call("attn_cross_fwd", q.device, q.data_ptr(), k.data_ptr(), v.data_ptr(), O.data_ptr(), L.data_ptr(),
+          _cross_strides(q, k, v, O), *args, ws_ptr, ws_len, B, Hq, Hkv, nq, nk, d, _scale(scale, d), int(bool(causal)), code)
+    return O, L
+
+
+def attn_cross_bwd(q, k, v, o, lse, do, scale: Optional[float] = None, causal: bool = False, start: int = 0, starts=None,
+                   k_lens=None, bias=None, bias_rows=None, bias_first: int = 0, out=None, workspace=None):
+    """The gradients of attn_cross_fwd's inputs from its O and L and the gradient of O: returns
+    (dQ, dK, dV), with a bias (dQ, dK, dV, dBias). Other arguments as there. ``out`` may hold
+    the results' tensors (dBias None: not wanted), which may be views."""
+    (B, Hq, Hkv, nq, nk, d), args, R = _cross_args(q, k, v, starts, start, k_lens, bias, bias_rows, bias_first)
+    code = _dtype_code(q)
+    for name, t in (("o", o), ("do", do)):
+        _rows(name, t, q.shape, q)
+    _check_out("lse", lse, (B, Hq, nq), torch.float32, q)
+    if out is None:
+        out = tuple(torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v) + (() if bias is None else (bias,)))
+    else:
+        out = tuple(out)
+        _need(len(out) == (3 if bias is None else 4), "out must hold (dQ, dK, dV), and dBias with a bias")
+        for name, t, like in zip(("dQ", "dK", "dV"), out, (q, k, v)):
+            _rows(name, t, like.shape, q)
+        if bias is not None and out[3] is not None:
+            _check_out("dBias", out[3], bias.shape, q.dtype, q)
+    dbias = out[3].data_ptr() if bias is not None and out[3] is not None else None
+    workspace, ws_ptr, ws_len = _cross_workspace(
+        workspace, int(lib().attn_cross_bwd_workspace_bytes(B, Hq, Hkv, nq, nk, d, code, R if dbias else 0)), q)
+    _call("attn_cross_bwd", q.device, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), lse.data_ptr(), do.data_ptr(),
+          *(t.data_ptr() for t in out[:3]), dbias, _cross_strides(q, k, v, o, do, *out[:3]), *args, ws_ptr, ws_len,
+          B, Hq, Hkv, nq, nk, d, _scale(scale, d), int(bool(causal)), code)
+    return out
+
+
+# --------------------------------------------------------- shared prefix --
+def attn_prefix_decode_workspace_bytes(B: int, Hq: int, Hkv: int, np: int, n: int, d: int) -> int:
+    return int(lib().attn_prefix_decode_workspace_bytes(B, Hq, Hkv, np, n, d))
+
+
+def attn_prefix_decode(q, k_prefix, v_prefix, k_cache, v_cache, k_new=None, v_new=None, cache_lens=None, n: Optional[int] = None,
+                       scale: Optional[float] = None, out=None, workspace=None):
+    """attn_decode for sequences that all begin with the same tokens: k_prefix, v_prefix
+    [Hkv, np, d] hold those once, the caches [B, Hkv, n_cap, d] what follows. k_new/v_new
+    ([B, Hkv, d]) are appended at row cache_lens[b], and q ([B, Hq, d]) attends to the prefix, to the
+    first cache_lens[b] rows and to the new token. n bounds the lengths (default: the
+    caches' room). Returns (O, L)."""
+    _need(isinstance(q, torch.Tensor) and q.dim() == 3 and q.is_cuda, "q must be a GPU tensor [B, Hq, d]")
+    _need(q.dtype == torch.bfloat16, "q must be bfloat16")
+    _need(isinstance(k_prefix, torch.Tensor) and k_prefix.dim() == 3, "k_prefix must be [Hkv, np, d]")
+    _need(isinstance(k_cache, torch.Tensor) and k_cache.dim() == 4, "k_cache must be [B, Hkv, n_cap, d]")
+    B, Hq, d = q.shape
+    Hkv, n_p = k_prefix.shape[:2]
+    n_cap = k_cache.shape[2]
+    append = k_new is not None
+    _need(append == (v_new is not None), "k_new and v_new belong together")
+    _check_out("q", q, q.shape, q.dtype, q)
+    for name, t, shape in (("k_prefix", k_prefix, (Hkv, n_p, d)), ("v_prefix", v_prefix, (Hkv, n_p, d)),
+                           ("k_cache", k_cache, (B, Hkv, n_cap, d)), ("v_cache", v_cache, (B, Hkv, n_cap, d))) + \
+            ((("k_new", k_new, (B, Hkv, d)), ("v_new", v_new, (B, Hkv, d))) if append else ()):
+        _check_out(name, t, shape, q.dtype, q)
+    if n is None:
+        _need(cache_lens is not None, "n is required without cache_lens")
+        n = n_cap - append
+    n = int(n)
+    _need(-2**31 <= n < 2**31, "n must fit 32 bits")
+    l_ptr = _ints("cache_lens", cache_lens, ((B,),), q)
+    if out is None:
+        O = torch.empty((B, Hq, d), dtype=q.dtype, device=q.device)
+        L = torch.empty((B, Hq), dtype=torch.float32, device=q.device)
+    else:
+        _need(len(out) == 2, "out must hold (O, L)")
+        O, L = out
+        _check_out("O", O, (B, Hq, d), q.dtype, q)
+        if L is not None:
+            _check_out("L", L, (B, Hq), torch.float32, q)
+    workspace, ws_ptr, ws_len = _cross_workspace(workspace, attn_prefix_decode_workspace_bytes(B, Hq, Hkv, n_p, n, d), q)
+    _call("attn_prefix_decode", q.device, q.data_ptr(), k_new.data_ptr() if append else None,
+          v_new.data_ptr() if append else None, k_prefix.data_ptr(), v_prefix.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(),
+          l_ptr, O.data_ptr(), L.data_ptr() if L is not None else None, ws_ptr, ws_len, B, Hq, Hkv, n_p, n, n_cap, d,
+          _scale(scale, d), ATTN_BF16)
     return O, L

@@ -31,6 +31,7 @@ SOURCES = {
     "split.hip": [],
     "f32x3.hip": [],
     "paged.hip": [],
+    "cross.hip": [],
     "bwd.hip": ["-mllvm", "-amdgpu-sched-strategy=iterative-ilp"],
 }
 

@@ -1,0 +1,405 @@
+// C ABI of attention to keys of another length and of the decode step behind a
+// shared prefix (declared in include/attn_mi355x.h): argument validation, plans and
+// launches. As in attn.hip, everything is validated on the host before any HIP call.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <climits>
+#include <cmath>
+#include <cstdint>
+#include <type_traits>
+
+#include "attn_mi355x.h"
+#include "cross.hpp"
+#include "launch.hpp"
+
+namespace {
+
+using attn::aligned;
+using attn::bf16;
+using attn::CrossArgs;
+using attn::Strides;
+
+bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+size_t up16(size_t x) { return (x + 15) & ~(size_t)15; }
+long long div_up(long long x, long long y) { return (x + y - 1) / y; }
+
+constexpr int kMaxLength = 1 << 29;
+constexpr long long kMaxBlocks = (1LL << 24) - 1;   // a launch has fewer than 2^32 threads
+// offsets inside a tile of 64 rows stay in 31 bits
+constexpr long long kMaxTokenStride = 1 << 22;
+
+int check_sizes(int B, int Hq, int Hkv, int nq, int nk, int d, int dtype) {
+  if (B < 1 || Hq < 1 || Hkv < 1 || nq < 1 || nk < 1 || Hq % Hkv != 0) return ATTN_E_SHAPE;
+  if (dtype != ATTN_BF16 && dtype != ATTN_F32) return ATTN_E_UNSUPPORTED;
+  if (d != 32 && d != 64 && d != 128) return ATTN_E_UNSUPPORTED;
+  if (nq > kMaxLength || nk > kMaxLength) return ATTN_E_SHAPE;
+  // the largest grids: row vectors and sums in pieces of 8 rows, key blocks
+  if ((__int128)B * Hq * nq > (__int128)kMaxBlocks * 4 || (__int128)B * Hkv * nk > (__int128)kMaxBlocks * 4) return ATTN_E_SHAPE;
+  return ATTN_OK;
+}
+
+// A tensor [B, H, n, d]
+int check_rows(const void* p, const Strides& s, int B, int H, int n, int elem) {
+  if (!attn::fits(s, B, H, n) || s.t > kMaxTokenStride) return ATTN_E_SHAPE;
+  return aligned(p, 16) && aligned(s, elem) ? ATTN_OK : ATTN_E_ALIGN;
+}
+
+struct Bias {
+  const void* table;
+  const int* rows;
+  int first, R, buckets;
+};
+int check_bias(const Bias& x, int elem) {
+  if (!x.table) return ATTN_OK;
+  if (!x.rows) return ATTN_E_NULL;
+  if (x.R < 2 || x.R > attn::kBiasMax || x.buckets < 1 || x.buckets > (1 << 20) || std::abs((long long)x.first) > (1 << 20))
+    return ATTN_E_SHAPE;
+  return aligned(x.table, elem) && aligned(x.rows, 4) ? ATTN_OK : ATTN_E_ALIGN;
+}
+
+int check_mask(const int* lens, const int* starts, int start, float scale, int causal) {
+  if (!std::isfinite(scale) || (causal != 0 && causal != 1)) return ATTN_E_ARG;
+  if (!starts && (start > (1 << 30) || start < -(1 << 30))) return ATTN_E_SHAPE;
+  return aligned(lens, 4) && aligned(starts, 4) ? ATTN_OK : ATTN_E_ALIGN;
+}
+
+void set_scale(CrossArgs& a, float scale, int dtype) {
+  a.scale = scale;
+  // as in attn.hip: a floor far below any score difference, so that 0 times an infinite score is none
+  a.sl2 = std::fmax(std::fabs(scale) * attn::kLog2e, 1e-30f);
+  a.qflip = std::signbit(scale) && scale != 0.f ? (dtype == ATTN_BF16 ? 0x80008000u : 0x80000000u) : 0u;
+}
+
+// ------------------------------------------------------------------- plans --
+// The forward takes cross_few_kernel where the 128-query workgroups would leave
+// compute units idle.
+bool few_queries(int B, int Hq, int nq) { return nq <= 64 || (long long)B * Hq * div_up(nq, 128) < 256; }
+
+struct FewPlan {
+  int pack, ntiles, splits, per;
+  long long groups;
+};
+// Parts of the keys: as many as leave every compute unit its one (d = 128) or two
+// workgroups, of at least 8 blocks of 32 keys, two for each wave.
+FewPlan few_plan(int B, int Hq, int Hkv, int nq, int nk, int d, bool bias) {
+  FewPlan p;
+  p.pack = bias ? 1 : Hq / Hkv;
+  p.ntiles = (int)div_up((long long)nq * p.pack, 32);
+  p.groups = (long long)B * (Hq / p.pack) * p.ntiles;
+  const int nb = (int)div_up(nk, 32), want = d == 128 ? 256 : 512;
+  p.splits = (int)std::max<long long>(1, std::min<long long>(want / std::max<long long>(p.groups, 1), nb / 8));
+  p.per = (int)(4 * div_up(div_up(nb, p.splits), 4));
+  p.splits = (int)div_up(nb, p.per);
+  return p;
+}
+size_t few_bytes(long long rows, int d, int parts) { return parts > 1 ? (size_t)parts * rows * (d + 2) * sizeof(float) : 0; }
+
+struct BwdPlan {
+  int q_tiles, q_splits, q_per;   // dQ: 128-query tiles; parts of the 64-key tiles
+  int k_tiles, k_splits, k_per;   // dK, dV: 128-key tiles; parts of the query tiles of all heads
+  size_t rows_at, drel_at, dq_at, dk_at, dv_at, bytes;
+};
+BwdPlan bwd_plan(int B, int Hq, int Hkv, int nq, int nk, int d, int dtype, int R) {
+  BwdPlan p;
+  const auto parts = [](long long groups, long long steps, int& splits, int& per) {
+    splits = groups >= 256 ? 1 : (int)std::max<long long>(1, std::min<long long>(512 / groups, steps / 4));
+    per = (int)div_up(steps, splits);
+    splits = (int)div_up(steps, per);
+  };
+  p.q_tiles = (int)div_up(nq, 128);
+  p.k_tiles = (int)div_up(nk, 128);
+  parts((long long)B * Hq * p.q_tiles, div_up(nk, 64), p.q_splits, p.q_per);
+  if (R > 0) {   // a row's sum of dS is formed in one workgroup
+    p.q_splits = 1;
+    p.q_per = (int)div_up(nk, 64);
+  }
+  const int bq = dtype == ATTN_F32 && d == 128 ? 32 : 64;
+  parts((long long)B * Hkv * p.k_tiles, (Hq / Hkv) * div_up(nq, bq), p.k_splits, p.k_per);
+  const size_t qrows = (size_t)B * Hq * nq, krows = (size_t)B * Hkv * nk;
+  p.rows_at = 0;
+  p.drel_at = up16(2 * qrows * sizeof(float));
+  p.dq_at = p.drel_at + (R > 0 ? up16((size_t)B * Hq * p.q_tiles * R * sizeof(float)) : 0);
+  p.dk_at = p.dq_at + (p.q_splits > 1 ? p.q_splits * qrows * d * sizeof(float) : 0);
+  p.dv_at = p.dk_at + (p.k_splits > 1 ? p.k_splits * krows * d * sizeof(float) : 0);
+  p.bytes = p.dv_at + (p.k_splits > 1 ? p.k_splits * krows * d * sizeof(float) : 0);
+  return p;
+}
+
+// ---------------------------------------------------------------- launches --
+// f(type, d, whether biased) as compile-time values
+template <typename F> void dispatch(int dtype, int d, bool bias, F&& f) {
+  const auto with_d = [&](auto t, auto bb) {
+    if (d == 32) f(t, std::integral_constant<int, 32>{}, bb);
+    else if (d == 64) f(t, std::integral_constant<int, 64>{}, bb);
+    else f(t, std::integral_constant<int, 128>{}, bb);
+  };
+  const auto with_bias = [&](auto t) {
+    if (bias) with_d(t, std::true_type{});
+    else with_d(t, std::false_type{});
+  };
+  if (dtype == ATTN_BF16) with_bias(bf16{});
+  else with_bias(0.f);
+}
+
+size_t bias_lds(const CrossArgs& a, int vectors) { return a.table ? (size_t)vectors * (a.R + 2 * attn::kBiasPad) * sizeof(float) : 0; }
+
+// Blocks and order of a grid of `heads` heads of `tiles` tiles each
+void set_grid(CrossArgs& a, long long heads, int tiles) {
+  a.nblocks = (int)(heads * tiles);
+  a.hgroup = a.causal ? attn::head_group((int)heads, tiles, 2) : 0;
+}
+
+int launched() { return hipGetLastError() == hipSuccess ? ATTN_OK : ATTN_E_HIP; }
+
+}  // namespace
+
+extern "C" size_t attn_cross_fwd_workspace_bytes(int B, int Hq, int Hkv, int nq, int nk, int d, int dtype, int bias_positions) {
+  if (check_sizes(B, Hq, Hkv, nq, nk, d, dtype) || bias_positions < 0) return 0;
+  if (!few_queries(B, Hq, nq)) return 0;
+  return few_bytes((long long)B * Hq * nq, d, few_plan(B, Hq, Hkv, nq, nk, d, bias_positions > 0).splits);
+}
+
+extern "C" int attn_cross_fwd(const void* q, const void* k, const void* v, void* o, float* L, const long long* strides,
+                              const int* k_lens, const int* starts, int start, const void* bias, const int* bias_rows,
+                              int bias_first, int bias_positions, int buckets, void* workspace, size_t workspace_bytes,
+                              int B, int Hq, int Hkv, int nq, int nk, int d, float scale, int causal, int dtype,
+                              void* stream) {
+  if (!q || !k || !v || !o || !L) return ATTN_E_NULL;
+  if (const int rc = check_sizes(B, Hq, Hkv, nq, nk, d, dtype)) return rc;
+  if (const int rc = check_mask(k_lens, starts, start, scale, causal)) return rc;
+  const int elem = dtype == ATTN_BF16 ? 2 : 4;
+  const Bias x = {bias, bias_rows, bias_first, bias_positions, buckets};
+  if (const int rc = check_bias(x, elem)) return rc;
+  CrossArgs a{};
+  a.qs = attn::strides_of(strides, B, Hq, nq, d);
+  a.ks = attn::strides_of(strides ? strides + 3 : nullptr, B, Hkv, nk, d);
+  a.vs = attn::strides_of(strides ? strides + 6 : nullptr, B, Hkv, nk, d);
+  a.os = attn::strides_of(strides ? strides + 9 : nullptr, B, Hq, nq, d);
+  if (const int rc = check_rows(q, a.qs, B, Hq, nq, elem)) return rc;
+  if (const int rc = check_rows(k, a.ks, B, Hkv, nk, elem)) return rc;
+  if (const int rc = check_rows(v, a.vs, B, Hkv, nk, elem)) return rc;
+  if (const int rc = check_rows(o, a.os, B, Hq, nq, elem)) return rc;
+  if (!aligned(L, 4)) return ATTN_E_ALIGN;
+  if (!attn::writable(a.os, B, Hq, nq, d)) return ATTN_E_ARG;
+  const bool few = few_queries(B, Hq, nq);
+  const FewPlan p = few_plan(B, Hq, Hkv, nq, nk, d, bias != nullptr);
+  const long long rows = (long long)B * Hq * nq;
+  const size_t need = few ? few_bytes(rows, d, p.splits) : 0;
+  if (need > 0) {
+    if (!workspace) return ATTN_E_NULL;
+    if (workspace_bytes < need) return ATTN_E_WORKSPACE;
+    if (!aligned(workspace, 16)) return ATTN_E_ALIGN;
+  }
+  if ((few ? p.groups * p.splits : (long long)B * Hq * div_up(nq, 128)) > kMaxBlocks) return ATTN_E_SHAPE;
+
+  a.q = q; a.k = k; a.v = v; a.o = o; a.lse = L;
+  a.lens = k_lens; a.starts = starts; a.start = start;
+  a.table = bias; a.rows = bias_rows; a.first = bias_first; a.R = bias_positions; a.buckets = buckets;
+  a.B = B; a.Hq = Hq; a.Hkv = Hkv; a.G = Hq / Hkv; a.nq = nq; a.nk = nk;
+  a.causal = causal;
+  a.nrows = rows;
+  set_scale(a, scale, dtype);
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  (void)hipGetLastError();
+  if (few) {
+    a.pack = p.pack; a.ntiles = p.ntiles; a.splits = p.splits; a.per = p.per;
+    a.rz = (long long)Hq * nq; a.rh = nq; a.ri = 1;
+    if (p.splits > 1) {
+      a.part = (float*)workspace;
+      a.part_ml = a.part + (size_t)p.splits * rows * d;
+    }
+    a.nblocks = (int)(p.groups * p.splits);
+    dispatch(dtype, d, bias != nullptr, [&](auto t, auto dd, auto bb) {
+      using T = decltype(t);
+      constexpr int D = decltype(dd)::value;
+      hipLaunchKernelGGL((attn::cross_few_kernel<T, D, decltype(bb)::value>), dim3(a.nblocks), dim3(256), bias_lds(a, 1), st, a);
+      if (a.splits > 1) hipLaunchKernelGGL((attn::cross_merge_kernel<T, D>), dim3((unsigned)div_up(rows, 4)), dim3(256), 0, st, a);
+    });
+  } else {
+    a.ntiles = (int)div_up(nq, 128);
+    set_grid(a, (long long)B * Hq, a.ntiles);
+    dispatch(dtype, d, bias != nullptr, [&](auto t, auto dd, auto bb) {
+      hipLaunchKernelGGL((attn::cross_fwd_kernel<decltype(t), decltype(dd)::value, decltype(bb)::value>), dim3(a.nblocks), dim3(256),
+                         bias_lds(a, 1), st, a);
+    });
+  }
+  return launched();
+}
+
+extern "C" size_t attn_cross_bwd_workspace_bytes(int B, int Hq, int Hkv, int nq, int nk, int d, int dtype, int bias_positions) {
+  if (check_sizes(B, Hq, Hkv, nq, nk, d, dtype) || bias_positions < 0 || bias_positions > attn::kBiasMax) return 0;
+  return bwd_plan(B, Hq, Hkv, nq, nk, d, dtype, bias_positions).bytes;
+}
+
+extern "C" int attn_cross_bwd(const void* q, const void* k, const void* v, const void* o, const float* L, const void* dout,
+                              void* dq, void* dk, void* dv, void* dbias, const long long* strides, const int* k_lens,
+                              const int* starts, int start, const void* bias, const int* bias_rows, int bias_first,
+                              int bias_positions, int buckets, void* workspace, size_t workspace_bytes, int B, int Hq,
+                              int Hkv, int nq, int nk, int d, float scale, int causal, int dtype, void* stream) {
+  if (!q || !k || !v || !o || !L || !dout || !dq || !dk || !dv || !workspace || (dbias && !bias)) return ATTN_E_NULL;
+  if (const int rc = check_sizes(B, Hq, Hkv, nq, nk, d, dtype)) return rc;
+  if (const int rc = check_mask(k_lens, starts, start, scale, causal)) return rc;
+  const int elem = dtype == ATTN_BF16 ? 2 : 4;
+  const Bias x = {bias, bias_rows, bias_first, bias_positions, buckets};
+  if (const int rc = check_bias(x, elem)) return rc;
+  CrossArgs a{};
+  const auto st3 = [&](int i, int H, int n) { return attn::strides_of(strides ? strides + 3 * i : nullptr, B, H, n, d); };
+  a.qs = st3(0, Hq, nq); a.ks = st3(1, Hkv, nk); a.vs = st3(2, Hkv, nk); a.os = st3(3, Hq, nq);
+  a.gs = st3(4, Hq, nq); a.dqs = st3(5, Hq, nq); a.dks = st3(6, Hkv, nk); a.dvs = st3(7, Hkv, nk);
+  const struct { const void* p; const Strides& s; int H, n; } all[8] = {
+      {q, a.qs, Hq, nq}, {k, a.ks, Hkv, nk}, {v, a.vs, Hkv, nk}, {o, a.os, Hq, nq},
+      {dout, a.gs, Hq, nq}, {dq, a.dqs, Hq, nq}, {dk, a.dks, Hkv, nk}, {dv, a.dvs, Hkv, nk}};
+  for (const auto& y : all)
+    if (const int rc = check_rows(y.p, y.s, B, y.H, y.n, elem)) return rc;
+  if (!aligned(L, 4) || !aligned(dbias, elem) || !aligned(workspace, 16)) return ATTN_E_ALIGN;
+  for (int i = 5; i < 8; ++i)
+    if (!attn::writable(all[i].s, B, all[i].H, all[i].n, d)) return ATTN_E_ARG;
+  if (attn::rows_meet(a.dks, Hkv, a.dvs, Hkv, B, nk, d, (reinterpret_cast<intptr_t>(dv) - reinterpret_cast<intptr_t>(dk)) / elem))
+    return ATTN_E_ARG;
+  const BwdPlan p = bwd_plan(B, Hq, Hkv, nq, nk, d, dtype, dbias ? bias_positions : 0);
+  if (workspace_bytes < p.bytes) return ATTN_E_WORKSPACE;
+  const long long qrows = (long long)B * Hq * nq, krows = (long long)B * Hkv * nk;
+  const long long q_blocks = (long long)B * Hq * p.q_tiles * p.q_splits, k_blocks = (long long)B * Hkv * p.k_tiles * p.k_splits;
+  if (q_blocks > kMaxBlocks || k_blocks > kMaxBlocks) return ATTN_E_SHAPE;
+
+  char* const ws = static_cast<char*>(workspace);
+  a.q = q; a.k = k; a.v = v; a.o = const_cast<void*>(o); a.lse = const_cast<float*>(L); a.dout = dout;
+  a.dq = dq; a.dk = dk; a.dv = dv;
+  a.dvec = (float*)(ws + p.rows_at);
+  a.lse2 = a.dvec + qrows;
+  a.lens = k_lens; a.starts = starts; a.start = start;
+  a.table = bias; a.rows = bias_rows; a.first = bias_first; a.R = bias_positions; a.buckets = buckets;
+  a.B = B; a.Hq = Hq; a.Hkv = Hkv; a.G = Hq / Hkv; a.nq = nq; a.nk = nk;
+  a.causal = causal;
+  set_scale(a, scale, dtype);
+  CrossArgs aq = a, ak = a;
+  aq.ntiles = p.q_tiles; aq.splits = p.q_splits; aq.per = p.q_per; aq.nrows = qrows;
+  aq.part = p.q_splits > 1 ? (float*)(ws + p.dq_at) : nullptr;
+  aq.drel = dbias ? (float*)(ws + p.drel_at) : nullptr;
+  set_grid(aq, (long long)B * Hq, p.q_tiles * p.q_splits);
+  ak.ntiles = p.k_tiles; ak.splits = p.k_splits; ak.per = p.k_per; ak.nrows = krows;
+  ak.part = p.k_splits > 1 ? (float*)(ws + p.dk_at) : nullptr;
+  ak.part2 = (float*)(ws + p.dv_at);
+  ak.nblocks = (int)k_blocks;
+
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  (void)hipGetLastError();
+  dispatch(dtype, d, bias != nullptr, [&](auto t, auto dd, auto bb) {
+    using T = decltype(t);
+    constexpr int D = decltype(dd)::value;
+    constexpr bool BIAS = decltype(bb)::value;
+    constexpr int rows_per = 256 / (D / attn::Elem<T>::CH);
+    const auto sum = [&](const float* part, void* out, const Strides& s, long long rows, int H, int n, int parts) {
+      hipLaunchKernelGGL((attn::cross_sum_kernel<T, D>), dim3((unsigned)div_up(rows * (D / 4), 256)), dim3(256), 0, st, part, out, s, rows,
+                         H, n, parts);
+    };
+    hipLaunchKernelGGL((attn::cross_prep_kernel<T, D>), dim3((unsigned)div_up(qrows, rows_per)), dim3(256), 0, st, aq);
+    hipLaunchKernelGGL((attn::cross_dkdv_kernel<T, D, BIAS>), dim3(ak.nblocks), dim3(256), bias_lds(ak, 1), st, ak);
+    hipLaunchKernelGGL((attn::cross_dq_kernel<T, D, BIAS>), dim3(aq.nblocks), dim3(256), bias_lds(aq, aq.drel ? 9 : 1), st, aq);
+    if (p.k_splits > 1) {
+      sum(ak.part, dk, a.dks, krows, Hkv, nk, p.k_splits);
+      sum(ak.part2, dv, a.dvs, krows, Hkv, nk, p.k_splits);
+    }
+    if (p.q_splits > 1) sum(aq.part, dq, a.dqs, qrows, Hq, nq, p.q_splits);
+    if constexpr (BIAS) {
+      if (dbias)
+        hipLaunchKernelGGL((attn::cross_dbias_kernel<T>), dim3(Hq), dim3(1024), (a.R + 1024) * sizeof(double), st, aq, dbias);
+    }
+  });
+  return launched();
+}
+
+// ------------------------------------------------------- shared prefix --
+namespace {
+// The parts of the prefix (its rows are those of the whole batch) and of the sequences' own
+// keys, which run together: each gets workgroups by its share of the blocks.
+struct PrefixPlan {
+  FewPlan prefix, own;
+  int parts;
+};
+PrefixPlan prefix_plan(int B, int Hq, int Hkv, int np, int n, int d) {
+  PrefixPlan p;
+  p.prefix = few_plan(1, Hq, Hkv, B, np, d, false);
+  if (n > 0) p.own = few_plan(B, Hq, Hkv, 1, n, d, false);
+  else p.own = FewPlan{Hq / Hkv, 0, 0, 0, 0};
+  p.parts = p.prefix.splits + p.own.splits;
+  return p;
+}
+int check_prefix_sizes(int B, int Hq, int Hkv, int np, int n, int d, int dtype) {
+  if (n < 0) return ATTN_E_SHAPE;
+  if (dtype == ATTN_F32) return ATTN_E_UNSUPPORTED;
+  if (const int rc = check_sizes(B, Hq, Hkv, 1, std::max(n, 1), d, dtype)) return rc;
+  return check_sizes(1, Hq, Hkv, B, np, d, dtype);
+}
+}  // namespace
+
+extern "C" size_t attn_prefix_decode_workspace_bytes(int B, int Hq, int Hkv, int np, int n, int d) {
+  if (check_prefix_sizes(B, Hq, Hkv, np, n, d, ATTN_BF16)) return 0;
+  return (size_t)prefix_plan(B, Hq, Hkv, np, n, d).parts * B * Hq * (d + 2) * sizeof(float);
+}
+
+extern "C" int attn_prefix_decode(const void* q, const void* k_new, const void* v_new, const void* k_prefix, const void* v_prefix,
+                                  void* k_cache, void* v_cache, const int* cache_lens, void* O, float* L, void* workspace,
+                                  size_t workspace_bytes, int B, int Hq, int Hkv, int np, int n, int n_cap, int d, float scale,
+                                  int dtype, void* stream) {
+  if (!q || !k_prefix || !v_prefix || !k_cache || !v_cache || !O || !workspace || (k_new == nullptr) != (v_new == nullptr))
+    return ATTN_E_NULL;
+  if (const int rc = check_prefix_sizes(B, Hq, Hkv, np, n, d, dtype)) return rc;
+  if (n_cap < 1 || n_cap < n + (k_new ? 1 : 0)) return ATTN_E_SHAPE;
+  if (!std::isfinite(scale)) return ATTN_E_ARG;
+  const void* const rows[] = {q, k_new, v_new, k_prefix, v_prefix, k_cache, v_cache, O, workspace};
+  for (const void* p : rows)
+    if (!aligned(p, 16)) return ATTN_E_ALIGN;
+  if (!aligned(cache_lens, 4) || !aligned(L, 4)) return ATTN_E_ALIGN;
+  const PrefixPlan p = prefix_plan(B, Hq, Hkv, np, n, d);
+  const long long qrows = (long long)B * Hq;
+  const long long blocks = p.prefix.groups * p.prefix.splits + p.own.groups * p.own.splits;
+  if (blocks > kMaxBlocks) return ATTN_E_SHAPE;
+  if (workspace_bytes < (size_t)p.parts * qrows * (d + 2) * sizeof(float)) return ATTN_E_WORKSPACE;
+
+  attn::PrefixArgs a{};
+  CrossArgs c{};
+  c.q = q; c.o = O; c.lse = L;
+  c.part = (float*)workspace;
+  c.part_ml = c.part + (size_t)p.parts * qrows * d;
+  c.nrows = qrows;
+  c.Hq = Hq; c.Hkv = Hkv; c.G = Hq / Hkv; c.pack = c.G;
+  c.rh = 1;
+  set_scale(c, scale, dtype);
+  CrossArgs& x = a.part[0];
+  x = c;
+  x.k = k_prefix; x.v = v_prefix;
+  x.qs = {0, d, (long long)Hq * d};
+  x.ks = x.vs = {0, (long long)np * d, d};
+  x.B = 1; x.nq = B; x.nk = np;
+  x.ri = Hq;
+  x.ntiles = p.prefix.ntiles; x.splits = p.prefix.splits; x.per = p.prefix.per;
+  x.nblocks = (int)(p.prefix.groups * p.prefix.splits);
+  CrossArgs& y = a.part[1];
+  y = c;
+  y.k = k_cache; y.v = v_cache;
+  y.qs = {(long long)Hq * d, d, 0};
+  y.ks = y.vs = {(long long)Hkv * n_cap * d, (long long)n_cap * d, d};
+  y.B = B; y.nq = 1; y.nk = n;
+  y.lens = cache_lens;
+  y.rz = Hq;
+  y.ntiles = p.own.ntiles; y.splits = std::max(p.own.splits, 1); y.per = p.own.per;
+  y.nblocks = (int)(p.own.groups * p.own.splits);
+  y.part0 = p.prefix.splits;
+  a.k_new = k_new; a.v_new = v_new; a.k_cache = k_cache; a.v_cache = v_cache;
+  a.n_cap = n_cap;
+  a.parts = p.parts;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  (void)hipGetLastError();
+  const unsigned merge = (unsigned)div_up(qrows, 4);
+  const auto go = [&](auto dd) {
+    constexpr int D = decltype(dd)::value;
+    hipLaunchKernelGGL((attn::prefix_few_kernel<D>), dim3((unsigned)blocks), dim3(256), 0, st, a);
+    hipLaunchKernelGGL((attn::prefix_merge_kernel<D>), dim3(merge), dim3(256), 0, st, a);
+  };
+  if (d == 32) go(std::integral_constant<int, 32>{});
+  else if (d == 64) go(std::integral_constant<int, 64>{});
+  else go(std::integral_constant<int, 128>{});
+  return launched();
+}

@@ -1,0 +1,1167 @@
+// Attention of nq queries to nk keys in strided layouts: grouped heads, a length
+// and a position for each sequence, a bias by relative position, and one decode
+// step behind a prefix that a batch shares.
+//
+//   cross_fwd_kernel     O, L; a workgroup owns 128 queries of a head
+//   cross_few_kernel     O, L where there are few queries: a workgroup owns 32
+//                        rows (query, head of the group) and one part of the keys
+//   cross_merge_kernel   joins the parts by their log-sum-exp
+//   cross_prep_kernel    the backward's row vectors: -D and L in base 2
+//   cross_dkdv_kernel    dK, dV; a workgroup owns 128 keys of a cache head and
+//                        goes over the queries of all heads of its group
+//   cross_dq_kernel      dQ and the bias gradient by relative position
+//   cross_sum_kernel     adds the parts of a gradient whose sum was split
+//   cross_dbias_kernel   the bias gradient by bucket
+//
+// With r = j - (start + i), the position of key j relative to query i:
+//   x_ij = scale q_i . k_j + bias(r), -inf where j >= len or (causal) r > 0
+//   L_i = ln sum_j exp(x_ij), P = exp(x - L), O = P V
+//   dV = P^T dO, dP = dO V^T, D_i = sum_c dO_ic O_ic, dS = P (dP - D)
+//   dQ = scale dS K, dK = scale dS^T Q, d bias(r) = the sum of dS_ij with that r
+// dK and dV of a cache head are the sums over its group of query heads, formed in
+// one workgroup's registers, or over parts in a fixed order: no result depends
+// on the order in which workgroups run. A row that sees no key has O = 0,
+// L = -inf and no gradient. Keys from len on are not read.
+#pragma once
+
+#include "kernels.hpp"
+#include "split.hpp"
+#include "strides.hpp"
+
+namespace attn {
+
+// A bias by relative position has at most this many positions of its own; nearer
+// and farther keys take the first and the last one's. The vectors in LDS run kBiasPad
+// further on both sides, so that a tile that reaches beyond needs no clamping: a
+// tile of 64 keys and 32 queries holds 95 relative positions.
+constexpr int kBiasMax = 2048, kBiasPad = 96;
+
+struct CrossArgs {
+  const void* q;
+  const void* k;
+  const void* v;
+  void* o;
+  float* lse;          // [B, Hq, nq]
+  const void* dout;
+  float* dvec;         // -D rows [B, Hq, nq]
+  float* lse2;         // L in base 2, +inf where the row sees no key
+  void* dq;
+  void* dk;
+  void* dv;
+  Strides qs, ks, vs, os, gs, dqs, dks, dvs;
+  const int* lens;     // [B] or null: nk
+  const int* starts;   // [B] or null: start
+  const void* table;   // bias [buckets, Hq]
+  const int* rows;     // [R]: the bucket of relative position first + t
+  float* part;         // parts of O (or of a gradient), then of (max, sum)
+  float* part_ml;
+  float* part2;        // parts of dV
+  float* drel;         // bias gradient by relative position, a row [R] for each dQ workgroup
+  long long rz, rh, ri;   // row of the parts: sequence, head, query
+  long long nrows;        // rows of a part
+  int start, first, R, buckets;
+  int B, Hq, Hkv, G, nq, nk;
+  int pack;            // query heads in a row tile of cross_few_kernel (1 or G)
+  int ntiles, nblocks, hgroup;
+  int splits, per;     // parts, and the steps of a part
+  int part0;           // the first part's number
+  float sl2;           // |scale| log2 e
+  float scale;
+  uint32_t qflip;      // sign mask of a negative scale
+  int causal;
+};
+
+__device__ __forceinline__ int seq_len(const CrossArgs& a, int b) {
+  return a.lens ? min(max(a.lens[b], 0), a.nk) : a.nk;
+}
+__device__ __forceinline__ int seq_start(const CrossArgs& a, int b) {
+  return a.starts ? min(max(a.starts[b], -(1 << 30)), 1 << 30) : a.start;
+}
+
+// ------------------------------------------------------------------ tiles --
+// `valid` rows of a strided matrix from x on, as a buffer: what lies behind them
+// is out of its range and reads as zeros.
+template <int D, typename T> __device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_rsrc(const T* x, long long ld, int valid) {
+  const int bytes = valid > 0 ? ((valid - 1) * (int)ld + D) * (int)sizeof(T) : 0;
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(x), (short)0, bytes, 0x00020000);
+}
+
+// A ROWS x D tile of a strided matrix in LDS, copied by a workgroup of four waves.
+// bf16: LDS DMA into the layout of RowRead and TransRead, two stages. float32:
+// through registers, one stage, rows padded to D + 4 (16-byte row reads of 16
+// rows fall on distinct banks). Rows from `valid` on are zeros.
+template <typename T, int ROWS, int D> struct CrossTile;
+template <int ROWS, int D> struct CrossTile<bf16, ROWS, D> {
+  static constexpr int ELEMS = ROWS * D, C = D / 8, NI = ROWS * D * 2 / 4096;
+  static constexpr bool TWO = true;
+  static_assert(NI >= 1, "a wave copies 1 KB at least");
+  unsigned off[NI];
+  int w;
+  __device__ __forceinline__ CrossTile(int w_, int lane, long long ld) : w(w_) {
+#pragma unroll
+    for (int j = 0; j < NI; ++j) {
+      const int L = 64 * (w * NI + j) + lane, s = L / C, slot = L % C;
+      off[j] = 2u * ((unsigned)((s & ~31) | perm32(s & 31)) * (unsigned)ld + 8u * (unsigned)(slot ^ swz<D>(s)));
+    }
+  }
+  __device__ __forceinline__ void issue(bf16* lds, const bf16* g, long long ld, int valid) {
+    const auto rs = rows_rsrc<D>(g, ld, min(valid, ROWS));
+#pragma unroll
+    for (int j = 0; j < NI; ++j) dma16(rs, off[j], (ATTN_LDS void*)(lds + 512 * (w * NI + j)));
+  }
+  __device__ __forceinline__ void commit(bf16*) const {}
+};
+template <int ROWS, int D> struct CrossTile<float, ROWS, D> {
+  static constexpr int LD = D + 4, ELEMS = ROWS * LD, C = D / 4, NI = ROWS * C / 256;
+  static constexpr bool TWO = false;
+  static_assert(NI >= 1 && NI * 256 == ROWS * C, "whole chunks for every thread");
+  unsigned off[NI];
+  int at[NI];
+  u32x4 r[NI];
+  __device__ __forceinline__ CrossTile(int w, int lane, long long ld) {
+#pragma unroll
+    for (int j = 0; j < NI; ++j) {
+      const int i = 64 * w + lane + 256 * j, row = i / C, ch = i % C;
+      off[j] = 4u * ((unsigned)row * (unsigned)ld + 4u * (unsigned)ch);
+      at[j] = srow(row) * LD + 4 * ch;
+    }
+  }
+  __device__ __forceinline__ void issue(float*, const float* g, long long ld, int valid) {
+    const auto rs = rows_rsrc<D>(g, ld, min(valid, ROWS));
+#pragma unroll
+    for (int j = 0; j < NI; ++j) r[j] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rs, off[j], 0, 0));
+  }
+  __device__ __forceinline__ void commit(float* lds) const {
+#pragma unroll
+    for (int j = 0; j < NI; ++j) *(u32x4*)(lds + at[j]) = r[j];
+  }
+};
+
+// acc += (rows of 32-row block rb of a tile) x (a row per lane), over d
+template <int D> __device__ __forceinline__ void mma_tile_rows(f32x16& acc, const bf16* tile, int rb, const RowRegs<bf16, D>& x, int h, int c) {
+#pragma unroll
+  for (int t = 0; t < D / 16; ++t) mma(acc, RowRead<bf16, D>::get(tile, rb, t, h, c), __builtin_bit_cast(bf16x8, x.r[t]));
+}
+template <int D> __device__ __forceinline__ void mma_tile_rows(f32x16& acc, const float* tile, int rb, const RowRegs<float, D>& x, int h, int c) {
+#pragma unroll
+  for (int u = 0; u < D / 8; ++u) {
+    const f32x4 y = *(const f32x4*)(tile + (32 * rb + c) * (D + 4) + 8 * u + 4 * h);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) mma(acc, y[e], __uint_as_float(x.r[u][e]));
+  }
+}
+// acc += (columns of block rb's 32 rows) x b, over the rows
+template <int D> __device__ __forceinline__ void mma_tile_cols(f32x16 (&acc)[D / 32], const bf16* tile, int rb, const f32x16& b, int h, int c) {
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    const bf16x8 f = FragFromAcc<bf16>::get(b, t);
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db) mma(acc[db], TransRead<bf16, D>::get(tile, rb, db, t, h, c), f);
+  }
+}
+template <int D> __device__ __forceinline__ void mma_tile_cols(f32x16 (&acc)[D / 32], const float* tile, int rb, const f32x16& b, int h, int c) {
+#pragma unroll
+  for (int t = 0; t < 16; ++t)
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db) mma(acc[db], tile[(32 * rb + perm32_inv(16 * h + t)) * (D + 4) + 32 * db + c], b[t]);
+}
+
+// A lane's row, or zeros where it has none
+template <typename T, int D> __device__ __forceinline__ void load_row(RowRegs<T, D>& x, const T* row, bool there, int h, uint32_t flip = 0u) {
+  if (there) x.load(row, h, flip);
+  else x.zero();
+}
+
+// A transposed accumulator's row (lane (h, c): columns 32 db + 8 q4 + 4 h + [0, 4)), times f
+template <typename T, int D> __device__ __forceinline__ void store_row(T* row, const f32x16 (&acc)[D / 32], float f, int h) {
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+    for (int q4 = 0; q4 < 4; ++q4)
+      Quad<T>::store(row + 32 * db + 8 * q4 + 4 * h, acc[db][4 * q4] * f, acc[db][4 * q4 + 1] * f, acc[db][4 * q4 + 2] * f,
+                     acc[db][4 * q4 + 3] * f);
+}
+
+// ------------------------------------------------------------------- bias --
+template <typename T> __device__ __forceinline__ float as_float(T x) { return (float)x; }
+
+// Head hq's bias by relative position, times log2 e, to LDS: entry kBiasPad + t is
+// that of first + t. A bucket that the table does not have counts as no bias. An entry
+// below -2^16, a type's lowest value among them, masks as -inf does: a row of such
+// scores alone has an L of which float32 holds no more than 1/128, too coarse for the
+// backward's exp(x - L), and next to any other score its P is 0 all the same.
+template <typename T> __device__ __forceinline__ void bias_fill(float* bv, const CrossArgs& a, int hq, int tid) {
+  for (int t = tid; t < a.R + 2 * kBiasPad; t += 256) {
+    const int k = a.rows[min(max(t - kBiasPad, 0), a.R - 1)];
+    const float x = (unsigned)k < (unsigned)a.buckets ? as_float(((const T*)a.table)[(long long)k * a.Hq + hq]) : 0.f;
+    bv[t] = x < -65536.f ? -INFINITY : x * kLog2e;
+  }
+}
+// Where the relative positions [lo, hi] of a tile lie: -1 all before the first
+// position's successor, 1 all from the last one on, 0 elsewhere.
+__device__ __forceinline__ int bias_side(const CrossArgs& a, int lo, int hi) {
+  return hi <= a.first ? -1 : lo >= a.first + a.R - 1 ? 1 : 0;
+}
+
+// ======================================================================
+// Forward. As fwd_kernel: a workgroup owns 128 queries of a head, 32 per wave; K and
+// V tiles of 64 keys in LDS; S^T = K Q^T, online softmax by column, O^T += V^T P^T.
+// ======================================================================
+template <typename T, int D, bool BIAS>
+__global__ void __launch_bounds__(256, sizeof(T) == 4 && D == 128 ? 1 : 2) cross_fwd_kernel(const CrossArgs a) {
+  constexpr int BQ = 128, BKV = 64, NKB = 2, NDB = D / 32;
+  using TL = CrossTile<T, BKV, D>;
+  // two stages in distinct LDS objects (the loop is unrolled by two), so that reads
+  // of one never wait for the copy into the other
+  __shared__ __attribute__((aligned(16))) T stA[2][TL::ELEMS];
+  __shared__ __attribute__((aligned(16))) T stB[2][TL::TWO ? TL::ELEMS : 8];
+  extern __shared__ __attribute__((aligned(16))) float bv[];
+
+  const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, c = lane & 31;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  int head, qt;
+  block_map(blockIdx.x, a.nblocks, a.ntiles, a.hgroup, a.causal, head, qt);
+  const int b = head / a.Hq, hq = head - b * a.Hq, hk = hq / a.G;
+  const int n = seq_len(a, b), start = seq_start(a, b);
+  const int q0 = qt * BQ, qw0 = q0 + 32 * w, qi = qw0 + c;
+  const T* Kg = (const T*)a.k + b * a.ks.b + hk * a.ks.h;
+  const T* Vg = (const T*)a.v + b * a.vs.b + hk * a.vs.h;
+
+  const int kv_end = a.causal ? max(0, min(n, start + min(q0 + BQ, a.nq))) : n;
+  const int nt = (kv_end + BKV - 1) / BKV;
+
+  TL kld(w, lane, a.ks.t), vld(w, lane, a.vs.t);
+  if (nt > 0) {
+    kld.issue(stA[0], Kg, a.ks.t, n);
+    vld.issue(stA[1], Vg, a.vs.t, n);
+  }
+  RowRegs<T, D> q;
+  load_row<T, D>(q, (const T*)a.q + b * a.qs.b + hq * a.qs.h + qi * a.qs.t, qi < a.nq, h, a.qflip);
+  if constexpr (BIAS) bias_fill<T>(bv, a, hq, tid);
+  kld.commit(stA[0]);
+  vld.commit(stA[1]);
+  __syncthreads();
+
+  f32x16 oacc[NDB];
+#pragma unroll
+  for (int db = 0; db < NDB; ++db) oacc[db] = zero16();
+  float m_use = -INFINITY, lsum = 0.f;
+  const float sl2 = a.sl2;
+
+  auto step = [&](int it, T* kc, T* vc, T* kn, T* vn) __attribute__((always_inline)) {
+    const int kv0 = it * BKV;
+    if (it + 1 < nt) {
+      kld.issue(kn, Kg + (kv0 + BKV) * a.ks.t, a.ks.t, n - kv0 - BKV);
+      vld.issue(vn, Vg + (kv0 + BKV) * a.vs.t, a.vs.t, n - kv0 - BKV);
+    }
+    if (!a.causal || kv0 <= start + qw0 + 31) {
+      f32x16 s[NKB];
+#pragma unroll
+      for (int kb = 0; kb < NKB; ++kb) {
+        s[kb] = zero16();
+        mma_tile_rows<D>(s[kb], kc, kb, q, h, c);
+      }
+      // lane (h, c): s[kb][j] is the score of key kv0 + 32 kb + 16 h + j and query qi
+      if constexpr (BIAS) {
+        const int side = bias_side(a, kv0 - (start + qw0 + 31), kv0 + BKV - 1 - (start + qw0));
+        if (side != 0) {
+          const float u = bv[side < 0 ? 0 : a.R + 2 * kBiasPad - 1];
+#pragma unroll
+          for (int kb = 0; kb < NKB; ++kb)
+#pragma unroll
+            for (int j = 0; j < 16; ++j) s[kb][j] = fmaf(s[kb][j], sl2, u);
+        } else {
+          const float* p = bv + (kBiasPad - a.first + kv0 + 16 * h - start - qi);
+#pragma unroll
+          for (int kb = 0; kb < NKB; ++kb)
+#pragma unroll
+            for (int j = 0; j < 16; ++j) s[kb][j] = fmaf(s[kb][j], sl2, p[32 * kb + j]);
+        }
+      }
+      if (kv0 + BKV > n || (a.causal && kv0 + BKV - 1 > start + qw0)) {
+        const int last = a.causal ? min(start + qi, n - 1) : n - 1;
+#pragma unroll
+        for (int kb = 0; kb < NKB; ++kb) {
+          const int lim = last - (kv0 + 32 * kb + 16 * h);
+#pragma unroll
+          for (int j = 0; j < 16; ++j) s[kb][j] = j > lim ? -INFINITY : s[kb][j];
+        }
+      }
+      float mx = -INFINITY;
+#pragma unroll
+      for (int kb = 0; kb < NKB; ++kb)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) mx = fmaxf(mx, s[kb][j]);
+      const float mt = halves_max(mx) * (BIAS ? 1.f : sl2);
+      const bool resc = mt > m_use + kRescaleThresh;
+      if (__builtin_amdgcn_ballot_w64(resc)) {
+        const float alpha = resc ? exp2_fast(m_use - mt) : 1.f;
+        if (resc) m_use = mt;
+        lsum *= alpha;
+#pragma unroll
+        for (int db = 0; db < NDB; ++db)
+#pragma unroll
+          for (int j = 0; j < 16; ++j) oacc[db][j] *= alpha;
+      }
+      const float mb = m_use == -INFINITY ? 0.f : -m_use;
+      float rs = 0.f;
+#pragma unroll
+      for (int kb = 0; kb < NKB; ++kb)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+          const float p = exp2_fast(BIAS ? s[kb][j] + mb : fmaf(s[kb][j], sl2, mb));
+          rs += p;
+          s[kb][j] = p;
+        }
+      lsum += rs;
+      __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+      for (int kb = 0; kb < NKB; ++kb) mma_tile_cols<D>(oacc, vc, kb, s[kb], h, c);
+      __builtin_amdgcn_s_setprio(0);
+    }
+    if constexpr (!TL::TWO) __syncthreads();
+    if (it + 1 < nt) {
+      kld.commit(kn);
+      vld.commit(vn);
+    }
+    __syncthreads();
+  };
+  for (int it = 0; it < nt; it += 2) {
+    step(it, stA[0], stA[1], TL::TWO ? stB[0] : stA[0], TL::TWO ? stB[1] : stA[1]);
+    if (it + 1 < nt) step(it + 1, TL::TWO ? stB[0] : stA[0], TL::TWO ? stB[1] : stA[1], stA[0], stA[1]);
+  }
+
+  const float l = halves_sum(lsum);
+  if (qi < a.nq) {
+    store_row<T, D>((T*)a.o + b * a.os.b + hq * a.os.h + qi * a.os.t, oacc, l > 0.f ? 1.f / l : l == 0.f ? 0.f : l, h);
+    if (h == 0) a.lse[(long long)head * a.nq + qi] = (m_use + log2f(l)) * kLn2;
+  }
+}
+
+// ======================================================================
+// Few queries: a workgroup owns 32 rows and one part of the keys. Row r of a cache
+// head is head r % pack of its group (all of it where there is no bias) and query
+// r / pack, so that a group's heads share every key that is read. The four waves
+// take the part's 32-key blocks in turn, each with its own softmax; their results
+// are merged in LDS, and where the keys are in several parts, the parts by
+// cross_merge_kernel. Decode steps are bound by the bytes of K and V, small grids by the
+// length of a wave's chain of blocks.
+// bf16: P multiplies V in two parts (the float cut to 16 bits, and the rest
+// rounded): one rounded part leaves O off by 1.5 times its own last rounding.
+// ======================================================================
+// 32 rows of a strided bf16 matrix into a tile of one wave
+template <int D> struct CrossWaveTile {
+  static constexpr int C = D / 8, NI = D / 16, ELEMS = 32 * D;
+  unsigned off[NI];
+  __device__ __forceinline__ CrossWaveTile(int lane, long long ld) {
+#pragma unroll
+    for (int j = 0; j < NI; ++j) {
+      const int L = 64 * j + lane, s = L / C, slot = L % C;
+      off[j] = 2u * ((unsigned)perm32(s) * (unsigned)ld + 8u * (unsigned)(slot ^ swz<D>(s)));
+    }
+  }
+  __device__ __forceinline__ void issue(bf16* lds, const bf16* g, long long ld, int valid) const {
+    const auto rs = rows_rsrc<D>(g, ld, min(valid, 32));
+#pragma unroll
+    for (int j = 0; j < NI; ++j) dma16(rs, off[j], (ATTN_LDS void*)(lds + 512 * j));
+  }
+};
+// float32 columns of 32 rows, as ColRegs, of a strided matrix
+template <int D> struct CrossCols {
+  static constexpr int NDB = D / 32, R = D == 128 ? 4 : 8;
+  float v[R][NDB];
+  __amdgpu_buffer_rsrc_t rs;
+  unsigned off, ld4;
+  __device__ __forceinline__ void get(int t) {
+#pragma unroll
+    for (int db = 0; db < NDB; ++db)
+      v[t % R][db] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rs, off + t * ld4 + 128u * db, 0, 0));
+  }
+  __device__ __forceinline__ void load(const float* g, long long ld, int valid, int h, int c) {
+    rs = rows_rsrc<D>(g, ld, min(valid, 32));
+    ld4 = 4u * (unsigned)ld;
+    off = 16u * h * ld4 + 4u * c;
+#pragma unroll
+    for (int t = 0; t < R; ++t) get(t);
+  }
+};
+template <int D> __device__ __forceinline__ void mma_cross_cols(f32x16 (&acc)[D / 32], CrossCols<D>& x, const f32x16& b) {
+#pragma unroll
+  for (int t = 0; t < 16; ++t) {
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db) mma(acc[db], x.v[t % CrossCols<D>::R][db], b[t]);
+    if (t + CrossCols<D>::R < 16) x.get(t + CrossCols<D>::R);
+  }
+}
+// acc += columns x p, p in two bf16 parts
+template <int D> __device__ __forceinline__ void mma_cols2(f32x16 (&acc)[D / 32], const bf16* tile, const f32x16& p, int h, int c) {
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    u32x4 first;
+    bf16x8 rest;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float x = p[8 * t + 2 * i], y = p[8 * t + 2 * i + 1];
+      first[i] = __builtin_amdgcn_perm(__float_as_uint(y), __float_as_uint(x), 0x07060302u);
+      rest[2 * i] = (bf16)(x - __uint_as_float(__float_as_uint(x) & 0xffff0000u));
+      rest[2 * i + 1] = (bf16)(y - __uint_as_float(__float_as_uint(y) & 0xffff0000u));
+    }
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db) {
+      const bf16x8 v = TransRead<bf16, D, 32>::get(tile, 0, db, t, h, c);
+      mma(acc[db], v, __builtin_bit_cast(bf16x8, first));
+      mma(acc[db], v, rest);
+    }
+  }
+}
+
+template <typename T, int D> struct FewLds {
+  // bf16: K and V tiles of the four waves; both: half of the merge buffer
+  static constexpr int FLOATS = sizeof(T) == 2 ? 4 * 2 * 32 * D / 2 : WaveMerge<D>::FLOATS;
+};
+
+template <typename T, int D, bool BIAS>
+__device__ __forceinline__ void cross_few(const CrossArgs& a, int bid, float* stA, float* stB, float (&ml)[2][4][32], float* bv) {
+  constexpr int NDB = D / 32;
+  constexpr bool B16 = sizeof(T) == 2;
+  using MG = WaveMerge<D>;
+  const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, c = lane & 31;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int Hp = a.Hq / a.pack;
+  int head, tile;   // of B x Hp, row tile x part
+  block_map(bid, a.nblocks, a.ntiles * a.splits, 0, false, head, tile);
+  const int rt = tile / a.splits, part = tile - rt * a.splits;
+  const int b = head / Hp, hp = head - b * Hp, hk = hp * a.pack / a.G;
+  const int n = seq_len(a, b), start = seq_start(a, b);
+  const int r0 = 32 * rt, nr = a.nq * a.pack;
+  const int i0 = r0 / a.pack, i1 = min(r0 + 31, nr - 1) / a.pack;   // the tile's first and last query
+  const int r = r0 + c, qi = min(r, nr - 1) / a.pack, hq = hp * a.pack + min(r, nr - 1) % a.pack;
+  const T* Kg = (const T*)a.k + b * a.ks.b + hk * a.ks.h;
+  const T* Vg = (const T*)a.v + b * a.vs.b + hk * a.vs.h;
+  const int kv_end = a.causal ? max(0, min(n, start + i1 + 1)) : n;
+  const int first = part * a.per, nb = min((kv_end + 31) / 32, first + a.per);   // 32-key blocks
+  const float sl2 = a.sl2;
+
+  f32x16 oacc[NDB];
+#pragma unroll
+  for (int db = 0; db < NDB; ++db) oacc[db] = zero16();
+  float m_use = -INFINITY, lsum = 0.f;
+
+  auto softmax = [&](int kb, f32x16& s) __attribute__((always_inline)) {
+    const int kv0 = 32 * kb;
+    if constexpr (BIAS) {
+      const int side = bias_side(a, kv0 - (start + i1), kv0 + 31 - (start + i0));
+      if (side != 0) {
+        const float u = bv[side < 0 ? 0 : a.R + 2 * kBiasPad - 1];
+#pragma unroll
+        for (int j = 0; j < 16; ++j) s[j] = fmaf(s[j], sl2, u);
+      } else {
+        const float* p = bv + (kBiasPad - a.first + kv0 + 16 * h - start - qi);
+#pragma unroll
+        for (int j = 0; j < 16; ++j) s[j] = fmaf(s[j], sl2, p[j]);
+      }
+    }
+    if (kv0 + 32 > n || (a.causal && kv0 + 31 > start + i0)) {
+      const int lim = (a.causal ? min(start + qi, n - 1) : n - 1) - (kv0 + 16 * h);
+#pragma unroll
+      for (int j = 0; j < 16; ++j) s[j] = j > lim ? -INFINITY : s[j];
+    }
+    float mx = -INFINITY;
+#pragma unroll
+    for (int j = 0; j < 16; ++j) mx = fmaxf(mx, s[j]);
+    const float mt = halves_max(mx) * (BIAS ? 1.f : sl2);
+    const bool resc = mt > m_use + kRescaleThresh;
+    if (__builtin_amdgcn_ballot_w64(resc)) {
+      const float alpha = resc ? exp2_fast(m_use - mt) : 1.f;
+      if (resc) m_use = mt;
+      lsum *= alpha;
+#pragma unroll
+      for (int db = 0; db < NDB; ++db)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) oacc[db][j] *= alpha;
+    }
+    const float mb = m_use == -INFINITY ? 0.f : -m_use;
+    float rs = 0.f;
+#pragma unroll
+    for (int j = 0; j < 16; ++j) {
+      s[j] = exp2_fast(BIAS ? s[j] + mb : fmaf(s[j], sl2, mb));
+      rs += s[j];
+    }
+    lsum += rs;
+  };
+
+  const T* Qg = (const T*)a.q + b * a.qs.b + hq * a.qs.h + qi * a.qs.t;
+  RowRegs<T, D> q;
+  const int b0 = first + w;   // this wave's blocks: b0, b0 + 4, ...
+  if constexpr (B16) {
+    using WT = CrossWaveTile<D>;
+    const WT kt(lane, a.ks.t), vt(lane, a.vs.t);
+    bf16* const tA = (bf16*)stA + w * 2 * WT::ELEMS;
+    bf16* const tB = (bf16*)stB + w * 2 * WT::ELEMS;
+    load_row<T, D>(q, Qg, r < nr, h, a.qflip);
+    auto issue = [&](int kb, bf16* t) __attribute__((always_inline)) {
+      kt.issue(t, Kg + 32LL * kb * a.ks.t, a.ks.t, n - 32 * kb);
+      vt.issue(t + WT::ELEMS, Vg + 32LL * kb * a.vs.t, a.vs.t, n - 32 * kb);
+    };
+    if (b0 < nb) issue(b0, tA);
+    if constexpr (BIAS) {
+      bias_fill<T>(bv, a, hq, tid);
+      __syncthreads();
+    }
+    auto step = [&](int kb, bf16* tc, bf16* tn) __attribute__((always_inline)) {
+      if (kb + 4 < nb) {
+        issue(kb + 4, tn);
+        wait_vm<2 * WT::NI>();   // this block's tiles are there
+      } else {
+        wait_vm<0>();
+      }
+      f32x16 s = zero16();
+      mma_tile_rows<D>(s, tc, 0, q, h, c);
+      softmax(kb, s);
+      mma_cols2<D>(oacc, tc + WT::ELEMS, s, h, c);
+      __builtin_amdgcn_s_waitcnt(0xC07F);   // reads done (lgkmcnt 0) before the stage is refilled
+    };
+    for (int kb = b0; kb < nb; kb += 8) {
+      step(kb, tA, tB);
+      if (kb + 4 < nb) step(kb + 4, tB, tA);
+    }
+  } else {
+    RowRegs<T, D> k;
+    CrossCols<D> v;
+    auto kload = [&](int kb) __attribute__((always_inline)) {
+      const int j = 32 * kb + perm32(c);
+      load_row<T, D>(k, Kg + j * a.ks.t, j < n, h);
+    };
+    auto vload = [&](int kb) __attribute__((always_inline)) { v.load(Vg + 32LL * kb * a.vs.t, a.vs.t, n - 32 * kb, h, c); };
+    if (b0 < nb) {
+      kload(b0);
+      vload(b0);
+    }
+    load_row<T, D>(q, Qg, r < nr, h, a.qflip);
+    if constexpr (BIAS) {
+      bias_fill<T>(bv, a, hq, tid);
+      __syncthreads();
+    }
+    for (int kb = b0; kb < nb; kb += 4) {
+      f32x16 s = zero16();
+      mma_rows<D>(s, k, q);
+      if (kb + 4 < nb) kload(kb + 4);
+      softmax(kb, s);
+      mma_cross_cols<D>(oacc, v, s);
+      if (kb + 4 < nb) vload(kb + 4);
+    }
+  }
+
+  // ---- merge: thread -> row qq and the 4-column chunks dp + 8 e
+  const float lw = halves_sum(lsum);
+  __syncthreads();
+  if (h == 0) {
+    ml[0][w][c] = m_use;
+    ml[1][w][c] = lw;
+  }
+  MG::put(stA, stB, w, h, c, oacc);
+  __syncthreads();
+  const int qq = tid >> 3, dp = tid & 7, rr = r0 + qq;
+  if (rr >= nr) return;
+  float M = -INFINITY, f[4], l = 0.f;
+#pragma unroll
+  for (int v = 0; v < 4; ++v) M = fmaxf(M, ml[0][v][qq]);
+#pragma unroll
+  for (int v = 0; v < 4; ++v) {
+    f[v] = M == -INFINITY ? 0.f : exp2_fast(ml[0][v][qq] - M);
+    l += f[v] * ml[1][v][qq];
+  }
+  const int i = rr / a.pack, hr = hp * a.pack + rr % a.pack;
+  if (a.part) {
+    const long long row = b * a.rz + hr * a.rh + i * a.ri, at = (long long)(a.part0 + part) * a.nrows + row;
+#pragma unroll
+    for (int e = 0; e < NDB; ++e) *(f32x4*)(a.part + at * D + 4 * (dp + 8 * e)) = MG::get(stA, stB, qq, dp + 8 * e, f);
+    if (dp == 0) *(f32x2*)(a.part_ml + 2 * at) = (f32x2){M, l};
+  } else {
+    const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;
+#pragma unroll
+    for (int v = 0; v < 4; ++v) f[v] *= inv;
+    T* o = (T*)a.o + b * a.os.b + hr * a.os.h + i * a.os.t;
+#pragma unroll
+    for (int e = 0; e < NDB; ++e) {
+      const f32x4 x = MG::get(stA, stB, qq, dp + 8 * e, f);
+      Quad<T>::store(o + 4 * (dp + 8 * e), x[0], x[1], x[2], x[3]);
+    }
+    if (dp == 0) a.lse[((long long)b * a.Hq + hr) * a.nq + i] = (M + log2f(l)) * kLn2;
+  }
+}
+
+template <typename T, int D, bool BIAS>
+__global__ void __launch_bounds__(256, D == 128 ? 1 : 2) cross_few_kernel(const CrossArgs a) {
+  __shared__ __attribute__((aligned(16))) float stA[FewLds<T, D>::FLOATS];
+  __shared__ __attribute__((aligned(16))) float stB[FewLds<T, D>::FLOATS];
+  __shared__ float ml[2][4][32];
+  extern __shared__ __attribute__((aligned(16))) float bv[];
+  cross_few<T, D, BIAS>(a, blockIdx.x, stA, stB, ml, bv);
+}
+
+// The parts of a row, joined: a wave for a row, D / 4 lanes across it and the other
+// lanes over the parts. Returns the lane's 4 columns (all lanes of a column
+// group alike), and the row's maximum and sum.
+template <int D> __device__ __forceinline__ f32x4 join_parts(const float* part, const float* ml, long long nrows, long long row, int parts, int lane,
+                                                            float& M, float& l) {
+  constexpr int CG = D / 4, SL = 64 / CG;
+  const int cg = lane % CG, sl = lane / CG;
+  M = -INFINITY;
+  for (int s = sl; s < parts; s += SL) M = fmaxf(M, ml[2 * (s * nrows + row)]);
+#pragma unroll
+  for (int x = CG; x < 64; x <<= 1) M = fmaxf(M, __shfl_xor(M, x));
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  l = 0.f;
+  for (int s = sl; s < parts; s += SL) {
+    const f32x2 y = *(const f32x2*)(ml + 2 * (s * nrows + row));
+    const float f = y[0] == -INFINITY ? 0.f : exp2_fast(y[0] - M);
+    const f32x4 x = *(const f32x4*)(part + (s * nrows + row) * D + 4 * cg);
+    l = fmaf(f, y[1], l);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] = fmaf(f, x[e], o[e]);
+  }
+#pragma unroll
+  for (int x = CG; x < 64; x <<= 1) {
+    l += __shfl_xor(l, x);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], x);
+  }
+  return o;
+}
+
+template <typename T, int D> __global__ void __launch_bounds__(256) cross_merge_kernel(const CrossArgs a) {
+  const int lane = threadIdx.x & 63;
+  const long long row = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);   // of [B, Hq, nq]
+  if (row >= a.nrows) return;
+  float M, l;
+  const f32x4 o = join_parts<D>(a.part, a.part_ml, a.nrows, row, a.splits, lane, M, l);
+  const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;
+  const long long head = row / a.nq;
+  const int b = (int)(head / a.Hq), hq = (int)(head % a.Hq), i = (int)(row % a.nq);
+  if (lane < D / 4) Quad<T>::store((T*)a.o + b * a.os.b + hq * a.os.h + i * a.os.t + 4 * lane, o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
+  if (lane == 0) a.lse[row] = (M + log2f(l)) * kLn2;
+}
+
+// ======================================================================
+// A decode step behind a shared prefix: the prefix's keys, seen by the rows of all
+// sequences together (part[0]: one "sequence" whose queries are the batch), and
+// every sequence's own keys (part[1]), in one launch; then their parts are joined with the
+// new token, whose key and value go to the caches at row len (nothing read them there).
+// ======================================================================
+struct PrefixArgs {
+  CrossArgs part[2];
+  const void* k_new;   // [B, Hkv, D] or null
+  const void* v_new;
+  void* k_cache;       // [B, Hkv, n_cap, D]
+  void* v_cache;
+  int n_cap, parts;
+};
+template <int D> __global__ void __launch_bounds__(256, D == 128 ? 1 : 2) prefix_few_kernel(const PrefixArgs a) {
+  __shared__ __attribute__((aligned(16))) float stA[FewLds<bf16, D>::FLOATS];
+  __shared__ __attribute__((aligned(16))) float stB[FewLds<bf16, D>::FLOATS];
+  __shared__ float ml[2][4][32];
+  const int own = (int)blockIdx.x >= a.part[0].nblocks;
+  cross_few<bf16, D, false>(a.part[own], (int)blockIdx.x - (own ? a.part[0].nblocks : 0), stA, stB, ml, nullptr);
+}
+template <int D> __global__ void __launch_bounds__(256) prefix_merge_kernel(const PrefixArgs a) {
+  const CrossArgs& p = a.part[1];
+  const int lane = threadIdx.x & 63;
+  const long long row = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);   // of [B, Hq]
+  if (row >= p.nrows) return;
+  float M, l;
+  f32x4 o = join_parts<D>(p.part, p.part_ml, p.nrows, row, a.parts, lane, M, l);
+  constexpr int CG = D / 4;
+  const int cg = lane % CG;
+  if (a.k_new) {
+    const int b = (int)(row / p.Hq), hq = (int)(row % p.Hq), hk = hq / p.G;
+    const long long at = ((long long)b * p.Hkv + hk) * D + 4 * cg;
+    const u32x2 kx = *(const u32x2*)((const bf16*)a.k_new + at), vx = *(const u32x2*)((const bf16*)a.v_new + at);
+    const f32x4 q = Quad<bf16>::load((const bf16*)p.q + row * D + 4 * cg);
+    const f32x4 k = Quad<bf16>::load((const bf16*)a.k_new + at), v = Quad<bf16>::load((const bf16*)a.v_new + at);
+    float x = q[0] * k[0] + q[1] * k[1] + q[2] * k[2] + q[3] * k[3];
+#pragma unroll
+    for (int y = 1; y < CG; y <<= 1) x += __shfl_xor(x, y);
+    x *= p.qflip ? -p.sl2 : p.sl2;
+    const float m = fmaxf(M, x);
+    const float f = M == -INFINITY ? 0.f : exp2_fast(M - m), g = m == -INFINITY ? 0.f : exp2_fast(x - m);
+    l = fmaf(l, f, g);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] = fmaf(o[e], f, g * v[e]);
+    M = m;
+    if (hq % p.G == 0 && lane < 2 * CG) {
+      const long long to = (((long long)b * p.Hkv + hk) * a.n_cap + seq_len(p, b)) * D + 4 * cg;
+      if (lane < CG) *(u32x2*)((bf16*)a.k_cache + to) = kx;
+      if (lane >= CG || CG == 64) *(u32x2*)((bf16*)a.v_cache + to) = vx;
+    }
+  }
+  const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;
+  if (lane < CG) Quad<bf16>::store((bf16*)p.o + row * D + 4 * cg, o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
+  if (lane == 0 && p.lse) p.lse[row] = (M + log2f(l)) * kLn2;
+}
+
+// ======================================================================
+// Backward pre-pass: -D_i = -sum_c dO_ic O_ic and L in base 2, +inf for a row that
+// sees no key, so that its P is 0.
+// ======================================================================
+template <typename T, int D> __global__ void __launch_bounds__(256) cross_prep_kernel(const CrossArgs a) {
+  constexpr int CH = Elem<T>::CH, G = D / CH, RPB = 256 / G;
+  const int tid = threadIdx.x, ch = tid % G;
+  const long long row = (long long)blockIdx.x * RPB + tid / G;   // of [B, Hq, nq]
+  const bool there = row < a.nrows;
+  float acc = 0.f;
+  if (there) {
+    const long long head = row / a.nq;
+    const int b = (int)(head / a.Hq), hq = (int)(head % a.Hq), i = (int)(row % a.nq);
+    const T* x = (const T*)a.o + b * a.os.b + hq * a.os.h + i * a.os.t + ch * CH;
+    const T* y = (const T*)a.dout + b * a.gs.b + hq * a.gs.h + i * a.gs.t + ch * CH;
+#pragma unroll
+    for (int e = 0; e < CH; e += 4) {
+      const f32x4 u = Quad<T>::load(x + e), v = Quad<T>::load(y + e);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) acc = fmaf(u[k], v[k], acc);
+    }
+  }
+#pragma unroll
+  for (int off = G / 2; off > 0; off >>= 1) acc += __shfl_xor(acc, off);
+  if (there && ch == 0) {
+    const float l = a.lse[row];
+    a.dvec[row] = -acc;
+    a.lse2[row] = l == -INFINITY ? INFINITY : l * kLog2e;
+  }
+}
+
+// ======================================================================
+// dK, dV: a workgroup owns 128 keys of a cache head, 32 per wave (K and V rows in
+// registers), and goes over the BQ-query tiles of all heads of its group, or, split,
+// over a run of them. Per 32-query block: S = Q K^T, dP = dO V^T (rows = queries),
+// P, dS, dV^T += dO^T P, dK^T += Q^T dS. Query rows past the end have L = +inf: P = 0.
+// ======================================================================
+template <typename T, int D> struct CrossDkdv {
+  static constexpr int BQ = sizeof(T) == 4 && D == 128 ? 32 : 64;
+};
+template <typename T, int D, bool BIAS>
+__global__ void __launch_bounds__(256, D == 128 ? 1 : 2) cross_dkdv_kernel(const CrossArgs a) {
+  constexpr int BKV = 128, BQ = CrossDkdv<T, D>::BQ, NQB = BQ / 32, NDB = D / 32;
+  using TL = CrossTile<T, BQ, D>;
+  __shared__ __attribute__((aligned(16))) T stA[2][TL::ELEMS];
+  __shared__ __attribute__((aligned(16))) T stB[2][TL::TWO ? TL::ELEMS : 8];
+  __shared__ __attribute__((aligned(16))) float ldA[2][BQ];
+  __shared__ __attribute__((aligned(16))) float ldB[2][TL::TWO ? BQ : 4];
+  extern __shared__ __attribute__((aligned(16))) float bv[];
+
+  const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, c = lane & 31;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  int head, tile;   // of B x Hkv, key block x part
+  block_map(blockIdx.x, a.nblocks, a.ntiles * a.splits, 0, false, head, tile);
+  const int kt = tile / a.splits, part = tile - kt * a.splits;
+  const int b = head / a.Hkv, hk = head - b * a.Hkv;
+  const int n = seq_len(a, b), start = seq_start(a, b);
+  const int k0 = kt * BKV, kw0 = k0 + 32 * w, kj = kw0 + c;
+
+  // query tiles [t0, nqt) of every head see the block; the part's are u0 to u1 of them all
+  const int nqt = (a.nq + BQ - 1) / BQ;
+  const int t0 = a.causal ? min(nqt, max(0, k0 - start) / BQ) : 0, per_head = nqt - t0;
+  const int all = k0 < n ? a.G * per_head : 0;
+  const int u0 = min(all, part * a.per), u1 = min(all, u0 + a.per);
+
+  TL qld(w, lane, a.qs.t), gld(w, lane, a.gs.t);
+  float lreg = 0.f;
+  auto place = [&](int u, int& g, int& q0) __attribute__((always_inline)) {
+    g = u / per_head;
+    q0 = (t0 + u - g * per_head) * BQ;
+  };
+  auto issue = [&](int u, T* ql, T* gl) __attribute__((always_inline)) {
+    int g, q0;
+    place(u, g, q0);
+    const int hq = hk * a.G + g;
+    qld.issue(ql, (const T*)a.q + b * a.qs.b + hq * a.qs.h + q0 * a.qs.t, a.qs.t, a.nq - q0);
+    gld.issue(gl, (const T*)a.dout + b * a.gs.b + hq * a.gs.h + q0 * a.gs.t, a.gs.t, a.nq - q0);
+    if (tid < 2 * BQ) {
+      const int i = q0 + tid % BQ;
+      const long long row = ((long long)b * a.Hq + hq) * a.nq + i;
+      lreg = i >= a.nq ? (tid < BQ ? INFINITY : 0.f) : (tid < BQ ? a.lse2 : a.dvec)[row];
+    }
+  };
+  auto commit = [&](T* ql, T* gl, float* ld) __attribute__((always_inline)) {
+    qld.commit(ql);
+    gld.commit(gl);
+    if (tid < 2 * BQ) ld[tid] = lreg;
+  };
+  if (u0 < u1) {
+    issue(u0, stA[0], stA[1]);
+    commit(stA[0], stA[1], ldA[0]);
+  }
+  RowRegs<T, D> k, v;
+  load_row<T, D>(k, (const T*)a.k + b * a.ks.b + hk * a.ks.h + kj * a.ks.t, kj < n, h, a.qflip);
+  load_row<T, D>(v, (const T*)a.v + b * a.vs.b + hk * a.vs.h + kj * a.vs.t, kj < n, h);
+  f32x16 dk[NDB], dv[NDB];
+#pragma unroll
+  for (int db = 0; db < NDB; ++db) dk[db] = dv[db] = zero16();
+  const float sl2 = a.sl2;
+  int bias_head = -1;   // of the group, whose bias LDS holds
+  __syncthreads();
+
+  auto step = [&](int u, T* qc, T* gc, float* lc, T* qn, T* gn, float* ln) __attribute__((always_inline)) {
+    int g, q0;
+    place(u, g, q0);
+    if (u + 1 < u1) issue(u + 1, qn, gn);
+    if constexpr (BIAS) {
+      if (g != bias_head) {   // the last step ended on a barrier
+        bias_fill<T>(bv, a, hk * a.G + g, tid);
+        bias_head = g;
+        __syncthreads();
+      }
+    }
+#pragma unroll
+    for (int qb = 0; qb < NQB; ++qb) {
+      const int qp0 = q0 + 32 * qb;
+      if (kw0 >= n || (a.causal && start + qp0 + 31 < kw0)) continue;
+      f32x16 s = zero16(), dp = zero16();
+      mma_tile_rows<D>(s, qc, qb, k, h, c);
+      mma_tile_rows<D>(dp, gc, qb, v, h, c);
+      // lane (h, c): element j is query qp0 + 16 h + j, key kj
+      float u_bias = 0.f;
+      const float* p = nullptr;
+      bool each = false;
+      if constexpr (BIAS) {
+        const int side = bias_side(a, kw0 - (start + qp0 + 31), kw0 + 31 - (start + qp0));
+        each = side == 0;
+        if (each) p = bv + (kBiasPad - a.first + kj - start - qp0 - 16 * h);
+        else u_bias = bv[side < 0 ? 0 : a.R + 2 * kBiasPad - 1];
+      }
+      const bool edge = kw0 + 31 >= n || (a.causal && start + qp0 < kw0 + 31);
+      const int lo = kj >= n ? 16 : a.causal ? kj - start - (qp0 + 16 * h) : 0;
+      if constexpr (BIAS) {
+        if (each) {
+#pragma unroll
+          for (int j = 0; j < 16; ++j) s[j] = fmaf(s[j], sl2, p[-j]);
+        } else {
+#pragma unroll
+          for (int j = 0; j < 16; ++j) s[j] = fmaf(s[j], sl2, u_bias);
+        }
+      }
+#pragma unroll
+      for (int j4 = 0; j4 < 4; ++j4) {
+        const f32x4 l4 = *(const f32x4*)&lc[32 * qb + 16 * h + 4 * j4];
+        const f32x4 d4 = *(const f32x4*)&lc[BQ + 32 * qb + 16 * h + 4 * j4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int j = 4 * j4 + e;
+          s[j] = exp2_fast(BIAS ? s[j] - l4[e] : fmaf(s[j], sl2, -l4[e]));
+          dp[j] = s[j] * (dp[j] + d4[e]);   // d4 holds -D
+        }
+      }
+      if (edge) {
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+          s[j] = j < lo ? 0.f : s[j];
+          dp[j] = j < lo ? 0.f : dp[j];
+        }
+      }
+      mma_tile_cols<D>(dv, gc, qb, s, h, c);
+      mma_tile_cols<D>(dk, qc, qb, dp, h, c);
+    }
+    if constexpr (!TL::TWO) __syncthreads();
+    if (u + 1 < u1) commit(qn, gn, ln);
+    __syncthreads();
+  };
+  for (int u = u0; u < u1; u += 2) {
+    step(u, stA[0], stA[1], ldA[0], TL::TWO ? stB[0] : stA[0], TL::TWO ? stB[1] : stA[1], TL::TWO ? ldB[0] : ldA[0]);
+    if (u + 1 < u1)
+      step(u + 1, TL::TWO ? stB[0] : stA[0], TL::TWO ? stB[1] : stA[1], TL::TWO ? ldB[0] : ldA[0], stA[0], stA[1], ldA[0]);
+  }
+
+  if (kj < a.nk) {
+    if (a.part) {
+      const long long at = ((long long)part * a.nrows + (long long)head * a.nk + kj) * D;
+      store_row<float, D>(a.part + at, dk, a.scale, h);
+      store_row<float, D>(a.part2 + at, dv, 1.f, h);
+    } else {
+      store_row<T, D>((T*)a.dk + b * a.dks.b + hk * a.dks.h + kj * a.dks.t, dk, a.scale, h);
+      store_row<T, D>((T*)a.dv + b * a.dvs.b + hk * a.dvs.h + kj * a.dvs.t, dv, 1.f, h);
+    }
+  }
+}
+
+// ======================================================================
+// dQ: a workgroup owns 128 queries of a head, 32 per wave (Q and dO rows in
+// registers), and goes over the 64-key tiles of K and V that they see, or a run of
+// them. Per 32-key block: S^T = K Q^T, dP^T = V dO^T, dS^T, dQ^T += K^T dS^T.
+//
+// The bias gradient (drel): dS is added up by relative position, in LDS where a tile
+// reaches into the positions that have a bias of their own, in registers elsewhere.
+// In LDS every wave and lane half has a row of its own: the 64 lanes of one add
+// then go to 64 addresses, and the sums come out the same every time.
+// D comes from an O that was rounded to bf16, so that dS = P (dP - D) is off by P e_i,
+// e_i being D's error. That is far below dQ's and dK's own rounding, but a bucket's sum
+// over whole rows loses almost all of dS, which adds up to 0 in a row, and none of P e_i.
+// The row's sum of dS gives e_i, so P times it is taken from each sum: for the keys
+// beyond the positions of their own from the sums of P there, for the others in a
+// second pass over their tiles (S only).
+// ======================================================================
+template <typename T, int D, bool BIAS>
+__global__ void __launch_bounds__(256, sizeof(T) == 4 ? 1 : 2) cross_dq_kernel(const CrossArgs a) {
+  constexpr int BQ = 128, BKV = 64, NKB = 2, NDB = D / 32;
+  using TL = CrossTile<T, BKV, D>;
+  __shared__ __attribute__((aligned(16))) T stA[2][TL::ELEMS];
+  __shared__ __attribute__((aligned(16))) T stB[2][TL::TWO ? TL::ELEMS : 8];
+  __shared__ float far[2][4];
+  extern __shared__ __attribute__((aligned(16))) float bv[];   // bias [RP], then sums [4 waves][2 halves][RP]
+
+  const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, c = lane & 31;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  int head, tile;
+  block_map(blockIdx.x, a.nblocks, a.ntiles * a.splits, a.hgroup, a.causal, head, tile);
+  const int qt = tile / a.splits, part = tile - qt * a.splits;
+  const int b = head / a.Hq, hq = head - b * a.Hq, hk = hq / a.G;
+  const int n = seq_len(a, b), start = seq_start(a, b);
+  const int q0 = qt * BQ, qw0 = q0 + 32 * w, qi = qw0 + c;
+  const T* Kg = (const T*)a.k + b * a.ks.b + hk * a.ks.h;
+  const T* Vg = (const T*)a.v + b * a.vs.b + hk * a.vs.h;
+  const int kv_end = a.causal ? max(0, min(n, start + min(q0 + BQ, a.nq))) : n;
+  const int it0 = part * a.per, nt = min((kv_end + BKV - 1) / BKV, it0 + a.per);
+  const int RP = a.R + 2 * kBiasPad;
+  const bool grad = BIAS && a.drel;
+
+  TL kld(w, lane, a.ks.t), vld(w, lane, a.vs.t);
+  auto issue = [&](TL& ld, T* lds, const T* g, long long st, int it) __attribute__((always_inline)) {
+    ld.issue(lds, g + (long long)it * BKV * st, st, n - it * BKV);
+  };
+  if (it0 < nt) {
+    issue(kld, stA[0], Kg, a.ks.t, it0);
+    issue(vld, stA[1], Vg, a.vs.t, it0);
+    kld.commit(stA[0]);
+    vld.commit(stA[1]);
+  }
+  RowRegs<T, D> q, g;
+  load_row<T, D>(q, (const T*)a.q + b * a.qs.b + hq * a.qs.h + qi * a.qs.t, qi < a.nq, h, a.qflip);
+  load_row<T, D>(g, (const T*)a.dout + b * a.gs.b + hq * a.gs.h + qi * a.gs.t, qi < a.nq, h);
+  const long long row = (long long)head * a.nq + qi;
+  const float lq = qi < a.nq ? a.lse2[row] : INFINITY, nd = qi < a.nq ? a.dvec[row] : 0.f;
+  float* const mine = bv + RP * (1 + 2 * w + h);
+  if constexpr (BIAS) {
+    bias_fill<T>(bv, a, hq, tid);
+    if (grad)
+      for (int t = tid; t < 8 * RP; t += 256) bv[RP + t] = 0.f;
+  }
+  __syncthreads();
+
+  f32x16 dqa[NDB];
+#pragma unroll
+  for (int db = 0; db < NDB; ++db) dqa[db] = zero16();
+  const float sl2 = a.sl2;
+  // of this lane's keys: sums of dS before, among and behind the positions of their own, of P among and behind
+  float s_lo = 0.f, s_in = 0.f, s_hi = 0.f, p_in = 0.f, p_hi = 0.f;
+  bool met_lo = false;   // wave-uniform
+
+  // x in base 2 less L of block kb of the tile at kv0, from the raw scores; returns the side
+  auto shift = [&](f32x16& s, int kb0) __attribute__((always_inline)) -> int {
+    int side = 0;
+    if constexpr (BIAS) {
+      side = bias_side(a, kb0 - (start + qw0 + 31), kb0 + 31 - (start + qw0));
+      if (side != 0) {
+        const float u = bv[side < 0 ? 0 : RP - 1] - lq;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) s[j] = fmaf(s[j], sl2, u);
+      } else {
+        const float* p = bv + (kBiasPad - a.first + kb0 + 16 * h - start - qi);
+#pragma unroll
+        for (int j = 0; j < 16; ++j) s[j] = fmaf(s[j], sl2, p[j] - lq);
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < 16; ++j) s[j] = fmaf(s[j], sl2, -lq);
+    }
+    return side;
+  };
+  auto lim_of = [&](int kb0) __attribute__((always_inline)) -> int {
+    return (a.causal ? min(start + qi, n - 1) : n - 1) - (kb0 + 16 * h);
+  };
+  auto add = [&](int kb0, int j, float x) __attribute__((always_inline)) {
+    __hip_atomic_fetch_add(mine + (kBiasPad - a.first + kb0 + 16 * h - start - qi + j), x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+  };
+
+  auto step = [&](int it, T* kc, T* vc, T* kn, T* vn) __attribute__((always_inline)) {
+    const int kv0 = it * BKV;
+    if (it + 1 < nt) {
+      issue(kld, kn, Kg, a.ks.t, it + 1);
+      issue(vld, vn, Vg, a.vs.t, it + 1);
+    }
+#pragma unroll
+    for (int kb = 0; kb < NKB; ++kb) {
+      const int kb0 = kv0 + 32 * kb;
+      if (kb0 >= n || (a.causal && kb0 > start + qw0 + 31)) continue;
+      __builtin_amdgcn_s_setprio(1);
+      f32x16 s = zero16(), dp = zero16();
+      mma_tile_rows<D>(s, kc, kb, q, h, c);
+      mma_tile_rows<D>(dp, vc, kb, g, h, c);
+      const int side = shift(s, kb0);
+      // lane (h, c): element j is key kb0 + 16 h + j, query qi
+#pragma unroll
+      for (int j = 0; j < 16; ++j) {
+        s[j] = exp2_fast(s[j]);
+        dp[j] = s[j] * (dp[j] + nd);   // nd holds -D
+      }
+      if (kb0 + 31 >= n || (a.causal && kb0 + 31 > start + qw0)) {
+        const int lim = lim_of(kb0);
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+          s[j] = j > lim ? 0.f : s[j];
+          dp[j] = j > lim ? 0.f : dp[j];
+        }
+      }
+      if constexpr (BIAS) {
+        if (grad) {
+          float sd = 0.f, sp = 0.f;
+#pragma unroll
+          for (int j = 0; j < 16; ++j) sd += dp[j];
+          if (side >= 0) {
+#pragma unroll
+            for (int j = 0; j < 16; ++j) sp += s[j];
+          }
+          if (side < 0) {
+            s_lo += sd;
+            met_lo = true;
+          } else if (side > 0) {
+            s_hi += sd;
+            p_hi += sp;
+          } else {
+            s_in += sd;
+            p_in += sp;
+#pragma unroll
+            for (int j = 0; j < 16; ++j) add(kb0, j, dp[j]);
+          }
+        }
+      }
+      __builtin_amdgcn_s_setprio(0);
+      mma_tile_cols<D>(dqa, kc, kb, dp, h, c);
+    }
+    if constexpr (!TL::TWO) __syncthreads();
+    if (it + 1 < nt) {
+      kld.commit(kn);
+      vld.commit(vn);
+    }
+    __syncthreads();
+  };
+  for (int it = it0; it < nt; it += 2) {
+    step(it, stA[0], stA[1], TL::TWO ? stB[0] : stA[0], TL::TWO ? stB[1] : stA[1]);
+    if (it + 1 < nt) step(it + 1, TL::TWO ? stB[0] : stA[0], TL::TWO ? stB[1] : stA[1], stA[0], stA[1]);
+  }
+
+  if (qi < a.nq) {
+    if (a.part) store_row<float, D>(a.part + ((long long)part * a.nrows + row) * D, dqa, a.scale, h);
+    else store_row<T, D>((T*)a.dq + b * a.dqs.b + hq * a.dqs.h + qi * a.dqs.t, dqa, a.scale, h);
+  }
+
+  if constexpr (BIAS) {
+    if (!grad) return;
+    // -e_i of this lane's query, both halves' keys; P of a row adds up to 1 (0 without keys)
+    const float e = halves_sum(s_lo + s_in + s_hi);
+    const float one = lq < INFINITY ? 1.f : 0.f;
+    const float q_in = halves_sum(p_in), q_hi = halves_sum(p_hi);
+    float f_lo = halves_sum(s_lo), f_hi = halves_sum(s_hi) - e * q_hi;
+    if (met_lo) f_lo -= e * fmaxf(one - q_in - q_hi, 0.f);
+    // tiles that reach into the positions of their own, for a wave of the workgroup
+    const int tb0 = max(0, a.first - 94 + start + q0) / BKV, tb1 = min(nt, (max(0, a.first + a.R - 1 + start + q0 + BQ - 1) + BKV) / BKV);
+    for (int it = tb0; it < tb1; ++it) {
+      issue(kld, stA[0], Kg, a.ks.t, it);
+      kld.commit(stA[0]);
+      __syncthreads();
+#pragma unroll
+      for (int kb = 0; kb < NKB; ++kb) {
+        const int kb0 = it * BKV + 32 * kb;
+        if (kb0 >= n || (a.causal && kb0 > start + qw0 + 31)) continue;
+        if (bias_side(a, kb0 - (start + qw0 + 31), kb0 + 31 - (start + qw0)) != 0) continue;
+        f32x16 s = zero16();
+        mma_tile_rows<D>(s, stA[0], kb, q, h, c);
+        shift(s, kb0);
+        const int lim = lim_of(kb0);
+#pragma unroll
+        for (int j = 0; j < 16; ++j) add(kb0, j, j > lim ? 0.f : -e * exp2_fast(s[j]));
+      }
+      __syncthreads();
+    }
+    // the queries' sums beyond, both halves of a wave holding the same
+#pragma unroll
+    for (int x = 1; x < 32; x <<= 1) {
+      f_lo += __shfl_xor(f_lo, x);
+      f_hi += __shfl_xor(f_hi, x);
+    }
+    if (lane == 0) {
+      far[0][w] = f_lo;
+      far[1][w] = f_hi;
+    }
+    __syncthreads();
+    float* const out = a.drel + (long long)(head * a.ntiles + qt) * a.R;
+    auto sum8 = [&](int t) __attribute__((always_inline)) -> float {
+      float x = 0.f;
+#pragma unroll
+      for (int y = 0; y < 8; ++y) x += bv[RP * (1 + y) + t];
+      return x;
+    };
+    for (int t = 1 + tid; t < a.R - 1; t += 256) out[t] = sum8(kBiasPad + t);
+    // the ends take what lies beyond
+    if (w < 2) {
+      const int from = w == 0 ? 0 : kBiasPad + a.R - 1;
+      float x = 0.f;
+      for (int t = lane; t <= kBiasPad; t += 64) x += sum8(from + t);
+#pragma unroll
+      for (int y = 1; y < 64; y <<= 1) x += __shfl_xor(x, y);
+      x += far[w][0] + far[w][1] + far[w][2] + far[w][3];
+      if (lane == 0) out[w == 0 ? 0 : a.R - 1] = x;
+    }
+  }
+}
+
+// A gradient whose sum was split: rows [rows, D] float32 of `parts` parts, added in order.
+// x: [B, H, n] rows with strides `s`.
+template <typename T, int D> __global__ void __launch_bounds__(256) cross_sum_kernel(const float* part, void* out, Strides s, long long rows, int H, int n, int parts) {
+  constexpr int CG = D / 4;
+  const long long i = (long long)blockIdx.x * 256 + threadIdx.x, row = i / CG;
+  const int cg = (int)(i % CG);
+  if (row >= rows) return;
+  f32x4 x = {0.f, 0.f, 0.f, 0.f};
+  for (int p = 0; p < parts; ++p) x += *(const f32x4*)(part + (p * rows + row) * D + 4 * cg);
+  const long long head = row / n;
+  const int b = (int)(head / H), hh = (int)(head % H), t = (int)(row % n);
+  Quad<T>::store((T*)out + b * s.b + hh * s.h + t * s.t + 4 * cg, x[0], x[1], x[2], x[3]);
+}
+
+// The bias gradient of head blockIdx.x: the dQ workgroups' sums by relative position, then
+// those of each bucket's positions, all in a fixed order and in 64 bits (a bucket's sum is
+// small against its terms).
+template <typename T> __global__ void __launch_bounds__(1024) cross_dbias_kernel(const CrossArgs a, void* dtable) {
+  extern __shared__ __attribute__((aligned(16))) double acc[];   // [R], then [1024]
+  const int tid = threadIdx.x, hq = blockIdx.x;
+  double* const tmp = acc + a.R;
+  const int per = a.ntiles;   // rows of a sequence and head
+  // position t0 + tid % 64 of the rows tid / 64, + 16, ...
+  for (int t0 = 0; t0 < a.R; t0 += 64) {
+    const int t = t0 + (tid & 63);
+    double x = 0.0;
+    if (t < a.R) {
+      const int N = a.B * per;
+      for (int r = tid >> 6; r < N; r += 16) {
+        const int b = r / per, qt = r - b * per;
+        x += (double)a.drel[(((long long)b * a.Hq + hq) * per + qt) * a.R + t];
+      }
+    }
+    __syncthreads();
+    tmp[tid] = x;
+    __syncthreads();
+    if (tid < 64 && t < a.R) {
+      double y = 0.0;
+      for (int r = 0; r < 16; ++r) y += tmp[64 * r + tid];
+      acc[t] = y;
+    }
+  }
+  __syncthreads();
+  for (int k = tid; k < a.buckets; k += 1024) {
+    double y = 0.0;
+    for (int t = 0; t < a.R; ++t) y += a.rows[t] == k ? acc[t] : 0.0;
+    ((T*)dtable)[(long long)k * a.Hq + hq] = (T)(float)y;
+  }
+}
+
+}  // namespace attn

@@ -17,7 +17,10 @@
 namespace {
 
 using attn::bf16;
+using attn::aligned;
+using attn::fits;
 using attn::Strides;
+using attn::strides_of;
 using attn::writable;
 
 bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
@@ -38,30 +41,6 @@ attn::Rotation rotation(const double* freqs, int r, float amplitude) {
   rot.r = freqs ? r : 0;
   rot.amplitude = amplitude;
   return rot;
-}
-
-// The caller's strides (sequence, head, token), or those of a dense [B, H, n, d].
-// That of an axis of one entry says nothing.
-Strides strides_of(const long long* s, int B, int H, int n, int d) {
-  Strides r = {(long long)H * n * d, (long long)n * d, d};
-  if (s) r = {s[0], s[1], s[2]};
-  if (B == 1) r.b = 0;
-  if (H == 1) r.h = 0;
-  if (n == 1) r.t = 0;
-  return r;
-}
-// Rows start at multiples of 16 bytes.
-bool aligned(const Strides& s, int elem) {
-  const int m = 16 / elem;
-  return s.b % m == 0 && s.h % m == 0 && s.t % m == 0;
-}
-bool fits(const Strides& s, int B, int H, int n) {   // offsets in 62 bits
-  __int128 far = 0;
-  for (const auto& [step, size] : {std::pair<long long, int>{s.b, B}, {s.h, H}, {s.t, n}}) {
-    if (step < 0) return false;
-    far += (__int128)step * (size - 1);
-  }
-  return far < ((__int128)1 << 60);
 }
 
 // Workgroups of 256 threads for `rows` rows, `per` to a workgroup; a launch has fewer

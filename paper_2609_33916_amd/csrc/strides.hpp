@@ -4,12 +4,37 @@
 
 #include <algorithm>
 #include <array>
+#include <utility>
 
 namespace attn {
 
 struct Strides {
   long long b, h, t;   // elements between sequences, heads, tokens; not negative, 0 along an axis of one entry
 };
+
+// The caller's strides (sequence, head, token), or those of a dense [B, H, n, d].
+// That of an axis of one entry says nothing.
+inline Strides strides_of(const long long* s, int B, int H, int n, int d) {
+  Strides r = {(long long)H * n * d, (long long)n * d, d};
+  if (s) r = {s[0], s[1], s[2]};
+  if (B == 1) r.b = 0;
+  if (H == 1) r.h = 0;
+  if (n == 1) r.t = 0;
+  return r;
+}
+// Rows start at multiples of 16 bytes.
+inline bool aligned(const Strides& s, int elem) {
+  const int m = 16 / elem;
+  return s.b % m == 0 && s.h % m == 0 && s.t % m == 0;
+}
+inline bool fits(const Strides& s, int B, int H, int n) {   // offsets in 62 bits
+  __int128 far = 0;
+  for (const auto& [step, size] : {std::pair<long long, int>{s.b, B}, {s.h, H}, {s.t, n}}) {
+    if (step < 0) return false;
+    far += (__int128)step * (size - 1);
+  }
+  return far < ((__int128)1 << 60);
+}
 
 // Rows of a written tensor must not overlap: from the smallest stride on, each
 // has to step over all that the smaller ones span.
