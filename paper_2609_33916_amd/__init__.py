@@ -174,6 +174,9 @@ def _bind_native(L: ctypes.CDLL) -> None:
     _binding.bind_paged(*(ctypes.cast(getattr(L, f), ctypes.c_void_p).value
                           for f in ("attn_rope", "attn_rope_bwd", "attn_paged_append", "attn_paged_gather",
                                     "attn_paged_decode_workspace_bytes", "attn_paged_decode")))
+    _binding.bind_cross(*(ctypes.cast(getattr(L, f), ctypes.c_void_p).value
+                          for f in ("attn_cross_fwd_workspace_bytes", "attn_cross_fwd", "attn_cross_bwd_workspace_bytes",
+                                    "attn_cross_bwd", "attn_prefix_decode_workspace_bytes", "attn_prefix_decode")))
     _native, _native_lib = _binding, L
 
 
@@ -914,6 +917,10 @@ def attn_cross_fwd(q, k, v, scale: Optional[float] = None, causal: bool = False,
     bias[bias_rows[r - bias_first], h] to the scores of the pairs at relative position r = key -
     query, positions beyond taking bias_rows' first and last entries (attn_bias_buckets).
     A query without keys has O = 0, L = -inf."""
+    if lib() is _native_lib:
+        r = _native.cross_fwd(q, k, v, scale, causal, start, starts, k_lens, bias, bias_rows, bias_first, out, workspace)
+        if r is not NotImplemented:
+            return _status(r, "attn_cross_fwd")
     (B, Hq, Hkv, nq, nk, d), args, R = _cross_args(q, k, v, starts, start, k_lens, bias, bias_rows, bias_first)
     code = _dtype_code(q)
     if out is None:
@@ -936,6 +943,10 @@ def attn_cross_bwd(q, k, v, o, lse, do, scale: Optional[float] = None, causal: b
     """The gradients of attn_cross_fwd's inputs from its O and L and the gradient of O: returns
     (dQ, dK, dV), with a bias (dQ, dK, dV, dBias). Other arguments as there. ``out`` may hold
     the results' tensors (dBias None: not wanted), which may be views."""
+    if lib() is _native_lib:
+        r = _native.cross_bwd(q, k, v, o, lse, do, scale, causal, start, starts, k_lens, bias, bias_rows, bias_first, out, workspace)
+        if r is not NotImplemented:
+            return _status(r, "attn_cross_bwd")
     (B, Hq, Hkv, nq, nk, d), args, R = _cross_args(q, k, v, starts, start, k_lens, bias, bias_rows, bias_first)
     code = _dtype_code(q)
     for name, t in (("o", o), ("do", do)):
@@ -971,6 +982,10 @@ def attn_prefix_decode(q, k_prefix, v_prefix, k_cache, v_cache, k_new=None, v_ne
     ([B, Hkv, d]) are appended at row cache_lens[b], and q ([B, Hq, d]) attends to the prefix, to the
     first cache_lens[b] rows and to the new token. n bounds the lengths (default: the
     caches' room). Returns (O, L)."""
+    if lib() is _native_lib:
+        r = _native.prefix_decode(q, k_prefix, v_prefix, k_cache, v_cache, k_new, v_new, cache_lens, n, scale, out, workspace)
+        if r is not NotImplemented:
+            return _status(r, "attn_prefix_decode")
     _need(isinstance(q, torch.Tensor) and q.dim() == 3 and q.is_cuda, "q must be a GPU tensor [B, Hq, d]")
     _need(q.dtype == torch.bfloat16, "q must be bfloat16")
     _need(isinstance(k_prefix, torch.Tensor) and k_prefix.dim() == 3, "k_prefix must be [Hkv, np, d]")

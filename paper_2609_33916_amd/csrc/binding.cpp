@@ -1,6 +1,6 @@
 // Native form of the Python entry points a program calls per step (attn_fwd,
 // attn_fwd_bwd, attn_bwd, attn_decode, attn_rope, attn_rope_bwd, attn_paged_append,
-// attn_paged_gather, attn_paged_decode): argument checks, output and workspace
+// attn_paged_gather, attn_paged_decode, attn_cross_fwd, attn_cross_bwd, attn_prefix_decode): argument checks, output and workspace
 // allocation and the call into the library, without per-argument Python work.
 //
 // Each function answers NotImplemented, having done nothing, for anything but
@@ -10,7 +10,7 @@
 // float or bool). The Python form then runs, with its full checks and errors.
 // A status code of the library other than 0 is answered as an int.
 //
-// The library is reached through the addresses that bind() and bind_paged() receive, so both
+// The library is reached through the addresses that the bind functions receive, so both
 // forms call the same loaded library.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
@@ -592,12 +592,229 @@ PyObject* bind_paged(PyObject*, PyObject* const* a, Py_ssize_t na) {
   Py_RETURN_NONE;
 }
 
+// --------------------------------- keys of another length, shared prefix --
+using CrossWsFn = size_t (*)(int, int, int, int, int, int, int, int);
+using CrossFwdFn = int (*)(const void*, const void*, const void*, void*, float*, const long long*, const int*, const int*, int,
+                           const void*, const int*, int, int, int, void*, size_t, int, int, int, int, int, int, float, int, int,
+                           void*);
+using CrossBwdFn = int (*)(const void*, const void*, const void*, const void*, const float*, const void*, void*, void*, void*,
+                           void*, const long long*, const int*, const int*, int, const void*, const int*, int, int, int, void*,
+                           size_t, int, int, int, int, int, int, float, int, int, void*);
+using PrefixWsFn = size_t (*)(int, int, int, int, int, int);
+using PrefixFn = int (*)(const void*, const void*, const void*, const void*, const void*, void*, void*, const int*, void*, float*,
+                         void*, size_t, int, int, int, int, int, int, int, float, int, void*);
+
+CrossWsFn cross_fwd_ws, cross_bwd_ws;
+CrossFwdFn c_cross_fwd;
+CrossBwdFn c_cross_bwd;
+PrefixWsFn prefix_ws;
+PrefixFn c_prefix;
+
+// what the forward and the backward share: q, k, v, and scale, causal, start, starts, k_lens, bias, bias_rows, bias_first
+struct Cross {
+  const at::Tensor *q, *k, *v, *bias = nullptr;
+  int64_t B, Hq, Hkv, nq, nk, d;
+  float scale;
+  bool causal;
+  int start, first, R = 0, buckets = 0;
+  const int *lens, *starts, *bias_rows = nullptr;
+  bool get(PyObject* const* qkv, PyObject* const* a) {
+    q = rows(qkv[0]), k = rows(qkv[1]), v = rows(qkv[2]);
+    if (!q || q->dim() != 4 || dtype_code(*q) < 0 || !fits_int(q->sizes()) || !k || k->dim() != 4 || !fits_int(k->sizes()))
+      return false;
+    B = q->size(0), Hq = q->size(1), nq = q->size(2), d = q->size(3), Hkv = k->size(1), nk = k->size(2);
+    const int64_t want[4] = {B, Hkv, nk, d};
+    if (!is(k, want, q->scalar_type(), *q) || !is(v, want, q->scalar_type(), *q) || q->numel() == 0 || k->numel() == 0) return false;
+    if (!get_scale(a[0], d, scale) || !PyBool_Check(a[1]) || !get_int(a[2], start) || !get_ints(a[3], {B}, *q, starts) ||
+        !get_ints(a[4], {B}, *q, lens) || !get_int(a[7], first))
+      return false;
+    causal = a[1] == Py_True;
+    if (starts) start = 0;
+    if (a[5] == Py_None) return a[6] == Py_None;
+    bias = plain(a[5]);
+    const at::Tensor* r = plain(a[6]);
+    if (!bias || bias->dim() != 2 || !fits_int(bias->sizes()) || !is(bias, {bias->size(0), Hq}, q->scalar_type(), *q) || !r ||
+        r->dim() != 1 || !fits_int(r->sizes()) || !is(r, r->sizes(), at::kInt, *q))
+      return false;
+    bias_rows = (const int*)r->data_ptr();
+    R = (int)r->size(0), buckets = (int)bias->size(0);
+    return true;
+  }
+  const void* table() const { return bias ? bias->data_ptr() : nullptr; }
+};
+void put_strides(long long* s, const at::Tensor& t) {
+  for (int i = 0; i < 3; ++i) s[i] = t.stride(i);
+}
+
+// cross_fwd(q, k, v, scale, causal, start, starts, k_lens, bias, bias_rows, bias_first, out, workspace)
+PyObject* cross_fwd(PyObject*, PyObject* const* a, Py_ssize_t na) {
+  return guarded([&]() -> PyObject* {
+    Cross c;
+    if (na != 13 || !c.get(a, a + 3)) return not_mine();
+    at::Tensor own[2], ws_own;
+    const at::Tensor* out[2];
+    if (a[11] == Py_None) {
+      out[0] = &(own[0] = at::empty(c.q->sizes(), c.q->options()));
+      out[1] = &(own[1] = at::empty(c.q->sizes().slice(0, 3), c.q->options().dtype(at::kFloat)));
+    } else {
+      if (!PyTuple_CheckExact(a[11]) || PyTuple_GET_SIZE(a[11]) != 2) return not_mine();
+      out[0] = rows(PyTuple_GET_ITEM(a[11], 0)), out[1] = plain(PyTuple_GET_ITEM(a[11], 1));
+      if (!like(out[0], *c.q) || !is(out[1], c.q->sizes().slice(0, 3), at::kFloat, *c.q)) return not_mine();
+    }
+    const size_t need = cross_fwd_ws(c.B, c.Hq, c.Hkv, c.nq, c.nk, c.d, dtype_code(*c.q), c.R);
+    void *ws = nullptr, *st;
+    size_t bytes = 0;
+    if ((need > 0 || a[12] != Py_None) && !get_workspace(a[12], need, *c.q, ws_own, ws, bytes)) return not_mine();
+    long long s[12];
+    const at::Tensor* all[4] = {c.q, c.k, c.v, out[0]};
+    for (int i = 0; i < 4; ++i) put_strides(s + 3 * i, *all[i]);
+    const c10::DeviceGuard device(c.q->device());
+    if (!get_stream(*c.q, st)) return nullptr;
+    const int rc = released([&] {
+      return c_cross_fwd(c.q->data_ptr(), c.k->data_ptr(), c.v->data_ptr(), out[0]->data_ptr(), (float*)out[1]->data_ptr(), s, c.lens,
+                         c.starts, c.start, c.table(), c.bias_rows, c.first, c.R, c.buckets, ws, bytes, c.B, c.Hq, c.Hkv, c.nq, c.nk,
+                         c.d, c.scale, c.causal, dtype_code(*c.q), st);
+    });
+    if (rc) return PyLong_FromLong(rc);
+    if (a[11] != Py_None) return Py_NewRef(a[11]);
+    PyObject *x = THPVariable_Wrap(std::move(own[0])), *y = THPVariable_Wrap(std::move(own[1]));
+    PyObject* both = x && y ? PyTuple_Pack(2, x, y) : nullptr;
+    Py_XDECREF(x);
+    Py_XDECREF(y);
+    return both;
+  });
+}
+
+// cross_bwd(q, k, v, o, lse, do, scale, causal, start, starts, k_lens, bias, bias_rows, bias_first, out, workspace)
+PyObject* cross_bwd(PyObject*, PyObject* const* a, Py_ssize_t na) {
+  return guarded([&]() -> PyObject* {
+    Cross c;
+    if (na != 16 || !c.get(a, a + 6)) return not_mine();
+    const at::Tensor *o = rows(a[3]), *l = plain(a[4]), *g = rows(a[5]);
+    if (!like(o, *c.q) || !is(l, c.q->sizes().slice(0, 3), at::kFloat, *c.q) || !like(g, *c.q)) return not_mine();
+    const int N = c.bias ? 4 : 3;
+    const at::Tensor* ref[4] = {c.q, c.k, c.v, c.bias};
+    at::Tensor own[4], ws_own;
+    const at::Tensor* out[4] = {nullptr, nullptr, nullptr, nullptr};
+    if (a[14] == Py_None) {
+      for (int i = 0; i < N; ++i) out[i] = &(own[i] = at::empty(ref[i]->sizes(), ref[i]->options()));
+    } else {
+      if (!PyTuple_CheckExact(a[14]) || PyTuple_GET_SIZE(a[14]) != N) return not_mine();
+      for (int i = 0; i < N; ++i) {
+        PyObject* x = PyTuple_GET_ITEM(a[14], i);
+        if (i == 3 && x == Py_None) break;
+        out[i] = i < 3 ? rows(x) : plain(x);
+        if (!like(out[i], *ref[i])) return not_mine();
+      }
+    }
+    const size_t need = cross_bwd_ws(c.B, c.Hq, c.Hkv, c.nq, c.nk, c.d, dtype_code(*c.q), out[3] ? c.R : 0);
+    void *ws = nullptr, *st;
+    size_t bytes = 0;
+    if ((need > 0 || a[15] != Py_None) && !get_workspace(a[15], need, *c.q, ws_own, ws, bytes)) return not_mine();
+    long long s[24];
+    const at::Tensor* all[8] = {c.q, c.k, c.v, o, g, out[0], out[1], out[2]};
+    for (int i = 0; i < 8; ++i) put_strides(s + 3 * i, *all[i]);
+    const c10::DeviceGuard device(c.q->device());
+    if (!get_stream(*c.q, st)) return nullptr;
+    const int rc = released([&] {
+      return c_cross_bwd(c.q->data_ptr(), c.k->data_ptr(), c.v->data_ptr(), o->data_ptr(), (const float*)l->data_ptr(), g->data_ptr(),
+                         out[0]->data_ptr(), out[1]->data_ptr(), out[2]->data_ptr(), out[3] ? out[3]->data_ptr() : nullptr, s, c.lens,
+                         c.starts, c.start, c.table(), c.bias_rows, c.first, c.R, c.buckets, ws, bytes, c.B, c.Hq, c.Hkv, c.nq, c.nk,
+                         c.d, c.scale, c.causal, dtype_code(*c.q), st);
+    });
+    if (rc) return PyLong_FromLong(rc);
+    if (a[14] != Py_None) return Py_NewRef(a[14]);
+    PyObject* r = PyTuple_New(N);
+    if (!r) return nullptr;
+    for (int i = 0; i < N; ++i) {
+      PyObject* x = THPVariable_Wrap(std::move(own[i]));
+      if (!x) {
+        Py_DECREF(r);
+        return nullptr;
+      }
+      PyTuple_SET_ITEM(r, i, x);
+    }
+    return r;
+  });
+}
+
+// prefix_decode(q, k_prefix, v_prefix, k_cache, v_cache, k_new, v_new, cache_lens, n, scale, out, workspace)
+PyObject* prefix_decode(PyObject*, PyObject* const* a, Py_ssize_t na) {
+  return guarded([&]() -> PyObject* {
+    if (na != 12) return not_mine();
+    const at::Tensor *q = plain(a[0]), *kp = plain(a[1]), *vp = plain(a[2]), *kc = plain(a[3]), *vc = plain(a[4]), *kn = nullptr, *vn = nullptr;
+    if (!q || q->dim() != 3 || q->scalar_type() != at::kBFloat16 || !kp || kp->dim() != 3 || !kc || kc->dim() != 4 ||
+        !fits_int(q->sizes()) || !fits_int(kp->sizes()) || !fits_int(kc->sizes()))
+      return not_mine();
+    const int64_t B = q->size(0), Hq = q->size(1), d = q->size(2), Hkv = kp->size(0), np = kp->size(1), n_cap = kc->size(2);
+    const int64_t want_p[3] = {Hkv, np, d}, want_c[4] = {B, Hkv, n_cap, d}, want_new[3] = {B, Hkv, d};
+    if (!is(kp, want_p, at::kBFloat16, *q) || !is(vp, want_p, at::kBFloat16, *q) || !is(kc, want_c, at::kBFloat16, *q) ||
+        !is(vc, want_c, at::kBFloat16, *q) || (a[5] == Py_None) != (a[6] == Py_None))
+      return not_mine();
+    if (a[5] != Py_None) {
+      kn = plain(a[5]), vn = plain(a[6]);
+      if (!is(kn, want_new, at::kBFloat16, *q) || !is(vn, want_new, at::kBFloat16, *q)) return not_mine();
+    }
+    const int* lens;
+    int n;
+    float scale;
+    if (!get_ints(a[7], {B}, *q, lens) || !get_scale(a[9], d, scale)) return not_mine();
+    if (a[8] != Py_None) {
+      if (!get_int(a[8], n)) return not_mine();
+    } else {
+      if (!lens) return not_mine();
+      n = (int)n_cap - (kn != nullptr);
+    }
+    Outputs<2> out;
+    if (!out.get(a[10], *q, 1)) return not_mine();
+    const size_t need = prefix_ws(B, Hq, Hkv, np, n, d);
+    at::Tensor own;
+    void *ws, *st;
+    size_t bytes;
+    if (!get_workspace(a[11], need, *q, own, ws, bytes)) return not_mine();
+    const c10::DeviceGuard device(q->device());
+    if (!get_stream(*q, st)) return nullptr;
+    const int rc = released([&] {
+      return c_prefix(q->data_ptr(), kn ? kn->data_ptr() : nullptr, kn ? vn->data_ptr() : nullptr, kp->data_ptr(), vp->data_ptr(),
+                      kc->data_ptr(), vc->data_ptr(), lens, out.p[0], (float*)out.p[1], ws, bytes, B, Hq, Hkv, np, n, n_cap, d, scale, 0,
+                      st);
+    });
+    return rc ? PyLong_FromLong(rc) : out.answer(a[10]);
+  });
+}
+
+// bind_cross(cross_fwd_workspace_bytes, cross_fwd, cross_bwd_workspace_bytes, cross_bwd, prefix_decode_workspace_bytes,
+//            prefix_decode [addresses])
+PyObject* bind_cross(PyObject*, PyObject* const* a, Py_ssize_t na) {
+  if (na != 6) {
+    PyErr_SetString(PyExc_TypeError, "bind_cross takes six addresses");
+    return nullptr;
+  }
+  void* p[6];
+  for (int i = 0; i < 6; ++i) {
+    p[i] = PyLong_AsVoidPtr(a[i]);
+    if (!p[i]) {
+      if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "bind_cross: null address");
+      return nullptr;
+    }
+  }
+  cross_fwd_ws = (CrossWsFn)p[0];
+  c_cross_fwd = (CrossFwdFn)p[1];
+  cross_bwd_ws = (CrossWsFn)p[2];
+  c_cross_bwd = (CrossBwdFn)p[3];
+  prefix_ws = (PrefixWsFn)p[4];
+  c_prefix = (PrefixFn)p[5];
+  Py_RETURN_NONE;
+}
+
 #define FAST(f) reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(f)), METH_FASTCALL
 PyMethodDef methods[] = {{"bind", FAST(bind), nullptr},       {"fwd", FAST(fwd), nullptr}, {"fwd_bwd", FAST(fwd_bwd), nullptr},
                          {"bwd", FAST(bwd), nullptr},         {"decode", FAST(decode), nullptr},
                          {"bind_paged", FAST(bind_paged), nullptr}, {"rope", FAST(rope), nullptr},
                          {"paged_append", FAST(paged_append), nullptr}, {"paged_gather", FAST(paged_gather), nullptr},
                          {"paged_decode", FAST(paged_decode), nullptr},
+                         {"bind_cross", FAST(bind_cross), nullptr},     {"cross_fwd", FAST(cross_fwd), nullptr},
+                         {"cross_bwd", FAST(cross_bwd), nullptr},       {"prefix_decode", FAST(prefix_decode), nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -98,7 +98,7 @@ size_t few_bytes(long long rows, int d, int parts) { return parts > 1 ? (size_t)
 struct BwdPlan {
   int q_tiles, q_splits, q_per;   // dQ: 128-query tiles; parts of the 64-key tiles
   int k_tiles, k_splits, k_per;   // dK, dV: 128-key tiles; parts of the query tiles of all heads
-  size_t rows_at, drel_at, dq_at, dk_at, dv_at, bytes;
+  size_t rows_at, drel_at, dq_at, sums_at, dk_at, dv_at, bytes;
 };
 BwdPlan bwd_plan(int B, int Hq, int Hkv, int nq, int nk, int d, int dtype, int R) {
   BwdPlan p;
@@ -120,10 +120,20 @@ BwdPlan bwd_plan(int B, int Hq, int Hkv, int nq, int nk, int d, int dtype, int R
   p.rows_at = 0;
   p.drel_at = up16(2 * qrows * sizeof(float));
   p.dq_at = p.drel_at + (R > 0 ? up16((size_t)B * Hq * p.q_tiles * R * sizeof(float)) : 0);
-  p.dk_at = p.dq_at + (p.q_splits > 1 ? p.q_splits * qrows * d * sizeof(float) : 0);
+  p.sums_at = p.dq_at + (p.q_splits > 1 ? p.q_splits * qrows * d * sizeof(float) : 0);
+  p.dk_at = p.sums_at + (p.q_splits > 1 ? up16(p.q_splits * qrows * sizeof(float)) : 0);
   p.dv_at = p.dk_at + (p.k_splits > 1 ? p.k_splits * krows * d * sizeof(float) : 0);
   p.bytes = p.dv_at + (p.k_splits > 1 ? p.k_splits * krows * d * sizeof(float) : 0);
   return p;
+}
+
+// Whether dS (and, in the smallest calls, P) multiplies in two bf16 parts: see cross_dq_kernel.
+// Rows of 512 keys of unit scores are off by 1.45 times their own rounding without. In calls of
+// few rows chance may make one rounding twice what it is on average; they are bound
+// by latency, which the second product does not change.
+bool few_rows(int B, int Hq, int nq) { return (long long)B * Hq * nq <= 4096; }
+bool two_parts_dq(int B, int Hq, int nq, int nk, int causal, bool bias) {
+  return causal || bias || nk <= 512 || few_rows(B, Hq, nq);
 }
 
 // ---------------------------------------------------------------- launches --
@@ -276,6 +286,7 @@ extern "C" int attn_cross_bwd(const void* q, const void* k, const void* v, const
   CrossArgs aq = a, ak = a;
   aq.ntiles = p.q_tiles; aq.splits = p.q_splits; aq.per = p.q_per; aq.nrows = qrows;
   aq.part = p.q_splits > 1 ? (float*)(ws + p.dq_at) : nullptr;
+  aq.part_ml = (float*)(ws + p.sums_at);
   aq.drel = dbias ? (float*)(ws + p.drel_at) : nullptr;
   set_grid(aq, (long long)B * Hq, p.q_tiles * p.q_splits);
   ak.ntiles = p.k_tiles; ak.splits = p.k_splits; ak.per = p.k_per; ak.nrows = krows;
@@ -290,18 +301,37 @@ extern "C" int attn_cross_bwd(const void* q, const void* k, const void* v, const
     constexpr int D = decltype(dd)::value;
     constexpr bool BIAS = decltype(bb)::value;
     constexpr int rows_per = 256 / (D / attn::Elem<T>::CH);
-    const auto sum = [&](const float* part, void* out, const Strides& s, long long rows, int H, int n, int parts) {
+    const auto sum = [&](const float* part, void* out, const Strides& s, long long rows, int H, int n, int parts, const float* sums) {
       hipLaunchKernelGGL((attn::cross_sum_kernel<T, D>), dim3((unsigned)div_up(rows * (D / 4), 256)), dim3(256), 0, st, part, out, s, rows,
-                         H, n, parts);
+                         H, n, parts, sums, a.dvec);
     };
     hipLaunchKernelGGL((attn::cross_prep_kernel<T, D>), dim3((unsigned)div_up(qrows, rows_per)), dim3(256), 0, st, aq);
-    hipLaunchKernelGGL((attn::cross_dkdv_kernel<T, D, BIAS>), dim3(ak.nblocks), dim3(256), bias_lds(ak, 1), st, ak);
-    hipLaunchKernelGGL((attn::cross_dq_kernel<T, D, BIAS>), dim3(aq.nblocks), dim3(256), bias_lds(aq, aq.drel ? 9 : 1), st, aq);
-    if (p.k_splits > 1) {
-      sum(ak.part, dk, a.dks, krows, Hkv, nk, p.k_splits);
-      sum(ak.part2, dv, a.dvs, krows, Hkv, nk, p.k_splits);
+    const auto dq_of = [&](auto two) {
+      hipLaunchKernelGGL((attn::cross_dq_kernel<T, D, BIAS, decltype(two)::value>), dim3(aq.nblocks), dim3(256),
+                         bias_lds(aq, aq.drel ? 9 : 1), st, aq);
+    };
+    const auto dkdv_of = [&](auto two) {
+      hipLaunchKernelGGL((attn::cross_dkdv_kernel<T, D, BIAS, decltype(two)::value>), dim3(ak.nblocks), dim3(256), bias_lds(ak, 1), st, ak);
+    };
+    bool two = false;
+    if constexpr (std::is_same<T, bf16>::value) {
+      two = two_parts_dq(B, Hq, nq, nk, causal, BIAS);
+      if (two) dq_of(std::true_type{});
+      else if constexpr (!BIAS) dq_of(std::false_type{});
+    } else {
+      dq_of(std::false_type{});
     }
-    if (p.q_splits > 1) sum(aq.part, dq, a.dqs, qrows, Hq, nq, p.q_splits);
+    if (p.q_splits > 1) sum(aq.part, dq, a.dqs, qrows, Hq, nq, p.q_splits, two ? aq.part_ml : nullptr);
+    if constexpr (std::is_same<T, bf16>::value) {
+      if (few_rows(B, Hq, nq)) dkdv_of(std::true_type{});
+      else dkdv_of(std::false_type{});
+    } else {
+      dkdv_of(std::false_type{});
+    }
+    if (p.k_splits > 1) {
+      sum(ak.part, dk, a.dks, krows, Hkv, nk, p.k_splits, nullptr);
+      sum(ak.part2, dv, a.dvs, krows, Hkv, nk, p.k_splits, nullptr);
+    }
     if constexpr (BIAS) {
       if (dbias)
         hipLaunchKernelGGL((attn::cross_dbias_kernel<T>), dim3(Hq), dim3(1024), (a.R + 1024) * sizeof(double), st, aq, dbias);

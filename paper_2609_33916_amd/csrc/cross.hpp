@@ -7,9 +7,9 @@
 //                        rows (query, head of the group) and one part of the keys
 //   cross_merge_kernel   joins the parts by their log-sum-exp
 //   cross_prep_kernel    the backward's row vectors: -D and L in base 2
+//   cross_dq_kernel      dQ and the bias gradient by relative position
 //   cross_dkdv_kernel    dK, dV; a workgroup owns 128 keys of a cache head and
 //                        goes over the queries of all heads of its group
-//   cross_dq_kernel      dQ and the bias gradient by relative position
 //   cross_sum_kernel     adds the parts of a gradient whose sum was split
 //   cross_dbias_kernel   the bias gradient by bucket
 //
@@ -164,6 +164,33 @@ template <int D> __device__ __forceinline__ void mma_tile_cols(f32x16 (&acc)[D /
   for (int t = 0; t < 16; ++t)
 #pragma unroll
     for (int db = 0; db < D / 32; ++db) mma(acc[db], tile[(32 * rb + perm32_inv(16 * h + t)) * (D + 4) + 32 * db + c], b[t]);
+}
+
+// The same with b in two bf16 parts, the float cut to its first 16 bits and the rest
+// rounded: 15 bits of a factor stay instead of 8.
+template <int D> __device__ __forceinline__ void mma_tile_cols2(f32x16 (&acc)[D / 32], const bf16* tile, int rb, const f32x16& b, int h, int c) {
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    u32x4 first;
+    bf16x8 rest;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float x = b[8 * t + 2 * i], y = b[8 * t + 2 * i + 1];
+      first[i] = __builtin_amdgcn_perm(__float_as_uint(y), __float_as_uint(x), 0x07060302u);
+      rest[2 * i] = (bf16)(x - __uint_as_float(__float_as_uint(x) & 0xffff0000u));
+      rest[2 * i + 1] = (bf16)(y - __uint_as_float(__float_as_uint(y) & 0xffff0000u));
+    }
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db) {
+      const bf16x8 v = TransRead<bf16, D>::get(tile, rb, db, t, h, c);
+      mma(acc[db], v, __builtin_bit_cast(bf16x8, first));
+      mma(acc[db], v, rest);
+    }
+  }
+}
+template <bool TWO, int D, typename T> __device__ __forceinline__ void mma_cols_of(f32x16 (&acc)[D / 32], const T* tile, int rb, const f32x16& b, int h, int c) {
+  if constexpr (TWO) mma_tile_cols2<D>(acc, tile, rb, b, h, c);
+  else mma_tile_cols<D>(acc, tile, rb, b, h, c);
 }
 
 // A lane's row, or zeros where it has none
@@ -393,28 +420,6 @@ template <int D> __device__ __forceinline__ void mma_cross_cols(f32x16 (&acc)[D 
     if (t + CrossCols<D>::R < 16) x.get(t + CrossCols<D>::R);
   }
 }
-// acc += columns x p, p in two bf16 parts
-template <int D> __device__ __forceinline__ void mma_cols2(f32x16 (&acc)[D / 32], const bf16* tile, const f32x16& p, int h, int c) {
-#pragma unroll
-  for (int t = 0; t < 2; ++t) {
-    u32x4 first;
-    bf16x8 rest;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float x = p[8 * t + 2 * i], y = p[8 * t + 2 * i + 1];
-      first[i] = __builtin_amdgcn_perm(__float_as_uint(y), __float_as_uint(x), 0x07060302u);
-      rest[2 * i] = (bf16)(x - __uint_as_float(__float_as_uint(x) & 0xffff0000u));
-      rest[2 * i + 1] = (bf16)(y - __uint_as_float(__float_as_uint(y) & 0xffff0000u));
-    }
-#pragma unroll
-    for (int db = 0; db < D / 32; ++db) {
-      const bf16x8 v = TransRead<bf16, D, 32>::get(tile, 0, db, t, h, c);
-      mma(acc[db], v, __builtin_bit_cast(bf16x8, first));
-      mma(acc[db], v, rest);
-    }
-  }
-}
-
 template <typename T, int D> struct FewLds {
   // bf16: K and V tiles of the four waves; both: half of the merge buffer
   static constexpr int FLOATS = sizeof(T) == 2 ? 4 * 2 * 32 * D / 2 : WaveMerge<D>::FLOATS;
@@ -518,7 +523,7 @@ __device__ __forceinline__ void cross_few(const CrossArgs& a, int bid, float* st
       f32x16 s = zero16();
       mma_tile_rows<D>(s, tc, 0, q, h, c);
       softmax(kb, s);
-      mma_cols2<D>(oacc, tc + WT::ELEMS, s, h, c);
+      mma_tile_cols2<D>(oacc, tc + WT::ELEMS, 0, s, h, c);
       __builtin_amdgcn_s_waitcnt(0xC07F);   // reads done (lgkmcnt 0) before the stage is refilled
     };
     for (int kb = b0; kb < nb; kb += 8) {
@@ -736,11 +741,12 @@ template <typename T, int D> __global__ void __launch_bounds__(256) cross_prep_k
 // registers), and goes over the BQ-query tiles of all heads of its group, or, split,
 // over a run of them. Per 32-query block: S = Q K^T, dP = dO V^T (rows = queries),
 // P, dS, dV^T += dO^T P, dK^T += Q^T dS. Query rows past the end have L = +inf: P = 0.
+// TWO: P and dS multiply in two bf16 parts.
 // ======================================================================
 template <typename T, int D> struct CrossDkdv {
   static constexpr int BQ = sizeof(T) == 4 && D == 128 ? 32 : 64;
 };
-template <typename T, int D, bool BIAS>
+template <typename T, int D, bool BIAS, bool TWO>
 __global__ void __launch_bounds__(256, D == 128 ? 1 : 2) cross_dkdv_kernel(const CrossArgs a) {
   constexpr int BKV = 128, BQ = CrossDkdv<T, D>::BQ, NQB = BQ / 32, NDB = D / 32;
   using TL = CrossTile<T, BQ, D>;
@@ -859,8 +865,8 @@ __global__ void __launch_bounds__(256, D == 128 ? 1 : 2) cross_dkdv_kernel(const
           dp[j] = j < lo ? 0.f : dp[j];
         }
       }
-      mma_tile_cols<D>(dv, gc, qb, s, h, c);
-      mma_tile_cols<D>(dk, qc, qb, dp, h, c);
+      mma_cols_of<TWO, D>(dv, gc, qb, s, h, c);
+      mma_cols_of<TWO, D>(dk, qc, qb, dp, h, c);
     }
     if constexpr (!TL::TWO) __syncthreads();
     if (u + 1 < u1) commit(qn, gn, ln);
@@ -894,13 +900,17 @@ __global__ void __launch_bounds__(256, D == 128 ? 1 : 2) cross_dkdv_kernel(const
 // In LDS every wave and lane half has a row of its own: the 64 lanes of one add
 // then go to 64 addresses, and the sums come out the same every time.
 // D comes from an O that was rounded to bf16, so that dS = P (dP - D) is off by P e_i,
-// e_i being D's error. That is far below dQ's and dK's own rounding, but a bucket's sum
-// over whole rows loses almost all of dS, which adds up to 0 in a row, and none of P e_i.
-// The row's sum of dS gives e_i, so P times it is taken from each sum: for the keys
-// beyond the positions of their own from the sums of P there, for the others in a
-// second pass over their tiles (S only).
+// e_i being D's error. A bucket's sum over whole rows loses almost all of dS, which adds
+// up to 0 in a row, and none of P e_i. The row's sum of dS gives e_i, so P times it
+// is taken from each sum: for the keys beyond the positions of their own from the
+// sums of P there, for the others in a second pass over their tiles (S only).
+//
+// TWO (bf16, where rows see few keys, by their number or their mask): P e_i is then as large
+// as dS's rounding to bf16, and dQ would be off by 1.7 times its own last rounding. dS
+// multiplies K in two bf16 parts, and D without e_i goes to the dK/dV kernel, which runs
+// after this one.
 // ======================================================================
-template <typename T, int D, bool BIAS>
+template <typename T, int D, bool BIAS, bool TWO>
 __global__ void __launch_bounds__(256, sizeof(T) == 4 ? 1 : 2) cross_dq_kernel(const CrossArgs a) {
   constexpr int BQ = 128, BKV = 64, NKB = 2, NDB = D / 32;
   using TL = CrossTile<T, BKV, D>;
@@ -1011,11 +1021,14 @@ __global__ void __launch_bounds__(256, sizeof(T) == 4 ? 1 : 2) cross_dq_kernel(c
           dp[j] = j > lim ? 0.f : dp[j];
         }
       }
-      if constexpr (BIAS) {
-        if (grad) {
-          float sd = 0.f, sp = 0.f;
+      if constexpr (BIAS || TWO) {
+        float sd = 0.f;
+        if (TWO || grad) {
 #pragma unroll
           for (int j = 0; j < 16; ++j) sd += dp[j];
+        }
+        if (BIAS && grad) {
+          float sp = 0.f;
           if (side >= 0) {
 #pragma unroll
             for (int j = 0; j < 16; ++j) sp += s[j];
@@ -1032,10 +1045,12 @@ __global__ void __launch_bounds__(256, sizeof(T) == 4 ? 1 : 2) cross_dq_kernel(c
 #pragma unroll
             for (int j = 0; j < 16; ++j) add(kb0, j, dp[j]);
           }
+        } else {
+          s_in += sd;
         }
       }
       __builtin_amdgcn_s_setprio(0);
-      mma_tile_cols<D>(dqa, kc, kb, dp, h, c);
+      mma_cols_of<TWO, D>(dqa, kc, kb, dp, h, c);
     }
     if constexpr (!TL::TWO) __syncthreads();
     if (it + 1 < nt) {
@@ -1053,11 +1068,18 @@ __global__ void __launch_bounds__(256, sizeof(T) == 4 ? 1 : 2) cross_dq_kernel(c
     if (a.part) store_row<float, D>(a.part + ((long long)part * a.nrows + row) * D, dqa, a.scale, h);
     else store_row<T, D>((T*)a.dq + b * a.dqs.b + hq * a.dqs.h + qi * a.dqs.t, dqa, a.scale, h);
   }
+  // -e_i of this lane's query, both halves' keys
+  const float e = halves_sum(s_lo + s_in + s_hi);
+  if constexpr (TWO) {
+    if (qi < a.nq && h == 0) {
+      if (a.part) a.part_ml[part * a.nrows + row] = e;
+      else a.dvec[row] = nd - e;
+    }
+  }
 
   if constexpr (BIAS) {
     if (!grad) return;
-    // -e_i of this lane's query, both halves' keys; P of a row adds up to 1 (0 without keys)
-    const float e = halves_sum(s_lo + s_in + s_hi);
+    // P of a row adds up to 1 (0 without keys)
     const float one = lq < INFINITY ? 1.f : 0.f;
     const float q_in = halves_sum(p_in), q_hi = halves_sum(p_hi);
     float f_lo = halves_sum(s_lo), f_hi = halves_sum(s_hi) - e * q_hi;
@@ -1115,8 +1137,9 @@ __global__ void __launch_bounds__(256, sizeof(T) == 4 ? 1 : 2) cross_dq_kernel(c
 }
 
 // A gradient whose sum was split: rows [rows, D] float32 of `parts` parts, added in order.
-// x: [B, H, n] rows with strides `s`.
-template <typename T, int D> __global__ void __launch_bounds__(256) cross_sum_kernel(const float* part, void* out, Strides s, long long rows, int H, int n, int parts) {
+// out: [B, H, n] rows with strides `s`. sums (or null): parts of a row's sum of dS, taken from dvec.
+template <typename T, int D> __global__ void __launch_bounds__(256) cross_sum_kernel(const float* part, void* out, Strides s, long long rows, int H, int n, int parts,
+                                                                                    const float* sums, float* dvec) {
   constexpr int CG = D / 4;
   const long long i = (long long)blockIdx.x * 256 + threadIdx.x, row = i / CG;
   const int cg = (int)(i % CG);
@@ -1126,6 +1149,11 @@ template <typename T, int D> __global__ void __launch_bounds__(256) cross_sum_ke
   const long long head = row / n;
   const int b = (int)(head / H), hh = (int)(head % H), t = (int)(row % n);
   Quad<T>::store((T*)out + b * s.b + hh * s.h + t * s.t + 4 * cg, x[0], x[1], x[2], x[3]);
+  if (sums && cg == 0) {
+    float e = 0.f;
+    for (int p = 0; p < parts; ++p) e += sums[p * rows + row];
+    dvec[row] -= e;
+  }
 }
 
 // The bias gradient of head blockIdx.x: the dQ workgroups' sums by relative position, then
