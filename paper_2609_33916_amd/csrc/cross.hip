@@ -97,7 +97,7 @@ size_t few_bytes(long long rows, int d, int parts) { return parts > 1 ? (size_t)
 
 struct BwdPlan {
   int q_tiles, q_splits, q_per;   // dQ: 128-query tiles; parts of the 64-key tiles
-  int k_tiles, k_splits, k_per;   // dK, dV: 128-key tiles; parts of the query tiles of all heads
+  int k_tiles, k_splits, k_per;   // dK, dV: 128-key tiles; parts of the query tiles of all heads (or of the heads)
   size_t rows_at, drel_at, dq_at, sums_at, dk_at, dv_at, bytes;
 };
 BwdPlan bwd_plan(int B, int Hq, int Hkv, int nq, int nk, int d, int dtype, int R) {
@@ -110,16 +110,19 @@ BwdPlan bwd_plan(int B, int Hq, int Hkv, int nq, int nk, int d, int dtype, int R
   p.q_tiles = (int)div_up(nq, 128);
   p.k_tiles = (int)div_up(nk, 128);
   parts((long long)B * Hq * p.q_tiles, div_up(nk, 64), p.q_splits, p.q_per);
-  if (R > 0) {   // a row's sum of dS is formed in one workgroup
-    p.q_splits = 1;
-    p.q_per = (int)div_up(nk, 64);
+  const int G = Hq / Hkv;
+  const long long groups = (long long)B * Hkv * p.k_tiles;
+  if (R > 0) {   // the bias gradient of a head and key block is formed in one workgroup: parts are runs of heads
+    p.k_splits = groups >= 256 ? 1 : (int)std::min<long long>(512 / groups, G);
+    p.k_per = (int)div_up(G, p.k_splits);
+    p.k_splits = (int)div_up(G, p.k_per);
+  } else {
+    parts(groups, G * div_up(nq, dtype == ATTN_F32 && d == 128 ? 32 : 64), p.k_splits, p.k_per);
   }
-  const int bq = dtype == ATTN_F32 && d == 128 ? 32 : 64;
-  parts((long long)B * Hkv * p.k_tiles, (Hq / Hkv) * div_up(nq, bq), p.k_splits, p.k_per);
   const size_t qrows = (size_t)B * Hq * nq, krows = (size_t)B * Hkv * nk;
   p.rows_at = 0;
   p.drel_at = up16(2 * qrows * sizeof(float));
-  p.dq_at = p.drel_at + (R > 0 ? up16((size_t)B * Hq * p.q_tiles * R * sizeof(float)) : 0);
+  p.dq_at = p.drel_at + (R > 0 ? up16((size_t)B * Hq * p.k_tiles * R * sizeof(float)) : 0);
   p.sums_at = p.dq_at + (p.q_splits > 1 ? p.q_splits * qrows * d * sizeof(float) : 0);
   p.dk_at = p.sums_at + (p.q_splits > 1 ? up16(p.q_splits * qrows * sizeof(float)) : 0);
   p.dv_at = p.dk_at + (p.k_splits > 1 ? p.k_splits * krows * d * sizeof(float) : 0);
@@ -127,12 +130,12 @@ BwdPlan bwd_plan(int B, int Hq, int Hkv, int nq, int nk, int d, int dtype, int R
   return p;
 }
 
-// Whether dS (and, in the smallest calls, P) multiplies in two bf16 parts: see cross_dq_kernel.
-// Rows of 512 keys of unit scores are off by 1.45 times their own rounding without. In calls of
+// Whether dQ is formed with dS in two bf16 parts and D corrected (FIX of cross_dq_kernel), and in the smallest
+// calls dK and dV with P and dS in two parts. Rows of 512 keys of unit scores are off by 1.45 times their own rounding without. In calls of
 // few rows chance may make one rounding twice what it is on average; they are bound
 // by latency, which the second product does not change.
 bool few_rows(int B, int Hq, int nq) { return (long long)B * Hq * nq <= 4096; }
-bool two_parts_dq(int B, int Hq, int nq, int nk, int causal, bool bias) {
+bool fix_dq(int B, int Hq, int nq, int nk, int causal, bool bias) {
   return causal || bias || nk <= 512 || few_rows(B, Hq, nq);
 }
 
@@ -152,7 +155,11 @@ template <typename F> void dispatch(int dtype, int d, bool bias, F&& f) {
   else with_bias(0.f);
 }
 
-size_t bias_lds(const CrossArgs& a, int vectors) { return a.table ? (size_t)vectors * (a.R + 2 * attn::kBiasPad) * sizeof(float) : 0; }
+size_t bias_lds(const CrossArgs& a, bool grad = false) {
+  if (!a.table) return 0;
+  const size_t row = (a.R + 2 * attn::kBiasPad + 3) & ~3;
+  return (grad ? 5 * row + 4 * attn::kDiagTile : row) * sizeof(float);
+}
 
 // Blocks and order of a grid of `heads` heads of `tiles` tiles each
 void set_grid(CrossArgs& a, long long heads, int tiles) {
@@ -223,7 +230,7 @@ extern "C" int attn_cross_fwd(const void* q, const void* k, const void* v, void*
     dispatch(dtype, d, bias != nullptr, [&](auto t, auto dd, auto bb) {
       using T = decltype(t);
       constexpr int D = decltype(dd)::value;
-      hipLaunchKernelGGL((attn::cross_few_kernel<T, D, decltype(bb)::value>), dim3(a.nblocks), dim3(256), bias_lds(a, 1), st, a);
+      hipLaunchKernelGGL((attn::cross_few_kernel<T, D, decltype(bb)::value>), dim3(a.nblocks), dim3(256), bias_lds(a), st, a);
       if (a.splits > 1) hipLaunchKernelGGL((attn::cross_merge_kernel<T, D>), dim3((unsigned)div_up(rows, 4)), dim3(256), 0, st, a);
     });
   } else {
@@ -231,7 +238,7 @@ extern "C" int attn_cross_fwd(const void* q, const void* k, const void* v, void*
     set_grid(a, (long long)B * Hq, a.ntiles);
     dispatch(dtype, d, bias != nullptr, [&](auto t, auto dd, auto bb) {
       hipLaunchKernelGGL((attn::cross_fwd_kernel<decltype(t), decltype(dd)::value, decltype(bb)::value>), dim3(a.nblocks), dim3(256),
-                         bias_lds(a, 1), st, a);
+                         bias_lds(a), st, a);
     });
   }
   return launched();
@@ -287,11 +294,11 @@ extern "C" int attn_cross_bwd(const void* q, const void* k, const void* v, const
   aq.ntiles = p.q_tiles; aq.splits = p.q_splits; aq.per = p.q_per; aq.nrows = qrows;
   aq.part = p.q_splits > 1 ? (float*)(ws + p.dq_at) : nullptr;
   aq.part_ml = (float*)(ws + p.sums_at);
-  aq.drel = dbias ? (float*)(ws + p.drel_at) : nullptr;
   set_grid(aq, (long long)B * Hq, p.q_tiles * p.q_splits);
   ak.ntiles = p.k_tiles; ak.splits = p.k_splits; ak.per = p.k_per; ak.nrows = krows;
   ak.part = p.k_splits > 1 ? (float*)(ws + p.dk_at) : nullptr;
   ak.part2 = (float*)(ws + p.dv_at);
+  ak.drel = dbias ? (float*)(ws + p.drel_at) : nullptr;
   ak.nblocks = (int)k_blocks;
 
   hipStream_t st = static_cast<hipStream_t>(stream);
@@ -308,20 +315,24 @@ extern "C" int attn_cross_bwd(const void* q, const void* k, const void* v, const
     hipLaunchKernelGGL((attn::cross_prep_kernel<T, D>), dim3((unsigned)div_up(qrows, rows_per)), dim3(256), 0, st, aq);
     const auto dq_of = [&](auto two) {
       hipLaunchKernelGGL((attn::cross_dq_kernel<T, D, BIAS, decltype(two)::value>), dim3(aq.nblocks), dim3(256),
-                         bias_lds(aq, aq.drel ? 9 : 1), st, aq);
+                         bias_lds(aq), st, aq);
     };
     const auto dkdv_of = [&](auto two) {
-      hipLaunchKernelGGL((attn::cross_dkdv_kernel<T, D, BIAS, decltype(two)::value>), dim3(ak.nblocks), dim3(256), bias_lds(ak, 1), st, ak);
+      hipLaunchKernelGGL((attn::cross_dkdv_kernel<T, D, BIAS, decltype(two)::value>), dim3(ak.nblocks), dim3(256), bias_lds(ak, ak.drel), st,
+                         ak);
     };
-    bool two = false;
-    if constexpr (std::is_same<T, bf16>::value) {
-      two = two_parts_dq(B, Hq, nq, nk, causal, BIAS);
-      if (two) dq_of(std::true_type{});
-      else if constexpr (!BIAS) dq_of(std::false_type{});
+    const bool fix = BIAS || (std::is_same<T, bf16>::value && fix_dq(B, Hq, nq, nk, causal, BIAS));
+    if constexpr (BIAS) {
+      dq_of(std::true_type{});
     } else {
-      dq_of(std::false_type{});
+      if constexpr (std::is_same<T, bf16>::value) {
+        if (fix) dq_of(std::true_type{});
+        else dq_of(std::false_type{});
+      } else {
+        dq_of(std::false_type{});
+      }
     }
-    if (p.q_splits > 1) sum(aq.part, dq, a.dqs, qrows, Hq, nq, p.q_splits, two ? aq.part_ml : nullptr);
+    if (p.q_splits > 1) sum(aq.part, dq, a.dqs, qrows, Hq, nq, p.q_splits, fix ? aq.part_ml : nullptr);
     if constexpr (std::is_same<T, bf16>::value) {
       if (few_rows(B, Hq, nq)) dkdv_of(std::true_type{});
       else dkdv_of(std::false_type{});
@@ -334,7 +345,8 @@ extern "C" int attn_cross_bwd(const void* q, const void* k, const void* v, const
     }
     if constexpr (BIAS) {
       if (dbias)
-        hipLaunchKernelGGL((attn::cross_dbias_kernel<T>), dim3(Hq), dim3(1024), (a.R + 1024) * sizeof(double), st, aq, dbias);
+        hipLaunchKernelGGL((attn::cross_dbias_kernel<T>), dim3(Hq), dim3(1024), (a.R + 1024) * sizeof(double) + a.R * sizeof(int), st,
+                           ak, dbias);
     }
   });
   return launched();

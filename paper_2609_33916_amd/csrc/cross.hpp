@@ -737,15 +737,154 @@ template <typename T, int D> __global__ void __launch_bounds__(256) cross_prep_k
 }
 
 // ======================================================================
+// dQ: a workgroup owns 128 queries of a head, 32 per wave (Q and dO rows in
+// registers), and goes over the 64-key tiles of K and V that they see, or a run of
+// them. Per 32-key block: S^T = K Q^T, dP^T = V dO^T, dS^T, dQ^T += K^T dS^T.
+//
+// FIX (a bias, or bf16 where rows see few keys, by their number or their mask): D comes from
+// an O that was rounded, so that dS = P (dP - D) is off by P e_i, e_i being D's error.
+// Where few keys share a row that is as large as dS's own rounding to bf16, and a
+// bucket's sum over whole rows loses almost all of dS, which adds up to 0 in a row, and
+// none of P e_i. The row's sum of dS is -e_i (P adds up to 1): D without it goes to the dK/dV
+// kernel, which runs after this one and forms the bias gradient, and here dS multiplies K in two
+// bf16 parts, so that dQ's error is e_i's and its own last rounding.
+// ======================================================================
+template <typename T, int D, bool BIAS, bool FIX>
+__global__ void __launch_bounds__(256, sizeof(T) == 4 ? 1 : 2) cross_dq_kernel(const CrossArgs a) {
+  constexpr int BQ = 128, BKV = 64, NKB = 2, NDB = D / 32;
+  using TL = CrossTile<T, BKV, D>;
+  __shared__ __attribute__((aligned(16))) T stA[2][TL::ELEMS];
+  __shared__ __attribute__((aligned(16))) T stB[2][TL::TWO ? TL::ELEMS : 8];
+  extern __shared__ __attribute__((aligned(16))) float bv[];
+
+  const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, c = lane & 31;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  int head, tile;
+  block_map(blockIdx.x, a.nblocks, a.ntiles * a.splits, a.hgroup, a.causal, head, tile);
+  const int qt = tile / a.splits, part = tile - qt * a.splits;
+  const int b = head / a.Hq, hq = head - b * a.Hq, hk = hq / a.G;
+  const int n = seq_len(a, b), start = seq_start(a, b);
+  const int q0 = qt * BQ, qw0 = q0 + 32 * w, qi = qw0 + c;
+  const T* Kg = (const T*)a.k + b * a.ks.b + hk * a.ks.h;
+  const T* Vg = (const T*)a.v + b * a.vs.b + hk * a.vs.h;
+  const int kv_end = a.causal ? max(0, min(n, start + min(q0 + BQ, a.nq))) : n;
+  const int it0 = part * a.per, nt = min((kv_end + BKV - 1) / BKV, it0 + a.per);
+
+  TL kld(w, lane, a.ks.t), vld(w, lane, a.vs.t);
+  auto issue = [&](TL& ld, T* lds, const T* g, long long st, int it) __attribute__((always_inline)) {
+    ld.issue(lds, g + (long long)it * BKV * st, st, n - it * BKV);
+  };
+  if (it0 < nt) {
+    issue(kld, stA[0], Kg, a.ks.t, it0);
+    issue(vld, stA[1], Vg, a.vs.t, it0);
+    kld.commit(stA[0]);
+    vld.commit(stA[1]);
+  }
+  RowRegs<T, D> q, g;
+  load_row<T, D>(q, (const T*)a.q + b * a.qs.b + hq * a.qs.h + qi * a.qs.t, qi < a.nq, h, a.qflip);
+  load_row<T, D>(g, (const T*)a.dout + b * a.gs.b + hq * a.gs.h + qi * a.gs.t, qi < a.nq, h);
+  const long long row = (long long)head * a.nq + qi;
+  const float lq = qi < a.nq ? a.lse2[row] : INFINITY, nd = qi < a.nq ? a.dvec[row] : 0.f;
+  if constexpr (BIAS) bias_fill<T>(bv, a, hq, tid);
+  __syncthreads();
+
+  f32x16 dqa[NDB];
+#pragma unroll
+  for (int db = 0; db < NDB; ++db) dqa[db] = zero16();
+  const float sl2 = a.sl2;
+  float sum = 0.f;   // of this lane's dS
+
+  auto step = [&](int it, T* kc, T* vc, T* kn, T* vn) __attribute__((always_inline)) {
+    const int kv0 = it * BKV;
+    if (it + 1 < nt) {
+      issue(kld, kn, Kg, a.ks.t, it + 1);
+      issue(vld, vn, Vg, a.vs.t, it + 1);
+    }
+#pragma unroll
+    for (int kb = 0; kb < NKB; ++kb) {
+      const int kb0 = kv0 + 32 * kb;
+      if (kb0 >= n || (a.causal && kb0 > start + qw0 + 31)) continue;
+      __builtin_amdgcn_s_setprio(1);
+      f32x16 s = zero16(), dp = zero16();
+      mma_tile_rows<D>(s, kc, kb, q, h, c);
+      mma_tile_rows<D>(dp, vc, kb, g, h, c);
+      // lane (h, c): element j is key kb0 + 16 h + j, query qi
+      if constexpr (BIAS) {
+        const int side = bias_side(a, kb0 - (start + qw0 + 31), kb0 + 31 - (start + qw0));
+        if (side != 0) {
+          const float u = bv[side < 0 ? 0 : a.R + 2 * kBiasPad - 1] - lq;
+#pragma unroll
+          for (int j = 0; j < 16; ++j) s[j] = fmaf(s[j], sl2, u);
+        } else {
+          const float* p = bv + (kBiasPad - a.first + kb0 + 16 * h - start - qi);
+#pragma unroll
+          for (int j = 0; j < 16; ++j) s[j] = fmaf(s[j], sl2, p[j] - lq);
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < 16; ++j) dp[j] = exp2_fast(BIAS ? s[j] : fmaf(s[j], sl2, -lq)) * (dp[j] + nd);   // nd holds -D
+      if (kb0 + 31 >= n || (a.causal && kb0 + 31 > start + qw0)) {
+        const int lim = (a.causal ? min(start + qi, n - 1) : n - 1) - (kb0 + 16 * h);
+#pragma unroll
+        for (int j = 0; j < 16; ++j) dp[j] = j > lim ? 0.f : dp[j];
+      }
+      if constexpr (FIX) {
+        float x = 0.f;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) x += dp[j];
+        sum += x;
+      }
+      __builtin_amdgcn_s_setprio(0);
+      mma_cols_of<FIX && sizeof(T) == 2, D>(dqa, kc, kb, dp, h, c);
+    }
+    if constexpr (!TL::TWO) __syncthreads();
+    if (it + 1 < nt) {
+      kld.commit(kn);
+      vld.commit(vn);
+    }
+    __syncthreads();
+  };
+  for (int it = it0; it < nt; it += 2) {
+    step(it, stA[0], stA[1], TL::TWO ? stB[0] : stA[0], TL::TWO ? stB[1] : stA[1]);
+    if (it + 1 < nt) step(it + 1, TL::TWO ? stB[0] : stA[0], TL::TWO ? stB[1] : stA[1], stA[0], stA[1]);
+  }
+
+  if (qi < a.nq) {
+    if (a.part) store_row<float, D>(a.part + ((long long)part * a.nrows + row) * D, dqa, a.scale, h);
+    else store_row<T, D>((T*)a.dq + b * a.dqs.b + hq * a.dqs.h + qi * a.dqs.t, dqa, a.scale, h);
+  }
+  if constexpr (FIX) {
+    const float e = halves_sum(sum);   // both halves' keys
+    if (qi < a.nq && h == 0) {
+      if (a.part) a.part_ml[part * a.nrows + row] = e;
+      else a.dvec[row] = nd - e;
+    }
+  }
+}
+
+// ======================================================================
 // dK, dV: a workgroup owns 128 keys of a cache head, 32 per wave (K and V rows in
 // registers), and goes over the BQ-query tiles of all heads of its group, or, split,
 // over a run of them. Per 32-query block: S = Q K^T, dP = dO V^T (rows = queries),
 // P, dS, dV^T += dO^T P, dK^T += Q^T dS. Query rows past the end have L = +inf: P = 0.
 // TWO: P and dS multiply in two bf16 parts.
+//
+// The bias gradient (drel, a row [R] for each query head and key block): dS is added up
+// by relative position. Blocks before or behind the positions that have a bias of their
+// own go into one register each; in the others a wave passes its 32 x 32 dS through LDS,
+// where lane l adds up the diagonal key - query = 32 - l, and adds the 64 sums to its own
+// row of positions. Always the same lanes add the same values, so the result is the same
+// every time. (ds_add_f32 takes its 64 lanes one after another: 16 of them a block made a
+// step of 16 x 8 heads, n = 512, d = 64 as slow as five without a gradient.)
 // ======================================================================
 template <typename T, int D> struct CrossDkdv {
   static constexpr int BQ = sizeof(T) == 4 && D == 128 ? 32 : 64;
 };
+// A wave's dS as [key][query], rows 68 floats apart with zeros behind the 32 queries and before the first row:
+// element (c, c - x) is there for every key c and every x from -31 to 32, and zero beyond the block. 16-byte
+// writes of 16 keys and 4-byte reads along diagonals fall on distinct banks.
+constexpr int kDiagRow = 68, kDiagLead = 36, kDiagTile = kDiagLead + 32 * kDiagRow;
+
 template <typename T, int D, bool BIAS, bool TWO>
 __global__ void __launch_bounds__(256, D == 128 ? 1 : 2) cross_dkdv_kernel(const CrossArgs a) {
   constexpr int BKV = 128, BQ = CrossDkdv<T, D>::BQ, NQB = BQ / 32, NDB = D / 32;
@@ -754,7 +893,8 @@ __global__ void __launch_bounds__(256, D == 128 ? 1 : 2) cross_dkdv_kernel(const
   __shared__ __attribute__((aligned(16))) T stB[2][TL::TWO ? TL::ELEMS : 8];
   __shared__ __attribute__((aligned(16))) float ldA[2][BQ];
   __shared__ __attribute__((aligned(16))) float ldB[2][TL::TWO ? BQ : 4];
-  extern __shared__ __attribute__((aligned(16))) float bv[];
+  __shared__ float far[2][4];
+  extern __shared__ __attribute__((aligned(16))) float bv[];   // bias [RP]; with a gradient sums [4 waves][RP], diagonals [4 waves]
 
   const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, c = lane & 31;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -764,12 +904,16 @@ __global__ void __launch_bounds__(256, D == 128 ? 1 : 2) cross_dkdv_kernel(const
   const int b = head / a.Hkv, hk = head - b * a.Hkv;
   const int n = seq_len(a, b), start = seq_start(a, b);
   const int k0 = kt * BKV, kw0 = k0 + 32 * w, kj = kw0 + c;
+  const int RP = (a.R + 2 * kBiasPad + 3) & ~3;
+  const bool grad = BIAS && a.drel;
 
-  // query tiles [t0, nqt) of every head see the block; the part's are u0 to u1 of them all
+  // query tiles [t0, nqt) of every head see the block; the part's are u0 to u1 of them all, with a
+  // bias gradient those of whole heads
   const int nqt = (a.nq + BQ - 1) / BQ;
   const int t0 = a.causal ? min(nqt, max(0, k0 - start) / BQ) : 0, per_head = nqt - t0;
   const int all = k0 < n ? a.G * per_head : 0;
-  const int u0 = min(all, part * a.per), u1 = min(all, u0 + a.per);
+  const int per = grad ? a.per * per_head : a.per;
+  const int u0 = min(all, part * per), u1 = min(all, u0 + per);
 
   TL qld(w, lane, a.qs.t), gld(w, lane, a.gs.t);
   float lreg = 0.f;
@@ -806,7 +950,44 @@ __global__ void __launch_bounds__(256, D == 128 ? 1 : 2) cross_dkdv_kernel(const
   for (int db = 0; db < NDB; ++db) dk[db] = dv[db] = zero16();
   const float sl2 = a.sl2;
   int bias_head = -1;   // of the group, whose bias LDS holds
+  float* const sums = bv + RP * (1 + w);
+  float* const diag = bv + 5 * RP + kDiagTile * w + kDiagLead;
+  float s_lo = 0.f, s_hi = 0.f;   // of this lane's dS: before and behind the positions of their own
+  auto clear = [&]() __attribute__((always_inline)) {
+    for (int t = lane; t < RP; t += 64) sums[t] = 0.f;
+    s_lo = s_hi = 0.f;
+  };
+  if (grad) {
+    clear();
+    for (int t = lane - kDiagLead; t < 32 * kDiagRow; t += 64) diag[t] = 0.f;
+  }
   __syncthreads();
+
+  // The sums of head g of the group to its row; the ends take what lies beyond. Between barriers.
+  auto flush = [&](int g) __attribute__((always_inline)) {
+    float* const out = a.drel + (((long long)b * a.Hq + hk * a.G + g) * a.ntiles + kt) * a.R;
+#pragma unroll
+    for (int x = 1; x < 64; x <<= 1) {
+      s_lo += __shfl_xor(s_lo, x);
+      s_hi += __shfl_xor(s_hi, x);
+    }
+    if (lane == 0) {
+      far[0][w] = s_lo;
+      far[1][w] = s_hi;
+    }
+    __syncthreads();
+    auto sum4 = [&](int t) __attribute__((always_inline)) -> float { return bv[RP + t] + bv[2 * RP + t] + bv[3 * RP + t] + bv[4 * RP + t]; };
+    for (int t = 1 + tid; t < a.R - 1; t += 256) out[t] = sum4(kBiasPad + t);
+    if (w < 2) {
+      const int from = w == 0 ? 0 : kBiasPad + a.R - 1;
+      float x = 0.f;
+      for (int t = lane; t <= kBiasPad; t += 64) x += sum4(from + t);
+#pragma unroll
+      for (int y = 1; y < 64; y <<= 1) x += __shfl_xor(x, y);
+      x += far[w][0] + far[w][1] + far[w][2] + far[w][3];
+      if (lane == 0) out[w == 0 ? 0 : a.R - 1] = x;
+    }
+  };
 
   auto step = [&](int u, T* qc, T* gc, float* lc, T* qn, T* gn, float* ln) __attribute__((always_inline)) {
     int g, q0;
@@ -814,6 +995,11 @@ __global__ void __launch_bounds__(256, D == 128 ? 1 : 2) cross_dkdv_kernel(const
     if (u + 1 < u1) issue(u + 1, qn, gn);
     if constexpr (BIAS) {
       if (g != bias_head) {   // the last step ended on a barrier
+        if (grad && bias_head >= 0) {
+          flush(bias_head);
+          __syncthreads();
+          clear();
+        }
         bias_fill<T>(bv, a, hk * a.G + g, tid);
         bias_head = g;
         __syncthreads();
@@ -827,26 +1013,21 @@ __global__ void __launch_bounds__(256, D == 128 ? 1 : 2) cross_dkdv_kernel(const
       mma_tile_rows<D>(s, qc, qb, k, h, c);
       mma_tile_rows<D>(dp, gc, qb, v, h, c);
       // lane (h, c): element j is query qp0 + 16 h + j, key kj
-      float u_bias = 0.f;
-      const float* p = nullptr;
-      bool each = false;
+      int side = 0;
       if constexpr (BIAS) {
-        const int side = bias_side(a, kw0 - (start + qp0 + 31), kw0 + 31 - (start + qp0));
-        each = side == 0;
-        if (each) p = bv + (kBiasPad - a.first + kj - start - qp0 - 16 * h);
-        else u_bias = bv[side < 0 ? 0 : a.R + 2 * kBiasPad - 1];
-      }
-      const bool edge = kw0 + 31 >= n || (a.causal && start + qp0 < kw0 + 31);
-      const int lo = kj >= n ? 16 : a.causal ? kj - start - (qp0 + 16 * h) : 0;
-      if constexpr (BIAS) {
-        if (each) {
+        side = bias_side(a, kw0 - (start + qp0 + 31), kw0 + 31 - (start + qp0));
+        if (side == 0) {
+          const float* p = bv + (kBiasPad - a.first + kj - start - qp0 - 16 * h);
 #pragma unroll
           for (int j = 0; j < 16; ++j) s[j] = fmaf(s[j], sl2, p[-j]);
         } else {
+          const float u_bias = bv[side < 0 ? 0 : a.R + 2 * kBiasPad - 1];
 #pragma unroll
           for (int j = 0; j < 16; ++j) s[j] = fmaf(s[j], sl2, u_bias);
         }
       }
+      const bool edge = kw0 + 31 >= n || (a.causal && start + qp0 < kw0 + 31);
+      const int lo = kj >= n ? 16 : a.causal ? kj - start - (qp0 + 16 * h) : 0;
 #pragma unroll
       for (int j4 = 0; j4 < 4; ++j4) {
         const f32x4 l4 = *(const f32x4*)&lc[32 * qb + 16 * h + 4 * j4];
@@ -863,6 +1044,26 @@ __global__ void __launch_bounds__(256, D == 128 ? 1 : 2) cross_dkdv_kernel(const
         for (int j = 0; j < 16; ++j) {
           s[j] = j < lo ? 0.f : s[j];
           dp[j] = j < lo ? 0.f : dp[j];
+        }
+      }
+      if constexpr (BIAS) {
+        if (grad) {
+          if (side != 0) {
+            float x = 0.f;
+#pragma unroll
+            for (int j = 0; j < 16; ++j) x += dp[j];
+            if (side < 0) s_lo += x;
+            else s_hi += x;
+          } else {
+#pragma unroll
+            for (int j = 0; j < 16; j += 4)
+              *(f32x4*)(diag + kDiagRow * c + 16 * h + j) = (f32x4){dp[j], dp[j + 1], dp[j + 2], dp[j + 3]};
+            const float* const p = diag + lane - 32;   // key t, query t - (32 - lane)
+            float x = 0.f;
+#pragma unroll
+            for (int t = 0; t < 32; ++t) x += p[t * (kDiagRow + 1)];
+            sums[kBiasPad - a.first + kw0 - start - qp0 + 32 - lane] += x;
+          }
         }
       }
       mma_cols_of<TWO, D>(dv, gc, qb, s, h, c);
@@ -888,250 +1089,14 @@ __global__ void __launch_bounds__(256, D == 128 ? 1 : 2) cross_dkdv_kernel(const
       store_row<T, D>((T*)a.dv + b * a.dvs.b + hk * a.dvs.h + kj * a.dvs.t, dv, 1.f, h);
     }
   }
-}
-
-// ======================================================================
-// dQ: a workgroup owns 128 queries of a head, 32 per wave (Q and dO rows in
-// registers), and goes over the 64-key tiles of K and V that they see, or a run of
-// them. Per 32-key block: S^T = K Q^T, dP^T = V dO^T, dS^T, dQ^T += K^T dS^T.
-//
-// The bias gradient (drel): dS is added up by relative position, in LDS where a tile
-// reaches into the positions that have a bias of their own, in registers elsewhere.
-// In LDS every wave and lane half has a row of its own: the 64 lanes of one add
-// then go to 64 addresses, and the sums come out the same every time.
-// D comes from an O that was rounded to bf16, so that dS = P (dP - D) is off by P e_i,
-// e_i being D's error. A bucket's sum over whole rows loses almost all of dS, which adds
-// up to 0 in a row, and none of P e_i. The row's sum of dS gives e_i, so P times it
-// is taken from each sum: for the keys beyond the positions of their own from the
-// sums of P there, for the others in a second pass over their tiles (S only).
-//
-// TWO (bf16, where rows see few keys, by their number or their mask): P e_i is then as large
-// as dS's rounding to bf16, and dQ would be off by 1.7 times its own last rounding. dS
-// multiplies K in two bf16 parts, and D without e_i goes to the dK/dV kernel, which runs
-// after this one.
-// ======================================================================
-template <typename T, int D, bool BIAS, bool TWO>
-__global__ void __launch_bounds__(256, sizeof(T) == 4 ? 1 : 2) cross_dq_kernel(const CrossArgs a) {
-  constexpr int BQ = 128, BKV = 64, NKB = 2, NDB = D / 32;
-  using TL = CrossTile<T, BKV, D>;
-  __shared__ __attribute__((aligned(16))) T stA[2][TL::ELEMS];
-  __shared__ __attribute__((aligned(16))) T stB[2][TL::TWO ? TL::ELEMS : 8];
-  __shared__ float far[2][4];
-  extern __shared__ __attribute__((aligned(16))) float bv[];   // bias [RP], then sums [4 waves][2 halves][RP]
-
-  const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, c = lane & 31;
-  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-  int head, tile;
-  block_map(blockIdx.x, a.nblocks, a.ntiles * a.splits, a.hgroup, a.causal, head, tile);
-  const int qt = tile / a.splits, part = tile - qt * a.splits;
-  const int b = head / a.Hq, hq = head - b * a.Hq, hk = hq / a.G;
-  const int n = seq_len(a, b), start = seq_start(a, b);
-  const int q0 = qt * BQ, qw0 = q0 + 32 * w, qi = qw0 + c;
-  const T* Kg = (const T*)a.k + b * a.ks.b + hk * a.ks.h;
-  const T* Vg = (const T*)a.v + b * a.vs.b + hk * a.vs.h;
-  const int kv_end = a.causal ? max(0, min(n, start + min(q0 + BQ, a.nq))) : n;
-  const int it0 = part * a.per, nt = min((kv_end + BKV - 1) / BKV, it0 + a.per);
-  const int RP = a.R + 2 * kBiasPad;
-  const bool grad = BIAS && a.drel;
-
-  TL kld(w, lane, a.ks.t), vld(w, lane, a.vs.t);
-  auto issue = [&](TL& ld, T* lds, const T* g, long long st, int it) __attribute__((always_inline)) {
-    ld.issue(lds, g + (long long)it * BKV * st, st, n - it * BKV);
-  };
-  if (it0 < nt) {
-    issue(kld, stA[0], Kg, a.ks.t, it0);
-    issue(vld, stA[1], Vg, a.vs.t, it0);
-    kld.commit(stA[0]);
-    vld.commit(stA[1]);
-  }
-  RowRegs<T, D> q, g;
-  load_row<T, D>(q, (const T*)a.q + b * a.qs.b + hq * a.qs.h + qi * a.qs.t, qi < a.nq, h, a.qflip);
-  load_row<T, D>(g, (const T*)a.dout + b * a.gs.b + hq * a.gs.h + qi * a.gs.t, qi < a.nq, h);
-  const long long row = (long long)head * a.nq + qi;
-  const float lq = qi < a.nq ? a.lse2[row] : INFINITY, nd = qi < a.nq ? a.dvec[row] : 0.f;
-  float* const mine = bv + RP * (1 + 2 * w + h);
   if constexpr (BIAS) {
-    bias_fill<T>(bv, a, hq, tid);
-    if (grad)
-      for (int t = tid; t < 8 * RP; t += 256) bv[RP + t] = 0.f;
-  }
-  __syncthreads();
-
-  f32x16 dqa[NDB];
-#pragma unroll
-  for (int db = 0; db < NDB; ++db) dqa[db] = zero16();
-  const float sl2 = a.sl2;
-  // of this lane's keys: sums of dS before, among and behind the positions of their own, of P among and behind
-  float s_lo = 0.f, s_in = 0.f, s_hi = 0.f, p_in = 0.f, p_hi = 0.f;
-  bool met_lo = false;   // wave-uniform
-
-  // x in base 2 less L of block kb of the tile at kv0, from the raw scores; returns the side
-  auto shift = [&](f32x16& s, int kb0) __attribute__((always_inline)) -> int {
-    int side = 0;
-    if constexpr (BIAS) {
-      side = bias_side(a, kb0 - (start + qw0 + 31), kb0 + 31 - (start + qw0));
-      if (side != 0) {
-        const float u = bv[side < 0 ? 0 : RP - 1] - lq;
-#pragma unroll
-        for (int j = 0; j < 16; ++j) s[j] = fmaf(s[j], sl2, u);
-      } else {
-        const float* p = bv + (kBiasPad - a.first + kb0 + 16 * h - start - qi);
-#pragma unroll
-        for (int j = 0; j < 16; ++j) s[j] = fmaf(s[j], sl2, p[j] - lq);
+    if (grad && bias_head >= 0) {
+      flush(bias_head);
+    } else if (grad) {   // no query sees these keys
+      for (int g = part * a.per; g < min(a.G, (part + 1) * a.per); ++g) {
+        float* const out = a.drel + (((long long)b * a.Hq + hk * a.G + g) * a.ntiles + kt) * a.R;
+        for (int t = tid; t < a.R; t += 256) out[t] = 0.f;
       }
-    } else {
-#pragma unroll
-      for (int j = 0; j < 16; ++j) s[j] = fmaf(s[j], sl2, -lq);
-    }
-    return side;
-  };
-  auto lim_of = [&](int kb0) __attribute__((always_inline)) -> int {
-    return (a.causal ? min(start + qi, n - 1) : n - 1) - (kb0 + 16 * h);
-  };
-  auto add = [&](int kb0, int j, float x) __attribute__((always_inline)) {
-    __hip_atomic_fetch_add(mine + (kBiasPad - a.first + kb0 + 16 * h - start - qi + j), x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
-  };
-
-  auto step = [&](int it, T* kc, T* vc, T* kn, T* vn) __attribute__((always_inline)) {
-    const int kv0 = it * BKV;
-    if (it + 1 < nt) {
-      issue(kld, kn, Kg, a.ks.t, it + 1);
-      issue(vld, vn, Vg, a.vs.t, it + 1);
-    }
-#pragma unroll
-    for (int kb = 0; kb < NKB; ++kb) {
-      const int kb0 = kv0 + 32 * kb;
-      if (kb0 >= n || (a.causal && kb0 > start + qw0 + 31)) continue;
-      __builtin_amdgcn_s_setprio(1);
-      f32x16 s = zero16(), dp = zero16();
-      mma_tile_rows<D>(s, kc, kb, q, h, c);
-      mma_tile_rows<D>(dp, vc, kb, g, h, c);
-      const int side = shift(s, kb0);
-      // lane (h, c): element j is key kb0 + 16 h + j, query qi
-#pragma unroll
-      for (int j = 0; j < 16; ++j) {
-        s[j] = exp2_fast(s[j]);
-        dp[j] = s[j] * (dp[j] + nd);   // nd holds -D
-      }
-      if (kb0 + 31 >= n || (a.causal && kb0 + 31 > start + qw0)) {
-        const int lim = lim_of(kb0);
-#pragma unroll
-        for (int j = 0; j < 16; ++j) {
-          s[j] = j > lim ? 0.f : s[j];
-          dp[j] = j > lim ? 0.f : dp[j];
-        }
-      }
-      if constexpr (BIAS || TWO) {
-        float sd = 0.f;
-        if (TWO || grad) {
-#pragma unroll
-          for (int j = 0; j < 16; ++j) sd += dp[j];
-        }
-        if (BIAS && grad) {
-          float sp = 0.f;
-          if (side >= 0) {
-#pragma unroll
-            for (int j = 0; j < 16; ++j) sp += s[j];
-          }
-          if (side < 0) {
-            s_lo += sd;
-            met_lo = true;
-          } else if (side > 0) {
-            s_hi += sd;
-            p_hi += sp;
-          } else {
-            s_in += sd;
-            p_in += sp;
-#pragma unroll
-            for (int j = 0; j < 16; ++j) add(kb0, j, dp[j]);
-          }
-        } else {
-          s_in += sd;
-        }
-      }
-      __builtin_amdgcn_s_setprio(0);
-      mma_cols_of<TWO, D>(dqa, kc, kb, dp, h, c);
-    }
-    if constexpr (!TL::TWO) __syncthreads();
-    if (it + 1 < nt) {
-      kld.commit(kn);
-      vld.commit(vn);
-    }
-    __syncthreads();
-  };
-  for (int it = it0; it < nt; it += 2) {
-    step(it, stA[0], stA[1], TL::TWO ? stB[0] : stA[0], TL::TWO ? stB[1] : stA[1]);
-    if (it + 1 < nt) step(it + 1, TL::TWO ? stB[0] : stA[0], TL::TWO ? stB[1] : stA[1], stA[0], stA[1]);
-  }
-
-  if (qi < a.nq) {
-    if (a.part) store_row<float, D>(a.part + ((long long)part * a.nrows + row) * D, dqa, a.scale, h);
-    else store_row<T, D>((T*)a.dq + b * a.dqs.b + hq * a.dqs.h + qi * a.dqs.t, dqa, a.scale, h);
-  }
-  // -e_i of this lane's query, both halves' keys
-  const float e = halves_sum(s_lo + s_in + s_hi);
-  if constexpr (TWO) {
-    if (qi < a.nq && h == 0) {
-      if (a.part) a.part_ml[part * a.nrows + row] = e;
-      else a.dvec[row] = nd - e;
-    }
-  }
-
-  if constexpr (BIAS) {
-    if (!grad) return;
-    // P of a row adds up to 1 (0 without keys)
-    const float one = lq < INFINITY ? 1.f : 0.f;
-    const float q_in = halves_sum(p_in), q_hi = halves_sum(p_hi);
-    float f_lo = halves_sum(s_lo), f_hi = halves_sum(s_hi) - e * q_hi;
-    if (met_lo) f_lo -= e * fmaxf(one - q_in - q_hi, 0.f);
-    // tiles that reach into the positions of their own, for a wave of the workgroup
-    const int tb0 = max(0, a.first - 94 + start + q0) / BKV, tb1 = min(nt, (max(0, a.first + a.R - 1 + start + q0 + BQ - 1) + BKV) / BKV);
-    for (int it = tb0; it < tb1; ++it) {
-      issue(kld, stA[0], Kg, a.ks.t, it);
-      kld.commit(stA[0]);
-      __syncthreads();
-#pragma unroll
-      for (int kb = 0; kb < NKB; ++kb) {
-        const int kb0 = it * BKV + 32 * kb;
-        if (kb0 >= n || (a.causal && kb0 > start + qw0 + 31)) continue;
-        if (bias_side(a, kb0 - (start + qw0 + 31), kb0 + 31 - (start + qw0)) != 0) continue;
-        f32x16 s = zero16();
-        mma_tile_rows<D>(s, stA[0], kb, q, h, c);
-        shift(s, kb0);
-        const int lim = lim_of(kb0);
-#pragma unroll
-        for (int j = 0; j < 16; ++j) add(kb0, j, j > lim ? 0.f : -e * exp2_fast(s[j]));
-      }
-      __syncthreads();
-    }
-    // the queries' sums beyond, both halves of a wave holding the same
-#pragma unroll
-    for (int x = 1; x < 32; x <<= 1) {
-      f_lo += __shfl_xor(f_lo, x);
-      f_hi += __shfl_xor(f_hi, x);
-    }
-    if (lane == 0) {
-      far[0][w] = f_lo;
-      far[1][w] = f_hi;
-    }
-    __syncthreads();
-    float* const out = a.drel + (long long)(head * a.ntiles + qt) * a.R;
-    auto sum8 = [&](int t) __attribute__((always_inline)) -> float {
-      float x = 0.f;
-#pragma unroll
-      for (int y = 0; y < 8; ++y) x += bv[RP * (1 + y) + t];
-      return x;
-    };
-    for (int t = 1 + tid; t < a.R - 1; t += 256) out[t] = sum8(kBiasPad + t);
-    // the ends take what lies beyond
-    if (w < 2) {
-      const int from = w == 0 ? 0 : kBiasPad + a.R - 1;
-      float x = 0.f;
-      for (int t = lane; t <= kBiasPad; t += 64) x += sum8(from + t);
-#pragma unroll
-      for (int y = 1; y < 64; y <<= 1) x += __shfl_xor(x, y);
-      x += far[w][0] + far[w][1] + far[w][2] + far[w][3];
-      if (lane == 0) out[w == 0 ? 0 : a.R - 1] = x;
     }
   }
 }
@@ -1156,39 +1121,41 @@ template <typename T, int D> __global__ void __launch_bounds__(256) cross_sum_ke
   }
 }
 
-// The bias gradient of head blockIdx.x: the dQ workgroups' sums by relative position, then
-// those of each bucket's positions, all in a fixed order and in 64 bits (a bucket's sum is
-// small against its terms).
+// The bias gradient of head blockIdx.x: the rows of drel by relative position, then the
+// positions of each bucket, all in a fixed order and in 64 bits (a bucket's sum is small
+// against its terms).
 template <typename T> __global__ void __launch_bounds__(1024) cross_dbias_kernel(const CrossArgs a, void* dtable) {
-  extern __shared__ __attribute__((aligned(16))) double acc[];   // [R], then [1024]
+  extern __shared__ __attribute__((aligned(16))) double acc[];   // [R], then [1024], then the positions' buckets [R]
   const int tid = threadIdx.x, hq = blockIdx.x;
   double* const tmp = acc + a.R;
-  const int per = a.ntiles;   // rows of a sequence and head
-  // position t0 + tid % 64 of the rows tid / 64, + 16, ...
-  for (int t0 = 0; t0 < a.R; t0 += 64) {
-    const int t = t0 + (tid & 63);
+  int* const rows = (int*)(tmp + 1024);
+  for (int t = tid; t < a.R; t += 1024) rows[t] = a.rows[t];
+  // position t0 + tid % 256 of the rows tid / 256, + 4, ...
+  const int N = a.B * a.ntiles;
+  for (int t0 = 0; t0 < a.R; t0 += 256) {
+    const int t = t0 + (tid & 255);
     double x = 0.0;
     if (t < a.R) {
-      const int N = a.B * per;
-      for (int r = tid >> 6; r < N; r += 16) {
-        const int b = r / per, qt = r - b * per;
-        x += (double)a.drel[(((long long)b * a.Hq + hq) * per + qt) * a.R + t];
+#pragma unroll 8
+      for (int r = tid >> 8; r < N; r += 4) {
+        const int b = r / a.ntiles, i = r - b * a.ntiles;
+        x += (double)a.drel[(((long long)b * a.Hq + hq) * a.ntiles + i) * a.R + t];
       }
     }
     __syncthreads();
     tmp[tid] = x;
     __syncthreads();
-    if (tid < 64 && t < a.R) {
-      double y = 0.0;
-      for (int r = 0; r < 16; ++r) y += tmp[64 * r + tid];
-      acc[t] = y;
-    }
+    if (tid < 256 && t < a.R) acc[t] = (tmp[tid] + tmp[256 + tid]) + (tmp[512 + tid] + tmp[768 + tid]);
   }
-  __syncthreads();
-  for (int k = tid; k < a.buckets; k += 1024) {
+  // buckets k0 to k0 + 31, 32 threads each, every 32nd position
+  for (int k0 = 0; k0 < a.buckets; k0 += 32) {
+    const int k = k0 + (tid >> 5), part = tid & 31;
     double y = 0.0;
-    for (int t = 0; t < a.R; ++t) y += a.rows[t] == k ? acc[t] : 0.0;
-    ((T*)dtable)[(long long)k * a.Hq + hq] = (T)(float)y;
+    __syncthreads();
+    for (int t = part; t < a.R; t += 32) y += rows[t] == k ? acc[t] : 0.0;
+#pragma unroll
+    for (int x = 1; x < 32; x <<= 1) y += __shfl_xor(y, x);
+    if (part == 0 && k < a.buckets) ((T*)dtable)[(long long)k * a.Hq + hq] = (T)(float)y;
   }
 }
 
