@@ -95,12 +95,24 @@ FewPlan few_plan(int B, int Hq, int Hkv, int nq, int nk, int d, bool bias) {
 }
 size_t few_bytes(long long rows, int d, int parts) { return parts > 1 ? (size_t)parts * rows * (d + 2) * sizeof(float) : 0; }
 
+// Whether dQ is formed with dS in two bf16 parts and D corrected (FIX of cross_dq_kernel), and in the smallest
+// calls dK and dV with P and dS in two parts. Rows of 512 keys of unit scores are off by 1.45 times their own rounding without. In calls of
+// few rows chance may make one rounding twice what it is on average; they are bound
+// by latency, which the second product does not change.
+bool few_rows(int B, int Hq, int nq) { return (long long)B * Hq * nq <= 4096; }
+bool fix_dq(int B, int Hq, int nq, int nk, int causal, bool bias) {
+  return causal || bias || nk <= 512 || few_rows(B, Hq, nq);
+}
+
+// cross_dkdv16_kernel, or cross_dkdv_kernel
+bool dkdv16(int B, int Hq, int nq, int d, int dtype, bool bias) { return dtype == ATTN_BF16 && d >= 64 && !bias && !few_rows(B, Hq, nq); }
+
 struct BwdPlan {
   int q_tiles, q_splits, q_per;   // dQ: 128-query tiles; parts of the 64-key tiles
-  int k_tiles, k_splits, k_per;   // dK, dV: 128-key tiles; parts of the query tiles of all heads (or of the heads)
+  int k_tiles, k_splits, k_per;   // dK, dV: tiles of keys; parts of the query tiles of all heads (or of the heads)
   size_t rows_at, drel_at, dq_at, sums_at, dk_at, dv_at, bytes;
 };
-BwdPlan bwd_plan(int B, int Hq, int Hkv, int nq, int nk, int d, int dtype, int R) {
+BwdPlan bwd_plan(int B, int Hq, int Hkv, int nq, int nk, int d, int dtype, bool bias, int R) {
   BwdPlan p;
   const auto parts = [](long long groups, long long steps, int& splits, int& per) {
     splits = groups >= 256 ? 1 : (int)std::max<long long>(1, std::min<long long>(512 / groups, steps / 4));
@@ -108,7 +120,8 @@ BwdPlan bwd_plan(int B, int Hq, int Hkv, int nq, int nk, int d, int dtype, int R
     splits = (int)div_up(steps, per);
   };
   p.q_tiles = (int)div_up(nq, 128);
-  p.k_tiles = (int)div_up(nk, 128);
+  const bool wide = dkdv16(B, Hq, nq, d, dtype, bias);
+  p.k_tiles = (int)div_up(nk, wide ? (d == 64 ? attn::CrossDkdv16<64>::BKV : attn::CrossDkdv16<128>::BKV) : 128);
   parts((long long)B * Hq * p.q_tiles, div_up(nk, 64), p.q_splits, p.q_per);
   const int G = Hq / Hkv;
   const long long groups = (long long)B * Hkv * p.k_tiles;
@@ -117,7 +130,7 @@ BwdPlan bwd_plan(int B, int Hq, int Hkv, int nq, int nk, int d, int dtype, int R
     p.k_per = (int)div_up(G, p.k_splits);
     p.k_splits = (int)div_up(G, p.k_per);
   } else {
-    parts(groups, G * div_up(nq, dtype == ATTN_F32 && d == 128 ? 32 : 64), p.k_splits, p.k_per);
+    parts(groups, G * div_up(nq, wide || (dtype == ATTN_F32 && d == 128) ? 32 : 64), p.k_splits, p.k_per);
   }
   const size_t qrows = (size_t)B * Hq * nq, krows = (size_t)B * Hkv * nk;
   p.rows_at = 0;
@@ -128,15 +141,6 @@ BwdPlan bwd_plan(int B, int Hq, int Hkv, int nq, int nk, int d, int dtype, int R
   p.dv_at = p.dk_at + (p.k_splits > 1 ? p.k_splits * krows * d * sizeof(float) : 0);
   p.bytes = p.dv_at + (p.k_splits > 1 ? p.k_splits * krows * d * sizeof(float) : 0);
   return p;
-}
-
-// Whether dQ is formed with dS in two bf16 parts and D corrected (FIX of cross_dq_kernel), and in the smallest
-// calls dK and dV with P and dS in two parts. Rows of 512 keys of unit scores are off by 1.45 times their own rounding without. In calls of
-// few rows chance may make one rounding twice what it is on average; they are bound
-// by latency, which the second product does not change.
-bool few_rows(int B, int Hq, int nq) { return (long long)B * Hq * nq <= 4096; }
-bool fix_dq(int B, int Hq, int nq, int nk, int causal, bool bias) {
-  return causal || bias || nk <= 512 || few_rows(B, Hq, nq);
 }
 
 // ---------------------------------------------------------------- launches --
@@ -246,7 +250,10 @@ extern "C" int attn_cross_fwd(const void* q, const void* k, const void* v, void*
 
 extern "C" size_t attn_cross_bwd_workspace_bytes(int B, int Hq, int Hkv, int nq, int nk, int d, int dtype, int bias_positions) {
   if (check_sizes(B, Hq, Hkv, nq, nk, d, dtype) || bias_positions < 0 || bias_positions > attn::kBiasMax) return 0;
-  return bwd_plan(B, Hq, Hkv, nq, nk, d, dtype, bias_positions).bytes;
+  // the larger of a call's without a bias and, with one, of those with and without its gradient
+  size_t most = 0;
+  for (const bool bias : {false, true}) most = std::max(most, bwd_plan(B, Hq, Hkv, nq, nk, d, dtype, bias, bias ? bias_positions : 0).bytes);
+  return most;
 }
 
 extern "C" int attn_cross_bwd(const void* q, const void* k, const void* v, const void* o, const float* L, const void* dout,
@@ -274,7 +281,7 @@ extern "C" int attn_cross_bwd(const void* q, const void* k, const void* v, const
     if (!attn::writable(all[i].s, B, all[i].H, all[i].n, d)) return ATTN_E_ARG;
   if (attn::rows_meet(a.dks, Hkv, a.dvs, Hkv, B, nk, d, (reinterpret_cast<intptr_t>(dv) - reinterpret_cast<intptr_t>(dk)) / elem))
     return ATTN_E_ARG;
-  const BwdPlan p = bwd_plan(B, Hq, Hkv, nq, nk, d, dtype, dbias ? bias_positions : 0);
+  const BwdPlan p = bwd_plan(B, Hq, Hkv, nq, nk, d, dtype, bias != nullptr, dbias ? bias_positions : 0);
   if (workspace_bytes < p.bytes) return ATTN_E_WORKSPACE;
   const long long qrows = (long long)B * Hq * nq, krows = (long long)B * Hkv * nk;
   const long long q_blocks = (long long)B * Hq * p.q_tiles * p.q_splits, k_blocks = (long long)B * Hkv * p.k_tiles * p.k_splits;
@@ -334,8 +341,13 @@ extern "C" int attn_cross_bwd(const void* q, const void* k, const void* v, const
     }
     if (p.q_splits > 1) sum(aq.part, dq, a.dqs, qrows, Hq, nq, p.q_splits, fix ? aq.part_ml : nullptr);
     if constexpr (std::is_same<T, bf16>::value) {
-      if (few_rows(B, Hq, nq)) dkdv_of(std::true_type{});
-      else dkdv_of(std::false_type{});
+      if (few_rows(B, Hq, nq)) {
+        dkdv_of(std::true_type{});
+      } else if constexpr (D >= 64 && !BIAS) {
+        hipLaunchKernelGGL((attn::cross_dkdv16_kernel<D>), dim3(ak.nblocks), dim3(256), 0, st, ak);
+      } else {
+        dkdv_of(std::false_type{});
+      }
     } else {
       dkdv_of(std::false_type{});
     }

@@ -8,7 +8,8 @@
 //   cross_merge_kernel   joins the parts by their log-sum-exp
 //   cross_prep_kernel    the backward's row vectors: -D and L in base 2
 //   cross_dq_kernel      dQ and the bias gradient by relative position
-//   cross_dkdv_kernel    dK, dV; a workgroup owns 128 keys of a cache head and
+//   cross_dkdv_kernel, cross_dkdv16_kernel
+//                        dK, dV; a workgroup owns 128 (192) keys of a cache head and
 //                        goes over the queries of all heads of its group
 //   cross_sum_kernel     adds the parts of a gradient whose sum was split
 //   cross_dbias_kernel   the bias gradient by bucket
@@ -1096,6 +1097,232 @@ __global__ void __launch_bounds__(256, D == 128 ? 1 : 2) cross_dkdv_kernel(const
       for (int g = part * a.per; g < min(a.G, (part + 1) * a.per); ++g) {
         float* const out = a.drel + (((long long)b * a.Hq + hk * a.G + g) * a.ntiles + kt) * a.R;
         for (int t = tid; t < a.R; t += 256) out[t] = 0.f;
+      }
+    }
+  }
+}
+
+// ======================================================================
+// dK, dV for bf16 calls that fill the chip, without a bias, d >= 64: as dkdv16_kernel, on
+// v_mfma_f32_16x16x32_bf16. A wave owns KB blocks of 16 keys (two at d = 128, three at
+// 64), which share every Q and dO operand that is read from LDS; K's operands come
+// from an LDS copy of the workgroup's keys, V's stay in registers, so that two workgroups
+// fit a compute unit and one's exponentials run under the other's products. A step is 32 queries:
+//   S = Q K^T, dP - D = dO V^T - D (the accumulators start from -D), P, dS,
+//   dV^T += dO^T P, dK^T += Q^T dS
+// Rows of queries past the end are masked with the causal mask's; keys past the
+// end give columns of their own, which are stored as zeros.
+// ======================================================================
+// ROWS x D rows of a strided matrix into the layout of Pad16 by four waves; rows from `valid` on are
+// zeros, as the spare chunks are
+template <int ROWS, int D> struct CrossTile16 {
+  static constexpr int CP = Pad16<D>::CP, C = Pad16<D>::C, TI = ROWS * CP / 64, NI = (TI + 3) / 4;
+  static_assert(ROWS * CP == TI * 64, "whole 1 KB copies");
+  unsigned off[NI];
+  int w;
+  __device__ __forceinline__ CrossTile16(int w_, int lane, long long ld) : w(w_) {
+#pragma unroll
+    for (int j = 0; j < NI; ++j) {
+      const int P = 64 * (w + 4 * j) + lane, s = P / CP, slot = P % CP;
+      off[j] = slot < C ? 2u * ((unsigned)s * (unsigned)ld + 8u * (unsigned)slot) : 0x80000000u;
+    }
+  }
+  __device__ __forceinline__ void issue(bf16* lds, const bf16* g, long long ld, int valid) const {
+    const auto rs = rows_rsrc<D>(g, ld, min(valid, ROWS));
+#pragma unroll
+    for (int j = 0; j < NI; ++j)
+      if (TI % 4 == 0 || w + 4 * j < TI) dma16(rs, off[j], (ATTN_LDS void*)(lds + 512 * (w + 4 * j)));
+  }
+};
+template <int D> struct CrossDkdv16 {
+  static constexpr int KB = D == 128 ? 2 : 3, BKV = 64 * KB;
+};
+template <int D>
+__global__ void __launch_bounds__(256, 2) cross_dkdv16_kernel(const CrossArgs a) {
+  constexpr int KB = CrossDkdv16<D>::KB, KW = 16 * KB, BKV = 4 * KW, BQ = 32, TD = D / 32, NDB = D / 16;
+  constexpr int RS = Pad16<D>::RS, TSZ = BQ * RS;
+  __shared__ __attribute__((aligned(16))) bf16 stA[2][TSZ];
+  __shared__ __attribute__((aligned(16))) bf16 stB[2][TSZ];
+  __shared__ __attribute__((aligned(16))) float ldA[2][64];
+  __shared__ __attribute__((aligned(16))) float ldB[2][64];
+  __shared__ __attribute__((aligned(16))) bf16 kst[BKV * RS];
+
+  const int tid = threadIdx.x, lane = tid & 63, g = lane >> 4, c = lane & 15;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  int head, tile;   // of B x Hkv, key block x part
+  block_map(blockIdx.x, a.nblocks, a.ntiles * a.splits, 0, false, head, tile);
+  const int kt = tile / a.splits, part = tile - kt * a.splits;
+  const int b = head / a.Hkv, hk = head - b * a.Hkv;
+  const int n = seq_len(a, b), start = seq_start(a, b);
+  const int k0 = kt * BKV, kj = k0 + KW * w + c;
+
+  const int nqt = (a.nq + BQ - 1) / BQ;
+  const int t0 = a.causal ? min(nqt, max(0, k0 - start) / BQ) : 0, per_head = nqt - t0;
+  const int all = k0 < n ? a.G * per_head : 0;
+  const int u0 = min(all, part * a.per), u1 = min(all, u0 + a.per);
+
+  const CrossTile16<BQ, D> qld(w, lane, a.qs.t), gld(w, lane, a.gs.t);
+  int ng = 0, nq0 = 0;   // the tile that is copied next: head of the group, first query
+  if (u0 < u1) {
+    ng = u0 / per_head;
+    nq0 = (t0 + u0 - ng * per_head) * BQ;
+  }
+  auto issue = [&](bf16 (&tl)[2][TSZ], float (&lr)[2][64]) __attribute__((always_inline)) {
+    const int hq = hk * a.G + ng;
+    qld.issue(tl[0], (const bf16*)a.q + b * a.qs.b + hq * a.qs.h + nq0 * a.qs.t, a.qs.t, a.nq - nq0);
+    gld.issue(tl[1], (const bf16*)a.dout + b * a.gs.b + hq * a.gs.h + nq0 * a.gs.t, a.gs.t, a.nq - nq0);
+    if (w < 2) {   // L and -D of the rows, zeros past the end
+      const float* x = (w == 0 ? a.lse2 : a.dvec) + ((long long)b * a.Hq + hq) * a.nq + nq0;
+      const auto rs = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(x), (short)0, 4 * min(BQ, a.nq - nq0), 0x00020000);
+      dma4(rs, 4u * (unsigned)lane, (ATTN_LDS void*)lr[w]);
+    }
+  };
+  if (u0 < u1) {
+    issue(stA, ldA);
+    const CrossTile16<BKV, D> kld(w, lane, a.ks.t);
+    kld.issue(kst, (const bf16*)a.k + b * a.ks.b + hk * a.ks.h + (long long)k0 * a.ks.t, a.ks.t, n - k0);
+  }
+  bf16x8 vf[KB][TD];
+#pragma unroll
+  for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+    for (int t = 0; t < TD; ++t) {
+      const int kr = kj + 16 * kb;
+      u32x4 y = {0u, 0u, 0u, 0u};
+      if (kr < n) y = *(const u32x4*)((const bf16*)a.v + b * a.vs.b + hk * a.vs.h + kr * a.vs.t + 32 * t + 8 * g);
+      vf[kb][t] = __builtin_bit_cast(bf16x8, y);
+    }
+  f32x4 dk[KB][NDB], dv[KB][NDB];
+#pragma unroll
+  for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+    for (int db = 0; db < NDB; ++db) dk[kb][db] = dv[kb][db] = (f32x4){0.f, 0.f, 0.f, 0.f};
+  const float sl2 = a.qflip ? -a.sl2 : a.sl2;
+  __syncthreads();
+
+  auto step = [&](int u, bf16 (&cur)[2][TSZ], float (&lcur)[2][64], bf16 (&nxt)[2][TSZ], float (&lnxt)[2][64])
+      __attribute__((always_inline)) {
+    const int q0 = nq0;
+    if (u + 1 < u1) {
+      nq0 += BQ;
+      if (nq0 >= a.nq) {
+        nq0 = t0 * BQ;
+        ++ng;
+      }
+      issue(nxt, lnxt);
+    }
+    const bool need_mask = (a.causal && start + q0 < k0 + BKV - 1) || q0 + BQ > a.nq;
+    __builtin_amdgcn_s_setprio(1);
+    f32x4 sv[KB][2], pv[KB][2];
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      const f32x4 init = *(const f32x4*)&lcur[1][16 * x + 4 * g];
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb) {
+        sv[kb][x] = (f32x4){0.f, 0.f, 0.f, 0.f};
+        pv[kb][x] = init;
+      }
+    }
+#pragma unroll
+    for (int t = 0; t < TD; ++t) {
+      bf16x8 kop[KB];
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb) kop[kb] = row_read16p<D>(kst, KB * w + kb, t, g, c);
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        const bf16x8 qa = row_read16p<D>(cur[0], x, t, g, c);
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) mma16(sv[kb][x], qa, kop[kb]);
+        const bf16x8 oa = row_read16p<D>(cur[1], x, t, g, c);
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) mma16(pv[kb][x], oa, vf[kb][t]);
+      }
+    }
+    if constexpr (D > 64) __builtin_amdgcn_s_setprio(0);
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      const f32x4 l4 = *(const f32x4*)&lcur[0][16 * x + 4 * g];
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) sv[kb][x][j] = exp2_fast(fmaf(sv[kb][x][j], sl2, -l4[j]));
+    }
+    __builtin_amdgcn_s_setprio(0);
+    const bf16x8 oa0 = tr_read16p<D>(cur[1], 0, 0, g, c), qa0 = tr_read16p<D>(cur[0], 0, 0, g, c);
+    // the products of S and dP with their reads eight ahead
+    ATTN_SCHED(kSchedDSRead, 8);
+#pragma unroll
+    for (int i = 0; i < 4 * TD * KB; ++i) {
+      ATTN_SCHED(kSchedMFMA, 1);
+      ATTN_SCHED(kSchedDSRead, 1);
+    }
+    if (need_mask) {
+      // queries qbase + j that see the key: lo <= j <= hi
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        const int qbase = q0 + 16 * x + 4 * g, hi = a.nq - 1 - qbase;
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) {
+          const int lo = a.causal ? kj + 16 * kb - start - qbase : 0;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) sv[kb][x][j] = (j < lo || j > hi) ? 0.f : sv[kb][x][j];
+        }
+      }
+    }
+    bf16x8 pf[KB], sf[KB];
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) {
+#pragma unroll
+      for (int x = 0; x < 2; ++x)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) pv[kb][x][j] = sv[kb][x][j] * pv[kb][x][j];
+      pf[kb] = frag16(sv[kb][0], sv[kb][1]);
+      sf[kb] = frag16(pv[kb][0], pv[kb][1]);
+    }
+#pragma unroll
+    for (int db = 0; db < NDB; ++db) {
+      const bf16x8 oa = db == 0 ? oa0 : tr_read16p<D>(cur[1], 0, db, g, c);
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb) mma16(dv[kb][db], oa, pf[kb]);
+      const bf16x8 qa = db == 0 ? qa0 : tr_read16p<D>(cur[0], 0, db, g, c);
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb) mma16(dk[kb][db], qa, sf[kb]);
+    }
+    ATTN_SCHED(kSchedDSRead, 4);
+#pragma unroll
+    for (int i = 0; i < 2 * KB * NDB; ++i) {
+      ATTN_SCHED(kSchedMFMA, 1);
+      ATTN_SCHED(kSchedDSRead, 1);
+    }
+    __syncthreads();
+  };
+  for (int u = u0; u < u1; u += 2) {
+    step(u, stA, ldA, stB, ldB);
+    if (u + 1 < u1) step(u + 1, stB, ldB, stA, ldA);
+  }
+
+#pragma unroll
+  for (int kb = 0; kb < KB; ++kb) {
+    const int kr = kj + 16 * kb;
+    if (kr >= a.nk) continue;
+    const bool there = kr < n;
+    if (a.part) {
+      const long long at = ((long long)part * a.nrows + (long long)head * a.nk + kr) * D;
+#pragma unroll
+      for (int db = 0; db < NDB; ++db) {
+        const int col = 16 * db + 4 * g;
+        *(f32x4*)(a.part + at + col) = there ? dk[kb][db] * a.scale : (f32x4){0.f, 0.f, 0.f, 0.f};
+        *(f32x4*)(a.part2 + at + col) = there ? dv[kb][db] : (f32x4){0.f, 0.f, 0.f, 0.f};
+      }
+    } else {
+      bf16* const ko = (bf16*)a.dk + b * a.dks.b + hk * a.dks.h + kr * a.dks.t;
+      bf16* const vo = (bf16*)a.dv + b * a.dvs.b + hk * a.dvs.h + kr * a.dvs.t;
+#pragma unroll
+      for (int db = 0; db < NDB; ++db) {
+        const int col = 16 * db + 4 * g;
+        const f32x4 x = there ? dk[kb][db] * a.scale : (f32x4){0.f, 0.f, 0.f, 0.f}, y = there ? dv[kb][db] : (f32x4){0.f, 0.f, 0.f, 0.f};
+        Quad<bf16>::store(ko + col, x[0], x[1], x[2], x[3]);
+        Quad<bf16>::store(vo + col, y[0], y[1], y[2], y[3]);
       }
     }
   }
