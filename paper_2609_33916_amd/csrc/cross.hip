@@ -79,13 +79,29 @@ bool few_queries(int B, int Hq, int nq) { return nq <= 64 || (long long)B * Hq *
 struct FewPlan {
   int pack, ntiles, splits, per;
   long long groups;
+  bool tiles;   // cross_fwd_kernel in parts: 128 rows a workgroup, `per` in tiles of 64 keys
 };
+// Rows of a head and keys enough that 128 rows a workgroup, which share every tile of keys, fill the chip in parts.
+bool wide_rows(long long heads, long long rows, int nk) {
+  return rows > 64 && heads * div_up(rows, 128) * (nk / 256) >= 256;
+}
 // Parts of the keys: as many as leave every compute unit its one (d = 128) or two
 // workgroups, of at least 8 blocks of 32 keys, two for each wave.
 FewPlan few_plan(int B, int Hq, int Hkv, int nq, int nk, int d, bool bias) {
   FewPlan p;
   p.pack = bias ? 1 : Hq / Hkv;
-  p.ntiles = (int)div_up((long long)nq * p.pack, 32);
+  const long long rows = (long long)nq * p.pack;
+  p.tiles = wide_rows(B * (Hq / p.pack), rows, nk);
+  if (p.tiles) {
+    p.ntiles = (int)div_up(rows, 128);
+    p.groups = (long long)B * (Hq / p.pack) * p.ntiles;
+    const int nt = (int)div_up(nk, 64);
+    p.splits = (int)std::max<long long>(1, std::min<long long>(512 / p.groups, nt / 4));
+    p.per = (int)div_up(nt, p.splits);
+    p.splits = (int)div_up(nt, p.per);
+    return p;
+  }
+  p.ntiles = (int)div_up(rows, 32);
   p.groups = (long long)B * (Hq / p.pack) * p.ntiles;
   const int nb = (int)div_up(nk, 32), want = d == 128 ? 256 : 512;
   p.splits = (int)std::max<long long>(1, std::min<long long>(want / std::max<long long>(p.groups, 1), nb / 8));
@@ -234,14 +250,17 @@ extern "C" int attn_cross_fwd(const void* q, const void* k, const void* v, void*
     dispatch(dtype, d, bias != nullptr, [&](auto t, auto dd, auto bb) {
       using T = decltype(t);
       constexpr int D = decltype(dd)::value;
-      hipLaunchKernelGGL((attn::cross_few_kernel<T, D, decltype(bb)::value>), dim3(a.nblocks), dim3(256), bias_lds(a), st, a);
+      if (p.tiles)
+        hipLaunchKernelGGL((attn::cross_fwd_kernel<T, D, decltype(bb)::value, true>), dim3(a.nblocks), dim3(256), bias_lds(a), st, a);
+      else
+        hipLaunchKernelGGL((attn::cross_few_kernel<T, D, decltype(bb)::value>), dim3(a.nblocks), dim3(256), bias_lds(a), st, a);
       if (a.splits > 1) hipLaunchKernelGGL((attn::cross_merge_kernel<T, D>), dim3((unsigned)div_up(rows, 4)), dim3(256), 0, st, a);
     });
   } else {
     a.ntiles = (int)div_up(nq, 128);
     set_grid(a, (long long)B * Hq, a.ntiles);
     dispatch(dtype, d, bias != nullptr, [&](auto t, auto dd, auto bb) {
-      hipLaunchKernelGGL((attn::cross_fwd_kernel<decltype(t), decltype(dd)::value, decltype(bb)::value>), dim3(a.nblocks), dim3(256),
+      hipLaunchKernelGGL((attn::cross_fwd_kernel<decltype(t), decltype(dd)::value, decltype(bb)::value, false>), dim3(a.nblocks), dim3(256),
                          bias_lds(a), st, a);
     });
   }
@@ -366,8 +385,7 @@ extern "C" int attn_cross_bwd(const void* q, const void* k, const void* v, const
 
 // ------------------------------------------------------- shared prefix --
 namespace {
-// The parts of the prefix (its rows are those of the whole batch) and of the sequences' own
-// keys, which run together: each gets workgroups by its share of the blocks.
+// The parts of the prefix, whose rows are those of the whole batch, and of the sequences' own keys.
 struct PrefixPlan {
   FewPlan prefix, own;
   int parts;
@@ -376,7 +394,7 @@ PrefixPlan prefix_plan(int B, int Hq, int Hkv, int np, int n, int d) {
   PrefixPlan p;
   p.prefix = few_plan(1, Hq, Hkv, B, np, d, false);
   if (n > 0) p.own = few_plan(B, Hq, Hkv, 1, n, d, false);
-  else p.own = FewPlan{Hq / Hkv, 0, 0, 0, 0};
+  else p.own = FewPlan{Hq / Hkv, 0, 0, 0, 0, false};
   p.parts = p.prefix.splits + p.own.splits;
   return p;
 }
@@ -449,7 +467,12 @@ extern "C" int attn_prefix_decode(const void* q, const void* k_new, const void* 
   const unsigned merge = (unsigned)div_up(qrows, 4);
   const auto go = [&](auto dd) {
     constexpr int D = decltype(dd)::value;
-    hipLaunchKernelGGL((attn::prefix_few_kernel<D>), dim3((unsigned)blocks), dim3(256), 0, st, a);
+    if (p.prefix.tiles) {
+      hipLaunchKernelGGL((attn::cross_fwd_kernel<bf16, D, false, true>), dim3(x.nblocks), dim3(256), 0, st, x);
+      x.nblocks = 0;
+    }
+    if (x.nblocks + y.nblocks > 0)
+      hipLaunchKernelGGL((attn::prefix_few_kernel<D>), dim3((unsigned)(x.nblocks + y.nblocks)), dim3(256), 0, st, a);
     hipLaunchKernelGGL((attn::prefix_merge_kernel<D>), dim3(merge), dim3(256), 0, st, a);
   };
   if (d == 32) go(std::integral_constant<int, 32>{});

@@ -234,8 +234,10 @@ __device__ __forceinline__ int bias_side(const CrossArgs& a, int lo, int hi) {
 // ======================================================================
 // Forward. As fwd_kernel: a workgroup owns 128 queries of a head, 32 per wave; K and
 // V tiles of 64 keys in LDS; S^T = K Q^T, online softmax by column, O^T += V^T P^T.
+// PART: it owns 128 rows (query, head of the group) and one part of the keys, as
+// cross_few_kernel its 32, and P multiplies in two bf16 parts.
 // ======================================================================
-template <typename T, int D, bool BIAS>
+template <typename T, int D, bool BIAS, bool PART>
 __global__ void __launch_bounds__(256, sizeof(T) == 4 && D == 128 ? 1 : 2) cross_fwd_kernel(const CrossArgs a) {
   constexpr int BQ = 128, BKV = 64, NKB = 2, NDB = D / 32;
   using TL = CrossTile<T, BKV, D>;
@@ -247,24 +249,31 @@ __global__ void __launch_bounds__(256, sizeof(T) == 4 && D == 128 ? 1 : 2) cross
 
   const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, c = lane & 31;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-  int head, qt;
-  block_map(blockIdx.x, a.nblocks, a.ntiles, a.hgroup, a.causal, head, qt);
-  const int b = head / a.Hq, hq = head - b * a.Hq, hk = hq / a.G;
+  int head, tile;   // PART: of B x Hq / pack, row tile x part
+  block_map(blockIdx.x, a.nblocks, PART ? a.ntiles * a.splits : a.ntiles, a.hgroup, a.causal, head, tile);
+  const int heads = PART ? a.Hq / a.pack : a.Hq;
+  const int qt = PART ? tile / a.splits : tile, part = PART ? tile - qt * a.splits : 0;
+  const int b = head / heads, hp = head - b * heads;
   const int n = seq_len(a, b), start = seq_start(a, b);
-  const int q0 = qt * BQ, qw0 = q0 + 32 * w, qi = qw0 + c;
+  // the workgroup's, the wave's and the lane's (first) query
+  const int r0 = qt * BQ, rw0 = r0 + 32 * w, r = rw0 + c, nr = PART ? a.nq * a.pack : a.nq;
+  const int qw0 = PART ? min(rw0, nr - 1) / a.pack : rw0, qw1 = PART ? min(rw0 + 31, nr - 1) / a.pack : rw0 + 31;
+  const int qi = PART ? min(r, nr - 1) / a.pack : r, hq = PART ? hp * a.pack + min(r, nr - 1) % a.pack : hp, hk = (PART ? hp * a.pack : hp) / a.G;
+  const bool there = r < nr;
   const T* Kg = (const T*)a.k + b * a.ks.b + hk * a.ks.h;
   const T* Vg = (const T*)a.v + b * a.vs.b + hk * a.vs.h;
 
-  const int kv_end = a.causal ? max(0, min(n, start + min(q0 + BQ, a.nq))) : n;
-  const int nt = (kv_end + BKV - 1) / BKV;
+  const int q_end = PART ? min(r0 + BQ - 1, nr - 1) / a.pack + 1 : min(r0 + BQ, a.nq);
+  const int kv_end = a.causal ? max(0, min(n, start + q_end)) : n;
+  const int it0 = PART ? part * a.per : 0, all = (kv_end + BKV - 1) / BKV, nt = PART ? min(all, it0 + a.per) : all;
 
   TL kld(w, lane, a.ks.t), vld(w, lane, a.vs.t);
-  if (nt > 0) {
-    kld.issue(stA[0], Kg, a.ks.t, n);
-    vld.issue(stA[1], Vg, a.vs.t, n);
+  if (it0 < nt) {
+    kld.issue(stA[0], Kg + (long long)it0 * BKV * a.ks.t, a.ks.t, n - it0 * BKV);
+    vld.issue(stA[1], Vg + (long long)it0 * BKV * a.vs.t, a.vs.t, n - it0 * BKV);
   }
   RowRegs<T, D> q;
-  load_row<T, D>(q, (const T*)a.q + b * a.qs.b + hq * a.qs.h + qi * a.qs.t, qi < a.nq, h, a.qflip);
+  load_row<T, D>(q, (const T*)a.q + b * a.qs.b + hq * a.qs.h + qi * a.qs.t, there, h, a.qflip);
   if constexpr (BIAS) bias_fill<T>(bv, a, hq, tid);
   kld.commit(stA[0]);
   vld.commit(stA[1]);
@@ -282,7 +291,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 4 && D == 128 ? 1 : 2) cross
       kld.issue(kn, Kg + (kv0 + BKV) * a.ks.t, a.ks.t, n - kv0 - BKV);
       vld.issue(vn, Vg + (kv0 + BKV) * a.vs.t, a.vs.t, n - kv0 - BKV);
     }
-    if (!a.causal || kv0 <= start + qw0 + 31) {
+    if (!a.causal || kv0 <= start + qw1) {
       f32x16 s[NKB];
 #pragma unroll
       for (int kb = 0; kb < NKB; ++kb) {
@@ -291,7 +300,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 4 && D == 128 ? 1 : 2) cross
       }
       // lane (h, c): s[kb][j] is the score of key kv0 + 32 kb + 16 h + j and query qi
       if constexpr (BIAS) {
-        const int side = bias_side(a, kv0 - (start + qw0 + 31), kv0 + BKV - 1 - (start + qw0));
+        const int side = bias_side(a, kv0 - (start + qw1), kv0 + BKV - 1 - (start + qw0));
         if (side != 0) {
           const float u = bv[side < 0 ? 0 : a.R + 2 * kBiasPad - 1];
 #pragma unroll
@@ -344,7 +353,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 4 && D == 128 ? 1 : 2) cross
       lsum += rs;
       __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-      for (int kb = 0; kb < NKB; ++kb) mma_tile_cols<D>(oacc, vc, kb, s[kb], h, c);
+      for (int kb = 0; kb < NKB; ++kb) mma_cols_of<PART && sizeof(T) == 2, D>(oacc, vc, kb, s[kb], h, c);
       __builtin_amdgcn_s_setprio(0);
     }
     if constexpr (!TL::TWO) __syncthreads();
@@ -354,15 +363,20 @@ __global__ void __launch_bounds__(256, sizeof(T) == 4 && D == 128 ? 1 : 2) cross
     }
     __syncthreads();
   };
-  for (int it = 0; it < nt; it += 2) {
+  for (int it = it0; it < nt; it += 2) {
     step(it, stA[0], stA[1], TL::TWO ? stB[0] : stA[0], TL::TWO ? stB[1] : stA[1]);
     if (it + 1 < nt) step(it + 1, TL::TWO ? stB[0] : stA[0], TL::TWO ? stB[1] : stA[1], stA[0], stA[1]);
   }
 
   const float l = halves_sum(lsum);
-  if (qi < a.nq) {
+  if (!there) return;
+  if (PART && a.part) {
+    const long long row = b * a.rz + hq * a.rh + qi * a.ri, at = (long long)(a.part0 + part) * a.nrows + row;
+    store_row<float, D>(a.part + at * D, oacc, 1.f, h);
+    if (h == 0) *(f32x2*)(a.part_ml + 2 * at) = (f32x2){m_use, l};
+  } else {
     store_row<T, D>((T*)a.o + b * a.os.b + hq * a.os.h + qi * a.os.t, oacc, l > 0.f ? 1.f / l : l == 0.f ? 0.f : l, h);
-    if (h == 0) a.lse[(long long)head * a.nq + qi] = (m_use + log2f(l)) * kLn2;
+    if (h == 0) a.lse[((long long)b * a.Hq + hq) * a.nq + qi] = (m_use + log2f(l)) * kLn2;
   }
 }
 
@@ -663,6 +677,7 @@ struct PrefixArgs {
   void* v_cache;
   int n_cap, parts;
 };
+// (part[0] with no workgroups: cross_fwd_kernel forms the prefix's parts)
 template <int D> __global__ void __launch_bounds__(256, D == 128 ? 1 : 2) prefix_few_kernel(const PrefixArgs a) {
   __shared__ __attribute__((aligned(16))) float stA[FewLds<bf16, D>::FLOATS];
   __shared__ __attribute__((aligned(16))) float stB[FewLds<bf16, D>::FLOATS];

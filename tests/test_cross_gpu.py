@@ -98,6 +98,15 @@ def test_large_grid(d, dtype, G):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("d", [32, 64, 128])
+def test_few_queries_on_many_keys(d, dtype):
+    """128 rows a workgroup, the keys in parts: heads of a group as rows, masks, a bias."""
+    Call(1, 4, 2, 101, 16500, d, dtype, k_lens=[16400], packed=True).check(False)
+    Call(2, 2, 1, 150, 12000, d, dtype, causal=True, starts=[11850, 5], k_lens=[12000, 9000]).check(False)
+    Call(1, 4, 2, 131, 9000, d, dtype, causal=True, start=8800, buckets=(32, 128, False)).check(False)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("nq,nk,lens", [(70, 200, [200, 0, 1, 77, 128]), (1, 300, [0, 300, 1, 64, 65]), (200, 64, [64, 0, 32, 33, 63]),
                                         (5, 40, [-3, 41, 40, 7, 100])])
 @pytest.mark.parametrize("d", [64, 128])

@@ -80,6 +80,12 @@ def test_long_prefix_in_parts(d):
     Step(4, 8, 2, 5000, 900, d, [899, 3, 450, 0]).check()
 
 
+@pytest.mark.parametrize("d", [32, 64, 128])
+def test_long_prefix_of_a_large_batch(d):
+    """Rows and keys enough for 128 rows of the batch to share a tile of keys."""
+    Step(21, 32, 4, 8500, 40, d, [7 * i % 40 for i in range(21)]).check()
+
+
 def test_without_append_lengths_and_defaults():
     Step(3, 4, 2, 90, 50, 64, [50, 0, 20], append=False).check()
     Step(3, 4, 2, 90, 50, 64, None).check(n=49)
