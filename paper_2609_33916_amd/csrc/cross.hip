@@ -85,36 +85,44 @@ struct FewPlan {
 bool wide_rows(long long heads, long long rows, int nk) {
   return rows > 64 && heads * div_up(rows, 128) * (nk / 256) >= 256;
 }
-// Parts of the keys: as many as leave every compute unit its one (d = 128) or two
-// workgroups, of at least 8 blocks of 32 keys, two for each wave.
-FewPlan few_plan(int B, int Hq, int Hkv, int nq, int nk, int d, bool bias) {
+// cross_fwd_kernel in parts, up to `want` workgroups
+FewPlan tile_plan(int B, int Hq, int Hkv, int nq, int nk, int want) {
   FewPlan p;
-  p.pack = bias ? 1 : Hq / Hkv;
-  const long long rows = (long long)nq * p.pack;
-  p.tiles = wide_rows(B * (Hq / p.pack), rows, nk);
-  if (p.tiles) {
-    p.ntiles = (int)div_up(rows, 128);
-    p.groups = (long long)B * (Hq / p.pack) * p.ntiles;
-    const int nt = (int)div_up(nk, 64);
-    p.splits = (int)std::max<long long>(1, std::min<long long>(512 / p.groups, nt / 4));
-    p.per = (int)div_up(nt, p.splits);
-    p.splits = (int)div_up(nt, p.per);
-    return p;
-  }
-  p.ntiles = (int)div_up(rows, 32);
-  p.groups = (long long)B * (Hq / p.pack) * p.ntiles;
-  const int nb = (int)div_up(nk, 32), want = d == 128 ? 256 : 512;
+  p.tiles = true;
+  p.pack = Hq / Hkv;
+  p.ntiles = (int)div_up((long long)nq * p.pack, 128);
+  p.groups = (long long)B * Hkv * p.ntiles;
+  const int nt = (int)div_up(nk, 64);
+  p.splits = (int)std::max<long long>(1, std::min<long long>(want / p.groups, nt / 4));
+  p.per = (int)div_up(nt, p.splits);
+  p.splits = (int)div_up(nt, p.per);
+  return p;
+}
+// cross_few_kernel: as many parts as give every compute unit two workgroups, of at least 8
+// blocks of 32 keys, two for each wave.
+FewPlan block_plan(int B, int Hq, int Hkv, int nq, int nk) {
+  FewPlan p;
+  p.tiles = false;
+  p.pack = Hq / Hkv;
+  p.ntiles = (int)div_up((long long)nq * p.pack, 32);
+  p.groups = (long long)B * Hkv * p.ntiles;
+  const int nb = (int)div_up(nk, 32), want = 512;
   p.splits = (int)std::max<long long>(1, std::min<long long>(want / std::max<long long>(p.groups, 1), nb / 8));
   p.per = (int)(4 * div_up(div_up(nb, p.splits), 4));
   p.splits = (int)div_up(nb, p.per);
   return p;
 }
+FewPlan few_plan(int B, int Hq, int Hkv, int nq, int nk, bool bias) {
+  if (bias) Hkv = Hq;   // a workgroup holds one head's bias
+  if (wide_rows((long long)B * Hkv, (long long)nq * (Hq / Hkv), nk)) return tile_plan(B, Hq, Hkv, nq, nk, 512);
+  return block_plan(B, Hq, Hkv, nq, nk);
+}
 size_t few_bytes(long long rows, int d, int parts) { return parts > 1 ? (size_t)parts * rows * (d + 2) * sizeof(float) : 0; }
 
 // Whether dQ is formed with dS in two bf16 parts and D corrected (FIX of cross_dq_kernel), and in the smallest
-// calls dK and dV with P and dS in two parts. Rows of 512 keys of unit scores are off by 1.45 times their own rounding without. In calls of
-// few rows chance may make one rounding twice what it is on average; they are bound
-// by latency, which the second product does not change.
+// calls dK and dV with P and dS in two parts. Rows of 512 keys of unit scores are off by 1.45 times
+// their own rounding without. In calls of few rows chance may make one rounding twice
+// what it is on average; they are bound by latency, which the second product does not change.
 bool few_rows(int B, int Hq, int nq) { return (long long)B * Hq * nq <= 4096; }
 bool fix_dq(int B, int Hq, int nq, int nk, int causal, bool bias) {
   return causal || bias || nk <= 512 || few_rows(B, Hq, nq);
@@ -194,7 +202,7 @@ int launched() { return hipGetLastError() == hipSuccess ? ATTN_OK : ATTN_E_HIP; 
 extern "C" size_t attn_cross_fwd_workspace_bytes(int B, int Hq, int Hkv, int nq, int nk, int d, int dtype, int bias_positions) {
   if (check_sizes(B, Hq, Hkv, nq, nk, d, dtype) || bias_positions < 0) return 0;
   if (!few_queries(B, Hq, nq)) return 0;
-  return few_bytes((long long)B * Hq * nq, d, few_plan(B, Hq, Hkv, nq, nk, d, bias_positions > 0).splits);
+  return few_bytes((long long)B * Hq * nq, d, few_plan(B, Hq, Hkv, nq, nk, bias_positions > 0).splits);
 }
 
 extern "C" int attn_cross_fwd(const void* q, const void* k, const void* v, void* o, float* L, const long long* strides,
@@ -220,7 +228,7 @@ extern "C" int attn_cross_fwd(const void* q, const void* k, const void* v, void*
   if (!aligned(L, 4)) return ATTN_E_ALIGN;
   if (!attn::writable(a.os, B, Hq, nq, d)) return ATTN_E_ARG;
   const bool few = few_queries(B, Hq, nq);
-  const FewPlan p = few_plan(B, Hq, Hkv, nq, nk, d, bias != nullptr);
+  const FewPlan p = few_plan(B, Hq, Hkv, nq, nk, bias != nullptr);
   const long long rows = (long long)B * Hq * nq;
   const size_t need = few ? few_bytes(rows, d, p.splits) : 0;
   if (need > 0) {
@@ -390,11 +398,12 @@ struct PrefixPlan {
   FewPlan prefix, own;
   int parts;
 };
-PrefixPlan prefix_plan(int B, int Hq, int Hkv, int np, int n, int d) {
+PrefixPlan prefix_plan(int B, int Hq, int Hkv, int np, int n) {
   PrefixPlan p;
-  p.prefix = few_plan(1, Hq, Hkv, B, np, d, false);
-  if (n > 0) p.own = few_plan(B, Hq, Hkv, 1, n, d, false);
-  else p.own = FewPlan{Hq / Hkv, 0, 0, 0, 0, false};
+  p.prefix = few_plan(1, Hq, Hkv, B, np, false);
+  if (p.prefix.tiles) p.prefix = tile_plan(1, Hq, Hkv, B, np, 256);
+  p.own = FewPlan{Hq / Hkv, 0, 0, 0, 0, false};
+  if (n > 0) p.own = block_plan(B, Hq, Hkv, 1, n);
   p.parts = p.prefix.splits + p.own.splits;
   return p;
 }
@@ -408,7 +417,7 @@ int check_prefix_sizes(int B, int Hq, int Hkv, int np, int n, int d, int dtype) 
 
 extern "C" size_t attn_prefix_decode_workspace_bytes(int B, int Hq, int Hkv, int np, int n, int d) {
   if (check_prefix_sizes(B, Hq, Hkv, np, n, d, ATTN_BF16)) return 0;
-  return (size_t)prefix_plan(B, Hq, Hkv, np, n, d).parts * B * Hq * (d + 2) * sizeof(float);
+  return (size_t)prefix_plan(B, Hq, Hkv, np, n).parts * B * Hq * (d + 2) * sizeof(float);
 }
 
 extern "C" int attn_prefix_decode(const void* q, const void* k_new, const void* v_new, const void* k_prefix, const void* v_prefix,
@@ -424,7 +433,7 @@ extern "C" int attn_prefix_decode(const void* q, const void* k_new, const void* 
   for (const void* p : rows)
     if (!aligned(p, 16)) return ATTN_E_ALIGN;
   if (!aligned(cache_lens, 4) || !aligned(L, 4)) return ATTN_E_ALIGN;
-  const PrefixPlan p = prefix_plan(B, Hq, Hkv, np, n, d);
+  const PrefixPlan p = prefix_plan(B, Hq, Hkv, np, n);
   const long long qrows = (long long)B * Hq;
   const long long blocks = p.prefix.groups * p.prefix.splits + p.own.groups * p.own.splits;
   if (blocks > kMaxBlocks) return ATTN_E_SHAPE;
@@ -467,12 +476,10 @@ extern "C" int attn_prefix_decode(const void* q, const void* k_new, const void* 
   const unsigned merge = (unsigned)div_up(qrows, 4);
   const auto go = [&](auto dd) {
     constexpr int D = decltype(dd)::value;
-    if (p.prefix.tiles) {
-      hipLaunchKernelGGL((attn::cross_fwd_kernel<bf16, D, false, true>), dim3(x.nblocks), dim3(256), 0, st, x);
-      x.nblocks = 0;
-    }
-    if (x.nblocks + y.nblocks > 0)
-      hipLaunchKernelGGL((attn::prefix_few_kernel<D>), dim3((unsigned)(x.nblocks + y.nblocks)), dim3(256), 0, st, a);
+    if (p.prefix.tiles)
+      hipLaunchKernelGGL((attn::prefix_tile_kernel<D>), dim3(8 * (unsigned)(div_up(x.nblocks, 8) + div_up(y.nblocks, 8))), dim3(256), 0, st, a);
+    else
+      hipLaunchKernelGGL((attn::prefix_few_kernel<D>), dim3((unsigned)blocks), dim3(256), 0, st, a);
     hipLaunchKernelGGL((attn::prefix_merge_kernel<D>), dim3(merge), dim3(256), 0, st, a);
   };
   if (d == 32) go(std::integral_constant<int, 32>{});

@@ -237,20 +237,18 @@ __device__ __forceinline__ int bias_side(const CrossArgs& a, int lo, int hi) {
 // PART: it owns 128 rows (query, head of the group) and one part of the keys, as
 // cross_few_kernel its 32, and P multiplies in two bf16 parts.
 // ======================================================================
+template <typename T, int D> struct FwdLds {
+  using TL = CrossTile<T, 64, D>;
+  static constexpr int A = TL::ELEMS, B = TL::TWO ? TL::ELEMS : 8;
+};
 template <typename T, int D, bool BIAS, bool PART>
-__global__ void __launch_bounds__(256, sizeof(T) == 4 && D == 128 ? 1 : 2) cross_fwd_kernel(const CrossArgs a) {
+__device__ __forceinline__ void cross_fwd(const CrossArgs& a, int bid, T (&stA)[2][FwdLds<T, D>::A], T (&stB)[2][FwdLds<T, D>::B], float* bv) {
   constexpr int BQ = 128, BKV = 64, NKB = 2, NDB = D / 32;
   using TL = CrossTile<T, BKV, D>;
-  // two stages in distinct LDS objects (the loop is unrolled by two), so that reads
-  // of one never wait for the copy into the other
-  __shared__ __attribute__((aligned(16))) T stA[2][TL::ELEMS];
-  __shared__ __attribute__((aligned(16))) T stB[2][TL::TWO ? TL::ELEMS : 8];
-  extern __shared__ __attribute__((aligned(16))) float bv[];
-
   const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, c = lane & 31;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   int head, tile;   // PART: of B x Hq / pack, row tile x part
-  block_map(blockIdx.x, a.nblocks, PART ? a.ntiles * a.splits : a.ntiles, a.hgroup, a.causal, head, tile);
+  block_map(bid, a.nblocks, PART ? a.ntiles * a.splits : a.ntiles, a.hgroup, a.causal, head, tile);
   const int heads = PART ? a.Hq / a.pack : a.Hq;
   const int qt = PART ? tile / a.splits : tile, part = PART ? tile - qt * a.splits : 0;
   const int b = head / heads, hp = head - b * heads;
@@ -380,6 +378,16 @@ __global__ void __launch_bounds__(256, sizeof(T) == 4 && D == 128 ? 1 : 2) cross
   }
 }
 
+template <typename T, int D, bool BIAS, bool PART>
+__global__ void __launch_bounds__(256, sizeof(T) == 4 && D == 128 ? 1 : 2) cross_fwd_kernel(const CrossArgs a) {
+  // two stages in distinct LDS objects (the loop is unrolled by two), so that reads
+  // of one never wait for the copy into the other
+  __shared__ __attribute__((aligned(16))) T stA[2][FwdLds<T, D>::A];
+  __shared__ __attribute__((aligned(16))) T stB[2][FwdLds<T, D>::B];
+  extern __shared__ __attribute__((aligned(16))) float bv[];
+  cross_fwd<T, D, BIAS, PART>(a, blockIdx.x, stA, stB, bv);
+}
+
 // ======================================================================
 // Few queries: a workgroup owns 32 rows and one part of the keys. Row r of a cache
 // head is head r % pack of its group (all of it where there is no bias) and query
@@ -435,10 +443,10 @@ template <int D> __device__ __forceinline__ void mma_cross_cols(f32x16 (&acc)[D 
     if (t + CrossCols<D>::R < 16) x.get(t + CrossCols<D>::R);
   }
 }
-template <typename T, int D> struct FewLds {
-  // bf16: K and V tiles of the four waves; both: half of the merge buffer
-  static constexpr int FLOATS = sizeof(T) == 2 ? 4 * 2 * 32 * D / 2 : WaveMerge<D>::FLOATS;
-};
+// LDS: the four waves' K tiles and their V tiles (bf16), each also half of the merge buffer. One stage:
+// the next block's K is copied from the end of the score products on, its V from the end of
+// the others, and the blocks in flight come from the waves: at d = 128 two workgroups fit a
+// compute unit, with two stages one.
 
 template <typename T, int D, bool BIAS>
 __device__ __forceinline__ void cross_few(const CrossArgs& a, int bid, float* stA, float* stB, float (&ml)[2][4][32], float* bv) {
@@ -515,35 +523,34 @@ __device__ __forceinline__ void cross_few(const CrossArgs& a, int bid, float* st
   const int b0 = first + w;   // this wave's blocks: b0, b0 + 4, ...
   if constexpr (B16) {
     using WT = CrossWaveTile<D>;
+    static_assert(4 * WT::ELEMS == 2 * MG::FLOATS, "a buffer holds four tiles");
     const WT kt(lane, a.ks.t), vt(lane, a.vs.t);
-    bf16* const tA = (bf16*)stA + w * 2 * WT::ELEMS;
-    bf16* const tB = (bf16*)stB + w * 2 * WT::ELEMS;
+    bf16* const kl = (bf16*)stA + w * WT::ELEMS;
+    bf16* const vl = (bf16*)stB + w * WT::ELEMS;
     load_row<T, D>(q, Qg, r < nr, h, a.qflip);
-    auto issue = [&](int kb, bf16* t) __attribute__((always_inline)) {
-      kt.issue(t, Kg + 32LL * kb * a.ks.t, a.ks.t, n - 32 * kb);
-      vt.issue(t + WT::ELEMS, Vg + 32LL * kb * a.vs.t, a.vs.t, n - 32 * kb);
-    };
-    if (b0 < nb) issue(b0, tA);
+    auto issue_k = [&](int kb) __attribute__((always_inline)) { kt.issue(kl, Kg + 32LL * kb * a.ks.t, a.ks.t, n - 32 * kb); };
+    auto issue_v = [&](int kb) __attribute__((always_inline)) { vt.issue(vl, Vg + 32LL * kb * a.vs.t, a.vs.t, n - 32 * kb); };
     if constexpr (BIAS) {
       bias_fill<T>(bv, a, hq, tid);
       __syncthreads();
     }
-    auto step = [&](int kb, bf16* tc, bf16* tn) __attribute__((always_inline)) {
-      if (kb + 4 < nb) {
-        issue(kb + 4, tn);
-        wait_vm<2 * WT::NI>();   // this block's tiles are there
-      } else {
-        wait_vm<0>();
-      }
+    if (b0 < nb) {
+      issue_k(b0);
+      issue_v(b0);
+    }
+    for (int kb = b0; kb < nb; kb += 4) {
+      const bool more = kb + 4 < nb;
+      wait_vm<WT::NI>();   // K is there
       f32x16 s = zero16();
-      mma_tile_rows<D>(s, tc, 0, q, h, c);
+      mma_tile_rows<D>(s, kl, 0, q, h, c);
+      __builtin_amdgcn_s_waitcnt(0xC07F);   // reads done (lgkmcnt 0) before the tile is refilled
+      if (more) issue_k(kb + 4);
       softmax(kb, s);
-      mma_tile_cols2<D>(oacc, tc + WT::ELEMS, 0, s, h, c);
-      __builtin_amdgcn_s_waitcnt(0xC07F);   // reads done (lgkmcnt 0) before the stage is refilled
-    };
-    for (int kb = b0; kb < nb; kb += 8) {
-      step(kb, tA, tB);
-      if (kb + 4 < nb) step(kb + 4, tB, tA);
+      if (more) wait_vm<WT::NI>();   // V is there
+      else wait_vm<0>();
+      mma_tile_cols2<D>(oacc, vl, 0, s, h, c);
+      __builtin_amdgcn_s_waitcnt(0xC07F);
+      if (more) issue_v(kb + 4);
     }
   } else {
     RowRegs<T, D> k;
@@ -612,9 +619,9 @@ __device__ __forceinline__ void cross_few(const CrossArgs& a, int bid, float* st
 }
 
 template <typename T, int D, bool BIAS>
-__global__ void __launch_bounds__(256, D == 128 ? 1 : 2) cross_few_kernel(const CrossArgs a) {
-  __shared__ __attribute__((aligned(16))) float stA[FewLds<T, D>::FLOATS];
-  __shared__ __attribute__((aligned(16))) float stB[FewLds<T, D>::FLOATS];
+__global__ void __launch_bounds__(256, sizeof(T) == 4 && D == 128 ? 1 : 2) cross_few_kernel(const CrossArgs a) {
+  __shared__ __attribute__((aligned(16))) float stA[WaveMerge<D>::FLOATS];
+  __shared__ __attribute__((aligned(16))) float stB[WaveMerge<D>::FLOATS];
   __shared__ float ml[2][4][32];
   extern __shared__ __attribute__((aligned(16))) float bv[];
   cross_few<T, D, BIAS>(a, blockIdx.x, stA, stB, ml, bv);
@@ -677,13 +684,27 @@ struct PrefixArgs {
   void* v_cache;
   int n_cap, parts;
 };
-// (part[0] with no workgroups: cross_fwd_kernel forms the prefix's parts)
-template <int D> __global__ void __launch_bounds__(256, D == 128 ? 1 : 2) prefix_few_kernel(const PrefixArgs a) {
-  __shared__ __attribute__((aligned(16))) float stA[FewLds<bf16, D>::FLOATS];
-  __shared__ __attribute__((aligned(16))) float stB[FewLds<bf16, D>::FLOATS];
+template <int D> __global__ void __launch_bounds__(256, 2) prefix_few_kernel(const PrefixArgs a) {
+  __shared__ __attribute__((aligned(16))) float stA[WaveMerge<D>::FLOATS];
+  __shared__ __attribute__((aligned(16))) float stB[WaveMerge<D>::FLOATS];
   __shared__ float ml[2][4][32];
   const int own = (int)blockIdx.x >= a.part[0].nblocks;
   cross_few<bf16, D, false>(a.part[own], (int)blockIdx.x - (own ? a.part[0].nblocks : 0), stA, stB, ml, nullptr);
+}
+// Large batches behind long prefixes: 128 rows of the batch share a tile of the prefix, whose
+// products bound them, while the sequences' own keys (a few rows each) are bound by memory.
+// The two kinds of workgroups take turns, eight at a time, so that each XCD gets both.
+template <int D> __global__ void __launch_bounds__(256, 2) prefix_tile_kernel(const PrefixArgs a) {
+  __shared__ __attribute__((aligned(16))) bf16 stA[2][FwdLds<bf16, D>::A];
+  __shared__ __attribute__((aligned(16))) bf16 stB[2][FwdLds<bf16, D>::B];
+  __shared__ float ml[2][4][32];
+  static_assert(sizeof(stA) == 4 * WaveMerge<D>::FLOATS && sizeof(stB) == sizeof(stA), "the same buffers");
+  const int np = (a.part[0].nblocks + 7) / 8, no = (a.part[1].nblocks + 7) / 8, all = np + no, t = blockIdx.x / 8;
+  const int before = (int)((long long)t * no / all), own = (int)((long long)(t + 1) * no / all) - before;   // 0 or 1
+  const int i = 8 * (own ? before : t - before) + blockIdx.x % 8;
+  if (i >= a.part[own].nblocks) return;
+  if (own) cross_few<bf16, D, false>(a.part[1], i, (float*)stA[0], (float*)stB[0], ml, nullptr);
+  else cross_fwd<bf16, D, false, true>(a.part[0], i, stA, stB, nullptr);
 }
 template <int D> __global__ void __launch_bounds__(256) prefix_merge_kernel(const PrefixArgs a) {
   const CrossArgs& p = a.part[1];
