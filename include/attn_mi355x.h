@@ -434,7 +434,7 @@ int attn_cross_bwd(const void* Q, const void* K, const void* V, const void* O, c
  * prefix, to rows [0, len_b) and to the new token. len_b = cache_lens[b] (device int32 [B])
  * clamped to [0, n], or n for all where NULL; n may be 0, n_cap >= n + 1 with an append, >= n
  * without. Tensors are dense, bfloat16 only, 16-byte aligned; O [B, Hq, d], L float32 [B, Hq] or NULL.
- * B Hq, B Hkv n and Hkv np are below 2^26. P keeps 15 bits. */
+ * B Hq, B Hkv n and Hkv np are below 2^26. P keeps 15 bits, 8 over the prefix of large batches. */
 size_t attn_prefix_decode_workspace_bytes(int B, int Hq, int Hkv, int np, int n, int d);
 
 int attn_prefix_decode(const void* q, const void* k_new, const void* v_new, const void* k_prefix, const void* v_prefix,

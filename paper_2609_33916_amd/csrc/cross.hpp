@@ -235,7 +235,7 @@ __device__ __forceinline__ int bias_side(const CrossArgs& a, int lo, int hi) {
 // Forward. As fwd_kernel: a workgroup owns 128 queries of a head, 32 per wave; K and
 // V tiles of 64 keys in LDS; S^T = K Q^T, online softmax by column, O^T += V^T P^T.
 // PART: it owns 128 rows (query, head of the group) and one part of the keys, as
-// cross_few_kernel its 32, and P multiplies in two bf16 parts.
+// cross_few_kernel its 32.
 // ======================================================================
 template <typename T, int D> struct FwdLds {
   using TL = CrossTile<T, 64, D>;
@@ -351,7 +351,7 @@ __device__ __forceinline__ void cross_fwd(const CrossArgs& a, int bid, T (&stA)[
       lsum += rs;
       __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-      for (int kb = 0; kb < NKB; ++kb) mma_cols_of<PART && sizeof(T) == 2, D>(oacc, vc, kb, s[kb], h, c);
+      for (int kb = 0; kb < NKB; ++kb) mma_tile_cols<D>(oacc, vc, kb, s[kb], h, c);
       __builtin_amdgcn_s_setprio(0);
     }
     if constexpr (!TL::TWO) __syncthreads();
@@ -628,25 +628,34 @@ __global__ void __launch_bounds__(256, sizeof(T) == 4 && D == 128 ? 1 : 2) cross
 }
 
 // The parts of a row, joined: a wave for a row, D / 4 lanes across it and the other
-// lanes over the parts. Returns the lane's 4 columns (all lanes of a column
-// group alike), and the row's maximum and sum.
+// lanes over the parts, four of each lane's in flight. Returns the lane's 4 columns (all
+// lanes of a column group alike), and the row's maximum and sum.
 template <int D> __device__ __forceinline__ f32x4 join_parts(const float* part, const float* ml, long long nrows, long long row, int parts, int lane,
                                                             float& M, float& l) {
-  constexpr int CG = D / 4, SL = 64 / CG;
+  constexpr int CG = D / 4, SL = 64 / CG, N = 4;
   const int cg = lane % CG, sl = lane / CG;
   M = -INFINITY;
-  for (int s = sl; s < parts; s += SL) M = fmaxf(M, ml[2 * (s * nrows + row)]);
+  for (int s = lane; s < parts; s += 64) M = fmaxf(M, ml[2 * (s * nrows + row)]);
 #pragma unroll
-  for (int x = CG; x < 64; x <<= 1) M = fmaxf(M, __shfl_xor(M, x));
+  for (int x = 1; x < 64; x <<= 1) M = fmaxf(M, __shfl_xor(M, x));
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
   l = 0.f;
-  for (int s = sl; s < parts; s += SL) {
-    const f32x2 y = *(const f32x2*)(ml + 2 * (s * nrows + row));
-    const float f = y[0] == -INFINITY ? 0.f : exp2_fast(y[0] - M);
-    const f32x4 x = *(const f32x4*)(part + (s * nrows + row) * D + 4 * cg);
-    l = fmaf(f, y[1], l);
+  for (int s0 = sl; s0 < parts; s0 += N * SL) {
+    f32x2 y[N];
+    f32x4 x[N];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) o[e] = fmaf(f, x[e], o[e]);
+    for (int k = 0; k < N; ++k) {
+      const long long at = min(s0 + k * SL, parts - 1) * nrows + row;
+      y[k] = *(const f32x2*)(ml + 2 * at);
+      x[k] = *(const f32x4*)(part + at * D + 4 * cg);
+    }
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      const float f = s0 + k * SL >= parts || y[k][0] == -INFINITY ? 0.f : exp2_fast(y[k][0] - M);
+      l = fmaf(f, y[k][1], l);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] = fmaf(f, x[k][e], o[e]);
+    }
   }
 #pragma unroll
   for (int x = CG; x < 64; x <<= 1) {
