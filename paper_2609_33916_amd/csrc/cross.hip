@@ -333,7 +333,7 @@ extern "C" int attn_cross_bwd(const void* q, const void* k, const void* v, const
   ak.part = p.k_splits > 1 ? (float*)(ws + p.dk_at) : nullptr;
   ak.part2 = (float*)(ws + p.dv_at);
   ak.drel = dbias ? (float*)(ws + p.drel_at) : nullptr;
-  ak.nblocks = (int)k_blocks;
+  set_grid(ak, (long long)B * Hkv, p.k_tiles * p.k_splits);
 
   hipStream_t st = static_cast<hipStream_t>(stream);
   (void)hipGetLastError();

@@ -945,7 +945,7 @@ __global__ void __launch_bounds__(256, D == 128 ? 1 : 2) cross_dkdv_kernel(const
   const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, c = lane & 31;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   int head, tile;   // of B x Hkv, key block x part
-  block_map(blockIdx.x, a.nblocks, a.ntiles * a.splits, 0, false, head, tile);
+  block_map(blockIdx.x, a.nblocks, a.ntiles * a.splits, a.hgroup, false, head, tile);
   const int kt = tile / a.splits, part = tile - kt * a.splits;
   const int b = head / a.Hkv, hk = head - b * a.Hkv;
   const int n = seq_len(a, b), start = seq_start(a, b);
@@ -1105,10 +1105,10 @@ __global__ void __launch_bounds__(256, D == 128 ? 1 : 2) cross_dkdv_kernel(const
             for (int j = 0; j < 16; j += 4)
               *(f32x4*)(diag + kDiagRow * c + 16 * h + j) = (f32x4){dp[j], dp[j + 1], dp[j + 2], dp[j + 3]};
             const float* const p = diag + lane - 32;   // key t, query t - (32 - lane)
-            float x = 0.f;
+            float x[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int t = 0; t < 32; ++t) x += p[t * (kDiagRow + 1)];
-            sums[kBiasPad - a.first + kw0 - start - qp0 + 32 - lane] += x;
+            for (int t = 0; t < 32; ++t) x[t & 3] += p[t * (kDiagRow + 1)];
+            sums[kBiasPad - a.first + kw0 - start - qp0 + 32 - lane] += (x[0] + x[1]) + (x[2] + x[3]);
           }
         }
       }
@@ -1195,7 +1195,7 @@ __global__ void __launch_bounds__(256, 2) cross_dkdv16_kernel(const CrossArgs a)
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 4, c = lane & 15;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   int head, tile;   // of B x Hkv, key block x part
-  block_map(blockIdx.x, a.nblocks, a.ntiles * a.splits, 0, false, head, tile);
+  block_map(blockIdx.x, a.nblocks, a.ntiles * a.splits, a.hgroup, false, head, tile);
   const int kt = tile / a.splits, part = tile - kt * a.splits;
   const int b = head / a.Hkv, hk = head - b * a.Hkv;
   const int n = seq_len(a, b), start = seq_start(a, b);
