@@ -34,7 +34,7 @@ int check_sizes(int B, int Hq, int Hkv, int nq, int nk, int d, int dtype) {
   if (dtype != ATTN_BF16 && dtype != ATTN_F32) return ATTN_E_UNSUPPORTED;
   if (d != 32 && d != 64 && d != 128) return ATTN_E_UNSUPPORTED;
   if (nq > kMaxLength || nk > kMaxLength) return ATTN_E_SHAPE;
-  // the largest grids: row vectors and sums in pieces of 8 rows, key blocks
+  // the largest grids: joined rows and sums in pieces of 4 and 8 rows
   if ((__int128)B * Hq * nq > (__int128)kMaxBlocks * 4 || (__int128)B * Hkv * nk > (__int128)kMaxBlocks * 4) return ATTN_E_SHAPE;
   return ATTN_OK;
 }
@@ -124,37 +124,41 @@ size_t few_bytes(long long rows, int d, int parts) { return parts > 1 ? (size_t)
 // their own rounding without. In calls of few rows chance may make one rounding twice
 // what it is on average; they are bound by latency, which the second product does not change.
 bool few_rows(int B, int Hq, int nq) { return (long long)B * Hq * nq <= 4096; }
-bool fix_dq(int B, int Hq, int nq, int nk, int causal, bool bias) {
-  return causal || bias || nk <= 512 || few_rows(B, Hq, nq);
-}
+bool fix_dq(int B, int Hq, int nq, int nk, int causal) { return causal || nk <= 512 || few_rows(B, Hq, nq); }
 
 // cross_dkdv16_kernel, or cross_dkdv_kernel
 bool dkdv16(int B, int Hq, int nq, int d, int dtype, bool bias) { return dtype == ATTN_BF16 && d >= 64 && !bias && !few_rows(B, Hq, nq); }
 
 struct BwdPlan {
-  int q_tiles, q_splits, q_per;   // dQ: 128-query tiles; parts of the 64-key tiles
-  int k_tiles, k_splits, k_per;   // dK, dV: tiles of keys; parts of the query tiles of all heads (or of the heads)
+  bool q_few, k_few;              // 32 queries or keys a workgroup, not 128 (192)
+  int q_tiles, q_splits, q_per;   // dQ: tiles of queries; parts of the keys' blocks
+  int k_tiles, k_splits, k_per;   // dK, dV: tiles of keys; parts of the query blocks of all heads, or of the heads
   size_t rows_at, drel_at, dq_at, sums_at, dk_at, dv_at, bytes;
 };
+// A grid of fewer than 256 tiles of 128 rows leaves compute units idle: 32 rows a workgroup. Grids that are
+// small even then are split, up to 512 workgroups, each of which has some steps of its own.
 BwdPlan bwd_plan(int B, int Hq, int Hkv, int nq, int nk, int d, int dtype, bool bias, int R) {
   BwdPlan p;
-  const auto parts = [](long long groups, long long steps, int& splits, int& per) {
-    splits = groups >= 256 ? 1 : (int)std::max<long long>(1, std::min<long long>(512 / groups, steps / 4));
+  const int G = Hq / Hkv;
+  const auto parts = [](long long groups, long long steps, int least, int& splits, int& per) {
+    splits = groups >= 256 ? 1 : (int)std::max<long long>(1, std::min<long long>(512 / groups, steps / least));
     per = (int)div_up(steps, splits);
     splits = (int)div_up(steps, per);
   };
-  p.q_tiles = (int)div_up(nq, 128);
-  const bool wide = dkdv16(B, Hq, nq, d, dtype, bias);
-  p.k_tiles = (int)div_up(nk, wide ? (d == 64 ? attn::CrossDkdv16<64>::BKV : attn::CrossDkdv16<128>::BKV) : 128);
-  parts((long long)B * Hq * p.q_tiles, div_up(nk, 64), p.q_splits, p.q_per);
-  const int G = Hq / Hkv;
+  p.q_few = (long long)B * Hq * div_up(nq, 128) < 256;
+  p.q_tiles = (int)div_up(nq, p.q_few ? 32 : 128);
+  parts((long long)B * Hq * p.q_tiles, div_up(nk, p.q_few ? 32 : 64), p.q_few ? 16 : 4, p.q_splits, p.q_per);
+  // (the bias gradient of d = 128 does not fit the LDS of the other)
+  p.k_few = (long long)B * Hkv * div_up(nk, 128) < (bias ? 128 : dtype == ATTN_BF16 && d <= 64 ? 384 : 256) && !(dtype == ATTN_BF16 && d == 128 && R > 0);
+  const bool wide = !p.k_few && dkdv16(B, Hq, nq, d, dtype, bias);
+  p.k_tiles = (int)div_up(nk, p.k_few ? 32 : wide ? (d == 64 ? attn::CrossDkdv16<64>::BKV : attn::CrossDkdv16<128>::BKV) : 128);
   const long long groups = (long long)B * Hkv * p.k_tiles;
-  if (R > 0) {   // the bias gradient of a head and key block is formed in one workgroup: parts are runs of heads
+  if (bias) {   // one head's bias at a time, and one workgroup for the bias gradient of a head and tile: runs of heads
     p.k_splits = groups >= 256 ? 1 : (int)std::min<long long>(512 / groups, G);
     p.k_per = (int)div_up(G, p.k_splits);
     p.k_splits = (int)div_up(G, p.k_per);
   } else {
-    parts(groups, G * div_up(nq, wide || (dtype == ATTN_F32 && d == 128) ? 32 : 64), p.k_splits, p.k_per);
+    parts(groups, G * div_up(nq, p.k_few || wide || (dtype == ATTN_F32 && d == 128) ? 32 : 64), p.k_few ? 16 : 4, p.k_splits, p.k_per);
   }
   const size_t qrows = (size_t)B * Hq * nq, krows = (size_t)B * Hkv * nk;
   p.rows_at = 0;
@@ -277,7 +281,7 @@ extern "C" int attn_cross_fwd(const void* q, const void* k, const void* v, void*
 
 extern "C" size_t attn_cross_bwd_workspace_bytes(int B, int Hq, int Hkv, int nq, int nk, int d, int dtype, int bias_positions) {
   if (check_sizes(B, Hq, Hkv, nq, nk, d, dtype) || bias_positions < 0 || bias_positions > attn::kBiasMax) return 0;
-  // the larger of a call's without a bias and, with one, of those with and without its gradient
+  // what a call needs, with a bias or without
   size_t most = 0;
   for (const bool bias : {false, true}) most = std::max(most, bwd_plan(B, Hq, Hkv, nq, nk, d, dtype, bias, bias ? bias_positions : 0).bytes);
   return most;
@@ -309,7 +313,7 @@ extern "C" int attn_cross_bwd(const void* q, const void* k, const void* v, const
   if (attn::rows_meet(a.dks, Hkv, a.dvs, Hkv, B, nk, d, (reinterpret_cast<intptr_t>(dv) - reinterpret_cast<intptr_t>(dk)) / elem))
     return ATTN_E_ARG;
   const BwdPlan p = bwd_plan(B, Hq, Hkv, nq, nk, d, dtype, bias != nullptr, dbias ? bias_positions : 0);
-  if (workspace_bytes < p.bytes) return ATTN_E_WORKSPACE;
+  if (workspace_bytes < attn_cross_bwd_workspace_bytes(B, Hq, Hkv, nq, nk, d, dtype, dbias ? bias_positions : 0)) return ATTN_E_WORKSPACE;
   const long long qrows = (long long)B * Hq * nq, krows = (long long)B * Hkv * nk;
   const long long q_blocks = (long long)B * Hq * p.q_tiles * p.q_splits, k_blocks = (long long)B * Hkv * p.k_tiles * p.k_splits;
   if (q_blocks > kMaxBlocks || k_blocks > kMaxBlocks) return ATTN_E_SHAPE;
@@ -341,40 +345,36 @@ extern "C" int attn_cross_bwd(const void* q, const void* k, const void* v, const
     using T = decltype(t);
     constexpr int D = decltype(dd)::value;
     constexpr bool BIAS = decltype(bb)::value;
-    constexpr int rows_per = 256 / (D / attn::Elem<T>::CH);
     const auto sum = [&](const float* part, void* out, const Strides& s, long long rows, int H, int n, int parts, const float* sums) {
       hipLaunchKernelGGL((attn::cross_sum_kernel<T, D>), dim3((unsigned)div_up(rows * (D / 4), 256)), dim3(256), 0, st, part, out, s, rows,
                          H, n, parts, sums, a.dvec);
     };
-    hipLaunchKernelGGL((attn::cross_prep_kernel<T, D>), dim3((unsigned)div_up(qrows, rows_per)), dim3(256), 0, st, aq);
-    const auto dq_of = [&](auto two) {
-      hipLaunchKernelGGL((attn::cross_dq_kernel<T, D, BIAS, decltype(two)::value>), dim3(aq.nblocks), dim3(256),
-                         bias_lds(aq), st, aq);
-    };
-    const auto dkdv_of = [&](auto two) {
-      hipLaunchKernelGGL((attn::cross_dkdv_kernel<T, D, BIAS, decltype(two)::value>), dim3(ak.nblocks), dim3(256), bias_lds(ak, ak.drel), st,
-                         ak);
-    };
-    const bool fix = BIAS || (std::is_same<T, bf16>::value && fix_dq(B, Hq, nq, nk, causal, BIAS));
-    if constexpr (BIAS) {
-      dq_of(std::true_type{});
-    } else {
-      if constexpr (std::is_same<T, bf16>::value) {
-        if (fix) dq_of(std::true_type{});
-        else dq_of(std::false_type{});
+    constexpr bool B16 = std::is_same<T, bf16>::value;
+    const auto dq_of = [&](auto fix) {
+      if (p.q_few) {
+        if constexpr (decltype(fix)::value == (B16 || BIAS))
+          hipLaunchKernelGGL((attn::cross_dq_few_kernel<T, D, BIAS, B16 || BIAS>), dim3(aq.nblocks), dim3(256), bias_lds(aq), st, aq);
       } else {
-        dq_of(std::false_type{});
+        hipLaunchKernelGGL((attn::cross_dq_kernel<T, D, BIAS, decltype(fix)::value>), dim3(aq.nblocks), dim3(256), bias_lds(aq), st, aq);
       }
+    };
+    const bool fix = BIAS || (B16 && (p.q_few || fix_dq(B, Hq, nq, nk, causal)));
+    if constexpr (BIAS || B16) {
+      if (fix) dq_of(std::true_type{});
+      else if constexpr (!BIAS) dq_of(std::false_type{});
+    } else {
+      dq_of(std::false_type{});
     }
     if (p.q_splits > 1) sum(aq.part, dq, a.dqs, qrows, Hq, nq, p.q_splits, fix ? aq.part_ml : nullptr);
-    if constexpr (std::is_same<T, bf16>::value) {
-      if (few_rows(B, Hq, nq)) {
-        dkdv_of(std::true_type{});
-      } else if constexpr (D >= 64 && !BIAS) {
-        hipLaunchKernelGGL((attn::cross_dkdv16_kernel<D>), dim3(ak.nblocks), dim3(256), 0, st, ak);
-      } else {
-        dkdv_of(std::false_type{});
-      }
+    const auto dkdv_of = [&](auto two) {
+      hipLaunchKernelGGL((attn::cross_dkdv_kernel<T, D, BIAS, decltype(two)::value>), dim3(ak.nblocks), dim3(256), bias_lds(ak, ak.drel), st, ak);
+    };
+    if (p.k_few) {
+      hipLaunchKernelGGL((attn::cross_dkdv_few_kernel<T, D, BIAS, B16>), dim3(ak.nblocks), dim3(256), bias_lds(ak, ak.drel), st, ak);
+    } else if constexpr (B16) {
+      if (few_rows(B, Hq, nq)) dkdv_of(std::true_type{});
+      else if constexpr (D >= 64 && !BIAS) hipLaunchKernelGGL((attn::cross_dkdv16_kernel<D>), dim3(ak.nblocks), dim3(256), 0, st, ak);
+      else dkdv_of(std::false_type{});
     } else {
       dkdv_of(std::false_type{});
     }

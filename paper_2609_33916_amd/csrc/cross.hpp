@@ -6,11 +6,13 @@
 //   cross_few_kernel     O, L where there are few queries: a workgroup owns 32
 //                        rows (query, head of the group) and one part of the keys
 //   cross_merge_kernel   joins the parts by their log-sum-exp
-//   cross_prep_kernel    the backward's row vectors: -D and L in base 2
-//   cross_dq_kernel      dQ and the bias gradient by relative position
+//   cross_dq_kernel      dQ, and the row vectors of what follows: -D and L in base 2
 //   cross_dkdv_kernel, cross_dkdv16_kernel
 //                        dK, dV; a workgroup owns 128 (192) keys of a cache head and
-//                        goes over the queries of all heads of its group
+//                        goes over the queries of all heads of its group; the bias gradient
+//                        by relative position
+//   cross_dq_few_kernel, cross_dkdv_few_kernel
+//                        the same for small grids: 32 queries or keys a workgroup
 //   cross_sum_kernel     adds the parts of a gradient whose sum was split
 //   cross_dbias_kernel   the bias gradient by bucket
 //
@@ -199,6 +201,29 @@ template <typename T, int D> __device__ __forceinline__ void load_row(RowRegs<T,
   if (there) x.load(row, h, flip);
   else x.zero();
 }
+
+// A row of dO and of O (and L), one per lane: -D = -sum_c dO_c O_c, and L in base 2, +inf for a
+// row that sees no key, so that its P is 0.
+template <int D> __device__ __forceinline__ float minus_d(const RowRegs<bf16, D>& g, const RowRegs<bf16, D>& o) {
+  float x = 0.f;
+#pragma unroll
+  for (int u = 0; u < RowRegs<bf16, D>::NU; ++u)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      x = fmaf(__uint_as_float(g.r[u][e] << 16), __uint_as_float(o.r[u][e] << 16), x);
+      x = fmaf(__uint_as_float(g.r[u][e] & 0xffff0000u), __uint_as_float(o.r[u][e] & 0xffff0000u), x);
+    }
+  return -halves_sum(x);
+}
+template <int D> __device__ __forceinline__ float minus_d(const RowRegs<float, D>& g, const RowRegs<float, D>& o) {
+  float x = 0.f;
+#pragma unroll
+  for (int u = 0; u < RowRegs<float, D>::NU; ++u)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x = fmaf(__uint_as_float(g.r[u][e]), __uint_as_float(o.r[u][e]), x);
+  return -halves_sum(x);
+}
+__device__ __forceinline__ float base2(float l) { return l == -INFINITY ? INFINITY : l * kLog2e; }
 
 // A transposed accumulator's row (lane (h, c): columns 32 db + 8 q4 + 4 h + [0, 4)), times f
 template <typename T, int D> __device__ __forceinline__ void store_row(T* row, const f32x16 (&acc)[D / 32], float f, int h) {
@@ -752,37 +777,6 @@ template <int D> __global__ void __launch_bounds__(256) prefix_merge_kernel(cons
 }
 
 // ======================================================================
-// Backward pre-pass: -D_i = -sum_c dO_ic O_ic and L in base 2, +inf for a row that
-// sees no key, so that its P is 0.
-// ======================================================================
-template <typename T, int D> __global__ void __launch_bounds__(256) cross_prep_kernel(const CrossArgs a) {
-  constexpr int CH = Elem<T>::CH, G = D / CH, RPB = 256 / G;
-  const int tid = threadIdx.x, ch = tid % G;
-  const long long row = (long long)blockIdx.x * RPB + tid / G;   // of [B, Hq, nq]
-  const bool there = row < a.nrows;
-  float acc = 0.f;
-  if (there) {
-    const long long head = row / a.nq;
-    const int b = (int)(head / a.Hq), hq = (int)(head % a.Hq), i = (int)(row % a.nq);
-    const T* x = (const T*)a.o + b * a.os.b + hq * a.os.h + i * a.os.t + ch * CH;
-    const T* y = (const T*)a.dout + b * a.gs.b + hq * a.gs.h + i * a.gs.t + ch * CH;
-#pragma unroll
-    for (int e = 0; e < CH; e += 4) {
-      const f32x4 u = Quad<T>::load(x + e), v = Quad<T>::load(y + e);
-#pragma unroll
-      for (int k = 0; k < 4; ++k) acc = fmaf(u[k], v[k], acc);
-    }
-  }
-#pragma unroll
-  for (int off = G / 2; off > 0; off >>= 1) acc += __shfl_xor(acc, off);
-  if (there && ch == 0) {
-    const float l = a.lse[row];
-    a.dvec[row] = -acc;
-    a.lse2[row] = l == -INFINITY ? INFINITY : l * kLog2e;
-  }
-}
-
-// ======================================================================
 // dQ: a workgroup owns 128 queries of a head, 32 per wave (Q and dO rows in
 // registers), and goes over the 64-key tiles of K and V that they see, or a run of
 // them. Per 32-key block: S^T = K Q^T, dP^T = V dO^T, dS^T, dQ^T += K^T dS^T.
@@ -830,7 +824,19 @@ __global__ void __launch_bounds__(256, sizeof(T) == 4 ? 1 : 2) cross_dq_kernel(c
   load_row<T, D>(q, (const T*)a.q + b * a.qs.b + hq * a.qs.h + qi * a.qs.t, qi < a.nq, h, a.qflip);
   load_row<T, D>(g, (const T*)a.dout + b * a.gs.b + hq * a.gs.h + qi * a.gs.t, qi < a.nq, h);
   const long long row = (long long)head * a.nq + qi;
-  const float lq = qi < a.nq ? a.lse2[row] : INFINITY, nd = qi < a.nq ? a.dvec[row] : 0.f;
+  float lq = INFINITY, nd;
+  {
+    RowRegs<T, D> o;
+    load_row<T, D>(o, (const T*)a.o + b * a.os.b + hq * a.os.h + qi * a.os.t, qi < a.nq, h);
+    nd = minus_d<D>(g, o);
+    if (qi < a.nq) {
+      lq = base2(a.lse[row]);
+      if (part == 0 && h == 0) {
+        a.lse2[row] = lq;
+        if (!FIX || a.part) a.dvec[row] = nd;
+      }
+    }
+  }
   if constexpr (BIAS) bias_fill<T>(bv, a, hq, tid);
   __syncthreads();
 
@@ -931,8 +937,74 @@ template <typename T, int D> struct CrossDkdv {
 // writes of 16 keys and 4-byte reads along diagonals fall on distinct banks.
 constexpr int kDiagRow = 68, kDiagLead = 36, kDiagTile = kDiagLead + 32 * kDiagRow;
 
+// The sums of dS by relative position of one wave, in the LDS behind the bias [RP]: sums [4 waves][RP], diagonals
+// [4 waves][kDiagTile].
+struct DiagSums {
+  float *all, *sums, *diag;
+  float lo, hi;   // of this lane: before and behind the positions of their own
+  int RP;
+  __device__ __forceinline__ DiagSums(const CrossArgs& a, float* bv, int w, int lane) : all(bv), lo(0.f), hi(0.f), RP((a.R + 2 * kBiasPad + 3) & ~3) {
+    sums = bv + RP * (1 + w);
+    diag = bv + 5 * RP + kDiagTile * w + kDiagLead;
+  }
+  __device__ __forceinline__ void clear(const CrossArgs&, int lane) {
+    for (int t = lane; t < RP; t += 64) sums[t] = 0.f;
+    lo = hi = 0.f;
+  }
+  __device__ __forceinline__ void open(const CrossArgs& a, int lane) {
+    clear(a, lane);
+    for (int t = lane - kDiagLead; t < 32 * kDiagRow; t += 64) diag[t] = 0.f;
+  }
+  // a 32 x 32 block: lane (h, c) holds queries 16 h + j of key c; rel: the first key's position relative to the first query
+  __device__ __forceinline__ void add(const CrossArgs& a, int side, int rel, const f32x16& dp, int h, int c, int lane) {
+    if (side != 0) {
+      float x = 0.f;
+#pragma unroll
+      for (int j = 0; j < 16; ++j) x += dp[j];
+      if (side < 0) lo += x;
+      else hi += x;
+    } else {
+#pragma unroll
+      for (int j = 0; j < 16; j += 4) *(f32x4*)(diag + kDiagRow * c + 16 * h + j) = (f32x4){dp[j], dp[j + 1], dp[j + 2], dp[j + 3]};
+      const float* const p = diag + lane - 32;   // key t, query t - (32 - lane)
+      float x[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int t = 0; t < 32; ++t) x[t & 3] += p[t * (kDiagRow + 1)];
+      sums[kBiasPad - a.first + rel + 32 - lane] += (x[0] + x[1]) + (x[2] + x[3]);
+    }
+  }
+  // The four waves' sums to row `row` of drel; the ends take what lies beyond. Has a barrier between the waves'
+  // writes and its reads.
+  __device__ __forceinline__ void flush(const CrossArgs& a, float (&far)[2][4], long long row, int w, int lane, int tid) {
+    float* const out = a.drel + row * a.R;
+#pragma unroll
+    for (int x = 1; x < 64; x <<= 1) {
+      lo += __shfl_xor(lo, x);
+      hi += __shfl_xor(hi, x);
+    }
+    if (lane == 0) {
+      far[0][w] = lo;
+      far[1][w] = hi;
+    }
+    __syncthreads();
+    auto sum4 = [&](int t) __attribute__((always_inline)) -> float {
+      return all[RP + t] + all[2 * RP + t] + all[3 * RP + t] + all[4 * RP + t];
+    };
+    for (int t = 1 + tid; t < a.R - 1; t += 256) out[t] = sum4(kBiasPad + t);
+    if (w < 2) {
+      const int from = w == 0 ? 0 : kBiasPad + a.R - 1;
+      float x = 0.f;
+      for (int t = lane; t <= kBiasPad; t += 64) x += sum4(from + t);
+#pragma unroll
+      for (int y = 1; y < 64; y <<= 1) x += __shfl_xor(x, y);
+      x += far[w][0] + far[w][1] + far[w][2] + far[w][3];
+      if (lane == 0) out[w == 0 ? 0 : a.R - 1] = x;
+    }
+  }
+};
+
 template <typename T, int D, bool BIAS, bool TWO>
-__global__ void __launch_bounds__(256, D == 128 ? 1 : 2) cross_dkdv_kernel(const CrossArgs a) {
+__global__ void __launch_bounds__(256, D == 128 || (sizeof(T) == 4 && D == 64 && BIAS) ? 1 : 2) cross_dkdv_kernel(const CrossArgs a) {
   constexpr int BKV = 128, BQ = CrossDkdv<T, D>::BQ, NQB = BQ / 32, NDB = D / 32;
   using TL = CrossTile<T, BQ, D>;
   __shared__ __attribute__((aligned(16))) T stA[2][TL::ELEMS];
@@ -950,15 +1022,14 @@ __global__ void __launch_bounds__(256, D == 128 ? 1 : 2) cross_dkdv_kernel(const
   const int b = head / a.Hkv, hk = head - b * a.Hkv;
   const int n = seq_len(a, b), start = seq_start(a, b);
   const int k0 = kt * BKV, kw0 = k0 + 32 * w, kj = kw0 + c;
-  const int RP = (a.R + 2 * kBiasPad + 3) & ~3;
   const bool grad = BIAS && a.drel;
 
   // query tiles [t0, nqt) of every head see the block; the part's are u0 to u1 of them all, with a
-  // bias gradient those of whole heads
+  // bias those of whole heads
   const int nqt = (a.nq + BQ - 1) / BQ;
   const int t0 = a.causal ? min(nqt, max(0, k0 - start) / BQ) : 0, per_head = nqt - t0;
   const int all = k0 < n ? a.G * per_head : 0;
-  const int per = grad ? a.per * per_head : a.per;
+  const int per = BIAS ? a.per * per_head : a.per;
   const int u0 = min(all, part * per), u1 = min(all, u0 + per);
 
   TL qld(w, lane, a.qs.t), gld(w, lane, a.gs.t);
@@ -996,43 +1067,11 @@ __global__ void __launch_bounds__(256, D == 128 ? 1 : 2) cross_dkdv_kernel(const
   for (int db = 0; db < NDB; ++db) dk[db] = dv[db] = zero16();
   const float sl2 = a.sl2;
   int bias_head = -1;   // of the group, whose bias LDS holds
-  float* const sums = bv + RP * (1 + w);
-  float* const diag = bv + 5 * RP + kDiagTile * w + kDiagLead;
-  float s_lo = 0.f, s_hi = 0.f;   // of this lane's dS: before and behind the positions of their own
-  auto clear = [&]() __attribute__((always_inline)) {
-    for (int t = lane; t < RP; t += 64) sums[t] = 0.f;
-    s_lo = s_hi = 0.f;
-  };
-  if (grad) {
-    clear();
-    for (int t = lane - kDiagLead; t < 32 * kDiagRow; t += 64) diag[t] = 0.f;
-  }
+  DiagSums ds(a, bv, w, lane);
+  if (grad) ds.open(a, lane);
   __syncthreads();
-
-  // The sums of head g of the group to its row; the ends take what lies beyond. Between barriers.
   auto flush = [&](int g) __attribute__((always_inline)) {
-    float* const out = a.drel + (((long long)b * a.Hq + hk * a.G + g) * a.ntiles + kt) * a.R;
-#pragma unroll
-    for (int x = 1; x < 64; x <<= 1) {
-      s_lo += __shfl_xor(s_lo, x);
-      s_hi += __shfl_xor(s_hi, x);
-    }
-    if (lane == 0) {
-      far[0][w] = s_lo;
-      far[1][w] = s_hi;
-    }
-    __syncthreads();
-    auto sum4 = [&](int t) __attribute__((always_inline)) -> float { return bv[RP + t] + bv[2 * RP + t] + bv[3 * RP + t] + bv[4 * RP + t]; };
-    for (int t = 1 + tid; t < a.R - 1; t += 256) out[t] = sum4(kBiasPad + t);
-    if (w < 2) {
-      const int from = w == 0 ? 0 : kBiasPad + a.R - 1;
-      float x = 0.f;
-      for (int t = lane; t <= kBiasPad; t += 64) x += sum4(from + t);
-#pragma unroll
-      for (int y = 1; y < 64; y <<= 1) x += __shfl_xor(x, y);
-      x += far[w][0] + far[w][1] + far[w][2] + far[w][3];
-      if (lane == 0) out[w == 0 ? 0 : a.R - 1] = x;
-    }
+    ds.flush(a, far, ((long long)b * a.Hq + hk * a.G + g) * a.ntiles + kt, w, lane, tid);
   };
 
   auto step = [&](int u, T* qc, T* gc, float* lc, T* qn, T* gn, float* ln) __attribute__((always_inline)) {
@@ -1044,7 +1083,7 @@ __global__ void __launch_bounds__(256, D == 128 ? 1 : 2) cross_dkdv_kernel(const
         if (grad && bias_head >= 0) {
           flush(bias_head);
           __syncthreads();
-          clear();
+          ds.clear(a, lane);
         }
         bias_fill<T>(bv, a, hk * a.G + g, tid);
         bias_head = g;
@@ -1093,24 +1132,7 @@ __global__ void __launch_bounds__(256, D == 128 ? 1 : 2) cross_dkdv_kernel(const
         }
       }
       if constexpr (BIAS) {
-        if (grad) {
-          if (side != 0) {
-            float x = 0.f;
-#pragma unroll
-            for (int j = 0; j < 16; ++j) x += dp[j];
-            if (side < 0) s_lo += x;
-            else s_hi += x;
-          } else {
-#pragma unroll
-            for (int j = 0; j < 16; j += 4)
-              *(f32x4*)(diag + kDiagRow * c + 16 * h + j) = (f32x4){dp[j], dp[j + 1], dp[j + 2], dp[j + 3]};
-            const float* const p = diag + lane - 32;   // key t, query t - (32 - lane)
-            float x[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int t = 0; t < 32; ++t) x[t & 3] += p[t * (kDiagRow + 1)];
-            sums[kBiasPad - a.first + kw0 - start - qp0 + 32 - lane] += (x[0] + x[1]) + (x[2] + x[3]);
-          }
-        }
+        if (grad) ds.add(a, side, kw0 - start - qp0, dp, h, c, lane);
       }
       mma_cols_of<TWO, D>(dv, gc, qb, s, h, c);
       mma_cols_of<TWO, D>(dk, qc, qb, dp, h, c);
@@ -1371,6 +1393,398 @@ __global__ void __launch_bounds__(256, 2) cross_dkdv16_kernel(const CrossArgs a)
       }
     }
   }
+}
+
+// ======================================================================
+// Small grids: as the two kernels above with 32 queries or 32 keys a workgroup, whose four
+// waves take the blocks of the other side in turn, each on its own; the waves' sums are added in
+// LDS at the end. Four times the workgroups and a quarter of their steps, for grids whose
+// time is the length of a workgroup's chain.
+// Operands that are read as rows come from memory straight to registers where nothing reads
+// them transposed; the others go through LDS tiles of the wave, two stages (bf16), or are
+// read by columns too (float32).
+// ======================================================================
+template <typename T, int D> struct CrossFewBwd {
+  // per buffer: the merge's half, or the tiles of four waves
+  static constexpr int DQ = WaveMerge<D>::FLOATS, DKV = WaveMerge<D>::FLOATS * (sizeof(T) == 2 ? 2 : 1);
+};
+template <typename T, int D, bool BIAS, bool FIX>
+__global__ void __launch_bounds__(256, D == 128 ? 1 : 2) cross_dq_few_kernel(const CrossArgs a) {
+  constexpr int NDB = D / 32;
+  constexpr bool B16 = sizeof(T) == 2;
+  using MG = WaveMerge<D>;
+  __shared__ __attribute__((aligned(16))) float stA[CrossFewBwd<T, D>::DQ];
+  __shared__ __attribute__((aligned(16))) float stB[CrossFewBwd<T, D>::DQ];
+  __shared__ float es[4][32];
+  extern __shared__ __attribute__((aligned(16))) float bv[];
+
+  const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, c = lane & 31;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  int head, tile;
+  block_map(blockIdx.x, a.nblocks, a.ntiles * a.splits, a.hgroup, a.causal, head, tile);
+  const int qt = tile / a.splits, part = tile - qt * a.splits;
+  const int b = head / a.Hq, hq = head - b * a.Hq, hk = hq / a.G;
+  const int n = seq_len(a, b), start = seq_start(a, b);
+  const int q0 = 32 * qt, qi = q0 + c;
+  const T* Kg = (const T*)a.k + b * a.ks.b + hk * a.ks.h;
+  const T* Vg = (const T*)a.v + b * a.vs.b + hk * a.vs.h;
+  const int kv_end = a.causal ? max(0, min(n, start + min(q0 + 32, a.nq))) : n;
+  const int first = part * a.per, nb = min((kv_end + 31) / 32, first + a.per), b0 = first + w;
+  const float sl2 = a.sl2;
+
+  RowRegs<T, D> q, g;
+  float lq = INFINITY, nd = 0.f;
+  const long long row = (long long)head * a.nq + qi;
+  auto own = [&]() __attribute__((always_inline)) {
+    load_row<T, D>(q, (const T*)a.q + b * a.qs.b + hq * a.qs.h + qi * a.qs.t, qi < a.nq, h, a.qflip);
+    load_row<T, D>(g, (const T*)a.dout + b * a.gs.b + hq * a.gs.h + qi * a.gs.t, qi < a.nq, h);
+    RowRegs<T, D> o;
+    load_row<T, D>(o, (const T*)a.o + b * a.os.b + hq * a.os.h + qi * a.os.t, qi < a.nq, h);
+    if (qi < a.nq) lq = base2(a.lse[row]);
+    nd = minus_d<D>(g, o);
+    if (qi < a.nq && part == 0 && w == 0 && h == 0) {
+      a.lse2[row] = lq;
+      if (!FIX || a.part) a.dvec[row] = nd;
+    }
+    if constexpr (BIAS) {
+      bias_fill<T>(bv, a, hq, tid);
+      __syncthreads();
+    }
+  };
+  f32x16 dqa[NDB];
+#pragma unroll
+  for (int db = 0; db < NDB; ++db) dqa[db] = zero16();
+  float sum = 0.f;
+  // dS of block kb from S and dP (which becomes dS)
+  auto grad = [&](int kb, f32x16& s, f32x16& dp) __attribute__((always_inline)) {
+    const int kb0 = 32 * kb;
+    if constexpr (BIAS) {
+      const int side = bias_side(a, kb0 - (start + q0 + 31), kb0 + 31 - (start + q0));
+      if (side != 0) {
+        const float u = bv[side < 0 ? 0 : a.R + 2 * kBiasPad - 1] - lq;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) s[j] = fmaf(s[j], sl2, u);
+      } else {
+        const float* p = bv + (kBiasPad - a.first + kb0 + 16 * h - start - qi);
+#pragma unroll
+        for (int j = 0; j < 16; ++j) s[j] = fmaf(s[j], sl2, p[j] - lq);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < 16; ++j) dp[j] = exp2_fast(BIAS ? s[j] : fmaf(s[j], sl2, -lq)) * (dp[j] + nd);
+    if (kb0 + 31 >= n || (a.causal && kb0 + 31 > start + q0)) {
+      const int lim = (a.causal ? min(start + qi, n - 1) : n - 1) - (kb0 + 16 * h);
+#pragma unroll
+      for (int j = 0; j < 16; ++j) dp[j] = j > lim ? 0.f : dp[j];
+    }
+    if constexpr (FIX) {
+      float x = 0.f;
+#pragma unroll
+      for (int j = 0; j < 16; ++j) x += dp[j];
+      sum += x;
+    }
+  };
+  auto rows_of = [&](const T* x, long long ld, int kb, RowRegs<T, D>& r) __attribute__((always_inline)) {
+    const int j = 32 * kb + perm32(c);
+    load_row<T, D>(r, x + j * ld, j < n, h);
+  };
+  if constexpr (B16) {
+    using WT = CrossWaveTile<D>;
+    const WT kt(lane, a.ks.t);
+    bf16* const tA = (bf16*)stA + w * WT::ELEMS;
+    bf16* const tB = (bf16*)stB + w * WT::ELEMS;
+    auto issue = [&](int kb, bf16* t) __attribute__((always_inline)) { kt.issue(t, Kg + 32LL * kb * a.ks.t, a.ks.t, n - 32 * kb); };
+    RowRegs<T, D> v;
+    own();
+    if (b0 < nb) {
+      issue(b0, tA);
+      rows_of(Vg, a.vs.t, b0, v);
+    }
+    auto step = [&](int kb, bf16* tc, bf16* tn) __attribute__((always_inline)) {
+      wait_vm<0>();   // this block's K tile and V rows
+      if (kb + 4 < nb) issue(kb + 4, tn);
+      f32x16 dp = zero16(), s = zero16();
+      mma_rows<D>(dp, v, g);
+      if (kb + 4 < nb) rows_of(Vg, a.vs.t, kb + 4, v);
+      mma_tile_rows<D>(s, tc, 0, q, h, c);
+      grad(kb, s, dp);
+      mma_cols_of<FIX, D>(dqa, tc, 0, dp, h, c);
+      __builtin_amdgcn_s_waitcnt(0xC07F);
+    };
+    for (int kb = b0; kb < nb; kb += 8) {
+      step(kb, tA, tB);
+      if (kb + 4 < nb) step(kb + 4, tB, tA);
+    }
+  } else {
+    RowRegs<T, D> k, v;
+    CrossCols<D> kc;
+    auto cols_of = [&](int kb) __attribute__((always_inline)) { kc.load(Kg + 32LL * kb * a.ks.t, a.ks.t, n - 32 * kb, h, c); };
+    if (b0 < nb) {
+      rows_of(Kg, a.ks.t, b0, k);
+      rows_of(Vg, a.vs.t, b0, v);
+      cols_of(b0);
+    }
+    own();
+    for (int kb = b0; kb < nb; kb += 4) {
+      const bool more = kb + 4 < nb;
+      f32x16 s = zero16(), dp = zero16();
+      mma_rows<D>(s, k, q);
+      if (more) rows_of(Kg, a.ks.t, kb + 4, k);
+      mma_rows<D>(dp, v, g);
+      if (more) rows_of(Vg, a.vs.t, kb + 4, v);
+      grad(kb, s, dp);
+      mma_cross_cols<D>(dqa, kc, dp);
+      if (more) cols_of(kb + 4);
+    }
+  }
+
+  __syncthreads();
+  if constexpr (FIX) {
+    const float e = halves_sum(sum);
+    if (h == 0) es[w][c] = e;
+  }
+  MG::put(stA, stB, w, h, c, dqa);
+  __syncthreads();
+  const int qq = tid >> 3, dp = tid & 7, qr = q0 + qq;
+  if (qr < a.nq) {
+    const float sc = a.scale, f[4] = {sc, sc, sc, sc};
+    const long long at = (long long)head * a.nq + qr;
+#pragma unroll
+    for (int e = 0; e < NDB; ++e) {
+      const f32x4 x = MG::get(stA, stB, qq, dp + 8 * e, f);
+      if (a.part) *(f32x4*)(a.part + (part * a.nrows + at) * D + 4 * (dp + 8 * e)) = x;
+      else Quad<T>::store((T*)a.dq + b * a.dqs.b + hq * a.dqs.h + qr * a.dqs.t + 4 * (dp + 8 * e), x[0], x[1], x[2], x[3]);
+    }
+  }
+  if constexpr (FIX) {
+    if (w == 0 && h == 0 && qi < a.nq) {
+      const float e = (es[0][c] + es[1][c]) + (es[2][c] + es[3][c]);
+      if (a.part) a.part_ml[part * a.nrows + row] = e;
+      else a.dvec[row] = nd - e;
+    }
+  }
+}
+
+template <typename T, int D, bool BIAS, bool TWO>
+__global__ void __launch_bounds__(256, sizeof(T) == 4 || D == 128 ? 1 : 2) cross_dkdv_few_kernel(const CrossArgs a) {
+  constexpr int NDB = D / 32;
+  constexpr bool B16 = sizeof(T) == 2;
+  using MG = WaveMerge<D>;
+  __shared__ __attribute__((aligned(16))) float stA[CrossFewBwd<T, D>::DKV];
+  __shared__ __attribute__((aligned(16))) float stB[CrossFewBwd<T, D>::DKV];
+  __shared__ __attribute__((aligned(16))) float ldA[4][2][64];   // L and -D of each wave's block
+  __shared__ __attribute__((aligned(16))) float ldB[4][2][64];
+  __shared__ float far[2][4];
+  extern __shared__ __attribute__((aligned(16))) float bv[];
+
+  const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, c = lane & 31;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  int head, tile;   // of B x Hkv, key block x part
+  block_map(blockIdx.x, a.nblocks, a.ntiles * a.splits, a.hgroup, false, head, tile);
+  const int kt = tile / a.splits, part = tile - kt * a.splits;
+  const int b = head / a.Hkv, hk = head - b * a.Hkv;
+  const int n = seq_len(a, b), start = seq_start(a, b);
+  const int k0 = 32 * kt, kj = k0 + c;
+  const float sl2 = a.sl2;
+
+  // as in cross_dkdv_kernel, in blocks of 32 queries; with a bias a part is a run of heads
+  const int nqb = (a.nq + 31) / 32;
+  const int t0 = a.causal ? min(nqb, max(0, k0 - start) / 32) : 0, per_head = nqb - t0;
+  const int all = k0 < n ? a.G * per_head : 0;
+  const int per = BIAS ? a.per * per_head : a.per;
+  const int u0 = min(all, part * per), u1 = min(all, u0 + per);
+  DiagSums ds(a, bv, w, lane);
+  const bool grad_bias = BIAS && a.drel;
+
+  f32x16 dk[NDB], dv[NDB];
+#pragma unroll
+  for (int db = 0; db < NDB; ++db) dk[db] = dv[db] = zero16();
+  RowRegs<T, D> k, v;
+  auto own = [&]() __attribute__((always_inline)) {
+    load_row<T, D>(k, (const T*)a.k + b * a.ks.b + hk * a.ks.h + kj * a.ks.t, kj < n, h, a.qflip);
+    load_row<T, D>(v, (const T*)a.v + b * a.vs.b + hk * a.vs.h + kj * a.vs.t, kj < n, h);
+  };
+  auto place = [&](int u, int& hq, int& q0) __attribute__((always_inline)) {
+    const int g = u / per_head;
+    hq = hk * a.G + g;
+    q0 = 32 * (t0 + u - g * per_head);
+  };
+  auto ldrows = [&](int hq, int q0, float (&ld)[4][2][64]) __attribute__((always_inline)) {
+    const long long row = ((long long)b * a.Hq + hq) * a.nq + q0;
+    const int bytes = 4 * min(32, a.nq - q0);   // zeros behind
+    dma4(__builtin_amdgcn_make_buffer_rsrc(a.lse2 + row, (short)0, bytes, 0x00020000), 4u * (unsigned)lane, (ATTN_LDS void*)ld[w][0]);
+    dma4(__builtin_amdgcn_make_buffer_rsrc(a.dvec + row, (short)0, bytes, 0x00020000), 4u * (unsigned)lane, (ATTN_LDS void*)ld[w][1]);
+  };
+  // P (in s) and dS (in dp) of the queries from q0 on; lane (h, c): query 16 h + j, key kj
+  auto grad = [&](int q0, const float (&ld)[4][2][64], f32x16& s, f32x16& dp) __attribute__((always_inline)) {
+    int side = 0;
+    if constexpr (BIAS) {
+      side = bias_side(a, k0 - (start + q0 + 31), k0 + 31 - (start + q0));
+      if (side == 0) {
+        const float* p = bv + (kBiasPad - a.first + kj - start - q0 - 16 * h);
+#pragma unroll
+        for (int j = 0; j < 16; ++j) s[j] = fmaf(s[j], sl2, p[-j]);
+      } else {
+        const float u = bv[side < 0 ? 0 : a.R + 2 * kBiasPad - 1];
+#pragma unroll
+        for (int j = 0; j < 16; ++j) s[j] = fmaf(s[j], sl2, u);
+      }
+    }
+    const int qb = q0 + 16 * h;
+    const bool edge = k0 + 31 >= n || q0 + 32 > a.nq || (a.causal && start + q0 < k0 + 31);
+    const int lo = kj >= n ? 16 : a.causal ? kj - start - qb : 0, hi = a.nq - 1 - qb;
+#pragma unroll
+    for (int j4 = 0; j4 < 4; ++j4) {
+      const f32x4 l4 = *(const f32x4*)&ld[w][0][16 * h + 4 * j4];
+      const f32x4 d4 = *(const f32x4*)&ld[w][1][16 * h + 4 * j4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int j = 4 * j4 + e;
+        s[j] = exp2_fast(BIAS ? s[j] - l4[e] : fmaf(s[j], sl2, -l4[e]));
+        dp[j] = s[j] * (dp[j] + d4[e]);   // d4 holds -D
+      }
+    }
+    if (edge) {
+#pragma unroll
+      for (int j = 0; j < 16; ++j) {
+        const bool out = j < lo || j > hi;
+        s[j] = out ? 0.f : s[j];
+        dp[j] = out ? 0.f : dp[j];
+      }
+    }
+    if constexpr (BIAS) {
+      if (grad_bias) ds.add(a, side, k0 - start - q0, dp, h, c, lane);
+    }
+  };
+  // blocks u0 to u1 of the part, or of one of its heads
+  auto run = [&](int from, int to) __attribute__((always_inline)) {
+    const int first = from + w;
+    if constexpr (B16) {
+      using WT = CrossWaveTile<D>;
+      const WT qt(lane, a.qs.t), gt(lane, a.gs.t);
+      bf16* const tA = (bf16*)stA + w * 2 * WT::ELEMS;
+      bf16* const tB = (bf16*)stB + w * 2 * WT::ELEMS;
+      auto issue = [&](int u, bf16* t, float (&ld)[4][2][64]) __attribute__((always_inline)) {
+        int hq, q0;
+        place(u, hq, q0);
+        qt.issue(t, (const bf16*)a.q + b * a.qs.b + hq * a.qs.h + q0 * a.qs.t, a.qs.t, a.nq - q0);
+        gt.issue(t + WT::ELEMS, (const bf16*)a.dout + b * a.gs.b + hq * a.gs.h + q0 * a.gs.t, a.gs.t, a.nq - q0);
+        ldrows(hq, q0, ld);
+      };
+      if (first < to) issue(first, tA, ldA);
+      auto step = [&](int u, bf16* tc, float (&lc)[4][2][64], bf16* tn, float (&ln)[4][2][64]) __attribute__((always_inline)) {
+        if (u + 4 < to) {
+          issue(u + 4, tn, ln);
+          wait_vm<2 * WT::NI + 2>();
+        } else {
+          wait_vm<0>();
+        }
+        int hq, q0;
+        place(u, hq, q0);
+        f32x16 s = zero16(), dp = zero16();
+        mma_tile_rows<D>(s, tc, 0, k, h, c);
+        mma_tile_rows<D>(dp, tc + WT::ELEMS, 0, v, h, c);
+        grad(q0, lc, s, dp);
+        mma_cols_of<TWO, D>(dv, tc + WT::ELEMS, 0, s, h, c);
+        mma_cols_of<TWO, D>(dk, tc, 0, dp, h, c);
+        __builtin_amdgcn_s_waitcnt(0xC07F);
+      };
+      for (int u = first; u < to; u += 8) {
+        step(u, tA, ldA, tB, ldB);
+        if (u + 4 < to) step(u + 4, tB, ldB, tA, ldA);
+      }
+    } else {
+      RowRegs<T, D> q, g;
+      CrossCols<D> qc, gc;
+      const T *Qg = nullptr, *Gg = nullptr;
+      int q0 = 0, hq = 0;
+      auto at = [&](int u) __attribute__((always_inline)) {
+        place(u, hq, q0);
+        Qg = (const T*)a.q + b * a.qs.b + hq * a.qs.h + q0 * a.qs.t;
+        Gg = (const T*)a.dout + b * a.gs.b + hq * a.gs.h + q0 * a.gs.t;
+      };
+      auto rows_of = [&](const T* x, long long ld, RowRegs<T, D>& r) __attribute__((always_inline)) {
+        load_row<T, D>(r, x + perm32(c) * ld, q0 + perm32(c) < a.nq, h);
+      };
+      if (first < to) {
+        at(first);
+        rows_of(Qg, a.qs.t, q);
+        rows_of(Gg, a.gs.t, g);
+        ldrows(hq, q0, ldA);
+        asm volatile("" ::: "memory");
+        gc.load(Gg, a.gs.t, a.nq - q0, h, c);
+        qc.load(Qg, a.qs.t, a.nq - q0, h, c);
+      }
+      auto step = [&](int u, float (&lc)[4][2][64], float (&ln)[4][2][64]) __attribute__((always_inline)) {
+        const bool more = u + 4 < to;
+        const int now = q0;
+        wait_vm<2 * CrossCols<D>::R * NDB>();   // all but the loads by columns, the L and D rows among them
+        f32x16 s = zero16(), dp = zero16();
+        mma_rows<D>(s, q, k);
+        if (more) {
+          at(u + 4);
+          rows_of(Qg, a.qs.t, q);
+        }
+        mma_rows<D>(dp, g, v);
+        if (more) {
+          rows_of(Gg, a.gs.t, g);
+          ldrows(hq, q0, ln);
+          asm volatile("" ::: "memory");   // before the loads by columns
+        }
+        grad(now, lc, s, dp);
+        mma_cross_cols<D>(dv, gc, s);
+        if (more) gc.load(Gg, a.gs.t, a.nq - q0, h, c);
+        mma_cross_cols<D>(dk, qc, dp);
+        if (more) qc.load(Qg, a.qs.t, a.nq - q0, h, c);
+        __builtin_amdgcn_s_waitcnt(0xC07F);
+      };
+      for (int u = first; u < to; u += 8) {
+        step(u, ldA, ldB);
+        if (u + 4 < to) step(u + 4, ldB, ldA);
+      }
+    }
+  };
+  own();
+  if constexpr (BIAS) {
+    if (grad_bias) ds.open(a, lane);
+    int done = part * a.per;
+    for (int g = done; g < min(a.G, (part + 1) * a.per) && all > 0; ++g) {
+      bias_fill<T>(bv, a, hk * a.G + g, tid);
+      __syncthreads();
+      run(g * per_head, (g + 1) * per_head);
+      if (grad_bias) {
+        ds.flush(a, far, ((long long)b * a.Hq + hk * a.G + g) * a.ntiles + kt, w, lane, tid);
+        __syncthreads();
+        ds.clear(a, lane);
+      }
+      __syncthreads();
+    }
+    if (grad_bias && all == 0) {   // no query sees these keys
+      for (int g = done; g < min(a.G, (part + 1) * a.per); ++g)
+        for (int t = tid; t < a.R; t += 256) a.drel[(((long long)b * a.Hq + hk * a.G + g) * a.ntiles + kt) * a.R + t] = 0.f;
+    }
+  } else {
+    run(u0, u1);
+  }
+
+  const int kk = tid >> 3, dp8 = tid & 7, kr = k0 + kk;
+  auto merge = [&](const f32x16 (&acc)[NDB], void* out, const Strides& st, float* parts, float sc) __attribute__((always_inline)) {
+    __syncthreads();
+    MG::put(stA, stB, w, h, c, acc);
+    __syncthreads();
+    if (kr < a.nk) {
+      const float f[4] = {sc, sc, sc, sc};
+#pragma unroll
+      for (int e = 0; e < NDB; ++e) {
+        const f32x4 x = MG::get(stA, stB, kk, dp8 + 8 * e, f);
+        const int col = 4 * (dp8 + 8 * e);
+        if (a.part) *(f32x4*)(parts + (part * a.nrows + (long long)head * a.nk + kr) * D + col) = x;
+        else Quad<T>::store((T*)out + b * st.b + hk * st.h + kr * st.t + col, x[0], x[1], x[2], x[3]);
+      }
+    }
+  };
+  merge(dv, a.dv, a.dvs, a.part2, 1.f);
+  merge(dk, a.dk, a.dks, a.part, a.scale);
 }
 
 // A gradient whose sum was split: rows [rows, D] float32 of `parts` parts, added in order.

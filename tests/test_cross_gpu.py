@@ -155,10 +155,19 @@ def test_bias(buckets, d, dtype):
         Call(2, 4, 2, nq, nk, d, dtype, buckets=buckets, **how).check(what=str((nq, nk, how)))
 
 
-@pytest.mark.parametrize("d", [64, 128])
-def test_bias_large_grid(d):
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("d", [32, 64, 128])
+def test_bias_large_grid(d, dtype):
     for how in ({}, {"causal": True}):
-        Call(2, 48, 16, 390, 390, d, BF16, buckets=(32, 128, not how), k_lens=[390, 200], **how).check(what=str(how))
+        Call(2, 96, 48, 390, 390, d, dtype, buckets=(32, 128, not how), k_lens=[390, 200], **how).check(what=str(how))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("d", [32, 64, 128])
+def test_few_queries_large_grid_of_keys(d, dtype):
+    for how in ({}, {"causal": True, "start": 1500}, {"buckets": (32, 128), "start": 1000}):
+        Call(2, 32, 16, 5, 1100, d, dtype, k_lens=[1100, 700], **how).check(what=str(how))
+        Call(1, 16, 16, 300, 2100, d, dtype, **how).check(what=str(how))
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
