@@ -112,8 +112,9 @@ FewPlan block_plan(int B, int Hq, int Hkv, int nq, int nk) {
   p.splits = (int)div_up(nb, p.per);
   return p;
 }
-FewPlan few_plan(int B, int Hq, int Hkv, int nq, int nk, bool bias) {
-  if (bias) Hkv = Hq;   // a workgroup holds one head's bias
+size_t bias_row_bytes(int R) { return ((R + 2 * attn::kBiasPad + 3) & ~3) * sizeof(float); }
+FewPlan few_plan(int B, int Hq, int Hkv, int nq, int nk, int R) {
+  if (R > 0 && Hq / Hkv * bias_row_bytes(R) > 24576) Hkv = Hq;   // a workgroup holds the biases of its heads
   if (wide_rows((long long)B * Hkv, (long long)nq * (Hq / Hkv), nk)) return tile_plan(B, Hq, Hkv, nq, nk, 512);
   return block_plan(B, Hq, Hkv, nq, nk);
 }
@@ -124,14 +125,14 @@ size_t few_bytes(long long rows, int d, int parts) { return parts > 1 ? (size_t)
 // their own rounding without. In calls of few rows chance may make one rounding twice
 // what it is on average; they are bound by latency, which the second product does not change.
 bool few_rows(int B, int Hq, int nq) { return (long long)B * Hq * nq <= 4096; }
-bool fix_dq(int B, int Hq, int nq, int nk, int causal) { return causal || nk <= 512 || few_rows(B, Hq, nq); }
+bool fix_dq(int B, int Hq, int nq, int nk, int causal) { return causal || nk <= attn::kFewKeys || few_rows(B, Hq, nq); }
 
 // cross_dkdv16_kernel, or cross_dkdv_kernel
 bool dkdv16(int B, int Hq, int nq, int d, int dtype, bool bias) { return dtype == ATTN_BF16 && d >= 64 && !bias && !few_rows(B, Hq, nq); }
 
 struct BwdPlan {
   bool q_few, k_few;              // 32 queries or keys a workgroup, not 128 (192)
-  int q_tiles, q_splits, q_per;   // dQ: tiles of queries; parts of the keys' blocks
+  int q_pack, q_tiles, q_splits, q_per;   // dQ: heads in a tile of rows, tiles; parts of the keys' blocks
   int k_tiles, k_splits, k_per;   // dK, dV: tiles of keys; parts of the query blocks of all heads, or of the heads
   size_t rows_at, drel_at, dq_at, sums_at, dk_at, dv_at, bytes;
 };
@@ -145,11 +146,13 @@ BwdPlan bwd_plan(int B, int Hq, int Hkv, int nq, int nk, int d, int dtype, bool 
     per = (int)div_up(steps, splits);
     splits = (int)div_up(steps, per);
   };
-  p.q_few = (long long)B * Hq * div_up(nq, 128) < 256;
-  p.q_tiles = (int)div_up(nq, p.q_few ? 32 : 128);
-  parts((long long)B * Hq * p.q_tiles, div_up(nk, p.q_few ? 32 : 64), p.q_few ? 16 : 4, p.q_splits, p.q_per);
+  p.q_few = nq <= 32 || (long long)B * Hq * div_up(nq, 128) < 256;
+  p.q_pack = nq <= 32 && (!bias || (R > 0 && G * bias_row_bytes(R) <= 24576)) ? G : 1;
+  p.q_tiles = (int)div_up((long long)nq * p.q_pack, p.q_few ? 32 : 128);
+  parts((long long)B * (Hq / p.q_pack) * p.q_tiles, div_up(nk, p.q_few ? 32 : 64), p.q_few ? 16 : 4, p.q_splits, p.q_per);
   // (the bias gradient of d = 128 does not fit the LDS of the other)
-  p.k_few = (long long)B * Hkv * div_up(nk, 128) < (bias ? 128 : dtype == ATTN_BF16 && d <= 64 ? 384 : 256) && !(dtype == ATTN_BF16 && d == 128 && R > 0);
+  const int limit = d == 128 ? (dtype == ATTN_BF16 ? 192 : 64) : bias ? (d == 32 ? 160 : 96) : dtype == ATTN_BF16 ? 384 : 256;
+  p.k_few = (long long)B * Hkv * div_up(nk, 128) < limit && !(d == 128 && R > 0);
   const bool wide = !p.k_few && dkdv16(B, Hq, nq, d, dtype, bias);
   p.k_tiles = (int)div_up(nk, p.k_few ? 32 : wide ? (d == 64 ? attn::CrossDkdv16<64>::BKV : attn::CrossDkdv16<128>::BKV) : 128);
   const long long groups = (long long)B * Hkv * p.k_tiles;
@@ -187,11 +190,8 @@ template <typename F> void dispatch(int dtype, int d, bool bias, F&& f) {
   else with_bias(0.f);
 }
 
-size_t bias_lds(const CrossArgs& a, bool grad = false) {
-  if (!a.table) return 0;
-  const size_t row = (a.R + 2 * attn::kBiasPad + 3) & ~3;
-  return (grad ? 5 * row + 4 * attn::kDiagTile : row) * sizeof(float);
-}
+size_t bias_lds(const CrossArgs& a, int heads = 1) { return a.table ? heads * bias_row_bytes(a.R) : 0; }
+size_t bias_grad_lds(const CrossArgs& a) { return a.drel ? 5 * bias_row_bytes(a.R) + 4 * attn::kDiagTile * sizeof(float) : bias_lds(a); }
 
 // Blocks and order of a grid of `heads` heads of `tiles` tiles each
 void set_grid(CrossArgs& a, long long heads, int tiles) {
@@ -206,7 +206,7 @@ int launched() { return hipGetLastError() == hipSuccess ? ATTN_OK : ATTN_E_HIP; 
 extern "C" size_t attn_cross_fwd_workspace_bytes(int B, int Hq, int Hkv, int nq, int nk, int d, int dtype, int bias_positions) {
   if (check_sizes(B, Hq, Hkv, nq, nk, d, dtype) || bias_positions < 0) return 0;
   if (!few_queries(B, Hq, nq)) return 0;
-  return few_bytes((long long)B * Hq * nq, d, few_plan(B, Hq, Hkv, nq, nk, bias_positions > 0).splits);
+  return few_bytes((long long)B * Hq * nq, d, few_plan(B, Hq, Hkv, nq, nk, bias_positions).splits);
 }
 
 extern "C" int attn_cross_fwd(const void* q, const void* k, const void* v, void* o, float* L, const long long* strides,
@@ -232,7 +232,7 @@ extern "C" int attn_cross_fwd(const void* q, const void* k, const void* v, void*
   if (!aligned(L, 4)) return ATTN_E_ALIGN;
   if (!attn::writable(a.os, B, Hq, nq, d)) return ATTN_E_ARG;
   const bool few = few_queries(B, Hq, nq);
-  const FewPlan p = few_plan(B, Hq, Hkv, nq, nk, bias != nullptr);
+  const FewPlan p = few_plan(B, Hq, Hkv, nq, nk, bias ? bias_positions : 0);
   const long long rows = (long long)B * Hq * nq;
   const size_t need = few ? few_bytes(rows, d, p.splits) : 0;
   if (need > 0) {
@@ -263,9 +263,9 @@ extern "C" int attn_cross_fwd(const void* q, const void* k, const void* v, void*
       using T = decltype(t);
       constexpr int D = decltype(dd)::value;
       if (p.tiles)
-        hipLaunchKernelGGL((attn::cross_fwd_kernel<T, D, decltype(bb)::value, true>), dim3(a.nblocks), dim3(256), bias_lds(a), st, a);
+        hipLaunchKernelGGL((attn::cross_fwd_kernel<T, D, decltype(bb)::value, true>), dim3(a.nblocks), dim3(256), bias_lds(a, a.pack), st, a);
       else
-        hipLaunchKernelGGL((attn::cross_few_kernel<T, D, decltype(bb)::value>), dim3(a.nblocks), dim3(256), bias_lds(a), st, a);
+        hipLaunchKernelGGL((attn::cross_few_kernel<T, D, decltype(bb)::value>), dim3(a.nblocks), dim3(256), bias_lds(a, a.pack), st, a);
       if (a.splits > 1) hipLaunchKernelGGL((attn::cross_merge_kernel<T, D>), dim3((unsigned)div_up(rows, 4)), dim3(256), 0, st, a);
     });
   } else {
@@ -315,7 +315,7 @@ extern "C" int attn_cross_bwd(const void* q, const void* k, const void* v, const
   const BwdPlan p = bwd_plan(B, Hq, Hkv, nq, nk, d, dtype, bias != nullptr, dbias ? bias_positions : 0);
   if (workspace_bytes < attn_cross_bwd_workspace_bytes(B, Hq, Hkv, nq, nk, d, dtype, dbias ? bias_positions : 0)) return ATTN_E_WORKSPACE;
   const long long qrows = (long long)B * Hq * nq, krows = (long long)B * Hkv * nk;
-  const long long q_blocks = (long long)B * Hq * p.q_tiles * p.q_splits, k_blocks = (long long)B * Hkv * p.k_tiles * p.k_splits;
+  const long long q_heads = (long long)B * (Hq / p.q_pack), q_blocks = q_heads * p.q_tiles * p.q_splits, k_blocks = (long long)B * Hkv * p.k_tiles * p.k_splits;
   if (q_blocks > kMaxBlocks || k_blocks > kMaxBlocks) return ATTN_E_SHAPE;
 
   char* const ws = static_cast<char*>(workspace);
@@ -327,12 +327,14 @@ extern "C" int attn_cross_bwd(const void* q, const void* k, const void* v, const
   a.table = bias; a.rows = bias_rows; a.first = bias_first; a.R = bias_positions; a.buckets = buckets;
   a.B = B; a.Hq = Hq; a.Hkv = Hkv; a.G = Hq / Hkv; a.nq = nq; a.nk = nk;
   a.causal = causal;
+  a.two = few_rows(B, Hq, nq);
   set_scale(a, scale, dtype);
   CrossArgs aq = a, ak = a;
   aq.ntiles = p.q_tiles; aq.splits = p.q_splits; aq.per = p.q_per; aq.nrows = qrows;
   aq.part = p.q_splits > 1 ? (float*)(ws + p.dq_at) : nullptr;
   aq.part_ml = (float*)(ws + p.sums_at);
-  set_grid(aq, (long long)B * Hq, p.q_tiles * p.q_splits);
+  aq.pack = p.q_pack;
+  set_grid(aq, q_heads, p.q_tiles * p.q_splits);
   ak.ntiles = p.k_tiles; ak.splits = p.k_splits; ak.per = p.k_per; ak.nrows = krows;
   ak.part = p.k_splits > 1 ? (float*)(ws + p.dk_at) : nullptr;
   ak.part2 = (float*)(ws + p.dv_at);
@@ -353,7 +355,8 @@ extern "C" int attn_cross_bwd(const void* q, const void* k, const void* v, const
     const auto dq_of = [&](auto fix) {
       if (p.q_few) {
         if constexpr (decltype(fix)::value == (B16 || BIAS))
-          hipLaunchKernelGGL((attn::cross_dq_few_kernel<T, D, BIAS, B16 || BIAS>), dim3(aq.nblocks), dim3(256), bias_lds(aq), st, aq);
+          hipLaunchKernelGGL((attn::cross_dq_few_kernel<T, D, BIAS, B16 || BIAS>), dim3(aq.nblocks), dim3(256), bias_lds(aq, aq.pack), st,
+                             aq);
       } else {
         hipLaunchKernelGGL((attn::cross_dq_kernel<T, D, BIAS, decltype(fix)::value>), dim3(aq.nblocks), dim3(256), bias_lds(aq), st, aq);
       }
@@ -367,12 +370,21 @@ extern "C" int attn_cross_bwd(const void* q, const void* k, const void* v, const
     }
     if (p.q_splits > 1) sum(aq.part, dq, a.dqs, qrows, Hq, nq, p.q_splits, fix ? aq.part_ml : nullptr);
     const auto dkdv_of = [&](auto two) {
-      hipLaunchKernelGGL((attn::cross_dkdv_kernel<T, D, BIAS, decltype(two)::value>), dim3(ak.nblocks), dim3(256), bias_lds(ak, ak.drel), st, ak);
+      hipLaunchKernelGGL((attn::cross_dkdv_kernel<T, D, BIAS, decltype(two)::value>), dim3(ak.nblocks), dim3(256), bias_grad_lds(ak), st, ak);
     };
     if (p.k_few) {
-      hipLaunchKernelGGL((attn::cross_dkdv_few_kernel<T, D, BIAS, B16>), dim3(ak.nblocks), dim3(256), bias_lds(ak, ak.drel), st, ak);
+      const auto few_of = [&](auto two) {
+        hipLaunchKernelGGL((attn::cross_dkdv_few_kernel<T, D, BIAS, decltype(two)::value>), dim3(ak.nblocks), dim3(256),
+                           bias_grad_lds(ak), st, ak);
+      };
+      if constexpr (B16) {
+        if (a.two) few_of(std::true_type{});
+        else few_of(std::false_type{});
+      } else {
+        few_of(std::false_type{});
+      }
     } else if constexpr (B16) {
-      if (few_rows(B, Hq, nq)) dkdv_of(std::true_type{});
+      if (a.two) dkdv_of(std::true_type{});
       else if constexpr (D >= 64 && !BIAS) hipLaunchKernelGGL((attn::cross_dkdv16_kernel<D>), dim3(ak.nblocks), dim3(256), 0, st, ak);
       else dkdv_of(std::false_type{});
     } else {
@@ -400,7 +412,7 @@ struct PrefixPlan {
 };
 PrefixPlan prefix_plan(int B, int Hq, int Hkv, int np, int n) {
   PrefixPlan p;
-  p.prefix = few_plan(1, Hq, Hkv, B, np, false);
+  p.prefix = few_plan(1, Hq, Hkv, B, np, 0);
   if (p.prefix.tiles) p.prefix = tile_plan(1, Hq, Hkv, B, np, 256);
   p.own = FewPlan{Hq / Hkv, 0, 0, 0, 0, false};
   if (n > 0) p.own = block_plan(B, Hq, Hkv, 1, n);

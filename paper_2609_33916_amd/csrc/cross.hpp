@@ -72,6 +72,7 @@ struct CrossArgs {
   float scale;
   uint32_t qflip;      // sign mask of a negative scale
   int causal;
+  int two;             // dS in two bf16 parts however many keys a row sees
 };
 
 __device__ __forceinline__ int seq_len(const CrossArgs& a, int b) {
@@ -243,11 +244,16 @@ template <typename T> __device__ __forceinline__ float as_float(T x) { return (f
 // below -2^16, a type's lowest value among them, masks as -inf does: a row of such
 // scores alone has an L of which float32 holds no more than 1/128, too coarse for the
 // backward's exp(x - L), and next to any other score its P is 0 all the same.
-template <typename T> __device__ __forceinline__ void bias_fill(float* bv, const CrossArgs& a, int hq, int tid) {
+// `heads` of them stand behind each other, bias_row apart.
+__device__ __forceinline__ int bias_row(const CrossArgs& a) { return (a.R + 2 * kBiasPad + 3) & ~3; }
+template <typename T> __device__ __forceinline__ void bias_fill(float* bv, const CrossArgs& a, int hq, int tid, int heads = 1) {
   for (int t = tid; t < a.R + 2 * kBiasPad; t += 256) {
     const int k = a.rows[min(max(t - kBiasPad, 0), a.R - 1)];
-    const float x = (unsigned)k < (unsigned)a.buckets ? as_float(((const T*)a.table)[(long long)k * a.Hq + hq]) : 0.f;
-    bv[t] = x < -65536.f ? -INFINITY : x * kLog2e;
+    const T* const row = (const T*)a.table + (long long)k * a.Hq + hq;
+    for (int i = 0; i < heads; ++i) {
+      const float x = (unsigned)k < (unsigned)a.buckets ? as_float(row[i]) : 0.f;
+      bv[i * bias_row(a) + t] = x < -65536.f ? -INFINITY : x * kLog2e;
+    }
   }
 }
 // Where the relative positions [lo, hi] of a tile lie: -1 all before the first
@@ -297,7 +303,10 @@ __device__ __forceinline__ void cross_fwd(const CrossArgs& a, int bid, T (&stA)[
   }
   RowRegs<T, D> q;
   load_row<T, D>(q, (const T*)a.q + b * a.qs.b + hq * a.qs.h + qi * a.qs.t, there, h, a.qflip);
-  if constexpr (BIAS) bias_fill<T>(bv, a, hq, tid);
+  if constexpr (BIAS) {
+    bias_fill<T>(bv, a, PART ? hp * a.pack : hq, tid, PART ? a.pack : 1);
+    if constexpr (PART) bv += (hq - hp * a.pack) * bias_row(a);   // this lane's head
+  }
   kld.commit(stA[0]);
   vld.commit(stA[1]);
   __syncthreads();
@@ -415,7 +424,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 4 && D == 128 ? 1 : 2) cross
 
 // ======================================================================
 // Few queries: a workgroup owns 32 rows and one part of the keys. Row r of a cache
-// head is head r % pack of its group (all of it where there is no bias) and query
+// head is head r % pack of its group (all of it, unless its biases do not fit LDS) and query
 // r / pack, so that a group's heads share every key that is read. The four waves
 // take the part's 32-key blocks in turn, each with its own softmax; their results
 // are merged in LDS, and where the keys are in several parts, the parts by
@@ -424,59 +433,65 @@ __global__ void __launch_bounds__(256, sizeof(T) == 4 && D == 128 ? 1 : 2) cross
 // bf16: P multiplies V in two parts (the float cut to 16 bits, and the rest
 // rounded): one rounded part leaves O off by 1.5 times its own last rounding.
 // ======================================================================
-// 32 rows of a strided bf16 matrix into a tile of one wave
-template <int D> struct CrossWaveTile {
-  static constexpr int C = D / 8, NI = D / 16, ELEMS = 32 * D;
+// 32 rows of a strided matrix in LDS, copied by one wave (LDS DMA); rows permuted as in RowRead. bf16: its layout.
+// float32: the 16-byte chunks of stored row s swizzled by f32_swz(s), so that reads of 16 rows at one chunk
+// fall on distinct banks, as reads along a row do.
+template <int D> __host__ __device__ constexpr int f32_swz(int s) { return D == 32 ? (s >> 1) & 7 : s & 15; }
+template <typename T, int D> struct CrossWaveTile {
+  static constexpr int E = 16 / (int)sizeof(T), C = D / E, NI = C / 2, ELEMS = 32 * D;
   unsigned off[NI];
   __device__ __forceinline__ CrossWaveTile(int lane, long long ld) {
 #pragma unroll
     for (int j = 0; j < NI; ++j) {
       const int L = 64 * j + lane, s = L / C, slot = L % C;
-      off[j] = 2u * ((unsigned)perm32(s) * (unsigned)ld + 8u * (unsigned)(slot ^ swz<D>(s)));
+      off[j] = (unsigned)sizeof(T) * ((unsigned)perm32(s) * (unsigned)ld + (unsigned)E * (unsigned)(slot ^ (E == 8 ? swz<D>(s) : f32_swz<D>(s))));
     }
   }
-  __device__ __forceinline__ void issue(bf16* lds, const bf16* g, long long ld, int valid) const {
+  __device__ __forceinline__ void issue(T* lds, const T* g, long long ld, int valid) const {
     const auto rs = rows_rsrc<D>(g, ld, min(valid, 32));
 #pragma unroll
-    for (int j = 0; j < NI; ++j) dma16(rs, off[j], (ATTN_LDS void*)(lds + 512 * j));
+    for (int j = 0; j < NI; ++j) dma16(rs, off[j], (ATTN_LDS void*)(lds + 64 * E * j));
   }
 };
-// float32 columns of 32 rows, as ColRegs, of a strided matrix
-template <int D> struct CrossCols {
-  static constexpr int NDB = D / 32, R = D == 128 ? 4 : 8;
-  float v[R][NDB];
-  __amdgpu_buffer_rsrc_t rs;
-  unsigned off, ld4;
-  __device__ __forceinline__ void get(int t) {
+template <int D> __device__ __forceinline__ void mma_wave_rows(f32x16& acc, const bf16* tile, const RowRegs<bf16, D>& x, int h, int c) {
+  mma_tile_rows<D>(acc, tile, 0, x, h, c);
+}
+template <int D> __device__ __forceinline__ void mma_wave_rows(f32x16& acc, const float* tile, const RowRegs<float, D>& x, int h, int c) {
 #pragma unroll
-    for (int db = 0; db < NDB; ++db)
-      v[t % R][db] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rs, off + t * ld4 + 128u * db, 0, 0));
-  }
-  __device__ __forceinline__ void load(const float* g, long long ld, int valid, int h, int c) {
-    rs = rows_rsrc<D>(g, ld, min(valid, 32));
-    ld4 = 4u * (unsigned)ld;
-    off = 16u * h * ld4 + 4u * c;
+  for (int u = 0; u < D / 8; ++u) {
+    const f32x4 y = *(const f32x4*)(tile + c * D + 4 * ((2 * u + h) ^ f32_swz<D>(c)));
 #pragma unroll
-    for (int t = 0; t < R; ++t) get(t);
-  }
-};
-template <int D> __device__ __forceinline__ void mma_cross_cols(f32x16 (&acc)[D / 32], CrossCols<D>& x, const f32x16& b) {
-#pragma unroll
-  for (int t = 0; t < 16; ++t) {
-#pragma unroll
-    for (int db = 0; db < D / 32; ++db) mma(acc[db], x.v[t % CrossCols<D>::R][db], b[t]);
-    if (t + CrossCols<D>::R < 16) x.get(t + CrossCols<D>::R);
+    for (int e = 0; e < 4; ++e) mma(acc, y[e], __uint_as_float(x.r[u][e]));
   }
 }
-// LDS: the four waves' K tiles and their V tiles (bf16), each also half of the merge buffer. One stage:
+template <bool TWO, int D> __device__ __forceinline__ void mma_wave_cols(f32x16 (&acc)[D / 32], const bf16* tile, const f32x16& b, int h, int c) {
+  mma_cols_of<TWO, D>(acc, tile, 0, b, h, c);
+}
+template <bool TWO, int D> __device__ __forceinline__ void mma_wave_cols(f32x16 (&acc)[D / 32], const float* tile, const f32x16& b, int h, int c) {
+  // Logical row 16 h + t is stored row 8 (t / 4) + 4 h + t % 4; of its swizzle, what depends on the lane and
+  // the bits that meet it make four bases, the rest is an offset.
+  const float* base[4];
+#pragma unroll
+  for (int v = 0; v < 4; ++v) {
+    const int x = D == 32 ? (c >> 2) ^ (2 * h) ^ (4 * (v >> 1) + (v & 1)) : (c >> 2) ^ (4 * h) ^ v;
+    base[v] = tile + 4 * h * D + 4 * x + (c & 3);
+  }
+#pragma unroll
+  for (int t = 0; t < 16; ++t) {
+    const int v = D == 32 ? 2 * ((t >> 2) & 1) + ((t >> 1) & 1) : t & 3, row = (8 * (t >> 2) + (t & 3)) * D;
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db) mma(acc[db], base[v][row + 4 * (D == 32 ? 0 : (8 * db) ^ (8 * ((t >> 2) & 1)))], b[t]);
+  }
+}
+// LDS: the four waves' K tiles and their V tiles, each also half of the merge buffer. One stage:
 // the next block's K is copied from the end of the score products on, its V from the end of
 // the others, and the blocks in flight come from the waves: at d = 128 two workgroups fit a
-// compute unit, with two stages one.
+// compute unit (bf16), with two stages one.
+template <typename T, int D> struct FewLds { static constexpr int FLOATS = 4 * 32 * D * (int)sizeof(T) / 4; };
 
 template <typename T, int D, bool BIAS>
 __device__ __forceinline__ void cross_few(const CrossArgs& a, int bid, float* stA, float* stB, float (&ml)[2][4][32], float* bv) {
   constexpr int NDB = D / 32;
-  constexpr bool B16 = sizeof(T) == 2;
   using MG = WaveMerge<D>;
   const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, c = lane & 31;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -546,62 +561,36 @@ __device__ __forceinline__ void cross_few(const CrossArgs& a, int bid, float* st
   const T* Qg = (const T*)a.q + b * a.qs.b + hq * a.qs.h + qi * a.qs.t;
   RowRegs<T, D> q;
   const int b0 = first + w;   // this wave's blocks: b0, b0 + 4, ...
-  if constexpr (B16) {
-    using WT = CrossWaveTile<D>;
-    static_assert(4 * WT::ELEMS == 2 * MG::FLOATS, "a buffer holds four tiles");
-    const WT kt(lane, a.ks.t), vt(lane, a.vs.t);
-    bf16* const kl = (bf16*)stA + w * WT::ELEMS;
-    bf16* const vl = (bf16*)stB + w * WT::ELEMS;
-    load_row<T, D>(q, Qg, r < nr, h, a.qflip);
-    auto issue_k = [&](int kb) __attribute__((always_inline)) { kt.issue(kl, Kg + 32LL * kb * a.ks.t, a.ks.t, n - 32 * kb); };
-    auto issue_v = [&](int kb) __attribute__((always_inline)) { vt.issue(vl, Vg + 32LL * kb * a.vs.t, a.vs.t, n - 32 * kb); };
-    if constexpr (BIAS) {
-      bias_fill<T>(bv, a, hq, tid);
-      __syncthreads();
-    }
-    if (b0 < nb) {
-      issue_k(b0);
-      issue_v(b0);
-    }
-    for (int kb = b0; kb < nb; kb += 4) {
-      const bool more = kb + 4 < nb;
-      wait_vm<WT::NI>();   // K is there
-      f32x16 s = zero16();
-      mma_tile_rows<D>(s, kl, 0, q, h, c);
-      __builtin_amdgcn_s_waitcnt(0xC07F);   // reads done (lgkmcnt 0) before the tile is refilled
-      if (more) issue_k(kb + 4);
-      softmax(kb, s);
-      if (more) wait_vm<WT::NI>();   // V is there
-      else wait_vm<0>();
-      mma_tile_cols2<D>(oacc, vl, 0, s, h, c);
-      __builtin_amdgcn_s_waitcnt(0xC07F);
-      if (more) issue_v(kb + 4);
-    }
-  } else {
-    RowRegs<T, D> k;
-    CrossCols<D> v;
-    auto kload = [&](int kb) __attribute__((always_inline)) {
-      const int j = 32 * kb + perm32(c);
-      load_row<T, D>(k, Kg + j * a.ks.t, j < n, h);
-    };
-    auto vload = [&](int kb) __attribute__((always_inline)) { v.load(Vg + 32LL * kb * a.vs.t, a.vs.t, n - 32 * kb, h, c); };
-    if (b0 < nb) {
-      kload(b0);
-      vload(b0);
-    }
-    load_row<T, D>(q, Qg, r < nr, h, a.qflip);
-    if constexpr (BIAS) {
-      bias_fill<T>(bv, a, hq, tid);
-      __syncthreads();
-    }
-    for (int kb = b0; kb < nb; kb += 4) {
-      f32x16 s = zero16();
-      mma_rows<D>(s, k, q);
-      if (kb + 4 < nb) kload(kb + 4);
-      softmax(kb, s);
-      mma_cross_cols<D>(oacc, v, s);
-      if (kb + 4 < nb) vload(kb + 4);
-    }
+  using WT = CrossWaveTile<T, D>;
+  static_assert(FewLds<T, D>::FLOATS >= MG::FLOATS, "the merge's half");
+  const WT kt(lane, a.ks.t), vt(lane, a.vs.t);
+  T* const kl = (T*)stA + w * WT::ELEMS;
+  T* const vl = (T*)stB + w * WT::ELEMS;
+  load_row<T, D>(q, Qg, r < nr, h, a.qflip);
+  auto issue_k = [&](int kb) __attribute__((always_inline)) { kt.issue(kl, Kg + 32LL * kb * a.ks.t, a.ks.t, n - 32 * kb); };
+  auto issue_v = [&](int kb) __attribute__((always_inline)) { vt.issue(vl, Vg + 32LL * kb * a.vs.t, a.vs.t, n - 32 * kb); };
+  if constexpr (BIAS) {
+    bias_fill<T>(bv, a, hp * a.pack, tid, a.pack);
+    bv += (hq - hp * a.pack) * bias_row(a);   // this lane's head
+    __syncthreads();
+  }
+  if (b0 < nb) {
+    issue_k(b0);
+    issue_v(b0);
+  }
+  for (int kb = b0; kb < nb; kb += 4) {
+    const bool more = kb + 4 < nb;
+    wait_vm<WT::NI>();   // K is there
+    f32x16 s = zero16();
+    mma_wave_rows<D>(s, kl, q, h, c);
+    __builtin_amdgcn_s_waitcnt(0xC07F);   // reads done (lgkmcnt 0) before the tile is refilled
+    if (more) issue_k(kb + 4);
+    softmax(kb, s);
+    if (more) wait_vm<WT::NI>();   // V is there
+    else wait_vm<0>();
+    mma_wave_cols<true, D>(oacc, vl, s, h, c);
+    __builtin_amdgcn_s_waitcnt(0xC07F);
+    if (more) issue_v(kb + 4);
   }
 
   // ---- merge: thread -> row qq and the 4-column chunks dp + 8 e
@@ -645,8 +634,8 @@ __device__ __forceinline__ void cross_few(const CrossArgs& a, int bid, float* st
 
 template <typename T, int D, bool BIAS>
 __global__ void __launch_bounds__(256, sizeof(T) == 4 && D == 128 ? 1 : 2) cross_few_kernel(const CrossArgs a) {
-  __shared__ __attribute__((aligned(16))) float stA[WaveMerge<D>::FLOATS];
-  __shared__ __attribute__((aligned(16))) float stB[WaveMerge<D>::FLOATS];
+  __shared__ __attribute__((aligned(16))) float stA[FewLds<T, D>::FLOATS];
+  __shared__ __attribute__((aligned(16))) float stB[FewLds<T, D>::FLOATS];
   __shared__ float ml[2][4][32];
   extern __shared__ __attribute__((aligned(16))) float bv[];
   cross_few<T, D, BIAS>(a, blockIdx.x, stA, stB, ml, bv);
@@ -786,9 +775,12 @@ template <int D> __global__ void __launch_bounds__(256) prefix_merge_kernel(cons
 // Where few keys share a row that is as large as dS's own rounding to bf16, and a
 // bucket's sum over whole rows loses almost all of dS, which adds up to 0 in a row, and
 // none of P e_i. The row's sum of dS is -e_i (P adds up to 1): D without it goes to the dK/dV
-// kernel, which runs after this one and forms the bias gradient, and here dS multiplies K in two
-// bf16 parts, so that dQ's error is e_i's and its own last rounding.
+// kernel, which runs after this one and forms the bias gradient. Here, in workgroups whose first
+// row sees at most kFewKeys keys, dS multiplies K in two bf16 parts, so that dQ's error is
+// e_i's and its own last rounding (with one part 1.5 times what that leaves: n = 2048,
+// d = 64, causal, with a bias; two parts for every row cost a fifth of the kernel's time there).
 // ======================================================================
+constexpr int kFewKeys = 512;
 template <typename T, int D, bool BIAS, bool FIX>
 __global__ void __launch_bounds__(256, sizeof(T) == 4 ? 1 : 2) cross_dq_kernel(const CrossArgs a) {
   constexpr int BQ = 128, BKV = 64, NKB = 2, NDB = D / 32;
@@ -809,6 +801,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 4 ? 1 : 2) cross_dq_kernel(c
   const T* Vg = (const T*)a.v + b * a.vs.b + hk * a.vs.h;
   const int kv_end = a.causal ? max(0, min(n, start + min(q0 + BQ, a.nq))) : n;
   const int it0 = part * a.per, nt = min((kv_end + BKV - 1) / BKV, it0 + a.per);
+  const bool two = FIX && sizeof(T) == 2 && (a.two || (a.causal ? min(n, start + q0 + 1) : n) <= kFewKeys);
 
   TL kld(w, lane, a.ks.t), vld(w, lane, a.vs.t);
   auto issue = [&](TL& ld, T* lds, const T* g, long long st, int it) __attribute__((always_inline)) {
@@ -845,6 +838,8 @@ __global__ void __launch_bounds__(256, sizeof(T) == 4 ? 1 : 2) cross_dq_kernel(c
   for (int db = 0; db < NDB; ++db) dqa[db] = zero16();
   const float sl2 = a.sl2;
   float sum = 0.f;   // of this lane's dS
+  // all keys of the wave's rows are in one block: dS itself is rid of P e_i, which there is as large as dS
+  const bool alone = FIX && (a.causal ? min(n, start + qw0 + 32) : n) <= 32;
 
   auto step = [&](int it, T* kc, T* vc, T* kn, T* vn) __attribute__((always_inline)) {
     const int kv0 = it * BKV;
@@ -874,20 +869,38 @@ __global__ void __launch_bounds__(256, sizeof(T) == 4 ? 1 : 2) cross_dq_kernel(c
         }
       }
 #pragma unroll
-      for (int j = 0; j < 16; ++j) dp[j] = exp2_fast(BIAS ? s[j] : fmaf(s[j], sl2, -lq)) * (dp[j] + nd);   // nd holds -D
+      for (int j = 0; j < 16; ++j) {
+        s[j] = exp2_fast(BIAS ? s[j] : fmaf(s[j], sl2, -lq));
+        dp[j] = s[j] * (dp[j] + nd);   // nd holds -D
+      }
       if (kb0 + 31 >= n || (a.causal && kb0 + 31 > start + qw0)) {
         const int lim = (a.causal ? min(start + qi, n - 1) : n - 1) - (kb0 + 16 * h);
 #pragma unroll
-        for (int j = 0; j < 16; ++j) dp[j] = j > lim ? 0.f : dp[j];
+        for (int j = 0; j < 16; ++j) {
+          dp[j] = j > lim ? 0.f : dp[j];
+          if constexpr (FIX) s[j] = j > lim ? 0.f : s[j];
+        }
       }
       if constexpr (FIX) {
         float x = 0.f;
 #pragma unroll
         for (int j = 0; j < 16; ++j) x += dp[j];
         sum += x;
+        if (alone) {
+          const float e = halves_sum(x);
+#pragma unroll
+          for (int j = 0; j < 16; ++j) dp[j] = fmaf(-e, s[j], dp[j]);
+        }
       }
       __builtin_amdgcn_s_setprio(0);
-      mma_cols_of<FIX && sizeof(T) == 2, D>(dqa, kc, kb, dp, h, c);
+      if constexpr (FIX && sizeof(T) == 2 && D == 128) {   // (both would spill)
+        mma_tile_cols2<D>(dqa, kc, kb, dp, h, c);
+      } else if constexpr (FIX && sizeof(T) == 2) {
+        if (two) mma_tile_cols2<D>(dqa, kc, kb, dp, h, c);
+        else mma_tile_cols<D>(dqa, kc, kb, dp, h, c);
+      } else {
+        mma_tile_cols<D>(dqa, kc, kb, dp, h, c);
+      }
     }
     if constexpr (!TL::TWO) __syncthreads();
     if (it + 1 < nt) {
@@ -943,7 +956,7 @@ struct DiagSums {
   float *all, *sums, *diag;
   float lo, hi;   // of this lane: before and behind the positions of their own
   int RP;
-  __device__ __forceinline__ DiagSums(const CrossArgs& a, float* bv, int w, int lane) : all(bv), lo(0.f), hi(0.f), RP((a.R + 2 * kBiasPad + 3) & ~3) {
+  __device__ __forceinline__ DiagSums(const CrossArgs& a, float* bv, int w, int lane) : all(bv), lo(0.f), hi(0.f), RP(bias_row(a)) {
     sums = bv + RP * (1 + w);
     diag = bv + 5 * RP + kDiagTile * w + kDiagLead;
   }
@@ -1400,13 +1413,14 @@ __global__ void __launch_bounds__(256, 2) cross_dkdv16_kernel(const CrossArgs a)
 // waves take the blocks of the other side in turn, each on its own; the waves' sums are added in
 // LDS at the end. Four times the workgroups and a quarter of their steps, for grids whose
 // time is the length of a workgroup's chain.
-// Operands that are read as rows come from memory straight to registers where nothing reads
-// them transposed; the others go through LDS tiles of the wave, two stages (bf16), or are
-// read by columns too (float32).
+// Operands that are read as rows only (V for dQ) come from memory straight to registers, the
+// others go through LDS tiles of the wave, in two stages where they fit.
+// cross_dq_few_kernel may pack the heads of a group as cross_few_kernel does.
 // ======================================================================
 template <typename T, int D> struct CrossFewBwd {
-  // per buffer: the merge's half, or the tiles of four waves
-  static constexpr int DQ = WaveMerge<D>::FLOATS, DKV = WaveMerge<D>::FLOATS * (sizeof(T) == 2 ? 2 : 1);
+  // per buffer: the merge's half, or the tiles of four waves (dK, dV: of Q and dO, one stage each, in bf16;
+  // Q in one and dO in the other in float32)
+  static constexpr int DQ = FewLds<T, D>::FLOATS, DKV = 4 * 32 * D;
 };
 template <typename T, int D, bool BIAS, bool FIX>
 __global__ void __launch_bounds__(256, D == 128 ? 1 : 2) cross_dq_few_kernel(const CrossArgs a) {
@@ -1416,41 +1430,48 @@ __global__ void __launch_bounds__(256, D == 128 ? 1 : 2) cross_dq_few_kernel(con
   __shared__ __attribute__((aligned(16))) float stA[CrossFewBwd<T, D>::DQ];
   __shared__ __attribute__((aligned(16))) float stB[CrossFewBwd<T, D>::DQ];
   __shared__ float es[4][32];
-  extern __shared__ __attribute__((aligned(16))) float bv[];
+  extern __shared__ __attribute__((aligned(16))) float biases[];
+  float* bv = biases;
 
   const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, c = lane & 31;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-  int head, tile;
+  int head, tile;   // of B x Hq / pack, row tile x part
   block_map(blockIdx.x, a.nblocks, a.ntiles * a.splits, a.hgroup, a.causal, head, tile);
-  const int qt = tile / a.splits, part = tile - qt * a.splits;
-  const int b = head / a.Hq, hq = head - b * a.Hq, hk = hq / a.G;
+  const int rt = tile / a.splits, part = tile - rt * a.splits;
+  const int Hp = a.Hq / a.pack, b = head / Hp, hp = head - b * Hp, hk = hp * a.pack / a.G;
   const int n = seq_len(a, b), start = seq_start(a, b);
-  const int q0 = 32 * qt, qi = q0 + c;
+  const int r0 = 32 * rt, r = r0 + c, nr = a.nq * a.pack;
+  const int i0 = r0 / a.pack, i1 = min(r0 + 31, nr - 1) / a.pack;   // the tile's first and last query
+  const int qi = min(r, nr - 1) / a.pack, hq = hp * a.pack + min(r, nr - 1) % a.pack;
+  const bool there = r < nr;
   const T* Kg = (const T*)a.k + b * a.ks.b + hk * a.ks.h;
   const T* Vg = (const T*)a.v + b * a.vs.b + hk * a.vs.h;
-  const int kv_end = a.causal ? max(0, min(n, start + min(q0 + 32, a.nq))) : n;
+  const int kv_end = a.causal ? max(0, min(n, start + i1 + 1)) : n;
   const int first = part * a.per, nb = min((kv_end + 31) / 32, first + a.per), b0 = first + w;
+  const bool two = B16 && (a.two || (a.causal ? min(n, start + i0 + 1) : n) <= kFewKeys);
   const float sl2 = a.sl2;
 
   RowRegs<T, D> q, g;
-  float lq = INFINITY, nd = 0.f;
-  const long long row = (long long)head * a.nq + qi;
-  auto own = [&]() __attribute__((always_inline)) {
-    load_row<T, D>(q, (const T*)a.q + b * a.qs.b + hq * a.qs.h + qi * a.qs.t, qi < a.nq, h, a.qflip);
-    load_row<T, D>(g, (const T*)a.dout + b * a.gs.b + hq * a.gs.h + qi * a.gs.t, qi < a.nq, h);
+  float lq = INFINITY;
+  const long long row = ((long long)b * a.Hq + hq) * a.nq + qi;
+  load_row<T, D>(q, (const T*)a.q + b * a.qs.b + hq * a.qs.h + qi * a.qs.t, there, h, a.qflip);
+  load_row<T, D>(g, (const T*)a.dout + b * a.gs.b + hq * a.gs.h + qi * a.gs.t, there, h);
+  float nd;
+  {
     RowRegs<T, D> o;
-    load_row<T, D>(o, (const T*)a.o + b * a.os.b + hq * a.os.h + qi * a.os.t, qi < a.nq, h);
-    if (qi < a.nq) lq = base2(a.lse[row]);
+    load_row<T, D>(o, (const T*)a.o + b * a.os.b + hq * a.os.h + qi * a.os.t, there, h);
+    if (there) lq = base2(a.lse[row]);
     nd = minus_d<D>(g, o);
-    if (qi < a.nq && part == 0 && w == 0 && h == 0) {
-      a.lse2[row] = lq;
-      if (!FIX || a.part) a.dvec[row] = nd;
-    }
-    if constexpr (BIAS) {
-      bias_fill<T>(bv, a, hq, tid);
-      __syncthreads();
-    }
-  };
+  }
+  if (there && part == 0 && w == 0 && h == 0) {
+    a.lse2[row] = lq;
+    if (!FIX || a.part) a.dvec[row] = nd;
+  }
+  if constexpr (BIAS) {
+    bias_fill<T>(bv, a, hp * a.pack, tid, a.pack);
+    bv += (hq - hp * a.pack) * bias_row(a);   // this lane's head
+    __syncthreads();
+  }
   f32x16 dqa[NDB];
 #pragma unroll
   for (int db = 0; db < NDB; ++db) dqa[db] = zero16();
@@ -1459,7 +1480,7 @@ __global__ void __launch_bounds__(256, D == 128 ? 1 : 2) cross_dq_few_kernel(con
   auto grad = [&](int kb, f32x16& s, f32x16& dp) __attribute__((always_inline)) {
     const int kb0 = 32 * kb;
     if constexpr (BIAS) {
-      const int side = bias_side(a, kb0 - (start + q0 + 31), kb0 + 31 - (start + q0));
+      const int side = bias_side(a, kb0 - (start + i1), kb0 + 31 - (start + i0));
       if (side != 0) {
         const float u = bv[side < 0 ? 0 : a.R + 2 * kBiasPad - 1] - lq;
 #pragma unroll
@@ -1471,71 +1492,59 @@ __global__ void __launch_bounds__(256, D == 128 ? 1 : 2) cross_dq_few_kernel(con
       }
     }
 #pragma unroll
-    for (int j = 0; j < 16; ++j) dp[j] = exp2_fast(BIAS ? s[j] : fmaf(s[j], sl2, -lq)) * (dp[j] + nd);
-    if (kb0 + 31 >= n || (a.causal && kb0 + 31 > start + q0)) {
+    for (int j = 0; j < 16; ++j) {
+      s[j] = exp2_fast(BIAS ? s[j] : fmaf(s[j], sl2, -lq));
+      dp[j] = s[j] * (dp[j] + nd);
+    }
+    if (kb0 + 31 >= n || (a.causal && kb0 + 31 > start + i0)) {
       const int lim = (a.causal ? min(start + qi, n - 1) : n - 1) - (kb0 + 16 * h);
 #pragma unroll
-      for (int j = 0; j < 16; ++j) dp[j] = j > lim ? 0.f : dp[j];
+      for (int j = 0; j < 16; ++j) {
+        dp[j] = j > lim ? 0.f : dp[j];
+        if constexpr (FIX) s[j] = j > lim ? 0.f : s[j];
+      }
     }
     if constexpr (FIX) {
       float x = 0.f;
 #pragma unroll
       for (int j = 0; j < 16; ++j) x += dp[j];
       sum += x;
+      if (kv_end <= 32) {   // as in cross_dq_kernel
+        const float e = halves_sum(x);
+#pragma unroll
+        for (int j = 0; j < 16; ++j) dp[j] = fmaf(-e, s[j], dp[j]);
+      }
     }
   };
   auto rows_of = [&](const T* x, long long ld, int kb, RowRegs<T, D>& r) __attribute__((always_inline)) {
     const int j = 32 * kb + perm32(c);
     load_row<T, D>(r, x + j * ld, j < n, h);
   };
-  if constexpr (B16) {
-    using WT = CrossWaveTile<D>;
-    const WT kt(lane, a.ks.t);
-    bf16* const tA = (bf16*)stA + w * WT::ELEMS;
-    bf16* const tB = (bf16*)stB + w * WT::ELEMS;
-    auto issue = [&](int kb, bf16* t) __attribute__((always_inline)) { kt.issue(t, Kg + 32LL * kb * a.ks.t, a.ks.t, n - 32 * kb); };
-    RowRegs<T, D> v;
-    own();
-    if (b0 < nb) {
-      issue(b0, tA);
-      rows_of(Vg, a.vs.t, b0, v);
-    }
-    auto step = [&](int kb, bf16* tc, bf16* tn) __attribute__((always_inline)) {
-      wait_vm<0>();   // this block's K tile and V rows
-      if (kb + 4 < nb) issue(kb + 4, tn);
-      f32x16 dp = zero16(), s = zero16();
-      mma_rows<D>(dp, v, g);
-      if (kb + 4 < nb) rows_of(Vg, a.vs.t, kb + 4, v);
-      mma_tile_rows<D>(s, tc, 0, q, h, c);
-      grad(kb, s, dp);
-      mma_cols_of<FIX, D>(dqa, tc, 0, dp, h, c);
-      __builtin_amdgcn_s_waitcnt(0xC07F);
-    };
-    for (int kb = b0; kb < nb; kb += 8) {
-      step(kb, tA, tB);
-      if (kb + 4 < nb) step(kb + 4, tB, tA);
-    }
-  } else {
-    RowRegs<T, D> k, v;
-    CrossCols<D> kc;
-    auto cols_of = [&](int kb) __attribute__((always_inline)) { kc.load(Kg + 32LL * kb * a.ks.t, a.ks.t, n - 32 * kb, h, c); };
-    if (b0 < nb) {
-      rows_of(Kg, a.ks.t, b0, k);
-      rows_of(Vg, a.vs.t, b0, v);
-      cols_of(b0);
-    }
-    own();
-    for (int kb = b0; kb < nb; kb += 4) {
-      const bool more = kb + 4 < nb;
-      f32x16 s = zero16(), dp = zero16();
-      mma_rows<D>(s, k, q);
-      if (more) rows_of(Kg, a.ks.t, kb + 4, k);
-      mma_rows<D>(dp, v, g);
-      if (more) rows_of(Vg, a.vs.t, kb + 4, v);
-      grad(kb, s, dp);
-      mma_cross_cols<D>(dqa, kc, dp);
-      if (more) cols_of(kb + 4);
-    }
+  using WT = CrossWaveTile<T, D>;
+  const WT kt(lane, a.ks.t);
+  T* const tA = (T*)stA + w * WT::ELEMS;
+  T* const tB = (T*)stB + w * WT::ELEMS;
+  auto issue = [&](int kb, T* t) __attribute__((always_inline)) { kt.issue(t, Kg + 32LL * kb * a.ks.t, a.ks.t, n - 32 * kb); };
+  RowRegs<T, D> v;
+  if (b0 < nb) {
+    issue(b0, tA);
+    rows_of(Vg, a.vs.t, b0, v);
+  }
+  auto step = [&](int kb, T* tc, T* tn) __attribute__((always_inline)) {
+    wait_vm<0>();   // this block's K tile and V rows
+    if (kb + 4 < nb) issue(kb + 4, tn);
+    f32x16 dp = zero16(), s = zero16();
+    mma_rows<D>(dp, v, g);
+    if (kb + 4 < nb) rows_of(Vg, a.vs.t, kb + 4, v);
+    mma_wave_rows<D>(s, tc, q, h, c);
+    grad(kb, s, dp);
+    if (two) mma_wave_cols<B16, D>(dqa, tc, dp, h, c);
+    else mma_wave_cols<false, D>(dqa, tc, dp, h, c);
+    __builtin_amdgcn_s_waitcnt(0xC07F);
+  };
+  for (int kb = b0; kb < nb; kb += 8) {
+    step(kb, tA, tB);
+    if (kb + 4 < nb) step(kb + 4, tB, tA);
   }
 
   __syncthreads();
@@ -1545,19 +1554,20 @@ __global__ void __launch_bounds__(256, D == 128 ? 1 : 2) cross_dq_few_kernel(con
   }
   MG::put(stA, stB, w, h, c, dqa);
   __syncthreads();
-  const int qq = tid >> 3, dp = tid & 7, qr = q0 + qq;
-  if (qr < a.nq) {
+  const int qq = tid >> 3, dp = tid & 7, rr = r0 + qq;
+  if (rr < nr) {
     const float sc = a.scale, f[4] = {sc, sc, sc, sc};
-    const long long at = (long long)head * a.nq + qr;
+    const int i = rr / a.pack, hr = hp * a.pack + rr % a.pack;
+    const long long at = ((long long)b * a.Hq + hr) * a.nq + i;
 #pragma unroll
     for (int e = 0; e < NDB; ++e) {
       const f32x4 x = MG::get(stA, stB, qq, dp + 8 * e, f);
       if (a.part) *(f32x4*)(a.part + (part * a.nrows + at) * D + 4 * (dp + 8 * e)) = x;
-      else Quad<T>::store((T*)a.dq + b * a.dqs.b + hq * a.dqs.h + qr * a.dqs.t + 4 * (dp + 8 * e), x[0], x[1], x[2], x[3]);
+      else Quad<T>::store((T*)a.dq + b * a.dqs.b + hr * a.dqs.h + i * a.dqs.t + 4 * (dp + 8 * e), x[0], x[1], x[2], x[3]);
     }
   }
   if constexpr (FIX) {
-    if (w == 0 && h == 0 && qi < a.nq) {
+    if (w == 0 && h == 0 && there) {
       const float e = (es[0][c] + es[1][c]) + (es[2][c] + es[3][c]);
       if (a.part) a.part_ml[part * a.nrows + row] = e;
       else a.dvec[row] = nd - e;
@@ -1566,14 +1576,14 @@ __global__ void __launch_bounds__(256, D == 128 ? 1 : 2) cross_dq_few_kernel(con
 }
 
 template <typename T, int D, bool BIAS, bool TWO>
-__global__ void __launch_bounds__(256, sizeof(T) == 4 || D == 128 ? 1 : 2) cross_dkdv_few_kernel(const CrossArgs a) {
+__global__ void __launch_bounds__(256, D == 128 ? 1 : 2) cross_dkdv_few_kernel(const CrossArgs a) {
   constexpr int NDB = D / 32;
   constexpr bool B16 = sizeof(T) == 2;
   using MG = WaveMerge<D>;
   __shared__ __attribute__((aligned(16))) float stA[CrossFewBwd<T, D>::DKV];
   __shared__ __attribute__((aligned(16))) float stB[CrossFewBwd<T, D>::DKV];
   __shared__ __attribute__((aligned(16))) float ldA[4][2][64];   // L and -D of each wave's block
-  __shared__ __attribute__((aligned(16))) float ldB[4][2][64];
+  __shared__ __attribute__((aligned(16))) float ldB[B16 ? 4 : 1][2][64];
   __shared__ float far[2][4];
   extern __shared__ __attribute__((aligned(16))) float bv[];
 
@@ -1659,34 +1669,39 @@ __global__ void __launch_bounds__(256, sizeof(T) == 4 || D == 128 ? 1 : 2) cross
   // blocks u0 to u1 of the part, or of one of its heads
   auto run = [&](int from, int to) __attribute__((always_inline)) {
     const int first = from + w;
+    using WT = CrossWaveTile<T, D>;
+    const WT qt(lane, a.qs.t), gt(lane, a.gs.t);
+    auto issue_q = [&](int hq, int q0, T* t) __attribute__((always_inline)) {
+      qt.issue(t, (const T*)a.q + b * a.qs.b + hq * a.qs.h + q0 * a.qs.t, a.qs.t, a.nq - q0);
+    };
+    auto issue_g = [&](int hq, int q0, T* t) __attribute__((always_inline)) {
+      gt.issue(t, (const T*)a.dout + b * a.gs.b + hq * a.gs.h + q0 * a.gs.t, a.gs.t, a.nq - q0);
+    };
+    int hq, q0;
     if constexpr (B16) {
-      using WT = CrossWaveTile<D>;
-      const WT qt(lane, a.qs.t), gt(lane, a.gs.t);
-      bf16* const tA = (bf16*)stA + w * 2 * WT::ELEMS;
-      bf16* const tB = (bf16*)stB + w * 2 * WT::ELEMS;
-      auto issue = [&](int u, bf16* t, float (&ld)[4][2][64]) __attribute__((always_inline)) {
-        int hq, q0;
+      T* const tA = (T*)stA + w * 2 * WT::ELEMS;
+      T* const tB = (T*)stB + w * 2 * WT::ELEMS;
+      auto issue = [&](int u, T* t, float (&ld)[4][2][64]) __attribute__((always_inline)) {
         place(u, hq, q0);
-        qt.issue(t, (const bf16*)a.q + b * a.qs.b + hq * a.qs.h + q0 * a.qs.t, a.qs.t, a.nq - q0);
-        gt.issue(t + WT::ELEMS, (const bf16*)a.dout + b * a.gs.b + hq * a.gs.h + q0 * a.gs.t, a.gs.t, a.nq - q0);
+        issue_q(hq, q0, t);
+        issue_g(hq, q0, t + WT::ELEMS);
         ldrows(hq, q0, ld);
       };
       if (first < to) issue(first, tA, ldA);
-      auto step = [&](int u, bf16* tc, float (&lc)[4][2][64], bf16* tn, float (&ln)[4][2][64]) __attribute__((always_inline)) {
+      auto step = [&](int u, T* tc, float (&lc)[4][2][64], T* tn, float (&ln)[4][2][64]) __attribute__((always_inline)) {
         if (u + 4 < to) {
           issue(u + 4, tn, ln);
           wait_vm<2 * WT::NI + 2>();
         } else {
           wait_vm<0>();
         }
-        int hq, q0;
         place(u, hq, q0);
         f32x16 s = zero16(), dp = zero16();
-        mma_tile_rows<D>(s, tc, 0, k, h, c);
-        mma_tile_rows<D>(dp, tc + WT::ELEMS, 0, v, h, c);
+        mma_wave_rows<D>(s, tc, k, h, c);
+        mma_wave_rows<D>(dp, tc + WT::ELEMS, v, h, c);
         grad(q0, lc, s, dp);
-        mma_cols_of<TWO, D>(dv, tc + WT::ELEMS, 0, s, h, c);
-        mma_cols_of<TWO, D>(dk, tc, 0, dp, h, c);
+        mma_wave_cols<TWO, D>(dv, tc + WT::ELEMS, s, h, c);
+        mma_wave_cols<TWO, D>(dk, tc, dp, h, c);
         __builtin_amdgcn_s_waitcnt(0xC07F);
       };
       for (int u = first; u < to; u += 8) {
@@ -1694,53 +1709,32 @@ __global__ void __launch_bounds__(256, sizeof(T) == 4 || D == 128 ? 1 : 2) cross
         if (u + 4 < to) step(u + 4, tB, ldB, tA, ldA);
       }
     } else {
-      RowRegs<T, D> q, g;
-      CrossCols<D> qc, gc;
-      const T *Qg = nullptr, *Gg = nullptr;
-      int q0 = 0, hq = 0;
-      auto at = [&](int u) __attribute__((always_inline)) {
-        place(u, hq, q0);
-        Qg = (const T*)a.q + b * a.qs.b + hq * a.qs.h + q0 * a.qs.t;
-        Gg = (const T*)a.dout + b * a.gs.b + hq * a.gs.h + q0 * a.gs.t;
-      };
-      auto rows_of = [&](const T* x, long long ld, RowRegs<T, D>& r) __attribute__((always_inline)) {
-        load_row<T, D>(r, x + perm32(c) * ld, q0 + perm32(c) < a.nq, h);
-      };
+      T* const ql = (T*)stA + w * WT::ELEMS;
+      T* const gl = (T*)stB + w * WT::ELEMS;
       if (first < to) {
-        at(first);
-        rows_of(Qg, a.qs.t, q);
-        rows_of(Gg, a.gs.t, g);
+        place(first, hq, q0);
+        issue_q(hq, q0, ql);
+        issue_g(hq, q0, gl);
         ldrows(hq, q0, ldA);
-        asm volatile("" ::: "memory");
-        gc.load(Gg, a.gs.t, a.nq - q0, h, c);
-        qc.load(Qg, a.qs.t, a.nq - q0, h, c);
       }
-      auto step = [&](int u, float (&lc)[4][2][64], float (&ln)[4][2][64]) __attribute__((always_inline)) {
+      for (int u = first; u < to; u += 4) {
         const bool more = u + 4 < to;
+        wait_vm<0>();
         const int now = q0;
-        wait_vm<2 * CrossCols<D>::R * NDB>();   // all but the loads by columns, the L and D rows among them
+        if (more) place(u + 4, hq, q0);
         f32x16 s = zero16(), dp = zero16();
-        mma_rows<D>(s, q, k);
+        mma_wave_rows<D>(s, ql, k, h, c);
+        mma_wave_rows<D>(dp, gl, v, h, c);
+        grad(now, ldA, s, dp);
+        mma_wave_cols<false, D>(dv, gl, s, h, c);
+        __builtin_amdgcn_s_waitcnt(0xC07F);   // dO and the rows of L and D are read
         if (more) {
-          at(u + 4);
-          rows_of(Qg, a.qs.t, q);
+          issue_g(hq, q0, gl);
+          ldrows(hq, q0, ldA);
         }
-        mma_rows<D>(dp, g, v);
-        if (more) {
-          rows_of(Gg, a.gs.t, g);
-          ldrows(hq, q0, ln);
-          asm volatile("" ::: "memory");   // before the loads by columns
-        }
-        grad(now, lc, s, dp);
-        mma_cross_cols<D>(dv, gc, s);
-        if (more) gc.load(Gg, a.gs.t, a.nq - q0, h, c);
-        mma_cross_cols<D>(dk, qc, dp);
-        if (more) qc.load(Qg, a.qs.t, a.nq - q0, h, c);
+        mma_wave_cols<false, D>(dk, ql, dp, h, c);
         __builtin_amdgcn_s_waitcnt(0xC07F);
-      };
-      for (int u = first; u < to; u += 8) {
-        step(u, ldA, ldB);
-        if (u + 4 < to) step(u + 4, ldB, ldA);
+        if (more) issue_q(hq, q0, ql);
       }
     }
   };

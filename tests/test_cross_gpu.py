@@ -153,6 +153,8 @@ def test_bias(buckets, d, dtype):
     for nq, nk, how in [(200, 200, {}), (333, 333, {"causal": True}), (1, 500, {"start": 499}), (77, 450, {"causal": True, "start": 373}),
                         (150, 400, {"k_lens": [400, 0]}), (40, 700, {"start": -300}), (64, 640, {"start": 900})]:
         Call(2, 4, 2, nq, nk, d, dtype, buckets=buckets, **how).check(what=str((nq, nk, how)))
+    Call(2, 12, 2, 7, 300, d, dtype, buckets=buckets, causal=True, start=290).check(what="grouped heads")
+    Call(1, 40, 1, 3, 90, d, dtype, buckets=buckets, k_lens=[70]).check(what="40 heads on one")
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
