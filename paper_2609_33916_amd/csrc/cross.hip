@@ -151,7 +151,7 @@ BwdPlan bwd_plan(int B, int Hq, int Hkv, int nq, int nk, int d, int dtype, bool 
   p.q_tiles = (int)div_up((long long)nq * p.q_pack, p.q_few ? 32 : 128);
   parts((long long)B * (Hq / p.q_pack) * p.q_tiles, div_up(nk, p.q_few ? 32 : 64), p.q_few ? 16 : 4, p.q_splits, p.q_per);
   // (the bias gradient of d = 128 does not fit the LDS of the other)
-  const int limit = d == 128 ? (dtype == ATTN_BF16 ? 192 : 64) : bias ? (d == 32 ? 160 : 96) : dtype == ATTN_BF16 ? 384 : 256;
+  const int limit = dtype == ATTN_F32 ? 256 : d == 128 ? 192 : bias ? (d == 32 ? 160 : 96) : 384;
   p.k_few = (long long)B * Hkv * div_up(nk, 128) < limit && !(d == 128 && R > 0);
   const bool wide = !p.k_few && dkdv16(B, Hq, nq, d, dtype, bias);
   p.k_tiles = (int)div_up(nk, p.k_few ? 32 : wide ? (d == 64 ? attn::CrossDkdv16<64>::BKV : attn::CrossDkdv16<128>::BKV) : 128);
@@ -312,6 +312,9 @@ extern "C" int attn_cross_bwd(const void* q, const void* k, const void* v, const
     if (!attn::writable(all[i].s, B, all[i].H, all[i].n, d)) return ATTN_E_ARG;
   if (attn::rows_meet(a.dks, Hkv, a.dvs, Hkv, B, nk, d, (reinterpret_cast<intptr_t>(dv) - reinterpret_cast<intptr_t>(dk)) / elem))
     return ATTN_E_ARG;
+  for (int i = 6; i < 8; ++i)
+    if (attn::ranges_meet(a.dqs, Hq, nq, all[i].s, Hkv, nk, B, d, (reinterpret_cast<intptr_t>(all[i].p) - reinterpret_cast<intptr_t>(dq)) / elem))
+      return ATTN_E_ARG;
   const BwdPlan p = bwd_plan(B, Hq, Hkv, nq, nk, d, dtype, bias != nullptr, dbias ? bias_positions : 0);
   if (workspace_bytes < attn_cross_bwd_workspace_bytes(B, Hq, Hkv, nq, nk, d, dtype, dbias ? bias_positions : 0)) return ATTN_E_WORKSPACE;
   const long long qrows = (long long)B * Hq * nq, krows = (long long)B * Hkv * nk;

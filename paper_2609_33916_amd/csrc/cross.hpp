@@ -1816,10 +1816,16 @@ template <typename T> __global__ void __launch_bounds__(1024) cross_dbias_kernel
     const int t = t0 + (tid & 255);
     double x = 0.0;
     if (t < a.R) {
-#pragma unroll 8
-      for (int r = tid >> 8; r < N; r += 4) {
-        const int b = r / a.ntiles, i = r - b * a.ntiles;
-        x += (double)a.drel[(((long long)b * a.Hq + hq) * a.ntiles + i) * a.R + t];
+      const float* const at = a.drel + (long long)hq * a.ntiles * a.R + t;
+      for (int r0 = tid >> 8; r0 < N; r0 += 32) {   // eight in flight
+        float y[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const unsigned r = min(r0 + 4 * i, N - 1), b = r / (unsigned)a.ntiles;
+          y[i] = at[((long long)b * (a.Hq - 1) * a.ntiles + r) * a.R];
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x += r0 + 4 * i < N ? (double)y[i] : 0.0;
       }
     }
     __syncthreads();

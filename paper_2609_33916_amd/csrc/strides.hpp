@@ -87,4 +87,15 @@ inline bool rows_meet(const Strides& x, int Hx, const Strides& y, int Hy, int B,
   return meet(meet, 0, delta);
 }
 
+// Whether tensors x [B, Hx, nx, d] and y [B, Hy, ny, d] of any lengths certainly meet: their ranges do, and one of
+// them has no gaps. y starts `delta` elements behind x.
+inline bool ranges_meet(const Strides& x, int Hx, int nx, const Strides& y, int Hy, int ny, int B, int d, __int128 delta) {
+  const auto end = [&](const Strides& s, int H, int n) {
+    return (__int128)s.b * (B - 1) + (__int128)s.h * (H - 1) + (__int128)s.t * (n - 1) + d;
+  };
+  const __int128 ex = end(x, Hx, nx), ey = end(y, Hy, ny);
+  if (delta >= ex || -delta >= ey) return false;
+  return ex == (__int128)B * Hx * nx * d || ey == (__int128)B * Hy * ny * d;
+}
+
 }  // namespace attn

@@ -175,6 +175,9 @@ def test_refusals_of_strides(L):
         assert bwd(L, strides=one(3 * t + 1, step[2])) == -7
     assert bwd(L, ptr={"dv": 8 * FAKE}) == -7   # dK's place
     assert bwd(L, ptr={"dv": 8 * FAKE + 2 * 64}) == -7
+    for x in ("dk", "dv"):   # in dQ's place, behind its start, before its end
+        assert bwd(L, ptr={x: 7 * FAKE}) == -7 and bwd(L, ptr={x: 7 * FAKE + 128}) == -7 and bwd(L, ptr={x: 7 * FAKE - 128}) == -7
+        assert bwd(L, ptr={x: 7 * FAKE + 4 * 8 * 64 * 2}, wsb=0) == -5   # right behind it: only the workspace is wrong
 
 
 def test_workspaces(L):
