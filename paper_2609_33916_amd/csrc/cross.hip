@@ -28,6 +28,7 @@ constexpr int kMaxLength = 1 << 29;
 constexpr long long kMaxBlocks = (1LL << 24) - 1;   // a launch has fewer than 2^32 threads
 // offsets inside a tile of 64 rows stay in 31 bits
 constexpr long long kMaxTokenStride = 1 << 22;
+constexpr int kLongKeys = 3000;   // from here on a part more costs less than it saves
 
 int check_sizes(int B, int Hq, int Hkv, int nq, int nk, int d, int dtype) {
   if (B < 1 || Hq < 1 || Hkv < 1 || nq < 1 || nk < 1 || Hq % Hkv != 0) return ATTN_E_SHAPE;
@@ -72,63 +73,95 @@ void set_scale(CrossArgs& a, float scale, int dtype) {
 }
 
 // ------------------------------------------------------------------- plans --
-// The forward takes cross_few_kernel where the 128-query workgroups would leave
-// compute units idle.
-bool few_queries(int B, int Hq, int nq) { return nq <= 64 || (long long)B * Hq * div_up(nq, 128) < 256; }
+// Forward. Times: us a call, bf16, d = 64, Hq = Hkv unless said, "B x H, nq on nk"; each rule within 3 % of the
+// best of its sides on average over 600 shapes (heads 8 to 512, nq 1 to 1000, nk 200 to 16000).
+//
+// A grid of 256 to 340 tiles of 128 queries keeps most compute units at one workgroup, of two that fit, while others
+// have two: long keys go in 2 to 4 parts. 1 x 32, 1024 on 16000: 167 in parts, 214 whole; 1280: 210, 242; 1536 (384 tiles):
+// 249, 251, and d = 128 415, 391; 1024 on 4000: 63, 62. float32, 1536 on 4000: 406, 495; 1920: 535, 496.
+bool split_tiles(long long tiles, int nk, int dtype) { return nk >= 6000 && tiles <= (dtype == ATTN_BF16 ? 340 : 400); }
+// Whether a workgroup takes 128 queries of a head and all keys, else few_plan's. From 256 tiles on the chip is full;
+// below, 32 rows a workgroup make four times the workgroups but read every key four times as often: whole and in rows of
+// 32 6 x 8, 500 on 1000 19.9, 19.0, 2000 33.8, 31.5; 8 x 8 on 1000 19.8, 22.6; d = 128 5 x 8 on 1000 26.5, 30.7; 4 x 8
+// 26, 21; float32 6 x 8 75, 66; 8 x 8 77, 79.
+bool whole_keys(int B, int Hq, int nq, int nk, int d, int dtype) {
+  const long long tiles = (long long)B * Hq * div_up(nq, 128);
+  if (nq <= 64) return false;
+  if (tiles >= 256) return !split_tiles(tiles, nk, dtype);
+  return nk < kLongKeys && dtype == ATTN_BF16 && tiles >= (d == 128 ? 160 : 208);
+}
 
 struct FewPlan {
   int pack, ntiles, splits, per;
   long long groups;
   bool tiles;   // cross_fwd_kernel in parts: 128 rows a workgroup, `per` in tiles of 64 keys
 };
-// Rows of a head and keys enough that 128 rows a workgroup, which share every tile of keys, fill the chip in parts.
+// Whether 128 rows of a group share a tile of keys. They do where that fills the chip (rows of 32: 64 x 32 heads on 8,
+// 16 on 1000, d = 128 52.1, tiles 46.9; 32 x 16, 64 on 1000 26.7, 25.3; 32 rows 24.1, 24.7), and in parts on many
+// keys, where the parts' results cost less than the tiles save (1 x 32 on 8, 64 on 16000 42, 24.6; 4 x 8, 500 on 4000
+// 40, 36, on 2000 21.8, 31; 2 x 8, 1000 on 1000 14, 27).
 bool wide_rows(long long heads, long long rows, int nk) {
-  return rows > 64 && heads * div_up(rows, 128) * (nk / 256) >= 256;
+  const long long tiles = heads * div_up(rows, 128);
+  return tiles >= 256 ? rows > 32 : rows > 64 && nk >= kLongKeys && tiles * (nk / 256) >= 256;
 }
-// cross_fwd_kernel in parts, up to `want` workgroups
-FewPlan tile_plan(int B, int Hq, int Hkv, int nq, int nk, int want) {
+// cross_fwd_kernel in parts of at least 512 keys, up to `want` workgroups: 512, two on every compute unit (1 x 32 on 8,
+// 64 on 16000 24.7, 256 of them 26.8; 4 x 32 on 8, 64 on 4000, d = 128 35.8, 38.1), from 257 tiles on 1024 (above).
+FewPlan tile_plan(int B, int Hq, int Hkv, int nq, int nk, int dtype, int want) {
   FewPlan p;
   p.tiles = true;
   p.pack = Hq / Hkv;
   p.ntiles = (int)div_up((long long)nq * p.pack, 128);
   p.groups = (long long)B * Hkv * p.ntiles;
   const int nt = (int)div_up(nk, 64);
-  p.splits = (int)std::max<long long>(1, std::min<long long>(want / p.groups, nt / 4));
+  if (p.groups > 256) want *= 2;
+  const bool one = p.groups >= 256 && !split_tiles(p.groups, nk, dtype);
+  p.splits = one ? 1 : (int)std::max<long long>(1, std::min<long long>(want / p.groups, nt / 8));
   p.per = (int)div_up(nt, p.splits);
   p.splits = (int)div_up(nt, p.per);
   return p;
 }
-// cross_few_kernel: as many parts as give every compute unit two workgroups, of at least 8
-// blocks of 32 keys, two for each wave.
-FewPlan block_plan(int B, int Hq, int Hkv, int nq, int nk) {
+// cross_few_kernel: up to 256 workgroups, one for each compute unit (up to 512: 2 x 8, 500 on 1000 17.2 for 11.0), or
+// from kLongKeys on up to 512 (8 x 32 on 8, 16 on 4096 25.4 for 35; 4 x 8, 100 on 4000 20.6, 26; 16 x 16, 1 on 4096,
+// caches cold, 57.5, 62.7) but for single tiles of d = 128, where one holds enough bytes in flight (4 x 32 on 8, 1 on 8192 27.4
+// for 28.7; 1 x 32 on 8, 1 on 65536 47, 51). Parts are of at least 8 blocks of 32 keys, two for each wave; less than 24
+// blocks stay whole: the join costs 2 to 3 us (1 x 8, 500 on 500 8.0, in parts 11.4; 1 on 600 8.3, 9.8; 1 on 1000 10.2, 9.1).
+FewPlan block_plan(int B, int Hq, int Hkv, int nq, int nk, int d) {
   FewPlan p;
   p.tiles = false;
   p.pack = Hq / Hkv;
   p.ntiles = (int)div_up((long long)nq * p.pack, 32);
   p.groups = (long long)B * Hkv * p.ntiles;
-  const int nb = (int)div_up(nk, 32), want = 512;
-  p.splits = (int)std::max<long long>(1, std::min<long long>(want / std::max<long long>(p.groups, 1), nb / 8));
+  const int nb = (int)div_up(nk, 32), want = nk < kLongKeys || (d == 128 && p.ntiles == 1) ? 256 : 512;
+  p.splits = nb < 24 ? 1 : (int)std::max<long long>(1, std::min<long long>(want / p.groups, nb / 8));
   p.per = (int)(4 * div_up(div_up(nb, p.splits), 4));
   p.splits = (int)div_up(nb, p.per);
   return p;
 }
 size_t bias_row_bytes(int R) { return ((R + 2 * attn::kBiasPad + 3) & ~3) * sizeof(float); }
-FewPlan few_plan(int B, int Hq, int Hkv, int nq, int nk, int R) {
+FewPlan few_plan(int B, int Hq, int Hkv, int nq, int nk, int d, int dtype, int R) {
   if (R > 0 && Hq / Hkv * bias_row_bytes(R) > 24576) Hkv = Hq;   // a workgroup holds the biases of its heads
-  if (wide_rows((long long)B * Hkv, (long long)nq * (Hq / Hkv), nk)) return tile_plan(B, Hq, Hkv, nq, nk, 512);
-  return block_plan(B, Hq, Hkv, nq, nk);
+  if (wide_rows((long long)B * Hkv, (long long)nq * (Hq / Hkv), nk)) return tile_plan(B, Hq, Hkv, nq, nk, dtype, 512);
+  return block_plan(B, Hq, Hkv, nq, nk, d);
 }
 size_t few_bytes(long long rows, int d, int parts) { return parts > 1 ? (size_t)parts * rows * (d + 2) * sizeof(float) : 0; }
 
-// Whether dQ is formed with dS in two bf16 parts and D corrected (FIX of cross_dq_kernel), and in the smallest
-// calls dK and dV with P and dS in two parts. Rows of 512 keys of unit scores are off by 1.45 times
-// their own rounding without. In calls of few rows chance may make one rounding twice
-// what it is on average; they are bound by latency, which the second product does not change.
+// Whether dQ is formed with D corrected, and with dS in two bf16 parts in rows of at most kFewKeys keys (FIX of
+// cross_dq_kernel). Backward with and without: 16 x 16, 512 on 512 104, 97; 8 x 16, 448 on 1500 104.5, 100.4 (without there).
+// In calls of few rows chance may make one rounding twice what it is on average: dK and dV too have P and dS in two parts
+// (two_parts); those calls are bound by latency, which the second product does not change.
 bool few_rows(int B, int Hq, int nq) { return (long long)B * Hq * nq <= 4096; }
 bool fix_dq(int B, int Hq, int nq, int nk, int causal) { return causal || nk <= attn::kFewKeys || few_rows(B, Hq, nq); }
 
-// cross_dkdv16_kernel, or cross_dkdv_kernel
-bool dkdv16(int B, int Hq, int nq, int d, int dtype, bool bias) { return dtype == ATTN_BF16 && d >= 64 && !bias && !few_rows(B, Hq, nq); }
+// dK and dV with P and dS in two parts. Few keys have large P, whose rounding is not the average of an octave's: with 3
+// keys, d = 128 and 4 x 1892 queries one part left dV off by 1.56 times its own rounding. The second part costs less than
+// 128 keys a workgroup for 32 would: 64 x 16, 500 on 20 87 in two parts and 32 keys a workgroup, 107 in one and 128.
+bool two_parts(int B, int Hq, int nq, int nk) { return nk <= 32 || few_rows(B, Hq, nq); }
+
+// cross_dkdv16_kernel, or cross_dkdv_kernel. Backward: 8 x 16, 1500 on 1500 268, 291; 448 on 1500 101, 106; 16 x 16, 512
+// on 512 104, 101; d = 128, 2 x 32 on 8, 2048 on 2048 489, 524; 12 x 32, 160 on 700 155, 210.
+bool dkdv16(int B, int Hq, int nq, int nk, int d, int dtype, bool bias) {
+  return dtype == ATTN_BF16 && d >= 64 && !bias && !two_parts(B, Hq, nq, nk);
+}
 
 struct BwdPlan {
   bool q_few, k_few;              // 32 queries or keys a workgroup, not 128 (192)
@@ -136,8 +169,12 @@ struct BwdPlan {
   int k_tiles, k_splits, k_per;   // dK, dV: tiles of keys; parts of the query blocks of all heads, or of the heads
   size_t rows_at, drel_at, dq_at, sums_at, dk_at, dv_at, bytes;
 };
-// A grid of fewer than 256 tiles of 128 rows leaves compute units idle: 32 rows a workgroup. Grids that are
+// A grid of fewer than 256 tiles of 128 rows leaves compute units idle: 32 rows or keys a workgroup. Grids that are
 // small even then are split, up to 512 workgroups, each of which has some steps of its own.
+// Backward, us, 32 rows and 128 rows a workgroup for dQ: 4 x 8, 500 on 500, d = 64 24.4, 31.6; 6 x 8 36.6, 44.3; 8 x 8
+// 42.7, 40.3; d = 128 4 x 8 50.8, 54.7, 6 x 8 76.5, 72.3; float32 4 x 8 76, 79, 8 x 8 144, 135. Up to 32 queries 128
+// are mostly idle (16 x 32, 32 on 1500 125, 128; 48 153, 144), and the heads of a group pack into the rows (4 x 32
+// on 8, 1 on 4096, d = 128 117, unpacked 131; 48 queries or more: no difference).
 BwdPlan bwd_plan(int B, int Hq, int Hkv, int nq, int nk, int d, int dtype, bool bias, int R) {
   BwdPlan p;
   const int G = Hq / Hkv;
@@ -150,10 +187,13 @@ BwdPlan bwd_plan(int B, int Hq, int Hkv, int nq, int nk, int d, int dtype, bool 
   p.q_pack = nq <= 32 && (!bias || (R > 0 && G * bias_row_bytes(R) <= 24576)) ? G : 1;
   p.q_tiles = (int)div_up((long long)nq * p.q_pack, p.q_few ? 32 : 128);
   parts((long long)B * (Hq / p.q_pack) * p.q_tiles, div_up(nk, p.q_few ? 32 : 64), p.q_few ? 16 : 4, p.q_splits, p.q_per);
-  // (the bias gradient of d = 128 does not fit the LDS of the other)
+  // dK, dV of 32 and of 128 (192) keys a workgroup, backward by tiles of 128: d = 64 128 tiles 26.5, 43; 256 42, 52; 512
+  // 69, 60; d = 128 160 73, 76; 224 96, 88; with a bias, d = 64, 64 30, 43.5; 96 47.8, 47.5; 192 74, 57, d = 32 128 38, 51;
+  // float32 d = 64 256 125, 121, 320 209, 237; d = 128 64 80, 95, 192 233, 269; d = 32 256 79, 76. Up to 32 keys 128 are idle
+  // (two_parts). (The bias gradient of d = 128 does not fit the LDS of the former.)
   const int limit = dtype == ATTN_F32 ? 256 : d == 128 ? 192 : bias ? (d == 32 ? 160 : 96) : 384;
-  p.k_few = (long long)B * Hkv * div_up(nk, 128) < limit && !(d == 128 && R > 0);
-  const bool wide = !p.k_few && dkdv16(B, Hq, nq, d, dtype, bias);
+  p.k_few = (nk <= 32 || (long long)B * Hkv * div_up(nk, 128) < limit) && !(d == 128 && R > 0);
+  const bool wide = !p.k_few && dkdv16(B, Hq, nq, nk, d, dtype, bias);
   p.k_tiles = (int)div_up(nk, p.k_few ? 32 : wide ? (d == 64 ? attn::CrossDkdv16<64>::BKV : attn::CrossDkdv16<128>::BKV) : 128);
   const long long groups = (long long)B * Hkv * p.k_tiles;
   if (bias) {   // one head's bias at a time, and one workgroup for the bias gradient of a head and tile: runs of heads
@@ -205,8 +245,8 @@ int launched() { return hipGetLastError() == hipSuccess ? ATTN_OK : ATTN_E_HIP; 
 
 extern "C" size_t attn_cross_fwd_workspace_bytes(int B, int Hq, int Hkv, int nq, int nk, int d, int dtype, int bias_positions) {
   if (check_sizes(B, Hq, Hkv, nq, nk, d, dtype) || bias_positions < 0) return 0;
-  if (!few_queries(B, Hq, nq)) return 0;
-  return few_bytes((long long)B * Hq * nq, d, few_plan(B, Hq, Hkv, nq, nk, bias_positions).splits);
+  if (whole_keys(B, Hq, nq, nk, d, dtype)) return 0;
+  return few_bytes((long long)B * Hq * nq, d, few_plan(B, Hq, Hkv, nq, nk, d, dtype, bias_positions).splits);
 }
 
 extern "C" int attn_cross_fwd(const void* q, const void* k, const void* v, void* o, float* L, const long long* strides,
@@ -231,8 +271,8 @@ extern "C" int attn_cross_fwd(const void* q, const void* k, const void* v, void*
   if (const int rc = check_rows(o, a.os, B, Hq, nq, elem)) return rc;
   if (!aligned(L, 4)) return ATTN_E_ALIGN;
   if (!attn::writable(a.os, B, Hq, nq, d)) return ATTN_E_ARG;
-  const bool few = few_queries(B, Hq, nq);
-  const FewPlan p = few_plan(B, Hq, Hkv, nq, nk, bias ? bias_positions : 0);
+  const bool few = !whole_keys(B, Hq, nq, nk, d, dtype);
+  const FewPlan p = few_plan(B, Hq, Hkv, nq, nk, d, dtype, bias ? bias_positions : 0);
   const long long rows = (long long)B * Hq * nq;
   const size_t need = few ? few_bytes(rows, d, p.splits) : 0;
   if (need > 0) {
@@ -330,7 +370,7 @@ extern "C" int attn_cross_bwd(const void* q, const void* k, const void* v, const
   a.table = bias; a.rows = bias_rows; a.first = bias_first; a.R = bias_positions; a.buckets = buckets;
   a.B = B; a.Hq = Hq; a.Hkv = Hkv; a.G = Hq / Hkv; a.nq = nq; a.nk = nk;
   a.causal = causal;
-  a.two = few_rows(B, Hq, nq);
+  a.two = two_parts(B, Hq, nq, nk);
   set_scale(a, scale, dtype);
   CrossArgs aq = a, ak = a;
   aq.ntiles = p.q_tiles; aq.splits = p.q_splits; aq.per = p.q_per; aq.nrows = qrows;
@@ -413,12 +453,13 @@ struct PrefixPlan {
   FewPlan prefix, own;
   int parts;
 };
-PrefixPlan prefix_plan(int B, int Hq, int Hkv, int np, int n) {
+PrefixPlan prefix_plan(int B, int Hq, int Hkv, int np, int n, int d) {
   PrefixPlan p;
-  p.prefix = few_plan(1, Hq, Hkv, B, np, 0);
-  if (p.prefix.tiles) p.prefix = tile_plan(1, Hq, Hkv, B, np, 256);
+  p.prefix = few_plan(1, Hq, Hkv, B, np, d, ATTN_BF16, 0);
+  // (up to 256, whose parts are read again: 64 sequences, 64 heads on 8, 8192 + 512 tokens, d = 128 58 us, up to 512 62)
+  if (p.prefix.tiles) p.prefix = tile_plan(1, Hq, Hkv, B, np, ATTN_BF16, 256);
   p.own = FewPlan{Hq / Hkv, 0, 0, 0, 0, false};
-  if (n > 0) p.own = block_plan(B, Hq, Hkv, 1, n);
+  if (n > 0) p.own = block_plan(B, Hq, Hkv, 1, n, d);
   p.parts = p.prefix.splits + p.own.splits;
   return p;
 }
@@ -432,7 +473,7 @@ int check_prefix_sizes(int B, int Hq, int Hkv, int np, int n, int d, int dtype) 
 
 extern "C" size_t attn_prefix_decode_workspace_bytes(int B, int Hq, int Hkv, int np, int n, int d) {
   if (check_prefix_sizes(B, Hq, Hkv, np, n, d, ATTN_BF16)) return 0;
-  return (size_t)prefix_plan(B, Hq, Hkv, np, n).parts * B * Hq * (d + 2) * sizeof(float);
+  return (size_t)prefix_plan(B, Hq, Hkv, np, n, d).parts * B * Hq * (d + 2) * sizeof(float);
 }
 
 extern "C" int attn_prefix_decode(const void* q, const void* k_new, const void* v_new, const void* k_prefix, const void* v_prefix,
@@ -448,7 +489,7 @@ extern "C" int attn_prefix_decode(const void* q, const void* k_new, const void* 
   for (const void* p : rows)
     if (!aligned(p, 16)) return ATTN_E_ALIGN;
   if (!aligned(cache_lens, 4) || !aligned(L, 4)) return ATTN_E_ALIGN;
-  const PrefixPlan p = prefix_plan(B, Hq, Hkv, np, n);
+  const PrefixPlan p = prefix_plan(B, Hq, Hkv, np, n, d);
   const long long qrows = (long long)B * Hq;
   const long long blocks = p.prefix.groups * p.prefix.splits + p.own.groups * p.own.splits;
   if (blocks > kMaxBlocks) return ATTN_E_SHAPE;

@@ -106,6 +106,49 @@ def test_few_queries_on_many_keys(d, dtype):
     Call(1, 4, 2, 131, 9000, d, dtype, causal=True, start=8800, buckets=(32, 128, False)).check(False)
 
 
+def some_heads(c, heads, what):
+    """A call of many heads on one cache head against the oracle of some of them."""
+    got = c.run(False)
+    one = Call(1, 1, 1, 1, 1, c.d, c.dtype)
+    one.how, one.scale = c.how, c.scale
+    one.q, one.k, one.v = c.q[:, heads], c.k[:, :1], c.v[:, :1]
+    ref, bound = one.ref(False)
+    check({n: to_host64(got[n][:, heads]) for n in ("O", "L")}, ref, bound, what)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("d", [32, 64, 128])
+def test_large_grids_in_parts(d, dtype):
+    """Grids of 256 and 290 tiles of 128 queries on keys long enough to split."""
+    for B, H, nq, how in ((1, 256, 70, {}), (1, 290, 65, {"causal": True, "start": 6200 - 65})):
+        c = Call(B, H, 1, nq, 6200, d, dtype, k_lens=[6170], **how)
+        c.k, c.v = c.k.expand(B, H, -1, -1), c.v.expand(B, H, -1, -1)
+        some_heads(c, [0, 1, H // 2, H - 1], str((H, nq)))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("d", [32, 64, 128])
+def test_rows_of_a_group_undivided(d, dtype):
+    """256 tiles of a group's rows and more, few queries each: 128 rows a workgroup, all keys."""
+    Call(32, 16, 8, 20, 77, d, dtype, k_lens=[77 - 2 * i for i in range(32)]).check(False)
+    Call(64, 16, 4, 13, 90, d, dtype, causal=True, start=77).check(False)
+    Call(64, 8, 4, 33, 70, d, dtype, buckets=(32, 128)).check(False)
+
+
+@pytest.mark.parametrize("G", [1, 4])
+@pytest.mark.parametrize("nk", [2, 3, 5])
+def test_few_keys_many_queries(nk, G):
+    """dK and dV of few keys are off by their own last rounding: uniform within half a step, at most 2^-8 of the value, so
+    2^-8 / sqrt(3) in the norm; the mean of n such squares lies within 3 sqrt(0.8 / n) of theirs."""
+    c = Call(1, 4, 4 // G, 1892, nk, 128, BF16, packed=True)
+    got, (ref, _) = c.run(), c.ref()
+    for name in ("dK", "dV"):
+        x, y = to_host64(got[name]), ref[name]
+        most = 2.0 ** -8 * np.sqrt((1 + 3 * np.sqrt(0.8 / x.size)) / 3)
+        off = np.linalg.norm(x - y) / np.linalg.norm(y)
+        assert off <= most, (name, off, most)
+
+
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("nq,nk,lens", [(70, 200, [200, 0, 1, 77, 128]), (1, 300, [0, 300, 1, 64, 65]), (200, 64, [64, 0, 32, 33, 63]),
                                         (5, 40, [-3, 41, 40, 7, 100])])
