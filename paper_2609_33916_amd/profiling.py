@@ -71,6 +71,9 @@ def short_name(kernel: str) -> str:
     dkdv16_kernel<D, CAUSAL, NW, BQ, MAT, AQ, KB>; dkdv_split_kernel ends in AQ,
     dq_kernel in MAT, as does the dkdv_kernel of traces of earlier builds."""
     k = kernel.replace("void ", "")
+    own = re.search(r"(?:cross|prefix)_[a-z0-9_]*kernel", k)   # named in full: dq_kernel and others are parts of these
+    if own:
+        return own.group(0)
     for key in ("decode_append_kernel", "decode_combine_kernel", "decode_kernel",
                 "mat_fwd_kernel", "bwd_prep_kernel", "zero_f32_kernel", "dq_finalize_kernel", "fwd_pp_kernel",
                 "fwd_kernel", "fwd_split_kernel", "bwd_split_kernel", "dkdv_split_kernel", "dq_split_kernel",

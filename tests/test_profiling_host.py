@@ -38,3 +38,12 @@ def test_short_names_of_small_grid_and_float32_kernels():
     assert f("void attn::dkdv_x3_kernel<32, false, 1, 64>(attn::BwdArgs)") == "dkdv_x3_kernel"
     assert f("void attn::dq_x3_kernel<128, true, 1, 32>(attn::BwdArgs)") == "dq_x3_kernel"
     assert f("void attn::mat_dkdv_kernel<64, false>(attn::BwdArgs)") == "mat_dkdv_kernel"
+
+
+def test_short_names_of_cross_kernels():
+    f = profiling.short_name
+    for name in ("cross_fwd_kernel", "cross_few_kernel", "cross_merge_kernel", "cross_dq_kernel", "cross_dq_few_kernel",
+                 "cross_dkdv_kernel", "cross_dkdv16_kernel", "cross_dkdv_few_kernel", "cross_sum_kernel", "cross_dbias_kernel",
+                 "prefix_few_kernel", "prefix_tile_kernel", "prefix_merge_kernel"):
+        assert f(f"void attn::{name}<float, 64, true, true>(attn::CrossArgs)") == name
+        assert f(f"_ZN4attn{len(name)}{name}IDF16bLi64ELb1ELb1EEEvNS_9CrossArgsE") == name
