@@ -456,8 +456,10 @@ struct PrefixPlan {
 PrefixPlan prefix_plan(int B, int Hq, int Hkv, int np, int n, int d) {
   PrefixPlan p;
   p.prefix = few_plan(1, Hq, Hkv, B, np, d, ATTN_BF16, 0);
-  // (up to 256, whose parts are read again: 64 sequences, 64 heads on 8, 8192 + 512 tokens, d = 128 58 us, up to 512 62)
-  if (p.prefix.tiles) p.prefix = tile_plan(1, Hq, Hkv, B, np, ATTN_BF16, 256);
+  // At d = 128 one workgroup of these and one of the others fill a compute unit: up to 256 (64 sequences, 64 heads on 8, 8192
+  // + 512 tokens 53 us, up to 512 63; 256 sequences, 32 on 8, 4096 + 256 76, 85); d = 64 has room for two (64 sequences, 32
+  // on 8, 32768 + 512 50, 44).
+  if (p.prefix.tiles) p.prefix = tile_plan(1, Hq, Hkv, B, np, ATTN_BF16, d == 128 ? 256 : 512);
   p.own = FewPlan{Hq / Hkv, 0, 0, 0, 0, false};
   if (n > 0) p.own = block_plan(B, Hq, Hkv, 1, n, d);
   p.parts = p.prefix.splits + p.own.splits;
@@ -533,7 +535,7 @@ extern "C" int attn_prefix_decode(const void* q, const void* k_new, const void* 
   const auto go = [&](auto dd) {
     constexpr int D = decltype(dd)::value;
     if (p.prefix.tiles)
-      hipLaunchKernelGGL((attn::prefix_tile_kernel<D>), dim3(8 * (unsigned)(div_up(x.nblocks, 8) + div_up(y.nblocks, 8))), dim3(256), 0, st, a);
+      hipLaunchKernelGGL((attn::prefix_tile_kernel<D>), dim3((unsigned)blocks), dim3(256), 0, st, a);
     else
       hipLaunchKernelGGL((attn::prefix_few_kernel<D>), dim3((unsigned)blocks), dim3(256), 0, st, a);
     hipLaunchKernelGGL((attn::prefix_merge_kernel<D>), dim3(merge), dim3(256), 0, st, a);

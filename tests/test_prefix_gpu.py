@@ -87,6 +87,12 @@ def test_long_prefix_of_a_large_batch(d):
     Step(21, 32, 4, 8500, 40, d, [7 * i % 40 for i in range(21)]).check(p_bits=2.0 ** -8)
 
 
+@pytest.mark.parametrize("n_p", [5, 70])
+def test_short_prefix_of_many_heads(n_p):
+    """256 tiles of the batch's rows: 128 rows a tile, the prefix whole."""
+    Step(33, 256, 256, n_p, 3, 32, [i % 3 for i in range(33)]).check(p_bits=2.0 ** -8)
+
+
 def test_without_append_lengths_and_defaults():
     Step(3, 4, 2, 90, 50, 64, [50, 0, 20], append=False).check()
     Step(3, 4, 2, 90, 50, 64, None).check(n=49)
