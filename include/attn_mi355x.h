@@ -389,7 +389,7 @@ int attn_paged_decode(const void* q, const void* k_new, const void* v_new, const
  * sequences, heads and tokens, three for each tensor in the order of the arguments, or is
  * NULL for dense tensors: views of fused projections need no copy. Strides are not
  * negative, a token's at most 2^22, rows start at multiples of 16 bytes, and the rows of an output
- * must not overlap each other (ATTN_E_ARG), nor another tensor's. (An input may have
+ * must not overlap each other, nor another tensor's (ATTN_E_ARG where that is certain). (An input may have
  * strides of 0; its gradient still comes for every entry.)
  *
  * k_lens: device int32 [B] (clamped to [0, nk]) or NULL (nk). Keys from len_b on are never
@@ -433,7 +433,8 @@ int attn_cross_bwd(const void* Q, const void* K, const void* V, const void* O, c
  * Hkv, d] (both NULL: no append) go to row len_b of the caches, and q [B, Hq, d] attends to the
  * prefix, to rows [0, len_b) and to the new token. len_b = cache_lens[b] (device int32 [B])
  * clamped to [0, n], or n for all where NULL; n may be 0, n_cap >= n + 1 with an append, >= n
- * without. Tensors are dense, bfloat16 only, 16-byte aligned; O [B, Hq, d], L float32 [B, Hq] or NULL.
+ * without. Tensors are dense, bfloat16 only, 16-byte aligned; O [B, Hq, d], L float32 [B, Hq] or NULL. O,
+ * and with an append the caches, must not reach into each other or into a tensor of keys or values (ATTN_E_ARG).
  * B Hq, B Hkv n and Hkv np are below 2^26. P keeps 15 bits, 8 over the prefix of large batches. */
 size_t attn_prefix_decode_workspace_bytes(int B, int Hq, int Hkv, int np, int n, int d);
 

@@ -852,6 +852,7 @@ def attn_bias_buckets(num_buckets: int, max_distance: int, bidirectional: bool =
     side = num_buckets // 2 if bidirectional else num_buckets
     near = side // 2
     _need(near >= 1, "too few buckets")
+    _need(side <= 2048 and max_distance < 2**62, "num_buckets or max_distance is too large")
     _need(max_distance > near, f"max_distance must be above the {near} nearest positions")
     far = side - near
     borders = []   # the first position of bucket near + k, k = 1, ...: the least p with p >= near (max_distance / near)^(k / far)

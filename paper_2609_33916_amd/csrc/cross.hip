@@ -46,6 +46,15 @@ int check_rows(const void* p, const Strides& s, int B, int H, int n, int elem) {
   return aligned(p, 16) && aligned(s, elem) ? ATTN_OK : ATTN_E_ALIGN;
 }
 
+struct Rows {
+  const void* p;
+  const Strides& s;
+  int H, n;
+};
+bool meet(const Rows& x, const Rows& y, int B, int d, int elem) {
+  return attn::ranges_meet(x.s, x.H, x.n, y.s, y.H, y.n, B, d, (reinterpret_cast<intptr_t>(y.p) - reinterpret_cast<intptr_t>(x.p)) / elem);
+}
+
 struct Bias {
   const void* table;
   const int* rows;
@@ -281,6 +290,8 @@ extern "C" int attn_cross_fwd(const void* q, const void* k, const void* v, void*
     if (!aligned(workspace, 16)) return ATTN_E_ALIGN;
   }
   if ((few ? p.groups * p.splits : (long long)B * Hq * div_up(nq, 128)) > kMaxBlocks) return ATTN_E_SHAPE;
+  for (const Rows& x : {Rows{q, a.qs, Hq, nq}, Rows{k, a.ks, Hkv, nk}, Rows{v, a.vs, Hkv, nk}})
+    if (meet({o, a.os, Hq, nq}, x, B, d, elem)) return ATTN_E_ARG;
 
   a.q = q; a.k = k; a.v = v; a.o = o; a.lse = L;
   a.lens = k_lens; a.starts = starts; a.start = start;
@@ -342,7 +353,7 @@ extern "C" int attn_cross_bwd(const void* q, const void* k, const void* v, const
   const auto st3 = [&](int i, int H, int n) { return attn::strides_of(strides ? strides + 3 * i : nullptr, B, H, n, d); };
   a.qs = st3(0, Hq, nq); a.ks = st3(1, Hkv, nk); a.vs = st3(2, Hkv, nk); a.os = st3(3, Hq, nq);
   a.gs = st3(4, Hq, nq); a.dqs = st3(5, Hq, nq); a.dks = st3(6, Hkv, nk); a.dvs = st3(7, Hkv, nk);
-  const struct { const void* p; const Strides& s; int H, n; } all[8] = {
+  const Rows all[8] = {
       {q, a.qs, Hq, nq}, {k, a.ks, Hkv, nk}, {v, a.vs, Hkv, nk}, {o, a.os, Hq, nq},
       {dout, a.gs, Hq, nq}, {dq, a.dqs, Hq, nq}, {dk, a.dks, Hkv, nk}, {dv, a.dvs, Hkv, nk}};
   for (const auto& y : all)
@@ -353,13 +364,15 @@ extern "C" int attn_cross_bwd(const void* q, const void* k, const void* v, const
   if (attn::rows_meet(a.dks, Hkv, a.dvs, Hkv, B, nk, d, (reinterpret_cast<intptr_t>(dv) - reinterpret_cast<intptr_t>(dk)) / elem))
     return ATTN_E_ARG;
   for (int i = 6; i < 8; ++i)
-    if (attn::ranges_meet(a.dqs, Hq, nq, all[i].s, Hkv, nk, B, d, (reinterpret_cast<intptr_t>(all[i].p) - reinterpret_cast<intptr_t>(dq)) / elem))
-      return ATTN_E_ARG;
+    if (meet(all[5], all[i], B, d, elem)) return ATTN_E_ARG;
   const BwdPlan p = bwd_plan(B, Hq, Hkv, nq, nk, d, dtype, bias != nullptr, dbias ? bias_positions : 0);
   if (workspace_bytes < attn_cross_bwd_workspace_bytes(B, Hq, Hkv, nq, nk, d, dtype, dbias ? bias_positions : 0)) return ATTN_E_WORKSPACE;
   const long long qrows = (long long)B * Hq * nq, krows = (long long)B * Hkv * nk;
   const long long q_heads = (long long)B * (Hq / p.q_pack), q_blocks = q_heads * p.q_tiles * p.q_splits, k_blocks = (long long)B * Hkv * p.k_tiles * p.k_splits;
   if (q_blocks > kMaxBlocks || k_blocks > kMaxBlocks) return ATTN_E_SHAPE;
+  for (int i = 0; i < 5; ++i)   // the inputs are read again after the first result is written
+    for (int j = 5; j < 8; ++j)
+      if (meet(all[j], all[i], B, d, elem)) return ATTN_E_ARG;
 
   char* const ws = static_cast<char*>(workspace);
   a.q = q; a.k = k; a.v = v; a.o = const_cast<void*>(o); a.lse = const_cast<float*>(L); a.dout = dout;
@@ -496,6 +509,15 @@ extern "C" int attn_prefix_decode(const void* q, const void* k_new, const void* 
   const long long blocks = p.prefix.groups * p.prefix.splits + p.own.groups * p.own.splits;
   if (blocks > kMaxBlocks) return ATTN_E_SHAPE;
   if (workspace_bytes < (size_t)p.parts * qrows * (d + 2) * sizeof(float)) return ATTN_E_WORKSPACE;
+  // what is written: O, and the caches with an append
+  const size_t cache = (size_t)B * Hkv * n_cap * d * 2, prefix = (size_t)Hkv * np * d * 2, fresh = k_new ? (size_t)B * Hkv * d * 2 : 0;
+  const struct { const void* p; size_t size; } all[] = {{O, (size_t)qrows * d * 2}, {k_cache, cache}, {v_cache, cache}, {k_prefix, prefix},
+                                                        {v_prefix, prefix}, {k_new, fresh}, {v_new, fresh}};
+  for (int i = 0; i < (k_new ? 3 : 1); ++i)
+    for (int j = i + 1; j < 7; ++j) {
+      const char *x = (const char*)all[i].p, *y = (const char*)all[j].p;
+      if (x < y + all[j].size && y < x + all[i].size) return ATTN_E_ARG;
+    }
 
   attn::PrefixArgs a{};
   CrossArgs c{};

@@ -87,15 +87,35 @@ inline bool rows_meet(const Strides& x, int Hx, const Strides& y, int Hy, int B,
   return meet(meet, 0, delta);
 }
 
-// Whether tensors x [B, Hx, nx, d] and y [B, Hy, ny, d] of any lengths certainly meet: their ranges do, and one of
-// them has no gaps. y starts `delta` elements behind x.
-inline bool ranges_meet(const Strides& x, int Hx, int nx, const Strides& y, int Hy, int ny, int B, int d, __int128 delta) {
-  const auto end = [&](const Strides& s, int H, int n) {
-    return (__int128)s.b * (B - 1) + (__int128)s.h * (H - 1) + (__int128)s.t * (n - 1) + d;
+// Whether a row of a tensor [B, H, n, d] has an element among [lo, lo + size), counted from its start. As in rows_meet, from
+// the largest step on only those rows matter that the smaller steps can still bring there.
+inline bool rows_reach(const Strides& x, int B, int H, int n, int d, __int128 lo, __int128 size) {
+  struct { __int128 step, last; } axis[3] = {{x.b, B - 1}, {x.h, H - 1}, {x.t, n - 1}};
+  std::sort(axis, axis + 3, [](const auto& p, const auto& q) { return p.step > q.step; });
+  const auto meet = [&](const auto& self, int k, __int128 at) -> bool {   // rows from `at` on
+    if (k == 3) return at > lo - d && at < lo + size;
+    const auto& a = axis[k];
+    if (a.step == 0) return self(self, k + 1, at);
+    __int128 reach = d - 1;
+    for (int j = k + 1; j < 3; ++j) reach += axis[j].step * axis[j].last;
+    const __int128 gap = lo - reach - at;   // from the first i with at + i step + reach >= lo
+    for (__int128 i = gap > 0 ? (gap + a.step - 1) / a.step : 0; i <= a.last && at + i * a.step < lo + size; ++i)
+      if (self(self, k + 1, at + i * a.step)) return true;
+    return false;
   };
-  const __int128 ex = end(x, Hx, nx), ey = end(y, Hy, ny);
-  if (delta >= ex || -delta >= ey) return false;
-  return ex == (__int128)B * Hx * nx * d || ey == (__int128)B * Hy * ny * d;
+  return meet(meet, 0, 0);
+}
+// Whether tensors x [B, Hx, nx, d] and y [B, Hy, ny, d] of any lengths certainly meet: their first rows do, or one of them
+// has no gaps and a row of the other reaches into it. y starts `delta` elements behind x.
+inline bool ranges_meet(const Strides& x, int Hx, int nx, const Strides& y, int Hy, int ny, int B, int d, __int128 delta) {
+  const auto dense = [&](const Strides& s, int H, int n) {
+    const __int128 size = (__int128)B * H * n * d;
+    const __int128 end = (__int128)s.b * (B - 1) + (__int128)s.h * (H - 1) + (__int128)s.t * (n - 1) + d;
+    return end == size && writable(s, B, H, n, d) ? size : 0;   // (an input's rows may lie on each other)
+  };
+  if (delta < d && -delta < d) return true;
+  const __int128 size_x = dense(x, Hx, nx), size_y = dense(y, Hy, ny);
+  return (size_x > 0 && rows_reach(y, B, Hy, ny, d, -delta, size_x)) || (size_y > 0 && rows_reach(x, B, Hx, nx, d, delta, size_y));
 }
 
 }  // namespace attn

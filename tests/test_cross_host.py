@@ -1,6 +1,9 @@
 """Attention to keys of another length and the decode step behind a shared prefix without a GPU: the oracle's
 pins, the buckets of relative positions, every refusal of the C ABI and of the Python form."""
 import ctypes
+import os
+import shutil
+import subprocess
 
 import numpy as np
 import pytest
@@ -12,6 +15,7 @@ from test_binding_host import FakeLib, gpu
 
 FAKE, MIS = 1 << 20, (1 << 20) + 2   # never dereferenced: validation fails first
 BF16, F32 = 0, 1
+CSRC = os.path.join(os.path.dirname(pkg.__file__), "csrc")
 
 
 # ------------------------------------------------------------------ oracle --
@@ -101,7 +105,8 @@ def test_buckets(n, far, both):
 
 
 def test_buckets_refused():
-    for args in ((31, 128), (2, 128), (32, 8), (32, 0), (32.0, 128), (32, 5000), (1, 10, False), (32, 16, False)):
+    for args in ((31, 128), (2, 128), (32, 8), (32, 0), (32.0, 128), (32, 5000), (1, 10, False), (32, 16, False),
+                 (10 ** 9, 10 ** 10), (4, 10 ** 400), (6, 2 ** 62)):
         with pytest.raises(ValueError):
             pkg.attn_bias_buckets(*args, device="cpu")
 
@@ -180,6 +185,89 @@ def test_refusals_of_strides(L):
         assert bwd(L, ptr={x: 7 * FAKE + 4 * 8 * 64 * 2}, wsb=0) == -5   # right behind it: only the workspace is wrong
 
 
+def test_refusals_of_results_in_place(L):
+    """An output on an input, or reaching into it."""
+    apart = {x: FAKE * (i + 1) for i, x in enumerate(("q", "k", "v", "o", "L"))}
+    for x in ("q", "k", "v"):
+        for at in (0, 128, -128):
+            assert fwd(L, ptr={**apart, "o": apart[x] + at}) == -7
+    packed = ll(4 * 8 * 64, 64, 4 * 64, *([2 * 9 * 64, 9 * 64, 64] * 2), 8 * 8 * 64, 64, 8 * 64)   # with gaps, on q's first row
+    assert fwd(L, strides=packed, ptr={**apart, "o": apart["q"]}) == -7
+    for x in ("q", "k", "v", "o", "do"):
+        i = ("q", "k", "v", "o", "L", "do").index(x)
+        for y in ("dq", "dk", "dv"):
+            for at in (0, 128, -128):
+                assert bwd(L, ptr={y: FAKE * (i + 1) + at}) == -7, (x, y, at)
+    # dQ [2, 2, 4, 64] between two sequences' dK: only the workspace is wrong
+    q, kv = [2 * 4 * 64, 4 * 64, 64], [2 * 9 * 64, 9 * 64, 64]
+    slots = ll(*q, *kv, *kv, *q, *q, *q, 2 * kv[0], *kv[1:], *kv)
+    small = dict(B=2, Hq=2, nq=4, strides=slots, wsb=0)
+    assert bwd(L, ptr={"dq": 8 * FAKE + 2 * kv[0]}, **small) == -5
+    assert bwd(L, ptr={"dq": 8 * FAKE + 2 * kv[0] - 128}, **small) == -7
+    assert bwd(L, ptr={"dq": 8 * FAKE + 4 * kv[0] - 2 * q[0] * 2}, **small) == -5   # right before the second
+    assert bwd(L, ptr={"dq": 8 * FAKE + 4 * kv[0] - 2 * q[0] * 2 + 128}, **small) == -7
+
+
+RANGES = r"""
+#include <cstdio>
+#include <cstdlib>
+#include <random>
+#include "strides.hpp"
+using attn::Strides;
+int main() {
+  std::mt19937 g(11);
+  auto pick = [&](int lo, int hi) { return lo + (int)(g() % (unsigned)(hi - lo + 1)); };
+  int met = 0, apart = 0;
+  const int d = 4;
+  struct Tensor { Strides s; int H, n; bool dense; };
+  auto draw = [&](int B, int gaps) {   // axes in a random order, each over the smaller ones and a gap, or not stepping at all
+    Tensor x{{0, 0, 0}, pick(1, 3), pick(1, 4), true};
+    int order[3] = {0, 1, 2}, size[3] = {B, x.H, x.n};
+    for (int i = 2; i > 0; --i) std::swap(order[i], order[pick(0, i)]);
+    long long step[3], span = d;
+    for (int i : order) {
+      const long long gap = gaps ? 4 * pick(0, 6) : 0;
+      step[i] = gaps == 2 && pick(0, 3) == 0 ? 0 : span + gap;
+      if (size[i] == 1) step[i] = 0;
+      else if (step[i] != span) x.dense = false;
+      if (step[i]) span = step[i] * size[i];
+    }
+    x.s = {step[0], step[1], step[2]};
+    return x;
+  };
+  for (int it = 0; it < 300000; ++it) {
+    const int B = pick(1, 3);
+    const Tensor a = draw(B, 0), b = draw(B, it % 3);
+    const bool swap = it % 2;
+    const Tensor &x = swap ? b : a, &y = swap ? a : b;
+    const long long delta = pick(-160, 160);
+    bool want = false;
+    for (int i = 0; i < B; ++i) for (int j = 0; j < x.H; ++j) for (int k = 0; k < x.n; ++k)
+      for (int l = 0; l < B; ++l) for (int m = 0; m < y.H; ++m) for (int o = 0; o < y.n; ++o)
+        want = want || std::llabs(delta + l * y.s.b + m * y.s.h + o * y.s.t - i * x.s.b - j * x.s.h - k * x.s.t) < d;
+    if (attn::ranges_meet(x.s, x.H, x.n, y.s, y.H, y.n, B, d, delta) != want) {
+      std::printf("%d: %lld %lld %lld, %lld %lld %lld, delta %lld: %d\n", it, x.s.b, x.s.h, x.s.t, y.s.b, y.s.h, y.s.t, delta, want);
+      return 1;
+    }
+    ++(want ? met : apart);
+  }
+  const Strides far{1LL << 50, 128, 1LL << 20}, dense{64LL << 27, 1LL << 27, 128};   // sizes whose products pass 64 bits
+  if (attn::ranges_meet(far, 64, 1 << 20, dense, 64, 1 << 20, 1 << 9, 128, -(1LL << 58))) return 1;
+  if (!attn::ranges_meet(dense, 64, 1 << 20, far, 64, 1 << 20, 1 << 9, 128, 1LL << 30)) return 1;
+  return met > 1000 && apart > 1000 ? 0 : 1;
+}
+"""
+
+
+@pytest.mark.skipif(shutil.which("g++") is None, reason="needs g++")
+def test_overlaps_against_all_pairs(tmp_path):
+    """Of two tensors, one of them without gaps, every overlap is found and no other (csrc/strides.hpp, compiled for the CPU)."""
+    (tmp_path / "ranges.cpp").write_text(RANGES)
+    exe = str(tmp_path / "ranges")
+    subprocess.run(["g++", "-std=c++17", "-O2", "-Wall", "-Werror", "-fsanitize=undefined", "-I", CSRC, str(tmp_path / "ranges.cpp"), "-o", exe], check=True)
+    subprocess.run([exe], check=True, timeout=120)
+
+
 def test_workspaces(L):
     assert L.attn_cross_fwd_workspace_bytes(1, 4, 2, 8, 9, 64, BF16, 0) == 0
     need = L.attn_cross_fwd_workspace_bytes(1, 4, 2, 1, 100000, 64, BF16, 0)
@@ -219,6 +307,16 @@ def test_refusals_of_prefix(L):
     for bad in ({"d": 96}, {"dtype": F32}, {"dtype": 5}):
         assert prefix(L, **bad) == -3, bad
     assert prefix(L, scale=float("inf")) == -7
+    # written tensors that reach into another one
+    names = ("q", "k_new", "v_new", "k_prefix", "v_prefix", "k_cache", "v_cache", "O")
+    apart = {x: FAKE * (i + 1) for i, x in enumerate(names)}
+    size = {"O": 2 * 4 * 64 * 2, "k_cache": 2 * 2 * 4 * 64 * 2, "v_cache": 2 * 2 * 4 * 64 * 2}
+    for x in size:
+        for y in names[1:]:
+            if x != y:
+                assert prefix(L, ptr={**apart, x: apart[y]}) == -7, (x, y)
+                assert prefix(L, ptr={**apart, y: apart[x] + size[x] - 16}) == -7, (x, y)
+    assert prefix(L, ptr={**apart, "k_new": None, "v_new": None, "O": apart["k_cache"]}) == -7
     need = L.attn_prefix_decode_workspace_bytes(2, 4, 2, 7, 3, 64)
     assert need == 2 * 2 * 4 * (64 + 2) * 4 and prefix(L, wsb=need - 1) == -5
     assert L.attn_prefix_decode_workspace_bytes(2, 4, 2, 7, 0, 64) == 2 * 4 * (64 + 2) * 4
