@@ -267,6 +267,9 @@ __device__ __forceinline__ int bias_side(const CrossArgs& a, int lo, int hi) {
 // V tiles of 64 keys in LDS; S^T = K Q^T, online softmax by column, O^T += V^T P^T.
 // PART: it owns 128 rows (query, head of the group) and one part of the keys, as
 // cross_few_kernel its 32.
+// Bound by the products and, the more the smaller d, by the softmax's VALU: 2 x 32 heads on 8, 4096 on
+// 16384, d = 128, bf16 1.93 ms, 1140 TFLOP/s, matrix cores 0.63 busy; 4 x 16, n = 2048, causal, d = 64, with a
+// bias 54 us, 0.37 busy. float32 takes the float32 matrix instructions (0.59 to 0.73 busy).
 // ======================================================================
 template <typename T, int D> struct FwdLds {
   using TL = CrossTile<T, 64, D>;
@@ -428,8 +431,9 @@ __global__ void __launch_bounds__(256, sizeof(T) == 4 && D == 128 ? 1 : 2) cross
 // r / pack, so that a group's heads share every key that is read. The four waves
 // take the part's 32-key blocks in turn, each with its own softmax; their results
 // are merged in LDS, and where the keys are in several parts, the parts by
-// cross_merge_kernel. Decode steps are bound by the bytes of K and V, small grids by the
-// length of a wave's chain of blocks.
+// cross_merge_kernel. Decode steps are bound by the bytes of K and V (32 x 16 heads, 1 on up to 1500, d = 64 26 us,
+// 5.7 TB/s; 16 x 16 on up to 4096 34 us, 6.0), small grids by the length of a wave's chain of blocks (8 heads, 64 on
+// 77 5.3 us, of which an empty kernel is 2.4).
 // bf16: P multiplies V in two parts (the float cut to 16 bits, and the rest
 // rounded): one rounded part leaves O off by 1.5 times its own last rounding.
 // ======================================================================
@@ -642,7 +646,8 @@ __global__ void __launch_bounds__(256, sizeof(T) == 4 && D == 128 ? 1 : 2) cross
 }
 
 // The parts of a row, joined: a wave for a row, D / 4 lanes across it and the other
-// lanes over the parts, four of each lane's in flight. Returns the lane's 4 columns (all
+// lanes over the parts, four of each lane's in flight. Bound by its launch and two dependent loads (256 rows of two parts, d =
+// 64 4.8 us), large ones by their bytes (4096 rows of nine parts, d = 128 7.3 us, 3.2 TB/s). Returns the lane's 4 columns (all
 // lanes of a column group alike), and the row's maximum and sum.
 template <int D> __device__ __forceinline__ f32x4 join_parts(const float* part, const float* ml, long long nrows, long long row, int parts, int lane,
                                                             float& M, float& l) {
@@ -768,6 +773,8 @@ template <int D> __global__ void __launch_bounds__(256) prefix_merge_kernel(cons
 // dQ: a workgroup owns 128 queries of a head, 32 per wave (Q and dO rows in
 // registers), and goes over the 64-key tiles of K and V that they see, or a run of
 // them. Per 32-key block: S^T = K Q^T, dP^T = V dO^T, dS^T, dQ^T += K^T dS^T.
+// Bound by the products: 2 x 32 heads on 8, 4096 on 16384, d = 128, bf16 2.72 ms, 1210 TFLOP/s of them, matrix cores 0.68
+// busy; at d = 64 by VALU (4 x 16, n = 2048, causal, with a bias 74 to 79 us, 0.37 busy).
 //
 // FIX (a bias, or bf16 where rows see few keys, by their number or their mask): D comes from
 // an O that was rounded, so that dS = P (dP - D) is off by P e_i, e_i being D's error.
@@ -932,6 +939,9 @@ __global__ void __launch_bounds__(256, sizeof(T) == 4 ? 1 : 2) cross_dq_kernel(c
 // over a run of them. Per 32-query block: S = Q K^T, dP = dO V^T (rows = queries),
 // P, dS, dV^T += dO^T P, dK^T += Q^T dS. Query rows past the end have L = +inf: P = 0.
 // TWO: P and dS multiply in two bf16 parts.
+// Bound by the two waves a SIMD that its registers leave room for, which wait half of their time: 4 x 16 heads, n = 2048,
+// causal, d = 64, with a bias and its gradient 125 to 130 us, 530 TFLOP/s of the products. float32: 4 x 8, 333 on up to 1000, d
+// = 64 65 us, matrix cores 0.73 busy.
 //
 // The bias gradient (drel, a row [R] for each query head and key block): dS is added up
 // by relative position. Blocks before or behind the positions that have a bias of their
@@ -1186,7 +1196,8 @@ __global__ void __launch_bounds__(256, D == 128 || (sizeof(T) == 4 && D == 64 &&
 // v_mfma_f32_16x16x32_bf16. A wave owns KB blocks of 16 keys (two at d = 128, three at
 // 64), which share every Q and dO operand that is read from LDS; K's operands come
 // from an LDS copy of the workgroup's keys, V's stay in registers, so that two workgroups
-// fit a compute unit and one's exponentials run under the other's products. A step is 32 queries:
+// fit a compute unit and one's exponentials run under the other's products: 2 x 32 heads on 8, 4096 on 16384, d = 128 3.4
+// ms, 1300 TFLOP/s of the products, matrix cores 0.65 busy at the clock that power allows. A step is 32 queries:
 //   S = Q K^T, dP - D = dO V^T - D (the accumulators start from -D), P, dS,
 //   dV^T += dO^T P, dK^T += Q^T dS
 // Rows of queries past the end are masked with the causal mask's; keys past the
@@ -1415,6 +1426,8 @@ __global__ void __launch_bounds__(256, 2) cross_dkdv16_kernel(const CrossArgs a)
 // Operands that are read as rows only (V for dQ) come from memory straight to registers, the
 // others go through LDS tiles of the wave, in two stages where they fit.
 // cross_dq_few_kernel may pack the heads of a group as cross_few_kernel does.
+// Bound by a wave's chain of blocks: 2 x 8 heads, n = 200, d = 32, float32, with a bias 10.6 us (dQ) and 15.4 (dK, dV); 1 x 8,
+// 500 on 500, d = 64, bf16 18.5 us both, 128 rows a workgroup 25.5.
 // ======================================================================
 template <typename T, int D> struct CrossFewBwd {
   // per buffer: the merge's half, or the tiles of four waves (dK, dV: of Q and dO, one stage each, in bf16;
@@ -1780,7 +1793,7 @@ __global__ void __launch_bounds__(256, D == 128 ? 1 : 2) cross_dkdv_few_kernel(c
   merge(dk, a.dk, a.dks, a.part, a.scale);
 }
 
-// A gradient whose sum was split: rows [rows, D] float32 of `parts` parts, added in order.
+// A gradient whose sum was split: rows [rows, D] float32 of `parts` parts, added in order; bound by their bytes, or its launch.
 // out: [B, H, n] rows with strides `s`. sums (or null): parts of a row's sum of dS, taken from dvec.
 template <typename T, int D> __global__ void __launch_bounds__(256) cross_sum_kernel(const float* part, void* out, Strides s, long long rows, int H, int n, int parts,
                                                                                     const float* sums, float* dvec) {
@@ -1802,7 +1815,7 @@ template <typename T, int D> __global__ void __launch_bounds__(256) cross_sum_ke
 
 // The bias gradient of head blockIdx.x: the rows of drel by relative position, then the
 // positions of each bucket, all in a fixed order and in 64 bits (a bucket's sum is small
-// against its terms).
+// against its terms). Bound by latency: 64 rows of 8 or 16 heads 6.2 us.
 template <typename T> __global__ void __launch_bounds__(1024) cross_dbias_kernel(const CrossArgs a, void* dtable) {
   extern __shared__ __attribute__((aligned(16))) double acc[];   // [R], then [1024], then the positions' buckets [R]
   const int tid = threadIdx.x, hq = blockIdx.x;
