@@ -176,6 +176,7 @@ struct BwdPlan {
   bool q_few, k_few;              // 32 queries or keys a workgroup, not 128 (192)
   int q_pack, q_tiles, q_splits, q_per;   // dQ: heads in a tile of rows, tiles; parts of the keys' blocks
   int k_tiles, k_splits, k_per;   // dK, dV: tiles of keys; parts of the query blocks of all heads, or of the heads
+  int k_qparts;                   // with a bias: parts of a head's queries, within k_splits
   size_t rows_at, drel_at, dq_at, sums_at, dk_at, dv_at, bytes;
 };
 // A grid of fewer than 256 tiles of 128 rows leaves compute units idle: 32 rows or keys a workgroup. Grids that are
@@ -205,17 +206,25 @@ BwdPlan bwd_plan(int B, int Hq, int Hkv, int nq, int nk, int d, int dtype, bool 
   const bool wide = !p.k_few && dkdv16(B, Hq, nq, nk, d, dtype, bias);
   p.k_tiles = (int)div_up(nk, p.k_few ? 32 : wide ? (d == 64 ? attn::CrossDkdv16<64>::BKV : attn::CrossDkdv16<128>::BKV) : 128);
   const long long groups = (long long)B * Hkv * p.k_tiles;
-  if (bias) {   // one head's bias at a time, and one workgroup for the bias gradient of a head and tile: runs of heads
+  p.k_qparts = 1;
+  const int steps = (int)div_up(nq, p.k_few || wide || (dtype == ATTN_F32 && d == 128) ? 32 : 64), least = p.k_few ? 16 : 4;
+  // With a bias, one head's at a time: runs of heads, and parts of one head's queries where that leaves units idle (backward in
+  // parts and whole: 1 x 8, 2048 on 2048, d = 64 88, 111; 1024 on 1024, d = 128 65, 86; 2 x 2 on 1, 1602 on 1602, causal, d =
+  // 128, float32 217, 559).
+  if (bias) {
     p.k_splits = groups >= 256 ? 1 : (int)std::min<long long>(512 / groups, G);
     p.k_per = (int)div_up(G, p.k_splits);
     p.k_splits = (int)div_up(G, p.k_per);
+    if (p.k_per == 1 && groups * p.k_splits < 256)
+      p.k_qparts = (int)std::max<long long>(1, std::min<long long>(512 / (groups * p.k_splits), steps / least));
+    p.k_splits *= p.k_qparts;
   } else {
-    parts(groups, G * div_up(nq, p.k_few || wide || (dtype == ATTN_F32 && d == 128) ? 32 : 64), p.k_few ? 16 : 4, p.k_splits, p.k_per);
+    parts(groups, (long long)G * steps, least, p.k_splits, p.k_per);
   }
   const size_t qrows = (size_t)B * Hq * nq, krows = (size_t)B * Hkv * nk;
   p.rows_at = 0;
   p.drel_at = up16(2 * qrows * sizeof(float));
-  p.dq_at = p.drel_at + (R > 0 ? up16((size_t)B * Hq * p.k_tiles * R * sizeof(float)) : 0);
+  p.dq_at = p.drel_at + (R > 0 ? up16((size_t)B * Hq * p.k_tiles * p.k_qparts * R * sizeof(float)) : 0);
   p.sums_at = p.dq_at + (p.q_splits > 1 ? p.q_splits * qrows * d * sizeof(float) : 0);
   p.dk_at = p.sums_at + (p.q_splits > 1 ? up16(p.q_splits * qrows * sizeof(float)) : 0);
   p.dv_at = p.dk_at + (p.k_splits > 1 ? p.k_splits * krows * d * sizeof(float) : 0);
@@ -394,6 +403,7 @@ extern "C" int attn_cross_bwd(const void* q, const void* k, const void* v, const
   ak.ntiles = p.k_tiles; ak.splits = p.k_splits; ak.per = p.k_per; ak.nrows = krows;
   ak.part = p.k_splits > 1 ? (float*)(ws + p.dk_at) : nullptr;
   ak.part2 = (float*)(ws + p.dv_at);
+  ak.qparts = p.k_qparts;
   ak.drel = dbias ? (float*)(ws + p.drel_at) : nullptr;
   set_grid(ak, (long long)B * Hkv, p.k_tiles * p.k_splits);
 

@@ -59,7 +59,8 @@ struct CrossArgs {
   float* part;         // parts of O (or of a gradient), then of (max, sum)
   float* part_ml;
   float* part2;        // parts of dV
-  float* drel;         // bias gradient by relative position, a row [R] for each dQ workgroup
+  float* drel;         // bias gradient by relative position, a row [R] for each query head, key block and part of its queries
+  int qparts;          // dK, dV with a bias: parts of a head's queries
   long long rz, rh, ri;   // row of the parts: sequence, head, query
   long long nrows;        // rows of a part
   int start, first, R, buckets;
@@ -1047,12 +1048,13 @@ __global__ void __launch_bounds__(256, D == 128 || (sizeof(T) == 4 && D == 64 &&
   const bool grad = BIAS && a.drel;
 
   // query tiles [t0, nqt) of every head see the block; the part's are u0 to u1 of them all, with a
-  // bias those of whole heads
+  // bias those of whole heads, or part qpart of one head's
   const int nqt = (a.nq + BQ - 1) / BQ;
   const int t0 = a.causal ? min(nqt, max(0, k0 - start) / BQ) : 0, per_head = nqt - t0;
   const int all = k0 < n ? a.G * per_head : 0;
-  const int per = BIAS ? a.per * per_head : a.per;
-  const int u0 = min(all, part * per), u1 = min(all, u0 + per);
+  const int hpart = BIAS ? part / a.qparts : part, qpart = BIAS ? part - hpart * a.qparts : 0;
+  const int per = BIAS ? a.per * per_head : a.per, len = BIAS ? (per + a.qparts - 1) / a.qparts : per;
+  const int u0 = min(all, hpart * per + min(per, qpart * len)), u1 = min(all, hpart * per + min(per, qpart * len + len));
 
   TL qld(w, lane, a.qs.t), gld(w, lane, a.gs.t);
   float lreg = 0.f;
@@ -1093,7 +1095,7 @@ __global__ void __launch_bounds__(256, D == 128 || (sizeof(T) == 4 && D == 64 &&
   if (grad) ds.open(a, lane);
   __syncthreads();
   auto flush = [&](int g) __attribute__((always_inline)) {
-    ds.flush(a, far, ((long long)b * a.Hq + hk * a.G + g) * a.ntiles + kt, w, lane, tid);
+    ds.flush(a, far, (((long long)b * a.Hq + hk * a.G + g) * a.ntiles + kt) * a.qparts + qpart, w, lane, tid);
   };
 
   auto step = [&](int u, T* qc, T* gc, float* lc, T* qn, T* gn, float* ln) __attribute__((always_inline)) {
@@ -1183,8 +1185,8 @@ __global__ void __launch_bounds__(256, D == 128 || (sizeof(T) == 4 && D == 64 &&
     if (grad && bias_head >= 0) {
       flush(bias_head);
     } else if (grad) {   // no query sees these keys
-      for (int g = part * a.per; g < min(a.G, (part + 1) * a.per); ++g) {
-        float* const out = a.drel + (((long long)b * a.Hq + hk * a.G + g) * a.ntiles + kt) * a.R;
+      for (int g = hpart * a.per; g < min(a.G, (hpart + 1) * a.per); ++g) {
+        float* const out = a.drel + ((((long long)b * a.Hq + hk * a.G + g) * a.ntiles + kt) * a.qparts + qpart) * a.R;
         for (int t = tid; t < a.R; t += 256) out[t] = 0.f;
       }
     }
@@ -1609,12 +1611,13 @@ __global__ void __launch_bounds__(256, D == 128 ? 1 : 2) cross_dkdv_few_kernel(c
   const int k0 = 32 * kt, kj = k0 + c;
   const float sl2 = a.sl2;
 
-  // as in cross_dkdv_kernel, in blocks of 32 queries; with a bias a part is a run of heads
+  // as in cross_dkdv_kernel, in blocks of 32 queries; with a bias a part is a run of heads, or a part of one
   const int nqb = (a.nq + 31) / 32;
   const int t0 = a.causal ? min(nqb, max(0, k0 - start) / 32) : 0, per_head = nqb - t0;
   const int all = k0 < n ? a.G * per_head : 0;
-  const int per = BIAS ? a.per * per_head : a.per;
-  const int u0 = min(all, part * per), u1 = min(all, u0 + per);
+  const int hpart = BIAS ? part / a.qparts : part, qpart = BIAS ? part - hpart * a.qparts : 0;
+  const int len = BIAS ? (per_head + a.qparts - 1) / a.qparts : a.per;   // of a head, or of all
+  const int u0 = min(all, part * a.per), u1 = min(all, u0 + a.per);
   DiagSums ds(a, bv, w, lane);
   const bool grad_bias = BIAS && a.drel;
 
@@ -1753,21 +1756,21 @@ __global__ void __launch_bounds__(256, D == 128 ? 1 : 2) cross_dkdv_few_kernel(c
   own();
   if constexpr (BIAS) {
     if (grad_bias) ds.open(a, lane);
-    int done = part * a.per;
-    for (int g = done; g < min(a.G, (part + 1) * a.per) && all > 0; ++g) {
+    const int g0 = hpart * a.per, g1 = min(a.G, g0 + a.per);
+    for (int g = g0; g < g1 && all > 0; ++g) {
       bias_fill<T>(bv, a, hk * a.G + g, tid);
       __syncthreads();
-      run(g * per_head, (g + 1) * per_head);
+      run(g * per_head + min(per_head, qpart * len), g * per_head + min(per_head, qpart * len + len));
       if (grad_bias) {
-        ds.flush(a, far, ((long long)b * a.Hq + hk * a.G + g) * a.ntiles + kt, w, lane, tid);
+        ds.flush(a, far, (((long long)b * a.Hq + hk * a.G + g) * a.ntiles + kt) * a.qparts + qpart, w, lane, tid);
         __syncthreads();
         ds.clear(a, lane);
       }
       __syncthreads();
     }
     if (grad_bias && all == 0) {   // no query sees these keys
-      for (int g = done; g < min(a.G, (part + 1) * a.per); ++g)
-        for (int t = tid; t < a.R; t += 256) a.drel[(((long long)b * a.Hq + hk * a.G + g) * a.ntiles + kt) * a.R + t] = 0.f;
+      for (int g = g0; g < g1; ++g)
+        for (int t = tid; t < a.R; t += 256) a.drel[((((long long)b * a.Hq + hk * a.G + g) * a.ntiles + kt) * a.qparts + qpart) * a.R + t] = 0.f;
     }
   } else {
     run(u0, u1);
@@ -1823,18 +1826,18 @@ template <typename T> __global__ void __launch_bounds__(1024) cross_dbias_kernel
   int* const rows = (int*)(tmp + 1024);
   for (int t = tid; t < a.R; t += 1024) rows[t] = a.rows[t];
   // position t0 + tid % 256 of the rows tid / 256, + 4, ...
-  const int N = a.B * a.ntiles;
+  const int per = a.ntiles * a.qparts, N = a.B * per;   // rows of a head and sequence, and of a head
   for (int t0 = 0; t0 < a.R; t0 += 256) {
     const int t = t0 + (tid & 255);
     double x = 0.0;
     if (t < a.R) {
-      const float* const at = a.drel + (long long)hq * a.ntiles * a.R + t;
+      const float* const at = a.drel + (long long)hq * per * a.R + t;
       for (int r0 = tid >> 8; r0 < N; r0 += 32) {   // eight in flight
         float y[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          const unsigned r = min(r0 + 4 * i, N - 1), b = r / (unsigned)a.ntiles;
-          y[i] = at[((long long)b * (a.Hq - 1) * a.ntiles + r) * a.R];
+          const unsigned r = min(r0 + 4 * i, N - 1), b = r / (unsigned)per;
+          y[i] = at[((long long)b * (a.Hq - 1) * per + r) * a.R];
         }
 #pragma unroll
         for (int i = 0; i < 8; ++i) x += r0 + 4 * i < N ? (double)y[i] : 0.0;

@@ -216,6 +216,15 @@ def test_few_queries_large_grid_of_keys(d, dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("d", [32, 64, 128])
+def test_bias_backward_in_parts_of_queries(d, dtype):
+    """Few heads, many queries: a head's queries in parts, some of which see no key of a block, or none of a short sequence."""
+    for how in ({}, {"causal": True}, {"causal": True, "start": -700}, {"start": 5, "k_lens": [0]}, {"k_lens": [300]}):
+        Call(1, 2, 1, 1100, 700, d, dtype, buckets=(32, 128, "causal" not in how), **how).check(what=str(how))
+    Call(1, 1, 1, 600, 17000, d, dtype, buckets=(32, 128), start=8000).check()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
 def test_bias_positions_of_all_sizes(dtype):
     """2 to 2048 positions of their own, in no order, some of no bucket, and far from the queries."""
     rng = np.random.default_rng(5)
